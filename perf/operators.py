@@ -209,9 +209,6 @@ def _library(st):
             st["rope"] = efim.Rope.from_table(st["rope_table"], case["interleaved"])
             st["norm"] = efim.QkNorm(st["q_weight"], st["k_weight"], EPS)
             st["split"] = st["qkv"].split([case["hq"] * case["dim"], case["hkv"] * case["dim"], case["hkv"] * case["dim"]], 1)
-        elif case["op"] == "verify":
-            need = efim.efim_verify_workspace_bytes(len(st["accepted"]), st["target"].shape[0], case["vocab"])
-            st["workspace"] = torch.empty(need, dtype=torch.uint8, device="cuda")
     return st["own"]
 
 
@@ -227,7 +224,7 @@ def _own_verify(st):
     efim.efim_verify_drafts(st["indptr"], st["tokens"], st["target"], st["accepted"], st["next"], uniform=st["uniform"],
                             noise=st["noise"], draft_probs=st.get("draft_probs"), temperature=st.get("temperature"),
                             target_is_probs=st["case"]["kind"] == "probs", out_tokens=st["out"], out_logprobs=st["logprobs"],
-                            workspace=st["workspace"], status=st["status"])
+                            status=st["status"])
     return dict(accepted=st["accepted"], next=st["next"], out=st["out"], logprobs=st["logprobs"])
 
 
