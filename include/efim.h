@@ -68,8 +68,11 @@ typedef enum {
 
 /* Bits OR-ed into *d_status by kernels. */
 #define EFIM_DEV_BAD_PAGE      0x1   /* block-table entry outside [0, num_pages)           */
-#define EFIM_DEV_BAD_POSITION  0x2   /* token position >= rope max_position, or beyond table */
+#define EFIM_DEV_BAD_POSITION  0x2   /* token position >= rope max_position, or beyond table;
+                                        a length or row range outside what the call was given */
 #define EFIM_DEV_TIMEOUT       0x4   /* a bounded wait inside a kernel expired               */
+#define EFIM_DEV_BAD_TOKEN     0x8   /* a drafted token id outside [0, vocab)                */
+#define EFIM_DEV_NO_TOKEN      0x10  /* a distribution without a token to pick (all masked, or NaN) */
 
 const char* efim_strerror(efim_status s);
 /* Text of the CUDA error behind the calling thread's most recent EFIM_ERR_CUDA. */
@@ -131,6 +134,32 @@ efim_status efim_kv_append(const efim_cache_desc* cache, const efim_batch_desc* 
                            const efim_rope_desc* rope,
                            void* d_q, const void* d_k_new, const void* d_v_new,
                            int32_t* d_status, void* stream);
+
+/*
+ * Step 1 for models that normalise each query and key head before the rotation (the paper has no counterpart: the norms are part
+ * of the model).  With x one head's head_dim values, in fp32 and rounded to bf16 once, at the end:
+ *   y_d = x_d / sqrt(mean_e x_e^2 + eps) * (w_d + weight_offset),   then rotated by the token's position as in efim_kv_append;
+ * k and v go into the pages as there (v as it is).  Without a rotary table y is stored as it is.
+ * d_q, d_k, d_v: token t's heads, packed, start q_stride (k_stride, v_stride) elements after token t-1's: a multiple of 8, at least
+ * the row's length, so that the three may be views of one projection's output.  Base pointers 16-byte aligned.
+ * d_q_out: packed [total_new_tokens][num_q_heads][head_dim]; it may be d_q where that is packed too, and must not overlap
+ * the three otherwise (EFIM_ERR_INVALID_ARG).  d_q and d_q_out may both be NULL (only k/v are processed).
+ * A bad page id or position sets a bit in *d_status and skips that token's k and v; its query row is written all the same,
+ * zeros where the rotary table has no row.  Heads of values beyond 1e18, whose squares leave fp32, come out right too; an
+ * infinity makes its place NaN and the head's other places 0, a NaN the whole head NaN.
+ * One kernel; no workspace; may be captured.
+ */
+typedef struct {
+  const void* d_q_weight;    /* [head_dim], 16-byte aligned, or NULL: weights (offset included) of 1 */
+  const void* d_k_weight;
+  int32_t weight_f32;        /* 0: bf16 weights, 1: fp32 */
+  float eps;                 /* > 0, finite */
+  float weight_offset;       /* 0, or 1 for models that store w - 1 */
+} efim_qk_norm_desc;
+efim_status efim_qk_norm_append(const efim_cache_desc* cache, const efim_batch_desc* batch, const efim_qk_norm_desc* norm,
+                                const efim_rope_desc* rope, const void* d_q, int64_t q_stride, const void* d_k,
+                                int64_t k_stride, const void* d_v, int64_t v_stride, void* d_q_out,
+                                int32_t* d_status, void* stream);
 
 /*
  * Step 2 (EFIM Sec. 1, Sec. 2.2: prefix and suffix KV are cache hits, so the
@@ -290,6 +319,66 @@ efim_status efim_decode_attn_static(const efim_cache_desc* cache, int32_t batch,
                                     const int32_t* d_block_table, int32_t max_pages_per_seq,
                                     const void* d_q, void* d_out, float* d_lse, float sm_scale,
                                     int32_t* d_status, void* stream);
+
+/*
+ * Step 3 with drafted tokens (the paper has no counterpart; infilled code repeats much of what stands around it).  A step feeds a
+ * sequence its pending token and k drafts as k+1 new tokens - efim_kv_append or efim_qk_norm_append, then
+ * efim_append_prefill_attn - and the model turns their k+1 rows into distributions over the next token.  The two calls here
+ * find drafts without a second model, and decide what a step has produced.
+ *
+ * efim_draft_lookup: drafts from each sequence's history T[0, len): the place whose preceding tokens agree longest with the history's
+ * last ones, between min_ngram and max_ngram (<= 32, EFIM_ERR_UNSUPPORTED above) tokens, the latest such place:
+ *   e* = argmax over 1 <= e < len of (min(max_ngram, |common suffix of T[0,e) and T[0,len)|), e)
+ *   d_drafts[s][i] = T[e* + i mod (len - e*)],  0 <= i < num_drafts;  d_draft_len[s] = num_drafts
+ * (past the history's end the draft repeats itself), or -1 and 0 where no place agrees.  d_history: rows of up to max_len
+ * token ids, history_stride elements apart; a length outside [0, max_len] is clamped and sets EFIM_DEV_BAD_POSITION.
+ */
+efim_status efim_draft_lookup(int32_t batch, const int32_t* d_history, int64_t history_stride, int32_t max_len,
+                              const int32_t* d_len, int32_t min_ngram, int32_t max_ngram, int32_t num_drafts,
+                              int32_t* d_drafts, int32_t* d_draft_len, int32_t* d_status, void* stream);
+
+/*
+ * efim_verify_drafts: rows d_row_indptr[s] .. d_row_indptr[s+1]-1 are sequence s's (the batch's d_q_indptr); d_tokens holds the
+ * step's new tokens, and row r's distribution p_r judges d_tokens[r+1] where that row is the sequence's, too.  From the first row on:
+ *   a draft x is accepted iff u_r q_r(x) < p_r(x)          (q_r(x) = 1 without d_draft_probs)
+ * At the first row that accepts nothing, or the sequence's last one, the next token is
+ *   argmax_j w_j / e_j, the lowest j among equals,  w = max(p_r - q_r, 0) at a refused draft (without d_draft_probs: p_r
+ *   without x; p_r itself where that leaves nothing), w = p_r behind the last draft
+ * with u uniform in [0, 1) and e exponentially distributed, all from the caller: the emitted tokens are then distributed as
+ * if the target had been sampled token by token.  With no drafts (one row) this is plain sampling.
+ * Target rows, target_stride elements apart (at least vocab; any alignment of the type): logits in bf16 or fp32, of which
+ * p_r = softmax(logits / temperature), or probabilities in fp32 (filtered, say; d_temperature is then NULL).  Logits of -inf have no
+ * probability; those at +inf share all of it.  A row with a NaN, or with nothing but -inf, accepts and picks nothing: next is
+ * -1 and EFIM_DEV_NO_TOKEN is set.  A draft outside [0, vocab) is refused and sets EFIM_DEV_BAD_TOKEN when its row is reached.
+ * temperature <= 0 (or no d_noise at all, with logits): greedy - a draft is accepted iff it is the row's largest logit (the lowest place
+ * among equals), and that is the next token.  Softmax statistics and probabilities are held in fp32.
+ * Results: d_accepted[s] drafts, d_next_token[s]; optionally out_stride entries a sequence of the tokens it goes on with (accepted drafts,
+ * next, then -1) and their natural log-probabilities in p (at temperature 1 where greedy; 0 past the end).  A
+ * sequence without rows accepts 0 and gets next -1.  The k/v of a sequence's first d_accepted[s] + 1 new tokens stay valid;
+ * the next step's tokens overwrite the rest.  One kernel; no workspace; may be captured; the same inputs give the same bits.
+ */
+#define EFIM_TARGET_LOGITS_BF16  0
+#define EFIM_TARGET_LOGITS_F32   1
+#define EFIM_TARGET_PROBS_F32    2
+typedef struct {
+  int32_t batch;
+  int32_t total_rows;            /* rows of d_target, d_tokens, d_draft_probs, d_uniform */
+  int32_t vocab;
+  int32_t target_kind;           /* EFIM_TARGET_* */
+  const int32_t* d_row_indptr;   /* [batch+1] */
+  const int32_t* d_tokens;       /* [total_rows] */
+  const void* d_target;          /* rows of [vocab] */
+  int64_t target_stride;
+  const float* d_draft_probs;    /* row r: the distribution that d_tokens[r+1] was drawn from (a sequence's last row is not read); or NULL: certain drafts */
+  int64_t draft_stride;
+  const float* d_uniform;        /* [total_rows]; not read at a sequence's last row */
+  const float* d_noise;          /* [batch] rows of [vocab], > 0; or NULL (logits only): every sequence greedy */
+  int64_t noise_stride;
+  const float* d_temperature;    /* [batch], or NULL: 1 */
+} efim_verify_desc;
+efim_status efim_verify_drafts(const efim_verify_desc* desc, int32_t* d_accepted, int32_t* d_next_token,
+                               int32_t* d_out_tokens, float* d_out_logprobs, int32_t out_stride, int32_t* d_status,
+                               void* stream);
 
 /*
  * Self-test of the bounded device wait (the paper has no counterpart).  Every wait inside

@@ -6,7 +6,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
-from ctypes import c_int32, c_void_p, c_float, c_double, c_size_t, c_char_p, POINTER, Structure
+from ctypes import c_int32, c_int64, c_void_p, c_float, c_double, c_size_t, c_char_p, POINTER, Structure
 
 import numpy as np
 
@@ -37,6 +37,18 @@ class _RopeDesc(Structure):
     _fields_ = [("d_cos_sin", c_void_p), ("max_position", c_int32), ("interleaved", c_int32)]
 
 
+class _QkNormDesc(Structure):
+    _fields_ = [("d_q_weight", c_void_p), ("d_k_weight", c_void_p), ("weight_f32", c_int32), ("eps", c_float),
+                ("weight_offset", c_float)]
+
+
+class _VerifyDesc(Structure):
+    _fields_ = [("batch", c_int32), ("total_rows", c_int32), ("vocab", c_int32), ("target_kind", c_int32),
+                ("d_row_indptr", c_void_p), ("d_tokens", c_void_p), ("d_target", c_void_p), ("target_stride", c_int64),
+                ("d_draft_probs", c_void_p), ("draft_stride", c_int64), ("d_uniform", c_void_p), ("d_noise", c_void_p),
+                ("noise_stride", c_int64), ("d_temperature", c_void_p)]
+
+
 EXPORTS = ("efim_last_cuda_error", "efim_strerror", "efim_version", "efim_rope_table_build", "efim_kv_append",
            "efim_prefill_workspace_bytes", "efim_append_prefill_attn",
            "efim_decode_workspace_bytes", "efim_decode_attn",
@@ -44,6 +56,7 @@ EXPORTS = ("efim_last_cuda_error", "efim_strerror", "efim_version", "efim_rope_t
            "efim_prefill_launch_count", "efim_decode_launch_count",
            "efim_prefill_plan_bytes", "efim_prefill_plan", "efim_append_prefill_attn_planned", "efim_decode_step",
            "efim_append_prefill_step", "efim_selftest_bounded_wait",
+           "efim_qk_norm_append", "efim_draft_lookup", "efim_verify_drafts",
            "efim_fragment_cuts", "efim_fim_split", "efim_fim_fragment_spans",
            "efim_frontend_create", "efim_frontend_destroy", "efim_frontend_transform", "efim_frontend_admit",
            "efim_frontend_finish", "efim_frontend_stats")
@@ -89,6 +102,15 @@ def load_library():
     lib.efim_append_prefill_step.argtypes = [POINTER(_CacheDesc), POINTER(_BatchDesc), POINTER(_RopeDesc), c_void_p,
                                              c_void_p, c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_size_t,
                                              c_int32, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.efim_qk_norm_append.restype = ctypes.c_int
+    lib.efim_qk_norm_append.argtypes = [POINTER(_CacheDesc), POINTER(_BatchDesc), POINTER(_QkNormDesc), POINTER(_RopeDesc),
+                                        c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
+    lib.efim_draft_lookup.restype = ctypes.c_int
+    lib.efim_draft_lookup.argtypes = [c_int32, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p,
+                                      c_void_p, c_void_p, c_void_p]
+    lib.efim_verify_drafts.restype = ctypes.c_int
+    lib.efim_verify_drafts.argtypes = [POINTER(_VerifyDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                       c_void_p]
     lib.efim_selftest_bounded_wait.restype = ctypes.c_int
     lib.efim_selftest_bounded_wait.argtypes = [ctypes.c_uint64, c_void_p, c_void_p, c_void_p]
     lib.efim_decode_workspace_bytes.restype = c_size_t
@@ -139,7 +161,8 @@ class _Calls:
         loader = importlib.machinery.ExtensionFileLoader("_calls", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
         loader.exec_module(module)
-        for m in ("kv_append", "append_prefill_attn", "append_prefill_step", "decode_attn", "decode_step"):
+        for m in ("kv_append", "append_prefill_attn", "append_prefill_step", "decode_attn", "decode_step",
+                  "qk_norm_append", "draft_lookup", "verify_drafts"):
             setattr(self, m, getattr(module, m))          # found directly from now on
         return self.__dict__[name]
 
@@ -193,6 +216,16 @@ def _stream_ptr(stream):
     return stream.cuda_stream
 
 
+def _torch():
+    import torch
+    return torch
+
+
+def _check(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
 class Cache:
     """Paged KV cache of one layer: two torch.bfloat16 CUDA tensors
     [num_pages, num_kv_heads, page_size, head_dim] owned by the caller."""
@@ -236,6 +269,29 @@ class Rope:
         self.table = torch.from_numpy(host).to(device)
         self.desc = _RopeDesc(self.table.data_ptr(), max_position, 1 if interleaved else 0)
 
+    @classmethod
+    def from_table(cls, table, interleaved=False):
+        """A table that is on the device already: fp32 [max_position, head_dim], cos then sin (with any scaling)."""
+        _check(table.dtype == _torch().float32 and table.dim() == 2 and table.is_contiguous(),
+               "the rotary table is a contiguous fp32 matrix")
+        rope = cls.__new__(cls)
+        rope.table = table
+        rope.desc = _RopeDesc(table.data_ptr(), table.shape[0], 1 if interleaved else 0)
+        return rope
+
+
+class QkNorm:
+    """Norms of query and key heads: weights [head_dim] in bf16 or fp32 on the device, or None for weights of one."""
+
+    def __init__(self, q_weight, k_weight, eps=1e-6, weight_offset=0.0):
+        torch = _torch()
+        given = [w for w in (q_weight, k_weight) if w is not None]
+        _check(all(w.dtype in (torch.bfloat16, torch.float32) and w.dim() == 1 and w.is_contiguous() for w in given)
+               and len({(w.dtype, w.shape) for w in given}) <= 1, "the norms' weights are two bf16 or two fp32 vectors of one length")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.desc = _QkNormDesc(_ptr(q_weight), _ptr(k_weight), 1 if given and given[0].dtype == torch.float32 else 0, eps,
+                                weight_offset)
+
 
 def efim_rope_table_build(base, head_dim, max_position) -> np.ndarray:
     out = np.empty((max_position, head_dim), dtype=np.float32)
@@ -250,6 +306,71 @@ def efim_kv_append(cache: Cache, batch: Batch, rope, q, k_new, v_new, status=Non
                           q, k_new, v_new, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_kv_append")
+
+
+def efim_qk_norm_append(cache: Cache, batch: Batch, norm: QkNorm, rope, q, k, v, q_out, status=None, stream=None):
+    """efim_kv_append with a norm of every q and k head before the rotation.  q, k and v: bf16, one row per new token (of any rank
+    past the first, packed), views of one buffer allowed; q_out: packed.  q and q_out may both be None."""
+    heads = cache.desc.num_kv_heads * cache.desc.head_dim
+    tokens = batch.desc.total_new_tokens
+    strides = [_row_stride(x, tokens, n) for x, n in ((q, cache.desc.num_q_heads * cache.desc.head_dim), (k, heads), (v, heads))]
+    st = _calls.qk_norm_append(_addr(cache.desc), _addr(batch.desc), _addr(norm.desc),
+                               _addr(rope.desc) if rope is not None else None, q, strides[0], k, strides[1], v, strides[2], q_out,
+                               status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_qk_norm_append")
+
+
+def _row_stride(x, rows, row):
+    """Elements from one row of x to the next; its rows are packed."""
+    if x is None:
+        return 0
+    shape, stride = x.shape, x.stride()
+    inner = 1
+    for n, step in zip(shape[:0:-1], stride[:0:-1]):
+        if step != inner and n != 1:
+            raise ValueError("the values of a token are packed")
+        inner *= n
+    if shape[0] != rows or inner != row:
+        raise ValueError(f"{rows} rows of {row} values are expected, not {tuple(shape)}")
+    return stride[0] if rows > 1 else row
+
+
+def efim_draft_lookup(history, lengths, min_ngram, max_ngram, drafts, draft_len, status=None, stream=None):
+    """Drafts for each row of `history` (int32 [batch, max_len], rows may be further apart) from what followed its last tokens
+    earlier on; drafts: int32 [batch, num_drafts]."""
+    batch, max_len = history.shape
+    if history.stride(1) != 1 or not drafts.is_contiguous():
+        raise ValueError("rows of the history, and the drafts, are packed")
+    st = _calls.draft_lookup(batch, history, history.stride(0) if batch > 1 else max_len, max_len, lengths, int(min_ngram),
+                             int(max_ngram), drafts.shape[1], drafts, draft_len, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_draft_lookup")
+
+
+def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform=None, noise=None, draft_probs=None,
+                       temperature=None, target_is_probs=False, out_tokens=None, out_logprobs=None, status=None, stream=None):
+    """Accepted drafts and next token of every sequence of a step.  target: [rows, vocab] logits in bf16 or fp32, or with
+    `target_is_probs` probabilities in fp32; draft_probs fp32 [rows, vocab]; noise fp32 [batch, vocab] (none: greedy);
+    out_tokens and out_logprobs: packed [batch, n] of the same n."""
+    rows, vocab = target.shape
+    kind = 2 if target_is_probs else 0 if target.element_size() == 2 else 1
+    strides = [_matrix_stride(x, vocab) for x in (target, draft_probs, noise)]
+    out = out_tokens if out_tokens is not None else out_logprobs
+    st = _calls.verify_drafts(row_indptr.shape[0] - 1, rows, vocab, kind, row_indptr, tokens, target, strides[0], draft_probs,
+                              strides[1], uniform, noise, strides[2], temperature, accepted, next_token, out_tokens, out_logprobs,
+                              out.shape[1] if out is not None else 0, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_verify_drafts")
+
+
+def _matrix_stride(x, columns):
+    if x is None:
+        return 0
+    step, unit = x.stride()
+    if unit != 1 or x.shape[1] != columns:
+        raise ValueError(f"rows of {columns} packed values are expected")
+    return step if x.shape[0] > 1 else columns
 
 
 def efim_prefill_workspace_bytes(cache: Cache, batch: Batch) -> int:

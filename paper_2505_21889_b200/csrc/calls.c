@@ -43,6 +43,10 @@ static int as_i32(PyObject* o, int32_t* out) {
   *out = (int32_t)v;
   return 1;
 }
+static int as_i64(PyObject* o, int64_t* out) {
+  *out = PyLong_AsLongLong(o);
+  return !(*out == -1 && PyErr_Occurred());
+}
 static int as_float(PyObject* o, float* out) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) return 0;
@@ -168,12 +172,60 @@ static PyObject* decode_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
                                           scale, p[13], ws, p[14], p[15]));
 }
 
+/* cache, batch, norm, rope, q, q_stride, k, k_stride, v, v_stride, q_out, status, stream */
+static PyObject* qk_norm_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[13];
+  int64_t q_stride, k_stride, v_stride;
+  if (!want(n, 13)) return NULL;
+  if (!PTR(0) || !PTR(1) || !PTR(2) || !PTR(3) || !PTR(4) || !as_i64(a[5], &q_stride) || !PTR(6) || !as_i64(a[7], &k_stride) ||
+      !PTR(8) || !as_i64(a[9], &v_stride) || !PTR(10) || !PTR(11) || !PTR(12))
+    return NULL;
+  RETURN_STATUS(efim_qk_norm_append(p[0], p[1], p[2], p[3], p[4], q_stride, p[6], k_stride, p[8], v_stride, p[10], p[11], p[12]));
+}
+
+/* batch, history, stride, max_len, len, min_ngram, max_ngram, num_drafts, drafts, draft_len, status, stream */
+static PyObject* draft_lookup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[12];
+  int64_t stride;
+  int32_t batch, max_len, lo, hi, num;
+  if (!want(n, 12)) return NULL;
+  if (!as_i32(a[0], &batch) || !PTR(1) || !as_i64(a[2], &stride) || !as_i32(a[3], &max_len) || !PTR(4) || !as_i32(a[5], &lo) ||
+      !as_i32(a[6], &hi) || !as_i32(a[7], &num) || !PTR(8) || !PTR(9) || !PTR(10) || !PTR(11))
+    return NULL;
+  RETURN_STATUS(efim_draft_lookup(batch, p[1], stride, max_len, p[4], lo, hi, num, p[8], p[9], p[10], p[11]));
+}
+
+/* batch, rows, vocab, kind, row_indptr, tokens, target, stride, draft_probs, stride, uniform, noise, stride, temperature, accepted,
+   next_token, out_tokens, out_logprobs, out_stride, status, stream */
+static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[21];
+  efim_verify_desc d;
+  int32_t out_stride;
+  if (!want(n, 21)) return NULL;
+  if (!as_i32(a[0], &d.batch) || !as_i32(a[1], &d.total_rows) || !as_i32(a[2], &d.vocab) || !as_i32(a[3], &d.target_kind) ||
+      !PTR(4) || !PTR(5) || !PTR(6) || !as_i64(a[7], &d.target_stride) || !PTR(8) || !as_i64(a[9], &d.draft_stride) || !PTR(10) ||
+      !PTR(11) || !as_i64(a[12], &d.noise_stride) || !PTR(13) || !PTR(14) || !PTR(15) || !PTR(16) || !PTR(17) ||
+      !as_i32(a[18], &out_stride) || !PTR(19) || !PTR(20))
+    return NULL;
+  d.d_row_indptr = p[4];
+  d.d_tokens = p[5];
+  d.d_target = p[6];
+  d.d_draft_probs = p[8];
+  d.d_uniform = p[10];
+  d.d_noise = p[11];
+  d.d_temperature = p[13];
+  RETURN_STATUS(efim_verify_drafts(&d, p[14], p[15], p[16], p[17], out_stride, p[19], p[20]));
+}
+
 static PyMethodDef methods[] = {
     {"kv_append", (PyCFunction)(void*)kv_append, METH_FASTCALL, NULL},
     {"append_prefill_attn", (PyCFunction)(void*)append_prefill_attn, METH_FASTCALL, NULL},
     {"append_prefill_step", (PyCFunction)(void*)append_prefill_step, METH_FASTCALL, NULL},
     {"decode_attn", (PyCFunction)(void*)decode_attn, METH_FASTCALL, NULL},
     {"decode_step", (PyCFunction)(void*)decode_step, METH_FASTCALL, NULL},
+    {"qk_norm_append", (PyCFunction)(void*)qk_norm_append, METH_FASTCALL, NULL},
+    {"draft_lookup", (PyCFunction)(void*)draft_lookup, METH_FASTCALL, NULL},
+    {"verify_drafts", (PyCFunction)(void*)verify_drafts, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

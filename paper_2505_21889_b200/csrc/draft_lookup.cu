@@ -1,0 +1,115 @@
+// efim_draft_lookup: drafts from a sequence's own history (infilled code repeats its prefix and suffix).  The place e of the
+// history whose preceding tokens agree longest with the history's last ones - up to max_ngram tokens, the latest such place - is
+// taken as what comes next:
+//   e* = argmax over 1 <= e < len of (min(max_ngram, |common suffix of T[0, e) and T[0, len)|), e),   draft_i = T[e* + i mod (len - e*)]
+// (the draft goes on with itself where it reaches the end of the history, as a repetition does).
+//
+// A cluster per sequence; the scan is for the last token, 16 bytes a load, and only places behind it look further back.
+#include "cluster.cuh"
+
+namespace efim {
+
+constexpr int LOOKUP_THREADS = 512;
+constexpr int LOOKUP_MAX_CTAS = 8;
+constexpr int LOOKUP_MAX_NGRAM = 32;
+
+struct LookupParams {
+  const int32_t* history;   // rows of [max_len], stride elements apart
+  const int32_t* len;       // [batch]
+  int32_t* drafts;          // [batch][num_drafts]
+  int32_t* draft_len;       // [batch]
+  int32_t* status;
+  long long stride;
+  int batch, max_len, min_ngram, max_ngram, num_drafts;
+};
+
+__global__ void __launch_bounds__(LOOKUP_THREADS) draft_lookup_kernel(const LookupParams p) {
+  __shared__ int s_tail[LOOKUP_MAX_NGRAM];
+  __shared__ unsigned long long s_key[LOOKUP_THREADS / 32];
+  __shared__ unsigned long long s_keys[LOOKUP_MAX_CTAS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
+  const int s = blockIdx.x / ctas;
+  cluster_arrive();
+  pdl_wait();
+  pdl_launch();
+  const int32_t* T = p.history + s * p.stride;
+  int len = *(p.len + s);
+  if (len < 0 || len > p.max_len) {
+    if (rank == 0 && tid == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_POSITION);
+    len = len < 0 ? 0 : p.max_len;
+  }
+  if (tid < LOOKUP_MAX_NGRAM) s_tail[tid] = tid < len ? T[len - 1 - tid] : 0;
+  cluster_wait();
+  __syncthreads();
+  // key: agreeing tokens, then the place
+  unsigned long long key = 0;
+  const int n = len - 1;                               // tokens that something comes after
+  if (n > 0) {
+    const int last = s_tail[0];
+    auto look = [&](int token, int at) {
+      if (token != last) return;
+      int m = 1;
+      while (m < p.max_ngram && m <= at && T[at - m] == s_tail[m]) ++m;
+      if (m >= p.min_ngram) key = max(key, (unsigned long long)m << 32 | (uint32_t)(at + 1));
+    };
+    const int lead = min(n, (int)(((16 - (reinterpret_cast<uintptr_t>(T) & 15)) & 15) / 4));
+    const int n_vec = (n - lead) / 4, tail = lead + n_vec * 4;
+    const int id = rank * LOOKUP_THREADS + tid, lanes = ctas * LOOKUP_THREADS;
+    if (id < lead) look(T[id], id);
+    if (tail + id < n) look(T[tail + id], tail + id);
+    const int4* vec = reinterpret_cast<const int4*>(T + lead);
+    constexpr int U = 4;
+    for (int v0 = id; v0 < n_vec; v0 += U * lanes) {
+      int4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * lanes < n_vec) w[u] = vec[v0 + u * lanes];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (v0 + u * lanes >= n_vec) break;
+        const int at = lead + (v0 + u * lanes) * 4;
+        look(w[u].x, at);
+        look(w[u].y, at + 1);
+        look(w[u].z, at + 2);
+        look(w[u].w, at + 3);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, d));
+  if (lane == 0) s_key[warp] = key;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < LOOKUP_THREADS / 32; ++w) key = max(key, s_key[w]);
+    store_remote(remote_smem(&s_keys[rank], 0), key);
+  }
+  cluster_sync();
+  if (rank != 0) return;
+  key = s_keys[0];
+  for (int k = 1; k < ctas; ++k) key = max(key, s_keys[k]);
+  const int e = (int)(uint32_t)key;
+  for (int i = tid; i < p.num_drafts; i += LOOKUP_THREADS)
+    p.drafts[(size_t)s * p.num_drafts + i] = key ? T[e + i % (len - e)] : -1;
+  if (tid == 0) p.draft_len[s] = key ? p.num_drafts : 0;
+}
+
+}  // namespace efim
+
+extern "C" efim_status efim_draft_lookup(int32_t batch, const int32_t* d_history, int64_t history_stride, int32_t max_len,
+                                         const int32_t* d_len, int32_t min_ngram, int32_t max_ngram, int32_t num_drafts,
+                                         int32_t* d_drafts, int32_t* d_draft_len, int32_t* d_status, void* stream) {
+  using namespace efim;
+  if (batch < 0 || max_len <= 0 || history_stride < max_len || num_drafts <= 0) return EFIM_ERR_INVALID_ARG;
+  if (min_ngram < 1 || max_ngram < min_ngram) return EFIM_ERR_INVALID_ARG;
+  if (max_ngram > LOOKUP_MAX_NGRAM) return EFIM_ERR_UNSUPPORTED;
+  if (batch == 0) return EFIM_OK;
+  if (!d_history || !d_len || !d_drafts || !d_draft_len || (reinterpret_cast<uintptr_t>(d_history) & 3)) return EFIM_ERR_INVALID_ARG;
+  LookupParams p{d_history, d_len, d_drafts, d_draft_len, d_status, history_stride, batch, max_len, min_ngram, max_ngram, num_drafts};
+  unsigned ctas = LOOKUP_MAX_CTAS;
+  while (ctas > 1 && ((long long)batch * ctas > 4LL * sm_count() || max_len / (int)ctas < 2048)) ctas /= 2;
+  if ((long long)batch * ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  EFIM_CUDA_TRY(launch_clusters(draft_lookup_kernel, ctas, dim3(batch * ctas), dim3(LOOKUP_THREADS),
+                                static_cast<cudaStream_t>(stream), p));
+  return EFIM_OK;
+}

@@ -3,6 +3,7 @@
 // they follow `<P>prefix<S>suffix<M>`, so token i of sequence s has position
 // cached_len[s] + i).  Pure streaming: every byte is read once and written once.
 #include "kv_append.cuh"
+#include "token_place.cuh"
 #include <math.h>
 
 namespace efim {
@@ -88,22 +89,8 @@ __global__ void __launch_bounds__(KV_APPEND_THREADS, 4) kv_append_kernel(const K
     if (p.cos_sin) fetch_heads(h0);
     fetch_copy(vin, lane);
   }
-  // sequence of this token: the last one that starts at or before t, one of [lo, lo + n)
-  int lo = 0, n = p.batch;
-  while (n > 32) {
-    const int step = (n + 31) / 32;
-    const bool le = wl * step < n && *(p.q_indptr + lo + wl * step) <= t;
-    const int i = 31 - __clz((int)(__ballot_sync(0xffffffffu, le) | 1u));
-    n = min(step, n - i * step);
-    lo += i * step;
-  }
-  int first = 0, cached = 0;
-  if (wl < n) {
-    first = *(p.q_indptr + lo + wl);
-    cached = *(p.cached_len + lo + wl);
-  }
-  const int i_seq = 31 - __clz((int)(__ballot_sync(0xffffffffu, wl < n && first <= t) | 1u));
-  const int pos = __shfl_sync(0xffffffffu, cached, i_seq) + t - __shfl_sync(0xffffffffu, first, i_seq);
+  const TokenPlace at = find_token(p.q_indptr, p.cached_len, p.batch, t, wl);
+  const int pos = at.pos;
   const int page_idx = pos >> 4;
   const bool in_table = !p.cos_sin || (pos >= 0 && pos < p.max_position);
   int err = 0, page = 0;
@@ -112,7 +99,7 @@ __global__ void __launch_bounds__(KV_APPEND_THREADS, 4) kv_append_kernel(const K
     if (!EVERY_ROW) return;
     err = EFIM_DEV_BAD_POSITION;
   } else {
-    page = *(p.block_table + (size_t)(lo + i_seq) * p.max_pages_per_seq + page_idx);
+    page = *(p.block_table + (size_t)at.seq * p.max_pages_per_seq + page_idx);
   }
   // rotary values: position j of the row's halves (8 of either), or the 4 pairs of vector j
   float c[8], sn[8];
