@@ -355,7 +355,9 @@ efim_status efim_draft_lookup(int32_t batch, const int32_t* d_history, int64_t h
  * Results: d_accepted[s] drafts, d_next_token[s]; optionally out_stride entries a sequence of the tokens it goes on with (accepted drafts,
  * next, then -1) and their natural log-probabilities in p (at temperature 1 where greedy; 0 past the end).  A
  * sequence without rows accepts 0 and gets next -1.  The k/v of a sequence's first d_accepted[s] + 1 new tokens stay valid;
- * the next step's tokens overwrite the rest.  One kernel; no workspace; may be captured; the same inputs give the same bits.
+ * the next step's tokens overwrite the rest.  Two kernels; may be captured; the same inputs give the same bits.  Workspace: 256-byte
+ * aligned, exclusively this call's until the stream has passed it; efim_verify_workspace_bytes() bytes serve every call with no more
+ * sequences, rows and places.
  */
 #define EFIM_TARGET_LOGITS_BF16  0
 #define EFIM_TARGET_LOGITS_F32   1
@@ -376,9 +378,10 @@ typedef struct {
   int64_t noise_stride;
   const float* d_temperature;    /* [batch], or NULL: 1 */
 } efim_verify_desc;
+size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab);
 efim_status efim_verify_drafts(const efim_verify_desc* desc, int32_t* d_accepted, int32_t* d_next_token,
-                               int32_t* d_out_tokens, float* d_out_logprobs, int32_t out_stride, int32_t* d_status,
-                               void* stream);
+                               int32_t* d_out_tokens, float* d_out_logprobs, int32_t out_stride,
+                               void* d_workspace, size_t workspace_bytes, int32_t* d_status, void* stream);
 
 /*
  * Self-test of the bounded device wait (the paper has no counterpart).  Every wait inside

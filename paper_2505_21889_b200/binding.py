@@ -56,7 +56,7 @@ EXPORTS = ("efim_last_cuda_error", "efim_strerror", "efim_version", "efim_rope_t
            "efim_prefill_launch_count", "efim_decode_launch_count",
            "efim_prefill_plan_bytes", "efim_prefill_plan", "efim_append_prefill_attn_planned", "efim_decode_step",
            "efim_append_prefill_step", "efim_selftest_bounded_wait",
-           "efim_qk_norm_append", "efim_draft_lookup", "efim_verify_drafts",
+           "efim_qk_norm_append", "efim_draft_lookup", "efim_verify_workspace_bytes", "efim_verify_drafts",
            "efim_fragment_cuts", "efim_fim_split", "efim_fim_fragment_spans",
            "efim_frontend_create", "efim_frontend_destroy", "efim_frontend_transform", "efim_frontend_admit",
            "efim_frontend_finish", "efim_frontend_stats")
@@ -110,7 +110,9 @@ def load_library():
                                       c_void_p, c_void_p, c_void_p]
     lib.efim_verify_drafts.restype = ctypes.c_int
     lib.efim_verify_drafts.argtypes = [POINTER(_VerifyDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
-                                       c_void_p]
+                                       c_size_t, c_void_p, c_void_p]
+    lib.efim_verify_workspace_bytes.restype = c_size_t
+    lib.efim_verify_workspace_bytes.argtypes = [c_int32, c_int32, c_int32]
     lib.efim_selftest_bounded_wait.restype = ctypes.c_int
     lib.efim_selftest_bounded_wait.argtypes = [ctypes.c_uint64, c_void_p, c_void_p, c_void_p]
     lib.efim_decode_workspace_bytes.restype = c_size_t
@@ -348,18 +350,30 @@ def efim_draft_lookup(history, lengths, min_ngram, max_ngram, drafts, draft_len,
         raise EfimError(st, "efim_draft_lookup")
 
 
+def efim_verify_workspace_bytes(batch: int, total_rows: int, vocab: int) -> int:
+    return int(load_library().efim_verify_workspace_bytes(batch, total_rows, vocab))
+
+
 def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform=None, noise=None, draft_probs=None,
-                       temperature=None, target_is_probs=False, out_tokens=None, out_logprobs=None, status=None, stream=None):
+                       temperature=None, target_is_probs=False, out_tokens=None, out_logprobs=None, workspace=None, status=None,
+                       stream=None):
     """Accepted drafts and next token of every sequence of a step.  target: [rows, vocab] logits in bf16 or fp32, or with
     `target_is_probs` probabilities in fp32; draft_probs fp32 [rows, vocab]; noise fp32 [batch, vocab] (none: greedy);
-    out_tokens and out_logprobs: packed [batch, n] of the same n."""
+    out_tokens and out_logprobs: packed [batch, n] of the same n.  Without a workspace one is taken from torch's allocator, on
+    torch's current stream, which the call then has to run on."""
+    batch = row_indptr.shape[0] - 1
     rows, vocab = target.shape
     kind = 2 if target_is_probs else 0 if target.element_size() == 2 else 1
     strides = [_matrix_stride(x, vocab) for x in (target, draft_probs, noise)]
     out = out_tokens if out_tokens is not None else out_logprobs
-    st = _calls.verify_drafts(row_indptr.shape[0] - 1, rows, vocab, kind, row_indptr, tokens, target, strides[0], draft_probs,
-                              strides[1], uniform, noise, strides[2], temperature, accepted, next_token, out_tokens, out_logprobs,
-                              out.shape[1] if out is not None else 0, status, _stream_ptr(stream))
+    if workspace is None:
+        if stream is not None and _stream_ptr(stream) != _current_stream():
+            raise ValueError("a call on another stream than torch's current one brings its workspace along")
+        torch = _torch()
+        workspace = torch.empty(efim_verify_workspace_bytes(batch, rows, vocab), dtype=torch.uint8, device=target.device)
+    st = _calls.verify_drafts(batch, rows, vocab, kind, row_indptr, tokens, target, strides[0], draft_probs, strides[1], uniform,
+                              noise, strides[2], temperature, accepted, next_token, out_tokens, out_logprobs,
+                              out.shape[1] if out is not None else 0, workspace, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_verify_drafts")
 

@@ -196,16 +196,17 @@ static PyObject* draft_lookup(PyObject* self, PyObject* const* a, Py_ssize_t n) 
 }
 
 /* batch, rows, vocab, kind, row_indptr, tokens, target, stride, draft_probs, stride, uniform, noise, stride, temperature, accepted,
-   next_token, out_tokens, out_logprobs, out_stride, status, stream */
+   next_token, out_tokens, out_logprobs, out_stride, workspace, status, stream */
 static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[21];
+  void* p[22];
   efim_verify_desc d;
   int32_t out_stride;
-  if (!want(n, 21)) return NULL;
+  size_t ws;
+  if (!want(n, 22)) return NULL;
   if (!as_i32(a[0], &d.batch) || !as_i32(a[1], &d.total_rows) || !as_i32(a[2], &d.vocab) || !as_i32(a[3], &d.target_kind) ||
       !PTR(4) || !PTR(5) || !PTR(6) || !as_i64(a[7], &d.target_stride) || !PTR(8) || !as_i64(a[9], &d.draft_stride) || !PTR(10) ||
       !PTR(11) || !as_i64(a[12], &d.noise_stride) || !PTR(13) || !PTR(14) || !PTR(15) || !PTR(16) || !PTR(17) ||
-      !as_i32(a[18], &out_stride) || !PTR(19) || !PTR(20))
+      !as_i32(a[18], &out_stride) || !as_workspace(a[19], &p[19], &ws) || !PTR(20) || !PTR(21))
     return NULL;
   d.d_row_indptr = p[4];
   d.d_tokens = p[5];
@@ -214,7 +215,7 @@ static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n)
   d.d_uniform = p[10];
   d.d_noise = p[11];
   d.d_temperature = p[13];
-  RETURN_STATUS(efim_verify_drafts(&d, p[14], p[15], p[16], p[17], out_stride, p[19], p[20]));
+  RETURN_STATUS(efim_verify_drafts(&d, p[14], p[15], p[16], p[17], out_stride, p[19], ws, p[20], p[21]));
 }
 
 static PyMethodDef methods[] = {

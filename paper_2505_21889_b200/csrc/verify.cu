@@ -2,24 +2,22 @@
 //
 // Row i of a sequence holds the target's distribution p_i after the step's token i; the draft it judges is token i + 1, drawn from
 // q_i (or with certainty).  With u_i uniform in [0, 1) and e exponential, all given:
-//   draft x is accepted  iff  u_i q_i(x) < p_i(x)                     (then its distribution is min(p, q) in that branch)
+//   draft x is accepted  iff  u_i q_i(x) < p_i(x)
 //   at the first row that accepts nothing, or the last one: next = argmax_j r_j / e_j,  r = (p - q)^+ or, behind the last draft, p
-// (argmax_j r_j / e_j is a draw from r / sum r: the smallest of exponential times with rates r_j.)  Together the emitted tokens are
+// (argmax_j r_j / e_j is a draw from r / sum r: the first of exponential times with rates r_j).  Together the emitted tokens are
 // distributed as if the target had been sampled token by token.  At temperature 0: accepted while the draft is the row's argmax.
 //
-// One thread-block cluster per sequence, each CTA with a slice of the vocabulary.  It walks the rows until one refuses, so what
-// lies behind a refusal is not read; per group of rows the CTAs swap their (maximum, sum, argmax) through distributed shared
-// memory and all of them decide alike.  The race for the next token then runs over the slices of that one row, which its CTAs
-// have just read (L2).  No workspace, nothing kept between calls.
-#include "cluster.cuh"
+// Two kernels.  The first takes every row's maximum and sum (its mass), a piece of a row per CTA.  The second has CTAs for pieces of the
+// vocabulary of every sequence: each joins the masses, finds the row at which its sequence stops and runs its piece of the race
+// for the next token there; the last of them to finish writes the result.
+#include "common.cuh"
 #include <float.h>
+#include <algorithm>
 
 namespace efim {
 
-constexpr int VERIFY_THREADS = 512;
+constexpr int VERIFY_THREADS = 256;
 constexpr int VERIFY_WARPS = VERIFY_THREADS / 32;
-constexpr int VERIFY_MAX_CTAS = 8;       // of a cluster
-constexpr int VERIFY_MAX_GROUP = 8;      // rows that are looked at together
 
 struct VerifyParams {
   const void* target;       // rows of [vocab], target_stride elements apart
@@ -34,8 +32,13 @@ struct VerifyParams {
   int32_t* out_tokens;      // [batch][out_stride] or null
   float* out_logprobs;      // the same
   int32_t* status;
+  uint4* part;              // [total_rows][pieces]: maximum, sum, place of the maximum
+  unsigned long long* key;  // [batch] best of the race so far
+  int* done;                // [batch] pieces of the race that are through
   long long target_stride, draft_stride, noise_stride;
-  int batch, total_rows, vocab, out_stride, group;
+  int batch, total_rows, vocab, out_stride;
+  int piece, pieces;        // places of a CTA of the first kernel, CTAs of a row
+  int race_piece, race_pieces;   // places of a CTA of the second, CTAs of a sequence
 };
 
 enum { TARGET_BF16 = EFIM_TARGET_LOGITS_BF16, TARGET_F32 = EFIM_TARGET_LOGITS_F32, TARGET_PROBS = EFIM_TARGET_PROBS_F32 };
@@ -51,6 +54,18 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// maximum over the warp; NaN lanes do not count
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Mass of a row's values seen so far: the largest, the sum of 2^((x - m) c), and the first place of the largest (where asked for).
 // A NaN among the values makes the sum NaN; values of -inf have no mass; at +inf those values share all of it.
 struct Mass {
@@ -61,347 +76,479 @@ __device__ __forceinline__ float weight_of(float x, float m, float c) {
   if (m == INFINITY) return x == INFINITY ? 1.f : x == x ? 0.f : x;
   return exp2_fast((x - (m == -INFINITY ? 0.f : m)) * c);
 }
-__device__ __forceinline__ void join(Mass& a, const Mass& b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == -INFINITY) {
-    a.l += b.l;                                       // 0, or NaN
-  } else {
-    const float fa = weight_of(a.m, m, c), fb = weight_of(b.m, m, c);
-    a.l = fmaf(a.l, fa, b.l * fb);
+// The lanes' masses together, in every lane.
+__device__ __forceinline__ Mass warp_join(Mass s, float c, bool want_at) {
+  Mass r{warp_max(s.m), 0.f, 0x7fffffff};
+  r.l = s.l * weight_of(s.m, r.m, c);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) r.l += __shfl_xor_sync(0xffffffffu, r.l, d);
+  if (want_at) r.at = (int)__reduce_min_sync(0xffffffffu, s.m == r.m ? (unsigned)s.at : 0x7fffffffu);
+  return r;
+}
+__device__ __forceinline__ void raise(Mass& s, float top, float c) {
+  if (s.m != -INFINITY) s.l *= weight_of(s.m, top, c);
+  s.m = top;
+}
+__device__ __forceinline__ void add_value(Mass& s, float x, int at, float c) {
+  if (x > s.m) {
+    raise(s, x, c);
+    s.at = at;
   }
-  if (b.m > a.m || (b.m == a.m && b.at < a.at)) a.at = b.at;
-  a.m = m;
+  s.l += weight_of(x, s.m, c);
 }
 
-// Adds `N` values, value e standing at place at0 + e.
-template <int N>
-__device__ __forceinline__ void add_values(Mass& s, const float* x, int at0, int place_step, int per_vec, float c, bool want_at) {
-  float top = x[0];
+// The 16 bytes of a vector, as its values
+template <typename T>
+__device__ __forceinline__ void values_of(const uint4& w, float* x) {
+  const uint32_t q[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
-  if (top > s.m) {
-    if (s.m != -INFINITY) s.l *= weight_of(s.m, top, c);
-    s.m = top;
-    if (want_at) {
-      int at = 0x7fffffff;
-#pragma unroll
-      for (int e = N - 1; e >= 0; --e)
-        if (x[e] == top) at = at0 + (e / per_vec) * place_step + e % per_vec;
-      s.at = at;
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) {
+      x[2 * e] = bf16lo(q[e]);
+      x[2 * e + 1] = bf16hi(q[e]);
+    } else {
+      x[e] = __uint_as_float(q[e]);
     }
   }
-  if (s.m == INFINITY) {
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ float top_of(const uint4* w, int n) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t m = w[0].x;
 #pragma unroll
-    for (int e = 0; e < N; ++e) s.l += weight_of(x[e], s.m, c);
+    for (int u = 0; u < n; ++u) m = max_bf16x2(max_bf16x2(max_bf16x2(m, w[u].x), w[u].y), max_bf16x2(w[u].z, w[u].w));
+    return fmaxf(bf16lo(m), bf16hi(m));
   } else {
-    const float m = s.m == -INFINITY ? 0.f : s.m;
+    float m = __uint_as_float(w[0].x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) s.l += exp2_fast((x[e] - m) * c);
+    for (int u = 0; u < n; ++u)
+      m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(w[u].x)), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
+    return m;
   }
 }
 
-// The mass of places [begin, end) of a row, by `lanes` lanes; this is lane `id` of them.
+// The mass of places [begin, end) of a row, by `lanes` lanes; this is lane `id` of them.  Places are seen in rising order by each lane.
 template <typename T>
 __device__ __forceinline__ Mass row_mass(const T* row, int begin, int end, int id, int lanes, float c, bool want_at) {
-  constexpr int EPV = 16 / sizeof(T), U = 4;          // values of a 16-byte vector, vectors in flight
+  constexpr int EPV = 16 / sizeof(T), U = 8;          // values of a 16-byte vector, vectors in flight
   Mass s{-INFINITY, 0.f, 0x7fffffff};
   if (begin >= end) return s;
   const int n = end - begin;
   const T* p = row + begin;
   const int lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
   const int n_vec = (n - lead) / EPV, tail = lead + n_vec * EPV;
-  if (id < lead) {
-    const float x = as_float(p[id]);
-    add_values<1>(s, &x, begin + id, 0, 1, c, want_at);
-  }
+  if (id < lead) add_value(s, as_float(p[id]), begin + id, c);
   const uint4* vec = reinterpret_cast<const uint4*>(p + lead);
   for (int v0 = id; v0 < n_vec; v0 += U * lanes) {
     uint4 w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (v0 + u * lanes < n_vec) {
-        w[u] = ldg_stream(vec + v0 + u * lanes);
-      } else {
-        const uint32_t low = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // -inf
-        w[u] = make_uint4(low, low, low, low);
-      }
+      const uint32_t low = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;     // -inf
+      w[u] = make_uint4(low, low, low, low);
+      if (v0 + u * lanes < n_vec) w[u] = ldg_stream(vec + v0 + u * lanes);
     }
-    float x[U * EPV];
+    const float top = top_of<T>(w, U);
+    if (top > s.m) {
+      raise(s, top, c);
+      if (want_at) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t q[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+        for (int u = U - 1; u >= 0; --u) {
+          float x[EPV];
+          values_of<T>(w[u], x);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (sizeof(T) == 2) {
-          x[u * EPV + 2 * e] = bf16lo(q[e]);
-          x[u * EPV + 2 * e + 1] = bf16hi(q[e]);
-        } else {
-          x[u * EPV + e] = __uint_as_float(q[e]);
+          for (int e = EPV - 1; e >= 0; --e)
+            if (x[e] == top) s.at = begin + lead + (v0 + u * lanes) * EPV + e;
         }
       }
     }
-    add_values<U * EPV>(s, x, begin + lead + v0 * EPV, lanes * EPV, EPV, c, want_at);
+    const float m = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (v0 + u * lanes >= n_vec) break;
+      float x[EPV];
+      values_of<T>(w[u], x);
+      if (s.m == INFINITY) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) s.l += weight_of(x[e], s.m, c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) s.l += exp2_fast((x[e] - m) * c);
+      }
+    }
   }
-  if (tail + id < n) {                                // fewer than a vector's
-    const float x = as_float(p[tail + id]);
-    add_values<1>(s, &x, begin + tail + id, 0, 1, c, want_at);
-  }
+  if (tail + id < n) add_value(s, as_float(p[tail + id]), begin + tail + id, c);      // fewer than a vector's
   return s;
 }
 
-// Times of the race: the largest r / e wins, the lowest place among equals.  0 for places that cannot win.
-__device__ __forceinline__ unsigned long long race_key(float r, float e, int at) {
-  const float t = r / e;
-  return r > 0.f && t > 0.f ? (unsigned long long)__float_as_uint(t) << 32 | (0xffffffffu - (uint32_t)at) : 0ull;
+// Probabilities of one row, from its logits or as they are.
+template <int KIND>
+struct Row {
+  float m, l, inv;
+  __device__ __forceinline__ float exact(float x) const {
+    if (KIND == TARGET_PROBS) return x;
+    return (m == INFINITY ? (x == INFINITY ? 1.f : 0.f) : expf((x - m) * inv)) / l;
+  }
+};
+
+// The race for the next token over places [begin, end) of a row: the largest r / e, r = (p - q)^+ or p, the lowest place among
+// equals.  `gone` is a place that does not take part.  Returns (r / e, place) as one number to be compared, 0 if nobody ran.
+//
+// An exact result costs two divisions and an exponential.  So every place gets a bound from above first, by the fast instructions (for
+// probabilities down to 2^-149 the exponent's two roundings are 150 * 2^-23 * ln 2, ex2 and rcp 2^-22 each, together below 2^-16),
+// and only places whose bound reaches the warp's best result so far are computed: a few a warp.
+constexpr float RACE_ABOVE = 1.f + 1.f / 65536;
+template <int KIND, bool VEC>
+__device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>::type* row, const float* noise, const float* q,
+                                                   int begin, int end, int gone, const Row<KIND>& of, float c) {
+  constexpr int N = 8;                                // places of a thread in flight: two groups of four, or eight apart
+  using T = typename TargetOf<KIND>::type;
+  const int tid = threadIdx.x;
+  const float m = of.m == INFINITY ? 0.f : of.m;      // (an infinite maximum: bounds of infinity, so everything is computed)
+  const float scale = KIND == TARGET_PROBS ? RACE_ABOVE : of.m == INFINITY ? INFINITY : RACE_ABOVE / of.l;
+  unsigned long long key = 0;
+  float best = 0.f;                                   // the warp's
+  auto place = [&](int a0, int i) { return VEC ? a0 + (i / 4) * 4 * VERIFY_THREADS + i % 4 : a0 + i * VERIFY_THREADS; };
+  const int first = begin + (VEC ? 4 * tid : tid);
+  // whole warps stay together: the first lane's place decides
+  for (int a0 = first; a0 - (VEC ? 4 : 1) * (tid & 31) < end; a0 += N * VERIFY_THREADS) {
+    float x[N], e[N], qx[N];
+    if constexpr (VEC) {
+#pragma unroll
+      for (int g = 0; g < N / 4; ++g) {
+        const int at = place(a0, 4 * g);
+        if (at < end) {
+          if constexpr (sizeof(T) == 2) {
+            const uint2 w = *reinterpret_cast<const uint2*>(row + at);
+            x[4 * g] = bf16lo(w.x);
+            x[4 * g + 1] = bf16hi(w.x);
+            x[4 * g + 2] = bf16lo(w.y);
+            x[4 * g + 3] = bf16hi(w.y);
+          } else {
+            *reinterpret_cast<float4*>(x + 4 * g) = *reinterpret_cast<const float4*>(row + at);
+          }
+          const uint4 w = ldg_stream(noise + at);
+          *reinterpret_cast<uint4*>(e + 4 * g) = w;
+          if (q) *reinterpret_cast<uint4*>(qx + 4 * g) = ldg_stream(q + at);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int at = place(a0, i);
+        if (at < end) {
+          x[i] = as_float(row[at]);
+          e[i] = noise[at];
+          if (q) qx[i] = q[at];
+        }
+      }
+    }
+    float above[N], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      above[i] = 0.f;
+      if (place(a0, i) < end) {
+        const float p = KIND == TARGET_PROBS ? x[i] : exp2_fast((x[i] - m) * c);
+        const float r = q ? fmaf(p, scale, -qx[i]) : p * scale;
+        above[i] = r * rcp_fast(e[i]) * RACE_ABOVE;
+      }
+      top = fmaxf(top, above[i]);
+    }
+    // from the highest bound down, as long as they reach the best result
+    for (float highest; (highest = warp_max(top)) > 0.f && highest >= best;) {
+      float t = 0.f;
+      if (top == highest) {
+        int at = 0;
+        float px = 0.f, ex = 1.f, qq = 0.f;
+        bool found = false;
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (!found && above[i] == highest) {
+            found = true;
+            at = place(a0, i);
+            px = x[i];
+            ex = e[i];
+            if (q) qq = qx[i];
+            above[i] = 0.f;
+          }
+          top = fmaxf(top, above[i]);
+        }
+        const float r = of.exact(px) - qq;
+        if (r > 0.f && at != gone) {
+          t = r / ex;
+          if (t > 0.f) key = max(key, (unsigned long long)__float_as_uint(t) << 32 | (0xffffffffu - (uint32_t)at));
+        }
+      }
+      best = fmaxf(best, warp_max(t));
+    }
+  }
+  return key;
+}
+
+// Temperature of a sequence, as a factor of its logits; greedy sequences take 1.
+struct Scale {
+  float inv, c;             // 1 / T, and log2(e) / T
+  bool greedy;
+};
+__device__ __forceinline__ Scale scale_of(const VerifyParams& p, int s) {
+  Scale r{1.f, 0.f, !p.noise};
+  if (p.noise && p.temperature) {
+    const float t = *(p.temperature + s);
+    r.greedy = !(t > 0.f);
+    r.inv = r.greedy ? 1.f : fminf(1.f / t, FLT_MAX);
+  }
+  r.c = fminf(r.inv * 1.4426950408889634f, FLT_MAX);
+  return r;
+}
+
+// What the second kernel's CTAs of a sequence meet in.
+__global__ void __launch_bounds__(VERIFY_THREADS) verify_init_kernel(const VerifyParams p) {
+  pdl_wait();
+  pdl_launch();
+  for (int s = blockIdx.x * VERIFY_THREADS + threadIdx.x; s < p.batch; s += gridDim.x * VERIFY_THREADS) {
+    p.key[s] = 0;
+    p.done[s] = 0;
+  }
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const VerifyParams p) {
+  using T = typename TargetOf<KIND>::type;
+  __shared__ Mass s_warp[VERIFY_WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x / p.pieces, piece = blockIdx.x % p.pieces;
+  pdl_wait();
+  pdl_launch();
+  for (int s = blockIdx.x * VERIFY_THREADS + tid; s < p.batch; s += gridDim.x * VERIFY_THREADS) {
+    p.key[s] = 0;
+    p.done[s] = 0;
+  }
+  // the row's sequence, the last that starts at or before it, of whose rows the range must be one that the call was given
+  int lo = 0, n = p.batch;
+  while (n > 32) {
+    const int step = (n + 31) / 32;
+    const bool le = lane * step < n && *(p.row_indptr + lo + lane * step) <= r;
+    const int i = 31 - __clz((int)(__ballot_sync(0xffffffffu, le) | 1u));
+    n = min(step, n - i * step);
+    lo += i * step;
+  }
+  lo += 31 - __clz((int)(__ballot_sync(0xffffffffu, lane < n && *(p.row_indptr + lo + lane) <= r) | 1u));
+  const Scale sc = scale_of(p, lo);
+  const int begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
+  const Mass mass = warp_join(row_mass<T>(static_cast<const T*>(p.target) + r * p.target_stride, begin, end, tid, VERIFY_THREADS, sc.c,
+                                          sc.greedy), sc.c, sc.greedy);
+  if (lane == 0) s_warp[warp] = mass;
+  __syncthreads();
+  if (warp == 0) {
+    const Mass sum = warp_join(lane < VERIFY_WARPS ? s_warp[lane] : Mass{-INFINITY, 0.f, 0x7fffffff}, sc.c, sc.greedy);
+    if (lane == 0)
+      p.part[blockIdx.x] = make_uint4(__float_as_uint(sum.m), __float_as_uint(sum.l), sum.at, 0);
+  }
 }
 
 struct RowResult {
-  float m, l, draft_logprob;
-  int at, ok;
+  float m, l, logprob;      // of the row, and of its draft
+  int at, ok;               // place of the maximum; draft accepted: 1, refused: 0, refused for what it is: -1
 };
 
 template <int KIND>
-__global__ void __launch_bounds__(VERIFY_THREADS, 2) verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const VerifyParams p) {
   using T = typename TargetOf<KIND>::type;
-  __shared__ __align__(16) uint4 s_part[2][VERIFY_MAX_GROUP][VERIFY_MAX_CTAS];    // of every CTA of the cluster, by turns
-  __shared__ Mass s_warp[VERIFY_WARPS];
-  __shared__ RowResult s_row[VERIFY_MAX_GROUP];
-  __shared__ ulonglong2 s_key[VERIFY_WARPS];
-  __shared__ __align__(16) ulonglong2 s_keys[VERIFY_MAX_CTAS];
-  __shared__ int s_stop;
-
+  __shared__ RowResult s_row[VERIFY_WARPS];
+  __shared__ unsigned long long s_key[VERIFY_WARPS];
+  __shared__ bool s_last, s_empty;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t rank = cluster_rank(), ctas = cluster_size();
-  const int s = blockIdx.x / ctas;
-  cluster_arrive();
-  pdl_wait();
-  pdl_launch();
-  const int r0 = *(p.row_indptr + s), r1 = *(p.row_indptr + s + 1);
+  const int s = blockIdx.x / p.race_pieces, piece = blockIdx.x % p.race_pieces;
   const T* target = static_cast<const T*>(p.target);
+  // (the kernel before this one wrote none of the inputs, and whatever came before that one is complete)
+  const int r0 = *(p.row_indptr + s), r1 = *(p.row_indptr + s + 1);
   const bool rows_ok = r0 >= 0 && r1 <= p.total_rows && r0 <= r1;
   const int n = rows_ok ? r1 - r0 : 0;
-  // slices are whole multiples of 16 bytes of every operand, so that they are as aligned as the rows
-  const int slice = ((p.vocab + (int)ctas - 1) / (int)ctas + 63) & ~63;
-  const int begin = min(p.vocab, (int)rank * slice), end = min(p.vocab, begin + slice);
-  float inv = 1.f;
-  bool greedy = KIND != TARGET_PROBS && !p.noise;
-  if (KIND != TARGET_PROBS && p.noise && p.temperature) {
-    const float t = *(p.temperature + s);
-    greedy = !(t > 0.f);
-    inv = greedy ? 1.f : fminf(1.f / t, FLT_MAX);
-  }
-  const float c = fminf(inv * 1.4426950408889634f, FLT_MAX);
+  const Scale sc = KIND == TARGET_PROBS ? Scale{1.f, 1.f, false} : scale_of(p, s);
+  const bool first = piece == 0;
+  const int begin = piece * p.race_piece, end = min(p.vocab, begin + p.race_piece);
+  int32_t* out_tokens = p.out_tokens ? p.out_tokens + (size_t)s * p.out_stride : nullptr;
+  float* out_logprobs = p.out_logprobs ? p.out_logprobs + (size_t)s * p.out_stride : nullptr;
 
-  cluster_wait();
-
-  // ---- rows until one accepts nothing
-  int stop = n - 1, turn = 0, status = rows_ok ? 0 : EFIM_DEV_BAD_POSITION;
+  // ---- rows until one accepts nothing: a warp a row
+  int stop = -1, status = rows_ok ? 0 : EFIM_DEV_BAD_POSITION;
   RowResult last{};
-  if (KIND == TARGET_PROBS) {
-    // the rows' probabilities are there: only the drafts' are looked up
-    for (int i0 = 0; i0 < n - 1; i0 += VERIFY_THREADS) {
-      if (tid == 0) s_stop = n - 1;
-      __syncthreads();
-      const int i = i0 + tid;
-      bool bad = false;
-      float px = 0.f;
-      if (i < n - 1) {
-        const int x = *(p.tokens + r0 + i + 1);
-        bad = x < 0 || x >= p.vocab;
-        float q = 1.f;
-        if (!bad) {
-          px = as_float(target[(r0 + i) * p.target_stride + x]);
+  bool waited = false;
+  for (int i0 = 0; i0 < n && stop < 0; i0 += VERIFY_WARPS) {
+    const int i = i0 + warp;
+    int x = -1;
+    float u = 0.f, q = 1.f, value = -INFINITY;
+    bool inside = false;
+    if (i < n - 1) {
+      x = *(p.tokens + r0 + i + 1);
+      inside = x >= 0 && x < p.vocab;
+      if (inside) {
+        value = as_float(target[(r0 + i) * p.target_stride + x]);
+        if (!sc.greedy) {
+          u = *(p.uniform + r0 + i);
           if (p.draft_probs) q = p.draft_probs[(r0 + i) * p.draft_stride + x];
         }
-        if (!(*(p.uniform + r0 + i) * q < px)) atomicMin(&s_stop, i);
       }
-      __syncthreads();
-      stop = s_stop;
-      if (i < stop && rank == 0) {
-        if (p.out_logprobs && i < p.out_stride) p.out_logprobs[(size_t)s * p.out_stride + i] = logf(px);
-      }
-      if (i == stop && bad && rank == 0) status |= EFIM_DEV_BAD_TOKEN;
-      __syncthreads();
-      if (stop < n - 1) break;
     }
-  } else if (n > 0) {
-    int group = p.group;
-    while (group > 1 && group / 2 >= n) group /= 2;
-    const int per_row = VERIFY_WARPS / group;         // warps of a row
-    for (int i0 = 0; i0 < n; i0 += group, turn ^= 1) {
-      const int mine = i0 + warp / per_row;
-      Mass mass{-INFINITY, 0.f, 0x7fffffff};
-      if (mine < n)
-        mass = row_mass<T>(target + (r0 + mine) * p.target_stride, begin, end, (warp % per_row) * 32 + lane, per_row * 32, c, greedy);
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        const Mass o{__shfl_xor_sync(0xffffffffu, mass.m, d), __shfl_xor_sync(0xffffffffu, mass.l, d),
-                     __shfl_xor_sync(0xffffffffu, mass.at, d)};
-        join(mass, o, c);
-      }
-      if (lane == 0) s_warp[warp] = mass;
-      __syncthreads();
-      // warp w sends row w's mass of this slice to every CTA
-      if (warp < group) {
-        Mass sum = s_warp[warp * per_row];
-        for (int w = 1; w < per_row; ++w) join(sum, s_warp[warp * per_row + w], c);
-        if (lane < (int)ctas)
-          store_remote(remote_smem(&s_part[turn][warp][rank], lane),
-                       make_uint4(__float_as_uint(sum.m), __float_as_uint(sum.l), sum.at, 0));
-      }
-      // the draft's value and its distribution's, on their way meanwhile
-      const int i = i0 + warp;
-      int x = -1;
-      float u = 0.f, q = 1.f, logit = -INFINITY;
-      if (warp < group && i < n - 1) {
-        x = *(p.tokens + r0 + i + 1);
-        if (x >= 0 && x < p.vocab) {
-          logit = as_float(target[(r0 + i) * p.target_stride + x]);
-          if (!greedy) {
-            u = *(p.uniform + r0 + i);
-            if (p.draft_probs) q = p.draft_probs[(r0 + i) * p.draft_stride + x];
-          }
-        }
-      }
-      cluster_sync();
-      if (warp < group) {
+    if (!waited) pdl_wait();
+    waited = true;
+    if (i < n) {
+      RowResult row{0.f, 1.f, 0.f, 0, 0};
+      if (KIND == TARGET_PROBS) {
+        row.ok = i < n - 1 && inside && u * q < value;
+        row.logprob = logf(value);
+      } else {
         Mass sum{-INFINITY, 0.f, 0x7fffffff};
-        for (int k = 0; k < (int)ctas; ++k) {
-          const uint4 w = s_part[turn][warp][k];
-          join(sum, Mass{__uint_as_float(w.x), __uint_as_float(w.y), (int)w.z}, c);
+        for (int k = lane; k < p.pieces; k += 32) {
+          const uint4 w = *(p.part + (size_t)(r0 + i) * p.pieces + k);
+          const Mass o{__uint_as_float(w.x), __uint_as_float(w.y), (int)w.z};
+          const float m = fmaxf(sum.m, o.m);
+          sum.l = sum.l * weight_of(sum.m, m, sc.c) + o.l * weight_of(o.m, m, sc.c);
+          if (o.m > sum.m) sum.at = o.at;              // (a lane's places rise)
+          sum.m = m;
         }
-        if (lane == 0) {
-          const bool any = sum.l > 0.f;                // (not NaN either)
-          float px = 0.f;
-          if (any && logit != -INFINITY) px = (sum.m == INFINITY ? (logit == INFINITY ? 1.f : 0.f) : expf((logit - sum.m) * inv)) / sum.l;
-          RowResult r;
-          r.m = sum.m;
-          r.l = sum.l;
-          r.at = sum.at;
-          r.ok = i < n - 1 && any && (greedy ? sum.at == x : u * q < px);
-          r.draft_logprob = sum.m == INFINITY ? logf(px) : (logit - sum.m) * inv - logf(sum.l);
-          s_row[warp] = r;
-          if (i < n - 1 && (x < 0 || x >= p.vocab)) s_row[warp].ok = -1;    // refused for what it is
-        }
+        sum = warp_join(sum, sc.c, sc.greedy);
+        row.m = sum.m;
+        row.l = sum.l;
+        row.at = sum.at;
+        const bool any = sum.l > 0.f;                  // (and not NaN)
+        const float px = !any || value == -INFINITY ? 0.f : Row<KIND>{sum.m, sum.l, sc.inv}.exact(value);
+        row.ok = i < n - 1 && any && inside && (sc.greedy ? sum.at == x : u * q < px);
+        row.logprob = sum.m == INFINITY ? logf(px) : (value - sum.m) * sc.inv - logf(sum.l);
       }
-      __syncthreads();
-      int stopped = -1;
-      for (int k = 0; k < group && i0 + k < n; ++k) {
-        if (s_row[k].ok <= 0) {
-          stopped = k;
-          break;
-        }
-      }
-      const int good = stopped < 0 ? group : stopped;
-      if (rank == 0 && tid < good && p.out_logprobs && i0 + tid < p.out_stride)
-        p.out_logprobs[(size_t)s * p.out_stride + i0 + tid] = s_row[tid].draft_logprob;
-      if (stopped >= 0) {
-        stop = i0 + stopped;
-        last = s_row[stopped];
-        if (last.ok < 0) status |= EFIM_DEV_BAD_TOKEN;
-        break;
+      if (i < n - 1 && !inside) row.ok = -1;
+      if (lane == 0) s_row[warp] = row;
+    }
+    __syncthreads();
+    const int count = min(VERIFY_WARPS, n - i0);
+    int good = 0;
+    while (good < count && s_row[good].ok > 0) ++good;
+    if (good < count) {
+      stop = i0 + good;
+      last = s_row[good];
+      if (last.ok < 0) status |= EFIM_DEV_BAD_TOKEN;
+    }
+    if (first && out_logprobs && tid < good && i0 + tid < p.out_stride) out_logprobs[i0 + tid] = s_row[tid].logprob;
+    __syncthreads();
+  }
+  if (!waited) pdl_wait();
+  pdl_launch();
+  if (first) {
+    for (int i = tid; i < p.out_stride; i += VERIFY_THREADS) {
+      if (i < stop) {
+        if (out_tokens) out_tokens[i] = *(p.tokens + r0 + i + 1);
+      } else if (i > max(stop, 0)) {
+        if (out_tokens) out_tokens[i] = -1;
+        if (out_logprobs) out_logprobs[i] = 0.f;
       }
     }
   }
 
   // ---- the next token
-  unsigned long long key = 0, all = 0;                 // of what the draft leaves, of the target's distribution
-  const bool judged = stop >= 0 && stop < n - 1;       // the row refused a draft
+  const bool judged = stop < n - 1;                    // the row refused a draft
   const bool sound = n > 0 && (KIND == TARGET_PROBS || last.l > 0.f);
-  if (sound && !greedy) {
+  const bool runs = sound && !sc.greedy;
+  unsigned long long key = 0;
+  if (!runs) {
+    if (!first) return;
+  } else {
     const T* row = target + (r0 + stop) * p.target_stride;
     const float* noise = p.noise + s * p.noise_stride;
     const float* q = judged && p.draft_probs ? p.draft_probs + (r0 + stop) * p.draft_stride : nullptr;
-    const int gone = judged && !p.draft_probs ? *(p.tokens + r0 + stop + 1) : -1;
-    const float total = last.l;
-    auto probability = [&](float x) {
-      if (KIND == TARGET_PROBS) return x;
-      return (last.m == INFINITY ? (x == INFINITY ? 1.f : 0.f) : expf((x - last.m) * inv)) / total;
-    };
-    auto take = [&](float x, float e, float qx, int at) {
-      const float pr = probability(x);
-      const unsigned long long k = race_key(pr, e, at);
-      all = max(all, k);
-      if (q) key = max(key, race_key(pr - qx, e, at));
-      else if (at != gone) key = max(key, k);
-    };
-    constexpr int U = 4;
-    for (int a0 = begin + tid; a0 < end; a0 += U * VERIFY_THREADS) {
-      float x[U], e[U], qx[U];
+    int gone = judged && !p.draft_probs ? *(p.tokens + r0 + stop + 1) : -1;
+    const Row<KIND> of{last.m, last.l, sc.inv};
+    const bool aligned = !((reinterpret_cast<uintptr_t>(row) & (4 * sizeof(T) - 1)) | (reinterpret_cast<uintptr_t>(noise) & 15) |
+                           (reinterpret_cast<uintptr_t>(q) & 15));
+    auto run = [&](int a, int b) {                     // the whole CTA's best, in thread 0
+      const int whole = aligned ? a + ((b - a) & ~3) : a;
+      unsigned long long k = race<KIND, true>(row, noise, q, a, whole, gone, of, sc.c);
+      k = max(k, race<KIND, false>(row, noise, q, whole, b, gone, of, sc.c));
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = a0 + u * VERIFY_THREADS;
-        if (at < end) {
-          x[u] = as_float(row[at]);
-          e[u] = noise[at];
-          qx[u] = q ? q[at] : 0.f;
-        }
+      for (int d = 16; d > 0; d >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, d));
+      if (lane == 0) s_key[warp] = k;
+      __syncthreads();
+      if (tid == 0)
+        for (int w = 1; w < VERIFY_WARPS; ++w) k = max(k, s_key[w]);
+      return k;
+    };
+    key = run(begin, end);
+    // the CTAs of a sequence meet: the last one through has the best of all
+    if (p.race_pieces > 1) {
+      if (tid == 0) {
+        if (key) atomicMax(p.key + s, key);
+        __threadfence();
+        s_last = atomicAdd(p.done + s, 1) == p.race_pieces - 1;
+        __threadfence();
+        if (s_last) key = *(volatile unsigned long long*)(p.key + s);
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (a0 + u * VERIFY_THREADS < end) take(x[u], e[u], qx[u], a0 + u * VERIFY_THREADS);
+      __syncthreads();
+      if (!s_last) return;
     }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      key = max(key, __shfl_xor_sync(0xffffffffu, key, d));
-      all = max(all, __shfl_xor_sync(0xffffffffu, all, d));
-    }
-    if (lane == 0) s_key[warp] = make_ulonglong2(key, all);
+    // where the draft's distribution leaves nothing (rounding alone refused it): the target's own
+    if (tid == 0) s_empty = key == 0 && (q || gone >= 0);
     __syncthreads();
-    if (tid == 0) {
-      for (int w = 1; w < VERIFY_WARPS; ++w) {
-        key = max(key, s_key[w].x);
-        all = max(all, s_key[w].y);
-      }
-      store_remote(remote_smem(&s_keys[rank].x, 0), key);
-      store_remote(remote_smem(&s_keys[rank].y, 0), all);
-    }
-    cluster_sync();
-  }
-  if (rank != 0) return;
-  if (tid == 0) {
-    int next = -1;
-    if (sound && greedy) {
-      next = last.at;
-    } else if (sound) {
-      for (int k = 0; k < (int)ctas; ++k) {
-        key = max(key, s_keys[k].x);
-        all = max(all, s_keys[k].y);
-      }
-      if (!key) key = all;                             // the draft's distribution leaves nothing: rounding alone refused it
-      if (key) next = (int)(0xffffffffu - (uint32_t)key);
-    }
-    float logprob = 0.f;
-    if (next >= 0) {
-      const float x = as_float(target[(r0 + stop) * p.target_stride + next]);
-      logprob = KIND == TARGET_PROBS ? logf(x) : last.m == INFINITY ? -logf(last.l) : (x - last.m) * inv - logf(last.l);
-    } else if (n > 0) {
-      status |= EFIM_DEV_NO_TOKEN;
-    }
-    const int acc = max(stop, 0);
-    p.accepted[s] = acc;
-    p.next_token[s] = next;
-    if (acc < p.out_stride) {
-      if (p.out_tokens) p.out_tokens[(size_t)s * p.out_stride + acc] = next;
-      if (p.out_logprobs) p.out_logprobs[(size_t)s * p.out_stride + acc] = logprob;
-    }
-    if (status && p.status) atomicOr(p.status, status);
-  }
-  for (int i = tid; i < p.out_stride; i += VERIFY_THREADS) {
-    if (i < stop) {
-      if (p.out_tokens) p.out_tokens[(size_t)s * p.out_stride + i] = *(p.tokens + r0 + i + 1);
-    } else if (i > max(stop, 0)) {
-      if (p.out_tokens) p.out_tokens[(size_t)s * p.out_stride + i] = -1;
-      if (p.out_logprobs) p.out_logprobs[(size_t)s * p.out_stride + i] = 0.f;
+    if (s_empty) {
+      q = nullptr;
+      gone = -1;
+      key = run(0, p.vocab);
     }
   }
+  if (tid != 0) return;
+  int next = -1;
+  if (sound && sc.greedy) next = last.at;
+  if (key) next = (int)(0xffffffffu - (uint32_t)key);
+  float logprob = 0.f;
+  if (next >= 0) {
+    const float x = as_float(target[(r0 + stop) * p.target_stride + next]);
+    logprob = KIND == TARGET_PROBS ? logf(x) : last.m == INFINITY ? -logf(last.l) : (x - last.m) * sc.inv - logf(last.l);
+  } else if (n > 0) {
+    status |= EFIM_DEV_NO_TOKEN;
+  }
+  const int acc = max(stop, 0);
+  p.accepted[s] = acc;
+  p.next_token[s] = next;
+  if (acc < p.out_stride) {
+    if (out_tokens) out_tokens[acc] = next;
+    if (out_logprobs) out_logprobs[acc] = logprob;
+  }
+  if (status && p.status) atomicOr(p.status, status);
+}
+
+// Places of a piece and pieces of a row (or a sequence) of `vocab` places, where there are `rows` of them: as many as fill the GPU once
+// (4 CTAs an SM), of 2,048 to `most` places.
+struct Pieces {
+  int size, count;
+};
+static Pieces pieces_of(long long rows, int vocab, int most) {
+  const long long wave = 4LL * sm_count(), want = std::max<long long>(1, wave / std::max<long long>(rows, 1));
+  long long size = (vocab + want - 1) / want;
+  size = std::min<long long>(most, std::max<long long>(2048, size));
+  size = (size + 63) / 64 * 64;
+  return {(int)size, (int)((vocab + size - 1) / size)};
+}
+constexpr int MASS_MOST_BYTES = 32768, RACE_MOST = 8192;
+
+// The most that a call of at most these rows over at most this vocabulary cuts its rows into: one wave, or the largest pieces.
+static size_t part_bytes(long long rows, int vocab) {
+  const long long least = (vocab + MASS_MOST_BYTES / 4 - 1) / (MASS_MOST_BYTES / 4);
+  return ((size_t)std::max(4LL * sm_count() + rows, rows * least) * sizeof(uint4) + 255) / 256 * 256;
 }
 
 }  // namespace efim
 
+extern "C" size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab) {
+  if (batch <= 0 || total_rows < 0 || vocab <= 0) return 0;
+  return efim::part_bytes(total_rows, vocab) + (size_t)batch * 16;
+}
+
 extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_accepted, int32_t* d_next_token,
-                                          int32_t* d_out_tokens, float* d_out_logprobs, int32_t out_stride, int32_t* d_status,
-                                          void* stream) {
+                                          int32_t* d_out_tokens, float* d_out_logprobs, int32_t out_stride, void* d_workspace,
+                                          size_t workspace_bytes, int32_t* d_status, void* stream) {
   using namespace efim;
   if (!d || d->batch < 0 || d->total_rows < 0 || d->vocab <= 0) return EFIM_ERR_INVALID_ARG;
   if (d->target_kind < EFIM_TARGET_LOGITS_BF16 || d->target_kind > EFIM_TARGET_PROBS_F32) return EFIM_ERR_INVALID_ARG;
@@ -417,6 +564,8 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
     if (d->d_draft_probs && d->draft_stride < d->vocab) return EFIM_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(d->d_noise) | reinterpret_cast<uintptr_t>(d->d_draft_probs)) & 3) return EFIM_ERR_INVALID_ARG;
   }
+  if (!d_workspace || workspace_bytes < efim_verify_workspace_bytes(d->batch, d->total_rows, d->vocab)) return EFIM_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return EFIM_ERR_INVALID_ARG;
   VerifyParams p{};
   p.target = d->d_target;
   p.row_indptr = d->d_row_indptr;
@@ -437,17 +586,28 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   p.total_rows = d->total_rows;
   p.vocab = d->vocab;
   p.out_stride = d_out_tokens || d_out_logprobs ? out_stride : 0;
-  // as many CTAs a sequence as fill the GPU, of at least 2048 places each
-  const int slots = 2 * sm_count();
-  int ctas = VERIFY_MAX_CTAS;
-  while (ctas > 1 && ((long long)d->batch * ctas > 4LL * slots || d->vocab / ctas < 2048)) ctas /= 2;
-  p.group = (long long)d->batch * ctas <= slots ? VERIFY_MAX_GROUP : 1;
-  if ((long long)d->batch * ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
-  auto launch = [&](auto kernel) {
-    return launch_clusters(kernel, ctas, dim3((unsigned)(d->batch * ctas)), dim3(VERIFY_THREADS), static_cast<cudaStream_t>(stream), p);
-  };
-  EFIM_CUDA_TRY(d->target_kind == EFIM_TARGET_LOGITS_BF16  ? launch(verify_kernel<TARGET_BF16>)
-                : d->target_kind == EFIM_TARGET_LOGITS_F32 ? launch(verify_kernel<TARGET_F32>)
-                                                           : launch(verify_kernel<TARGET_PROBS>));
+  char* ws = static_cast<char*>(d_workspace);
+  p.part = reinterpret_cast<uint4*>(ws);
+  p.key = reinterpret_cast<unsigned long long*>(ws + part_bytes(d->total_rows, d->vocab));
+  p.done = reinterpret_cast<int*>(p.key + d->batch);
+  const Pieces mass = pieces_of(d->total_rows, d->vocab, d->target_kind == EFIM_TARGET_LOGITS_BF16 ? MASS_MOST_BYTES / 2 : MASS_MOST_BYTES / 4);
+  const Pieces race = pieces_of(d->batch, d->vocab, RACE_MOST);
+  p.piece = mass.size;
+  p.pieces = mass.count;
+  p.race_piece = race.size;
+  p.race_pieces = race.count;
+  if ((long long)mass.count * d->total_rows > 0x7fffffffLL || (long long)race.count * d->batch > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const dim3 block(VERIFY_THREADS), pick((unsigned)(race.count * d->batch));
+  if (d->target_kind == EFIM_TARGET_PROBS_F32 || d->total_rows == 0) {
+    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3(1), block, 0, s, p));
+  } else {
+    EFIM_CUDA_TRY(launch_pdl(d->target_kind == EFIM_TARGET_LOGITS_BF16 ? verify_mass_kernel<TARGET_BF16> : verify_mass_kernel<TARGET_F32>,
+                             dim3((unsigned)(mass.count * d->total_rows)), block, 0, s, p));
+  }
+  EFIM_CUDA_TRY(launch_pdl(d->target_kind == EFIM_TARGET_LOGITS_BF16  ? verify_pick_kernel<TARGET_BF16>
+                           : d->target_kind == EFIM_TARGET_LOGITS_F32 ? verify_pick_kernel<TARGET_F32>
+                                                                      : verify_pick_kernel<TARGET_PROBS>,
+                           pick, block, 0, s, p));
   return EFIM_OK;
 }

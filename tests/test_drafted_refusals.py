@@ -8,7 +8,7 @@ import paper_2505_21889_b200 as efim
 from paper_2505_21889_b200 import binding as B
 from paper_2505_21889_b200 import build as efim_build
 
-OK, INVALID_ARG, UNSUPPORTED = 0, 1, 2
+OK, INVALID_ARG, UNSUPPORTED, WORKSPACE = 0, 1, 2, 4
 
 
 @pytest.fixture(scope="module")
@@ -62,16 +62,18 @@ def test_lookup(lib):
     assert _lookup(lib, batch=0, hist=None) == OK
 
 
-def _verify(lib, accepted=0x1000, nxt=0x2000, out=None, logs=None, out_stride=0, **changed):
+def _verify(lib, accepted=0x1000, nxt=0x2000, out=None, logs=None, out_stride=0, ws=0x100000, ws_bytes=None, **changed):
     fields = dict(batch=2, total_rows=6, vocab=1000, target_kind=0, d_row_indptr=0x3000, d_tokens=0x4000, d_target=0x5002,
                   target_stride=1001, d_draft_probs=0x6004, draft_stride=1000, d_uniform=0x7000, d_noise=0x8000, noise_stride=1000,
                   d_temperature=0x9000)
     desc = B._VerifyDesc(**{**fields, **changed})
-    return lib.efim_verify_drafts(ctypes.byref(desc), accepted, nxt, out, logs, out_stride, None, None)
+    if ws_bytes is None:
+        ws_bytes = lib.efim_verify_workspace_bytes(desc.batch, desc.total_rows, desc.vocab)
+    return lib.efim_verify_drafts(ctypes.byref(desc), accepted, nxt, out, logs, out_stride, ws, ws_bytes, None, None)
 
 
 def test_verify(lib):
-    assert lib.efim_verify_drafts(None, 0x1000, 0x1000, None, None, 0, None, None) == INVALID_ARG
+    assert lib.efim_verify_drafts(None, 0x1000, 0x1000, None, None, 0, 0x1000, 1 << 20, None, None) == INVALID_ARG
     for bad in (dict(batch=-1), dict(total_rows=-1), dict(vocab=0), dict(target_kind=3), dict(target_kind=-1), dict(d_row_indptr=None),
                 dict(d_tokens=None), dict(d_target=None), dict(target_stride=999), dict(d_target=0x5001), dict(target_kind=1),
                 dict(draft_stride=999), dict(d_draft_probs=0x6002), dict(d_uniform=None), dict(noise_stride=999),
@@ -79,6 +81,12 @@ def test_verify(lib):
                 dict(target_kind=2, d_target=0x5004), dict(target_kind=2, d_target=0x5004, d_temperature=None, d_noise=None)):
         assert _verify(lib, **bad) == INVALID_ARG, bad
     assert _verify(lib, batch=0, d_row_indptr=None) == OK
+    need = lib.efim_verify_workspace_bytes(2, 6, 1000)
+    assert need > 0 and _verify(lib, ws_bytes=need - 1) == _verify(lib, ws=None) == WORKSPACE
+    assert _verify(lib, ws=0x100010) == INVALID_ARG
+    for smaller in ((1, 6, 1000), (2, 1, 1000), (2, 6, 1), (2, 0, 1000)):
+        assert 0 < lib.efim_verify_workspace_bytes(*smaller) <= need
+    assert lib.efim_verify_workspace_bytes(0, 6, 1000) == lib.efim_verify_workspace_bytes(2, 6, 0) == 0
 
 
 def test_python_side():
