@@ -50,13 +50,12 @@ __device__ __forceinline__ float as_float(uint16_t x) { return __uint_as_float((
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-
 __device__ __forceinline__ float rcp_fast(float x) {
   float y;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 // maximum over the warp; NaN lanes do not count
@@ -65,153 +64,181 @@ __device__ __forceinline__ float warp_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
+// two floats at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 x, x, y, z;\n"
+      "mov.b64 {%0, %1}, x;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
 
-// Mass of a row's values seen so far: the largest, the sum of 2^((x - m) c), and the first place of the largest (where asked for).
-// A NaN among the values makes the sum NaN; values of -inf have no mass; at +inf those values share all of it.
+// Mass of a row's values: the largest, m; the sum l of 2^(x c - ref(m)); and the first place of the largest (where asked for).
+// ref(m) is the whole number next to m c: x c - ref is then one fused product with one rounding, of what is left, and masses of
+// different m are joined by exact powers of two.  Where m c passes 2^30 (no fp32 logits there are closer than 2^6 in x c) it is m c
+// itself, by way of (x - m) c; so it is for infinite m.  A NaN among the values makes the sum NaN; values of -inf have no mass; at
+// +inf those values share all of it.
 struct Mass {
   float m, l;
   int at;
 };
-__device__ __forceinline__ float weight_of(float x, float m, float c) {
-  if (m == INFINITY) return x == INFINITY ? 1.f : x == x ? 0.f : x;
-  return exp2_fast((x - (m == -INFINITY ? 0.f : m)) * c);
+__device__ __forceinline__ Mass no_mass() { return {-INFINITY, 0.f, 0x7fffffff}; }
+__device__ __forceinline__ bool has_ref(float m, float c) { return fabsf(m * c) < 1073741824.f; }
+// x c - ref(m), x <= m
+__device__ __forceinline__ float below_ref(float x, float m, float c) {
+  if (has_ref(m, c)) return fmaf(x, c, -rintf(m * c));
+  if (x == m) return m == -INFINITY ? -INFINITY : 0.f;
+  return (x - m) * c;
+}
+// what a sum at `from` is worth at `to` >= from
+__device__ __forceinline__ float shift(float from, float to, float c) {
+  if (has_ref(from, c) && has_ref(to, c)) return exp2_fast(rintf(from * c) - rintf(to * c));
+  if (from == to) return 1.f;
+  return exp2_fast((from - to) * c);
 }
 // The lanes' masses together, in every lane.
 __device__ __forceinline__ Mass warp_join(Mass s, float c, bool want_at) {
   Mass r{warp_max(s.m), 0.f, 0x7fffffff};
-  r.l = s.l * weight_of(s.m, r.m, c);
+  r.l = s.l * shift(s.m, r.m, c);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) r.l += __shfl_xor_sync(0xffffffffu, r.l, d);
   if (want_at) r.at = (int)__reduce_min_sync(0xffffffffu, s.m == r.m ? (unsigned)s.at : 0x7fffffffu);
   return r;
 }
-__device__ __forceinline__ void raise(Mass& s, float top, float c) {
-  if (s.m != -INFINITY) s.l *= weight_of(s.m, top, c);
-  s.m = top;
-}
-__device__ __forceinline__ void add_value(Mass& s, float x, int at, float c) {
-  if (x > s.m) {
-    raise(s, x, c);
-    s.at = at;
-  }
-  s.l += weight_of(x, s.m, c);
-}
 
-// The 16 bytes of a vector, as its values
-template <typename T>
-__device__ __forceinline__ void values_of(const uint4& w, float* x) {
-  const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if constexpr (sizeof(T) == 2) {
-      x[2 * e] = bf16lo(q[e]);
-      x[2 * e + 1] = bf16hi(q[e]);
-    } else {
-      x[e] = __uint_as_float(q[e]);
-    }
-  }
-}
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// Values 2 e and 2 e + 1 of the 16 bytes of a vector
 template <typename T>
-__device__ __forceinline__ float top_of(const uint4* w, int n) {
-  if constexpr (sizeof(T) == 2) {
-    uint32_t m = w[0].x;
-#pragma unroll
-    for (int u = 0; u < n; ++u) m = max_bf16x2(max_bf16x2(max_bf16x2(m, w[u].x), w[u].y), max_bf16x2(w[u].z, w[u].w));
-    return fmaxf(bf16lo(m), bf16hi(m));
-  } else {
-    float m = __uint_as_float(w[0].x);
-#pragma unroll
-    for (int u = 0; u < n; ++u)
-      m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(w[u].x)), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
-    return m;
-  }
+__device__ __forceinline__ float2 pair_of(const uint4& w, int e) {
+  const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+  if constexpr (sizeof(T) == 2) return make_float2(bf16lo(q[e]), bf16hi(q[e]));
+  else return make_float2(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1]));
 }
 
-// The mass of places [begin, end) of a row, by `lanes` lanes; this is lane `id` of them.  Places are seen in rising order by each lane.
+// A thread's share of a piece of a row: up to MASS_VECTORS vectors of 16 bytes, a CTA's threads apart, and one value before and behind
+// the vectors of a piece that is not aligned.  All of it is on its way before anything is computed.
+constexpr int MASS_VECTORS = 8;
 template <typename T>
-__device__ __forceinline__ Mass row_mass(const T* row, int begin, int end, int id, int lanes, float c, bool want_at) {
-  constexpr int EPV = 16 / sizeof(T), U = 8;          // values of a 16-byte vector, vectors in flight
-  Mass s{-INFINITY, 0.f, 0x7fffffff};
-  if (begin >= end) return s;
-  const int n = end - begin;
-  const T* p = row + begin;
-  const int lead = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
-  const int n_vec = (n - lead) / EPV, tail = lead + n_vec * EPV;
-  if (id < lead) add_value(s, as_float(p[id]), begin + id, c);
-  const uint4* vec = reinterpret_cast<const uint4*>(p + lead);
-  for (int v0 = id; v0 < n_vec; v0 += U * lanes) {
-    uint4 w[U];
+struct Share {
+  static constexpr int EPV = 16 / sizeof(T);
+  uint4 w[MASS_VECTORS];
+  const T* values;
+  float head, tail;
+  int first, n_vec, begin, n;                         // first value of the vectors, vectors, place of the first value, values
+  __device__ __forceinline__ void fetch(const T* row, int begin_, int end) {
+    begin = begin_;
+    n = end - begin;
+    const T* p = values = row + begin;
+    first = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
+    n_vec = (n - first) / EPV;
+    const uint4* vec = reinterpret_cast<const uint4*>(p + first);
+    const uint32_t low = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;       // -inf
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t low = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;     // -inf
+    for (int u = 0; u < MASS_VECTORS; ++u) {
+      const int v = threadIdx.x + u * VERIFY_THREADS;
       w[u] = make_uint4(low, low, low, low);
-      if (v0 + u * lanes < n_vec) w[u] = ldg_stream(vec + v0 + u * lanes);
+      if (v < n_vec) w[u] = ldg_stream(vec + v);
     }
-    const float top = top_of<T>(w, U);
-    if (top > s.m) {
-      raise(s, top, c);
-      if (want_at) {
+    head = (int)threadIdx.x < first ? as_float(p[threadIdx.x]) : -INFINITY;
+    const int rest = first + n_vec * EPV + threadIdx.x;
+    tail = rest < n ? as_float(p[rest]) : -INFINITY;
+  }
+  __device__ __forceinline__ Mass mass(float c, bool want_at) const {
+    Mass s = no_mass();
+    if constexpr (sizeof(T) == 2) {
+      uint32_t m = w[0].x;
 #pragma unroll
-        for (int u = U - 1; u >= 0; --u) {
-          float x[EPV];
-          values_of<T>(w[u], x);
+      for (int u = 0; u < MASS_VECTORS; ++u)
+        m = max_bf16x2(max_bf16x2(max_bf16x2(m, w[u].x), w[u].y), max_bf16x2(w[u].z, w[u].w));
+      s.m = fmaxf(bf16lo(m), bf16hi(m));
+    } else {
+      s.m = __uint_as_float(w[0].x);
 #pragma unroll
-          for (int e = EPV - 1; e >= 0; --e)
-            if (x[e] == top) s.at = begin + lead + (v0 + u * lanes) * EPV + e;
+      for (int u = 0; u < MASS_VECTORS; ++u)
+        s.m = fmaxf(fmaxf(fmaxf(s.m, __uint_as_float(w[u].x)), __uint_as_float(w[u].y)),
+                    fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
+    }
+    s.m = fmaxf(fmaxf(s.m, -INFINITY), fmaxf(head, tail));                 // (not NaN where all values are)
+    if (want_at) {
+      // from the last place to the first
+      if (tail == s.m) s.at = begin + first + n_vec * EPV + threadIdx.x;
+#pragma unroll
+      for (int u = MASS_VECTORS - 1; u >= 0; --u)
+#pragma unroll
+        for (int e = EPV / 2 - 1; e >= 0; --e) {
+          const float2 x = pair_of<T>(w[u], e);
+          const int at = begin + first + (threadIdx.x + u * VERIFY_THREADS) * EPV + 2 * e;
+          if (x.y == s.m) s.at = at + 1;
+          if (x.x == s.m) s.at = at;
+        }
+      if (head == s.m) s.at = begin + threadIdx.x;
+    }
+    if (has_ref(s.m, c)) {
+      const float2 cc = make_float2(c, c), ref = make_float2(-rintf(s.m * c), -rintf(s.m * c));
+      float2 l = make_float2(exp2_fast(fmaf(head, c, ref.x)), exp2_fast(fmaf(tail, c, ref.x)));
+#pragma unroll
+      for (int u = 0; u < MASS_VECTORS; ++u) {
+        if (u * VERIFY_THREADS >= n_vec) break;                            // the whole CTA
+#pragma unroll
+        for (int e = 0; e < EPV / 2; ++e) {
+          const float2 y = fma2(pair_of<T>(w[u], e), cc, ref);
+          l = add2(l, make_float2(exp2_fast(y.x), exp2_fast(y.y)));
         }
       }
+      s.l = l.x + l.y;
+    } else {
+      // rare: one value after the other, read again
+      s.l = exp2_fast(below_ref(head, s.m, c)) + exp2_fast(below_ref(tail, s.m, c));
+#pragma unroll 1
+      for (int v = threadIdx.x; v < n_vec; v += VERIFY_THREADS)
+#pragma unroll 1
+        for (int e = 0; e < EPV; ++e) s.l += exp2_fast(below_ref(as_float(values[first + v * EPV + e]), s.m, c));
     }
-    const float m = s.m == -INFINITY ? 0.f : s.m;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (v0 + u * lanes >= n_vec) break;
-      float x[EPV];
-      values_of<T>(w[u], x);
-      if (s.m == INFINITY) {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) s.l += weight_of(x[e], s.m, c);
-      } else {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) s.l += exp2_fast((x[e] - m) * c);
-      }
-    }
+    return s;
   }
-  if (tail + id < n) add_value(s, as_float(p[tail + id]), begin + tail + id, c);      // fewer than a vector's
-  return s;
-}
+};
 
-// Probabilities of one row, from its logits or as they are.
+// Probabilities of one row, from its logits or as they are: m, and l = sum of 2^((x - m) c).
 template <int KIND>
 struct Row {
-  float m, l, inv;
-  __device__ __forceinline__ float exact(float x) const {
-    if (KIND == TARGET_PROBS) return x;
-    return (m == INFINITY ? (x == INFINITY ? 1.f : 0.f) : expf((x - m) * inv)) / l;
+  float m, l, c;
+  // (x - m) c, where it is not 0 times or less infinity
+  __device__ __forceinline__ float below(float x) const { return x == m ? 0.f : (x - m) * c; }
+  __device__ __forceinline__ float exact(float x) const { return KIND == TARGET_PROBS ? x : exp2f(below(x)) / l; }
+  __device__ __forceinline__ float log_of(float x) const {
+    return KIND == TARGET_PROBS ? logf(x) : below(x) * 0.6931471805599453f - logf(l);
   }
 };
 
 // The race for the next token over places [begin, end) of a row: the largest r / e, r = (p - q)^+ or p, the lowest place among
 // equals.  `gone` is a place that does not take part.  Returns (r / e, place) as one number to be compared, 0 if nobody ran.
 //
-// An exact result costs two divisions and an exponential.  So every place gets a bound from above first, by the fast instructions (for
-// probabilities down to 2^-149 the exponent's two roundings are 150 * 2^-23 * ln 2, ex2 and rcp 2^-22 each, together below 2^-16),
-// and only places whose bound reaches the warp's best result so far are computed: a few a warp.
+// An exact result costs two divisions and an exponential.  So every place gets a bound from above first, by the fast instructions (in a
+// probability: the exponent's rounding 150 * 2^-24 * ln 2, ex2 2^-22, the factor 2^-23; rcp and the products 2^-22 more; the
+// bound is 2^-16 higher, twice), and only places whose bound reaches the best result known so far are computed: a few a warp.
+// `known` is a lower limit of the best, from other CTAs of the race: what it leaves out cannot win.  (Probabilities below 2^-126 are taken
+// for 0 here.)
 constexpr float RACE_ABOVE = 1.f + 1.f / 65536;
 template <int KIND, bool VEC>
 __device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>::type* row, const float* noise, const float* q,
-                                                   int begin, int end, int gone, const Row<KIND>& of, float c) {
+                                                   int begin, int end, int gone, const Row<KIND>& of, float known) {
   constexpr int N = 8;                                // places of a thread in flight: two groups of four, or eight apart
   using T = typename TargetOf<KIND>::type;
   const int tid = threadIdx.x;
-  const float m = of.m == INFINITY ? 0.f : of.m;      // (an infinite maximum: bounds of infinity, so everything is computed)
-  const float scale = KIND == TARGET_PROBS ? RACE_ABOVE : of.m == INFINITY ? INFINITY : RACE_ABOVE / of.l;
+  const bool plain = KIND == TARGET_PROBS || has_ref(of.m, of.c);
+  const float scale = KIND == TARGET_PROBS ? RACE_ABOVE : RACE_ABOVE / (of.l * exp2_fast(below_ref(of.m, of.m, of.c))), ref = KIND == TARGET_PROBS ? 0.f : rintf(of.m * of.c);
   unsigned long long key = 0;
-  float best = 0.f;                                   // the warp's
+  float best = known;                                 // the warp's
   auto place = [&](int a0, int i) { return VEC ? a0 + (i / 4) * 4 * VERIFY_THREADS + i % 4 : a0 + i * VERIFY_THREADS; };
   const int first = begin + (VEC ? 4 * tid : tid);
   // whole warps stay together: the first lane's place decides
@@ -252,7 +279,7 @@ __device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>
     for (int i = 0; i < N; ++i) {
       above[i] = 0.f;
       if (place(a0, i) < end) {
-        const float p = KIND == TARGET_PROBS ? x[i] : exp2_fast((x[i] - m) * c);
+        const float p = KIND == TARGET_PROBS ? x[i] : exp2_fast(plain ? fmaf(x[i], of.c, -ref) : below_ref(x[i], of.m, of.c));
         const float r = q ? fmaf(p, scale, -qx[i]) : p * scale;
         above[i] = r * rcp_fast(e[i]) * RACE_ABOVE;
       }
@@ -292,17 +319,16 @@ __device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>
 
 // Temperature of a sequence, as a factor of its logits; greedy sequences take 1.
 struct Scale {
-  float inv, c;             // 1 / T, and log2(e) / T
+  float c;                  // log2(e) / T
   bool greedy;
 };
 __device__ __forceinline__ Scale scale_of(const VerifyParams& p, int s) {
-  Scale r{1.f, 0.f, !p.noise};
+  Scale r{1.4426950408889634f, !p.noise};
   if (p.noise && p.temperature) {
     const float t = *(p.temperature + s);
     r.greedy = !(t > 0.f);
-    r.inv = r.greedy ? 1.f : fminf(1.f / t, FLT_MAX);
+    if (!r.greedy) r.c = fminf(1.4426950408889634f / t, FLT_MAX);
   }
-  r.c = fminf(r.inv * 1.4426950408889634f, FLT_MAX);
   return r;
 }
 
@@ -328,6 +354,8 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const Ve
     p.key[s] = 0;
     p.done[s] = 0;
   }
+  Share<T> share;
+  share.fetch(static_cast<const T*>(p.target) + r * p.target_stride, piece * p.piece, min(p.vocab, (piece + 1) * p.piece));
   // the row's sequence, the last that starts at or before it, of whose rows the range must be one that the call was given
   int lo = 0, n = p.batch;
   while (n > 32) {
@@ -339,13 +367,11 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const Ve
   }
   lo += 31 - __clz((int)(__ballot_sync(0xffffffffu, lane < n && *(p.row_indptr + lo + lane) <= r) | 1u));
   const Scale sc = scale_of(p, lo);
-  const int begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
-  const Mass mass = warp_join(row_mass<T>(static_cast<const T*>(p.target) + r * p.target_stride, begin, end, tid, VERIFY_THREADS, sc.c,
-                                          sc.greedy), sc.c, sc.greedy);
+  const Mass mass = warp_join(share.mass(sc.c, sc.greedy), sc.c, sc.greedy);
   if (lane == 0) s_warp[warp] = mass;
   __syncthreads();
   if (warp == 0) {
-    const Mass sum = warp_join(lane < VERIFY_WARPS ? s_warp[lane] : Mass{-INFINITY, 0.f, 0x7fffffff}, sc.c, sc.greedy);
+    const Mass sum = warp_join(lane < VERIFY_WARPS ? s_warp[lane] : no_mass(), sc.c, sc.greedy);
     if (lane == 0)
       p.part[blockIdx.x] = make_uint4(__float_as_uint(sum.m), __float_as_uint(sum.l), sum.at, 0);
   }
@@ -369,7 +395,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   const int r0 = *(p.row_indptr + s), r1 = *(p.row_indptr + s + 1);
   const bool rows_ok = r0 >= 0 && r1 <= p.total_rows && r0 <= r1;
   const int n = rows_ok ? r1 - r0 : 0;
-  const Scale sc = KIND == TARGET_PROBS ? Scale{1.f, 1.f, false} : scale_of(p, s);
+  const Scale sc = KIND == TARGET_PROBS ? Scale{1.f, false} : scale_of(p, s);
   const bool first = piece == 0;
   const int begin = piece * p.race_piece, end = min(p.vocab, begin + p.race_piece);
   int32_t* out_tokens = p.out_tokens ? p.out_tokens + (size_t)s * p.out_stride : nullptr;
@@ -403,23 +429,24 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
         row.ok = i < n - 1 && inside && u * q < value;
         row.logprob = logf(value);
       } else {
-        Mass sum{-INFINITY, 0.f, 0x7fffffff};
+        Mass sum = no_mass();
         for (int k = lane; k < p.pieces; k += 32) {
           const uint4 w = *(p.part + (size_t)(r0 + i) * p.pieces + k);
           const Mass o{__uint_as_float(w.x), __uint_as_float(w.y), (int)w.z};
           const float m = fmaxf(sum.m, o.m);
-          sum.l = sum.l * weight_of(sum.m, m, sc.c) + o.l * weight_of(o.m, m, sc.c);
+          sum.l = sum.l * shift(sum.m, m, sc.c) + o.l * shift(o.m, m, sc.c);
           if (o.m > sum.m) sum.at = o.at;              // (a lane's places rise)
           sum.m = m;
         }
         sum = warp_join(sum, sc.c, sc.greedy);
         row.m = sum.m;
-        row.l = sum.l;
+        row.l = sum.l / exp2_fast(below_ref(sum.m, sum.m, sc.c));    // (exactly 1 where there is one token)
         row.at = sum.at;
-        const bool any = sum.l > 0.f;                  // (and not NaN)
-        const float px = !any || value == -INFINITY ? 0.f : Row<KIND>{sum.m, sum.l, sc.inv}.exact(value);
+        const bool any = row.l > 0.f;                  // (and not NaN)
+        const Row<KIND> of{row.m, row.l, sc.c};
+        const float px = any ? of.exact(value) : 0.f;
         row.ok = i < n - 1 && any && inside && (sc.greedy ? sum.at == x : u * q < px);
-        row.logprob = sum.m == INFINITY ? logf(px) : (value - sum.m) * sc.inv - logf(sum.l);
+        row.logprob = of.log_of(value);
       }
       if (i < n - 1 && !inside) row.ok = -1;
       if (lane == 0) s_row[warp] = row;
@@ -461,13 +488,13 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
     const float* noise = p.noise + s * p.noise_stride;
     const float* q = judged && p.draft_probs ? p.draft_probs + (r0 + stop) * p.draft_stride : nullptr;
     int gone = judged && !p.draft_probs ? *(p.tokens + r0 + stop + 1) : -1;
-    const Row<KIND> of{last.m, last.l, sc.inv};
+    const Row<KIND> of{last.m, last.l, sc.c};
     const bool aligned = !((reinterpret_cast<uintptr_t>(row) & (4 * sizeof(T) - 1)) | (reinterpret_cast<uintptr_t>(noise) & 15) |
                            (reinterpret_cast<uintptr_t>(q) & 15));
-    auto run = [&](int a, int b) {                     // the whole CTA's best, in thread 0
+    auto run = [&](int a, int b, float known) {        // the whole CTA's best, in thread 0
       const int whole = aligned ? a + ((b - a) & ~3) : a;
-      unsigned long long k = race<KIND, true>(row, noise, q, a, whole, gone, of, sc.c);
-      k = max(k, race<KIND, false>(row, noise, q, whole, b, gone, of, sc.c));
+      unsigned long long k = race<KIND, true>(row, noise, q, a, whole, gone, of, known);
+      k = max(k, race<KIND, false>(row, noise, q, whole, b, gone, of, known));
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, d));
       if (lane == 0) s_key[warp] = k;
@@ -476,7 +503,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
         for (int w = 1; w < VERIFY_WARPS; ++w) k = max(k, s_key[w]);
       return k;
     };
-    key = run(begin, end);
+    key = run(begin, end, __uint_as_float((uint32_t)(*(volatile unsigned long long*)(p.key + s) >> 32)));
     // the CTAs of a sequence meet: the last one through has the best of all
     if (p.race_pieces > 1) {
       if (tid == 0) {
@@ -495,7 +522,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
     if (s_empty) {
       q = nullptr;
       gone = -1;
-      key = run(0, p.vocab);
+      key = run(0, p.vocab, 0.f);
     }
   }
   if (tid != 0) return;
@@ -505,7 +532,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   float logprob = 0.f;
   if (next >= 0) {
     const float x = as_float(target[(r0 + stop) * p.target_stride + next]);
-    logprob = KIND == TARGET_PROBS ? logf(x) : last.m == INFINITY ? -logf(last.l) : (x - last.m) * sc.inv - logf(last.l);
+    logprob = Row<KIND>{last.m, last.l, sc.c}.log_of(x);
   } else if (n > 0) {
     status |= EFIM_DEV_NO_TOKEN;
   }
@@ -531,7 +558,7 @@ static Pieces pieces_of(long long rows, int vocab, int most) {
   size = (size + 63) / 64 * 64;
   return {(int)size, (int)((vocab + size - 1) / size)};
 }
-constexpr int MASS_MOST_BYTES = 32768, RACE_MOST = 8192;
+constexpr int MASS_MOST_BYTES = MASS_VECTORS * VERIFY_THREADS * 16, RACE_MOST = 8192;
 
 // The most that a call of at most these rows over at most this vocabulary cuts its rows into: one wave, or the largest pieces.
 static size_t part_bytes(long long rows, int vocab) {
