@@ -5,6 +5,7 @@
 //   y_d = x_d (mean_e x_e^2 + eps)^(-1/2) (w_d + offset),  then the pairs of y are rotated; one rounding to bf16 at the end.
 #include "token_place.cuh"
 #include <float.h>
+#include <algorithm>
 
 namespace efim {
 
@@ -26,10 +27,15 @@ struct QkNormParams {
   float eps, weight_offset;
   int batch, max_pages_per_seq, total_new_tokens;
   int num_pages, Hq, Hkv, max_position, interleaved, weight_f32;
+  int warps;                // of a token
   int early_next;           // let the next kernel start its set-up while this one runs
 };
 
 constexpr int QK_NORM_THREADS = 256;
+
+// A value that is the same in a warp's lanes, in a form that tells the compiler so (it cannot know of the warp's index): what depends
+// on it is computed once a warp, and its branches are not compiled for lanes that part.
+__device__ __forceinline__ int uniform(int x) { return __reduce_max_sync(0xffffffffu, x); }
 
 // 8 weights from position d on, as the products take them
 __device__ __forceinline__ void load_weights(const void* weight, int f32, float offset, int d, float* w) {
@@ -55,61 +61,55 @@ __device__ __forceinline__ void load_weights(const void* weight, int f32, float 
   for (int i = 0; i < 8; ++i) w[i] += offset;
 }
 
-// WPT warps per new token.  A lane holds vector j of a head row and its partner j + D/16 (both halves of the row, 16 values), so
-// D/16 lanes have a head: the sum of squares is 16 products in a lane and log2(D/16) shuffles, and either pairing of the rotation
-// stays inside the lane.  Its rotary values are loaded once, its weights once for q and once for k.
-template <int D, int WPT>
-__global__ void __launch_bounds__(QK_NORM_THREADS, 3) qk_norm_append_kernel(const QkNormParams p) {
+// A token's q and k heads go to its warps (WARPS, or p.warps where that is 0) in groups of HW = 512 / D, v's vectors, which are
+// copied, to their lanes.  A lane holds vector j of a head row and its partner j + D/16 (16 values), so D/16 lanes have a head: the sum of
+// squares is 16 products in a lane and log2(D/16) shuffles, and either pairing of the rotation stays inside the lane, whose rotary
+// values are loaded once.  A warp's first rows are on their way before its token's sequence is looked up, then the next group's while
+// one is computed.
+//
+// Bound: HBM with many tokens (25,600 at 32/8 heads x 128: 107 us, 6.0 TB/s), and close to it the instructions of a group: 64 registers and
+// four CTAs an SM even with a few bytes spilled (three CTAs 2-5 % longer with many tokens, two 16 %), weights taken from L1 when they are
+// needed (held in registers the kernel spilled and took 25 % longer, in shared memory as fp32 5 %), warp-wide values marked as such.
+// Not kept: a warp that walks several tokens in a row (code of one loop more: 40 % longer), two groups on their way (2-3 %),
+// v's heads in the groups' loop (8 %), warps of v's alone (6 %).
+template <int D, int WARPS>
+__global__ void __launch_bounds__(QK_NORM_THREADS, 4) qk_norm_append_kernel(const QkNormParams p) {
   constexpr int VEC = D / 8, HALF = VEC / 2;    // 16-byte vectors of a head row, lanes that have it
-  constexpr int LANES = 32 * WPT;
-  constexpr int HW = 32 / HALF, HP = WPT * HW;  // heads that a warp, and a token's warps, have at once
-  constexpr int COPIES = WPT == 1 ? 4 : 2;      // vectors of v in flight per lane
-  const int lane = threadIdx.x % LANES, wl = threadIdx.x & 31;
-  const int t = blockIdx.x * (QK_NORM_THREADS / LANES) + threadIdx.x / LANES;
+  constexpr int HW = 32 / HALF;
+  constexpr int COPIES = WARPS == 1 ? 4 : 2;    // vectors of v in flight per lane
+  const int lane = threadIdx.x & 31;
+  const int flat = blockIdx.x * (QK_NORM_THREADS / 32) + uniform(threadIdx.x >> 5);
+  const int warps = WARPS ? WARPS : p.warps;
+  const int t = flat / warps, part = flat % warps;
   pdl_wait();
   if (p.early_next) pdl_launch();
   if (t >= p.total_new_tokens) return;
-  const int nq = p.q ? p.Hq : 0, nh = nq + p.Hkv, n_vec = p.Hkv * VEC;
-  const uint4* qin = reinterpret_cast<const uint4*>(p.q + (p.q ? t * p.q_stride : 0));
-  const uint4* kin = reinterpret_cast<const uint4*>(p.k + t * p.k_stride);
+  const int nq = p.q ? p.Hq : 0, nh = nq + p.Hkv;
+  const int j = lane % HALF, sub = lane / HALF, step = warps * HW;
+  const uint4* qin = reinterpret_cast<const uint4*>(p.q + (p.q ? t * p.q_stride : 0)) + j;
+  const uint4* kin = reinterpret_cast<const uint4*>(p.k + t * p.k_stride) + j;
   const uint4* vin = reinterpret_cast<const uint4*>(p.v + t * p.v_stride);
-  const int j = lane % HALF;
-  // the warp's first head, the same for its lanes, and this lane's among the warp's
-  const int base0 = (lane >> 5) * HW, sub = wl / HALF;
-  uint4 a[2], b[2], v[COPIES];
-  auto fetch_heads = [&](int base) {            // vectors of heads base + sub and base + sub + HP
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int h = base + sub + i * HP;
-      a[i] = b[i] = make_uint4(0, 0, 0, 0);
-      if (h < nh) {
-        const uint4* row = (h < nq ? qin + h * VEC : kin + (h - nq) * VEC) + j;
-        a[i] = ldg_stream(row);
-        b[i] = ldg_stream(row + HALF);
-      }
+  const int n_vec = p.Hkv * VEC, v0 = part * 32 + lane, v_step = warps * 32;
+  const int base0 = part * HW;
+  uint4 a, b, v[COPIES];                        // the next head's vectors, v's
+  auto fetch = [&](int h) {
+    a = b = make_uint4(0, 0, 0, 0);
+    if (h < nh) {
+      const uint4* row = h < nq ? qin + h * VEC : kin + (h - nq) * VEC;
+      a = ldg_stream(row);
+      b = ldg_stream(row + HALF);
     }
   };
-  auto fetch_copy = [&](int u0) {
+  auto fetch_v = [&](int u0) {
 #pragma unroll
     for (int i = 0; i < COPIES; ++i)
-      if (u0 + LANES * i < n_vec) v[i] = ldg_stream(vin + u0 + LANES * i);
+      if (u0 + v_step * i < n_vec) v[i] = ldg_stream(vin + u0 + v_step * i);
   };
-  fetch_heads(base0);
-  fetch_copy(lane);
-  // what the products take from the weights, for the heads of one kind
-  float w[16];
-  int kind = -1;
-  auto weights_for = [&](int want) {
-    if (kind == want) return;
-    kind = want;
-    const void* weight = want ? p.k_weight : p.q_weight;
-    load_weights(weight, p.weight_f32, p.weight_offset, j * 8, w);
-    load_weights(weight, p.weight_f32, p.weight_offset, (j + HALF) * 8, w + 8);
-  };
-  weights_for(base0 + sub >= nq);
+  fetch(base0 + sub);
+  fetch_v(v0);
 
-  const TokenPlace at = find_token(p.q_indptr, p.cached_len, p.batch, t, wl);
-  const int pos = at.pos, page_idx = pos >> 4;
+  const TokenPlace at = find_token(p.q_indptr, p.cached_len, p.batch, t, lane);
+  const int pos = uniform(at.pos), page_idx = pos >> 4;
   const bool in_table = !p.cos_sin || (pos >= 0 && pos < p.max_position);
   bool placed = pos >= 0 && page_idx < p.max_pages_per_seq && in_table;   // k and v have a place in the cache
   int page = 0;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(QK_NORM_THREADS, 3) qk_norm_append_kernel(cons
     page = *(p.block_table + (size_t)at.seq * p.max_pages_per_seq + page_idx);
   }
   float c[8], s[8];
-  if (p.cos_sin && in_table) {
+  if (p.cos_sin && in_table && base0 < nh) {
     // 8 pairs: (f, f + D/2) from f = 8 j on, or the 4 + 4 neighbours of the two vectors
     const float* cs = p.cos_sin + (size_t)pos * D + j * (p.interleaved ? 4 : 8);
     const int second = p.interleaved ? D / 4 : 4;
@@ -134,79 +134,79 @@ __global__ void __launch_bounds__(QK_NORM_THREADS, 3) qk_norm_append_kernel(cons
   }
   const size_t pool_tok = ((size_t)page * p.Hkv) * 16 * D + (size_t)(pos & 15) * D;   // + h * 16 * D
   if (placed) {
-    for (int u0 = lane; u0 < n_vec; u0 += COPIES * LANES) {
-      if (u0 != lane) fetch_copy(u0);
+    for (int u0 = v0; u0 < n_vec; u0 += COPIES * v_step) {
+      if (u0 != v0) fetch_v(u0);
 #pragma unroll
       for (int i = 0; i < COPIES; ++i) {
-        const int u = u0 + LANES * i;
+        const int u = u0 + v_step * i;
         if (u < n_vec) *reinterpret_cast<uint4*>(p.v_pool + pool_tok + (size_t)(u / VEC) * 16 * D + (u % VEC) * 8) = v[i];
       }
     }
   }
-  uint4* q_out = reinterpret_cast<uint4*>(p.q_out + (size_t)t * p.Hq * D);
-  for (int base = base0; base < nh; base += 2 * HP) {
-    if (base != base0) fetch_heads(base);
+  uint16_t* q_out = p.q_out + (size_t)t * p.Hq * D + j * 8;
+#pragma unroll 1
+  for (int base = base0; base < nh; base += step) {    // (the same for a warp's lanes: the sums below are the whole warp's)
+    const int h = base + sub;
+    float x[16];
+    {
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int h = base + sub + i * HP;
-      if (base + i * HP >= nh) break;           // the whole warp
-      float x[16];
-      {
-        const uint32_t* wa = reinterpret_cast<const uint32_t*>(&a[i]);
-        const uint32_t* wb = reinterpret_cast<const uint32_t*>(&b[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[2 * e] = bf16lo(wa[e]);
-          x[2 * e + 1] = bf16hi(wa[e]);
-          x[8 + 2 * e] = bf16lo(wb[e]);
-          x[8 + 2 * e + 1] = bf16hi(wb[e]);
-        }
+      for (int e = 0; e < 8; ++e) {
+        x[2 * e] = bf16lo(w[e]);
+        x[2 * e + 1] = bf16hi(w[e]);
       }
-      auto squares = [&]() {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-        for (int d = HALF / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        return ss;
-      };
-      float ss = squares(), eps = p.eps;
-      if (__any_sync(0xffffffffu, !(ss <= FLT_MAX))) {
-        // Squares of values beyond 1e18 leave fp32: such heads are taken 2^-70 as large (exact, and eps no longer counts beside
-        // them).  A row with an infinity or a NaN stays what the formula makes of it.
-        const float down = ss <= FLT_MAX ? 1.f : 8.470329472543003e-22f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] *= down;
-        if (down != 1.f) eps = 0.f;
-        ss = squares();
-      }
-      if (h >= nh || (h >= nq && !placed)) continue;
-      const float r = rsqrtf(fmaf(ss, 1.f / D, eps));
-      weights_for(h >= nq);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = x[e] * r * w[e];
-      uint32_t y[8];
-      if (!p.cos_sin) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
-      } else if (!in_table) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = 0;   // no rotation for this row: a query of zeros
-      } else if (!p.interleaved) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          y[e / 2] = pack_bf16x2(fmaf(x[e], c[e], -(x[8 + e] * s[e])), fmaf(x[e + 1], c[e + 1], -(x[9 + e] * s[e + 1])));
-          y[4 + e / 2] = pack_bf16x2(fmaf(x[8 + e], c[e], x[e] * s[e]), fmaf(x[9 + e], c[e + 1], x[e + 1] * s[e + 1]));
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          y[e] = pack_bf16x2(fmaf(x[2 * e], c[e], -(x[2 * e + 1] * s[e])), fmaf(x[2 * e + 1], c[e], x[2 * e] * s[e]));
-      }
-      uint4* dst = h < nq ? q_out + h * VEC : reinterpret_cast<uint4*>(p.k_pool + pool_tok + (size_t)(h - nq) * 16 * D);
-      dst[j] = make_uint4(y[0], y[1], y[2], y[3]);
-      dst[j + HALF] = make_uint4(y[4], y[5], y[6], y[7]);
     }
+    if (base + step < nh) fetch(h + step);
+    auto squares = [&]() {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+      for (int d = HALF / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+      return ss;
+    };
+    float ss = squares(), eps = p.eps;
+    if (__any_sync(0xffffffffu, !(ss <= FLT_MAX))) {
+      // Squares of values beyond 1e18 leave fp32: such heads are taken 2^-70 as large (exact, and eps no longer counts beside
+      // them).  A row with an infinity or a NaN stays what the formula makes of it.
+      const float down = ss <= FLT_MAX ? 1.f : 8.470329472543003e-22f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] *= down;
+      if (down != 1.f) eps = 0.f;
+      ss = squares();
+    }
+    if (h >= nh || (h >= nq && !placed)) continue;
+    const float r = rsqrtf(fmaf(ss, 1.f / D, eps));
+    // (from L1 after a warp's first heads: in registers beside the rotary values they made the kernel spill)
+    const void* weight = h < nq ? p.q_weight : p.k_weight;
+    float w[8];
+    load_weights(weight, p.weight_f32, p.weight_offset, j * 8, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = x[e] * r * w[e];
+    load_weights(weight, p.weight_f32, p.weight_offset, (j + HALF) * 8, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[8 + e] = x[8 + e] * r * w[e];
+    uint32_t y[8];
+    if (!p.cos_sin) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+    } else if (!in_table) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = 0;     // no rotation for this row: a query of zeros
+    } else if (!p.interleaved) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        y[e / 2] = pack_bf16x2(fmaf(x[e], c[e], -(x[8 + e] * s[e])), fmaf(x[e + 1], c[e + 1], -(x[9 + e] * s[e + 1])));
+        y[4 + e / 2] = pack_bf16x2(fmaf(x[8 + e], c[e], x[e] * s[e]), fmaf(x[9 + e], c[e + 1], x[e + 1] * s[e + 1]));
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        y[e] = pack_bf16x2(fmaf(x[2 * e], c[e], -(x[2 * e + 1] * s[e])), fmaf(x[2 * e + 1], c[e], x[2 * e] * s[e]));
+    }
+    uint4* dst = reinterpret_cast<uint4*>(h < nq ? q_out + h * D : p.k_pool + pool_tok + (size_t)(h - nq) * 16 * D + j * 8);
+    dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+    dst[HALF] = make_uint4(y[4], y[5], y[6], y[7]);
   }
 }
 
@@ -272,20 +272,24 @@ extern "C" efim_status efim_qk_norm_append(const efim_cache_desc* cache, const e
   p.num_pages = cache->num_pages;
   p.Hq = cache->num_q_heads;
   p.Hkv = cache->num_kv_heads;
-  const long long resident = 3 * sm_count();
-  const long long vectors = ((d_q ? cache->num_q_heads : 0) + 2LL * cache->num_kv_heads) * (D / 8);   // of the rows that a token moves
-  const int wpt = T <= resident ? 8 : T <= 2 * resident || vectors >= 1024 ? 4 : vectors >= 384 || T <= 4 * resident ? 2 : 1;
-  const unsigned grid = (unsigned)((T * wpt * 32 + QK_NORM_THREADS - 1) / QK_NORM_THREADS);
-  p.early_next = grid <= (unsigned)sm_count();
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3(grid), dim3(QK_NORM_THREADS), 0, s, p); };
-  auto launch_d = [&](auto dim) {
-    constexpr int DIM = decltype(dim)::value;
-    return wpt == 1   ? launch(qk_norm_append_kernel<DIM, 1>)
-           : wpt == 2 ? launch(qk_norm_append_kernel<DIM, 2>)
-           : wpt == 4 ? launch(qk_norm_append_kernel<DIM, 4>)
-                      : launch(qk_norm_append_kernel<DIM, 8>);
+  // Warps of a token: as many as are resident at once, up to one for every group of q's and k's heads; with more tokens one, or two
+  // from ten groups on.  Microseconds with 1 / 2 / 4 / a warp per group: 64 tokens at 32/8 heads x 128 8.3 / 5.5 / 4.3 / 2.7, 900 at 28/4 7.3 / 5.6 /
+  // 5.3 / 6.4, 2,336 at 32/8 14.3 / 12.8 / 13.7 / 16.4, at 32/32 25.5 / 22.0 / 22.7 / 25 or more, 20,000 at 28/4 64.1 / 66.8 / 73.5 / 91, at 32/8 84.5 /
+  // 83.4 / 93.6 / 116, at 32/32 171 / 166 / 167 / 180 or more, at 4/4 x 64 15.8 / 20.4.
+  const int hw = 512 / D, heads = (d_q ? cache->num_q_heads : 0) + cache->num_kv_heads, groups = (heads + hw - 1) / hw;
+  const long long resident = 4LL * (QK_NORM_THREADS / 32) * sm_count();
+  p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 10 ? 2 : 1, resident / T));
+  const long long ctas = (T * p.warps + QK_NORM_THREADS / 32 - 1) / (QK_NORM_THREADS / 32);
+  if (ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  p.early_next = ctas <= sm_count();
+  auto launch = [&](auto kernel) {
+    return launch_pdl(kernel, dim3((unsigned)ctas), dim3(QK_NORM_THREADS), 0, static_cast<cudaStream_t>(stream), p);
   };
-  EFIM_CUDA_TRY(D == 128 ? launch_d(std::integral_constant<int, 128>{}) : launch_d(std::integral_constant<int, 64>{}));
+  EFIM_CUDA_TRY(D == 128 ? (p.warps == 1   ? launch(qk_norm_append_kernel<128, 1>)
+                            : p.warps == 2 ? launch(qk_norm_append_kernel<128, 2>)
+                                           : launch(qk_norm_append_kernel<128, 0>))
+                         : (p.warps == 1   ? launch(qk_norm_append_kernel<64, 1>)
+                            : p.warps == 2 ? launch(qk_norm_append_kernel<64, 2>)
+                                           : launch(qk_norm_append_kernel<64, 0>)));
   return EFIM_OK;
 }

@@ -12,12 +12,19 @@
 // for the next token there; the last of them to finish writes the result.
 #include "common.cuh"
 #include <float.h>
+#include <stdlib.h>
 #include <algorithm>
 
 namespace efim {
 
 constexpr int VERIFY_THREADS = 256;
 constexpr int VERIFY_WARPS = VERIFY_THREADS / 32;
+
+struct __align__(16) RowResult {
+  float m, l, logprob;      // maximum and sum of the row, log-probability of its draft
+  int at, ok;               // place of the maximum; draft accepted: 1, refused: 0, refused for what it is: -1
+  int unused[3];
+};
 
 struct VerifyParams {
   const void* target;       // rows of [vocab], target_stride elements apart
@@ -33,8 +40,11 @@ struct VerifyParams {
   float* out_logprobs;      // the same
   int32_t* status;
   uint4* part;              // [total_rows][pieces]: maximum, sum, place of the maximum
+  RowResult* result;        // [total_rows], where rows are taken in order
   unsigned long long* key;  // [batch] best of the race so far
   int* done;                // [batch] pieces of the race that are through
+  int* stop;                // [batch] first row so far that accepts nothing, where rows are taken in order
+  int* through;             // [total_rows] pieces of the row that are through, the same
   long long target_stride, draft_stride, noise_stride;
   int batch, total_rows, vocab, out_stride;
   int piece, pieces;        // places of a CTA of the first kernel, CTAs of a row
@@ -64,21 +74,6 @@ __device__ __forceinline__ float warp_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
-// two floats at a time
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 x, x, y, z;\n"
-      "mov.b64 {%0, %1}, x;\n}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return r;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 r;
-  asm("{\n.reg .b64 x, y;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-
 // Mass of a row's values: the largest, m; the sum l of 2^(x c - ref(m)); and the first place of the largest (where asked for).
 // ref(m) is the whole number next to m c: x c - ref is then one fused product with one rounding, of what is left, and masses of
 // different m are joined by exact powers of two.  Where m c passes 2^30 (no fp32 logits there are closer than 2^6 in x c) it is m c
@@ -332,21 +327,86 @@ __device__ __forceinline__ Scale scale_of(const VerifyParams& p, int s) {
   return r;
 }
 
-// What the second kernel's CTAs of a sequence meet in.
+// The draft that a row judges, and what it is judged by: inputs alone.
+struct Draft {
+  int x;
+  bool any, inside;         // the row has a draft; it is one of the vocabulary
+  float value, q, u;        // of the target's row, of its own distribution, uniform
+};
+template <int KIND>
+__device__ __forceinline__ Draft draft_of(const VerifyParams& p, int r, bool any, const Scale& sc) {
+  Draft d{-1, any, false, -INFINITY, 1.f, 0.f};
+  if (!any) return d;
+  d.x = *(p.tokens + r + 1);
+  d.inside = d.x >= 0 && d.x < p.vocab;
+  if (d.inside) {
+    d.value = as_float(static_cast<const typename TargetOf<KIND>::type*>(p.target)[r * p.target_stride + d.x]);
+    if (!sc.greedy) {
+      d.u = *(p.uniform + r);
+      if (p.draft_probs) d.q = p.draft_probs[r * p.draft_stride + d.x];
+    }
+  }
+  return d;
+}
+// What row r makes of it, by a warp, from the masses of the row's pieces.
+template <int KIND>
+__device__ __forceinline__ RowResult judge(const VerifyParams& p, int r, const Draft& d, const Scale& sc) {
+  RowResult row{0.f, 1.f, 0.f, 0, 0};
+  if (KIND == TARGET_PROBS) {
+    row.ok = d.inside && d.u * d.q < d.value;
+    row.logprob = logf(d.value);
+  } else {
+    Mass sum = no_mass();
+    for (int k = threadIdx.x & 31; k < p.pieces; k += 32) {
+      const uint4 w = __ldcg(p.part + (size_t)r * p.pieces + k);
+      const Mass o{__uint_as_float(w.x), __uint_as_float(w.y), (int)w.z};
+      const float m = fmaxf(sum.m, o.m);
+      sum.l = sum.l * shift(sum.m, m, sc.c) + o.l * shift(o.m, m, sc.c);
+      if (o.m > sum.m) sum.at = o.at;                  // (a lane's places rise)
+      sum.m = m;
+    }
+    sum = warp_join(sum, sc.c, sc.greedy);
+    row.m = sum.m;
+    row.l = sum.l / exp2_fast(below_ref(sum.m, sum.m, sc.c));    // (exactly 1 where there is one token)
+    row.at = sum.at;
+    const bool some = row.l > 0.f;                     // (and not NaN)
+    const Row<KIND> of{row.m, row.l, sc.c};
+    const float px = some ? of.exact(d.value) : 0.f;
+    row.ok = some && d.inside && (sc.greedy ? sum.at == d.x : d.u * d.q < px);
+    row.logprob = of.log_of(d.value);
+  }
+  if (d.any && !d.inside) row.ok = -1;
+  return row;
+}
+
+// What the CTAs of the others meet in.
 __global__ void __launch_bounds__(VERIFY_THREADS) verify_init_kernel(const VerifyParams p) {
   pdl_wait();
   pdl_launch();
   for (int s = blockIdx.x * VERIFY_THREADS + threadIdx.x; s < p.batch; s += gridDim.x * VERIFY_THREADS) {
     p.key[s] = 0;
     p.done[s] = 0;
+    p.stop[s] = 0x7fffffff;
   }
+  for (int r = blockIdx.x * VERIFY_THREADS + threadIdx.x; r < p.total_rows; r += gridDim.x * VERIFY_THREADS) p.through[r] = 0;
 }
+
+// The masses of all rows, a CTA a piece.
+template <int KIND>
+__device__ __forceinline__ Mass piece_mass(const Share<typename TargetOf<KIND>::type>& share, const Scale& sc, Mass* s_warp) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Mass mass = warp_join(share.mass(sc.c, sc.greedy), sc.c, sc.greedy);
+  if (lane == 0) s_warp[warp] = mass;
+  __syncthreads();
+  return warp == 0 ? warp_join(lane < VERIFY_WARPS ? s_warp[lane] : no_mass(), sc.c, sc.greedy) : mass;      // (of the first warp)
+}
+__device__ __forceinline__ uint4 packed(const Mass& s) { return make_uint4(__float_as_uint(s.m), __float_as_uint(s.l), s.at, 0); }
 
 template <int KIND>
 __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const VerifyParams p) {
   using T = typename TargetOf<KIND>::type;
   __shared__ Mass s_warp[VERIFY_WARPS];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31;
   const int r = blockIdx.x / p.pieces, piece = blockIdx.x % p.pieces;
   pdl_wait();
   pdl_launch();
@@ -356,7 +416,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const Ve
   }
   Share<T> share;
   share.fetch(static_cast<const T*>(p.target) + r * p.target_stride, piece * p.piece, min(p.vocab, (piece + 1) * p.piece));
-  // the row's sequence, the last that starts at or before it, of whose rows the range must be one that the call was given
+  // the row's sequence: the last that starts at or before it
   int lo = 0, n = p.batch;
   while (n > 32) {
     const int step = (n + 31) / 32;
@@ -366,23 +426,55 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const Ve
     lo += i * step;
   }
   lo += 31 - __clz((int)(__ballot_sync(0xffffffffu, lane < n && *(p.row_indptr + lo + lane) <= r) | 1u));
-  const Scale sc = scale_of(p, lo);
-  const Mass mass = warp_join(share.mass(sc.c, sc.greedy), sc.c, sc.greedy);
-  if (lane == 0) s_warp[warp] = mass;
-  __syncthreads();
-  if (warp == 0) {
-    const Mass sum = warp_join(lane < VERIFY_WARPS ? s_warp[lane] : no_mass(), sc.c, sc.greedy);
-    if (lane == 0)
-      p.part[blockIdx.x] = make_uint4(__float_as_uint(sum.m), __float_as_uint(sum.l), sum.at, 0);
+  const Mass sum = piece_mass<KIND>(share, scale_of(p, lo), s_warp);
+  if (tid == 0) p.part[blockIdx.x] = packed(sum);
+}
+
+// The same, first rows first: all sequences' first rows, then their second ones, and so on.  The last piece of a row to be through judges
+// it, and rows behind one that has refused are left out by CTAs that start after that.
+template <int KIND>
+__global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_ordered_kernel(const VerifyParams p) {
+  using T = typename TargetOf<KIND>::type;
+  __shared__ Mass s_warp[VERIFY_WARPS];
+  __shared__ int s_stop;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per_place = p.batch * p.pieces, rest = blockIdx.x % per_place;
+  const int s = rest / p.pieces, piece = rest % p.pieces;
+  const int r0 = *(p.row_indptr + s), r1 = *(p.row_indptr + s + 1);
+  const int n = r0 >= 0 && r1 <= p.total_rows ? r1 - r0 : 0;
+  const Scale sc = scale_of(p, s);
+  pdl_wait();
+  pdl_launch();
+  for (int i = blockIdx.x / per_place; i < n; i += gridDim.x / per_place) {
+    if (tid == 0) s_stop = *reinterpret_cast<volatile int*>(p.stop + s);
+    __syncthreads();
+    if (s_stop < i) break;
+    const int r = r0 + i;
+    Share<T> share;
+    share.fetch(static_cast<const T*>(p.target) + r * p.target_stride, piece * p.piece, min(p.vocab, (piece + 1) * p.piece));
+    const Mass sum = piece_mass<KIND>(share, sc, s_warp);
+    if (warp == 0) {
+      int before = 0;
+      if (lane == 0) {
+        p.part[(size_t)r * p.pieces + piece] = packed(sum);
+        __threadfence();
+        before = atomicAdd(p.through + r, 1);
+        __threadfence();
+      }
+      if (__shfl_sync(0xffffffffu, before, 0) == p.pieces - 1) {
+        const RowResult row = judge<KIND>(p, r, draft_of<KIND>(p, r, i < n - 1, sc), sc);
+        if (lane == 0) {
+          p.result[r] = row;
+          if (row.ok <= 0) atomicMin(p.stop + s, i);
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
-struct RowResult {
-  float m, l, logprob;      // of the row, and of its draft
-  int at, ok;               // place of the maximum; draft accepted: 1, refused: 0, refused for what it is: -1
-};
-
-template <int KIND>
+// The end of every sequence: the row it stops at (found here, or DECIDED already), and the race.
+template <int KIND, bool DECIDED>
 __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const VerifyParams p) {
   using T = typename TargetOf<KIND>::type;
   __shared__ RowResult s_row[VERIFY_WARPS];
@@ -401,68 +493,42 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   int32_t* out_tokens = p.out_tokens ? p.out_tokens + (size_t)s * p.out_stride : nullptr;
   float* out_logprobs = p.out_logprobs ? p.out_logprobs + (size_t)s * p.out_stride : nullptr;
 
-  // ---- rows until one accepts nothing: a warp a row
   int stop = -1, status = rows_ok ? 0 : EFIM_DEV_BAD_POSITION;
   RowResult last{};
   bool waited = false;
-  for (int i0 = 0; i0 < n && stop < 0; i0 += VERIFY_WARPS) {
-    const int i = i0 + warp;
-    int x = -1;
-    float u = 0.f, q = 1.f, value = -INFINITY;
-    bool inside = false;
-    if (i < n - 1) {
-      x = *(p.tokens + r0 + i + 1);
-      inside = x >= 0 && x < p.vocab;
-      if (inside) {
-        value = as_float(target[(r0 + i) * p.target_stride + x]);
-        if (!sc.greedy) {
-          u = *(p.uniform + r0 + i);
-          if (p.draft_probs) q = p.draft_probs[(r0 + i) * p.draft_stride + x];
-        }
-      }
-    }
-    if (!waited) pdl_wait();
+  if constexpr (DECIDED) {
+    pdl_wait();
     waited = true;
-    if (i < n) {
-      RowResult row{0.f, 1.f, 0.f, 0, 0};
-      if (KIND == TARGET_PROBS) {
-        row.ok = i < n - 1 && inside && u * q < value;
-        row.logprob = logf(value);
-      } else {
-        Mass sum = no_mass();
-        for (int k = lane; k < p.pieces; k += 32) {
-          const uint4 w = *(p.part + (size_t)(r0 + i) * p.pieces + k);
-          const Mass o{__uint_as_float(w.x), __uint_as_float(w.y), (int)w.z};
-          const float m = fmaxf(sum.m, o.m);
-          sum.l = sum.l * shift(sum.m, m, sc.c) + o.l * shift(o.m, m, sc.c);
-          if (o.m > sum.m) sum.at = o.at;              // (a lane's places rise)
-          sum.m = m;
-        }
-        sum = warp_join(sum, sc.c, sc.greedy);
-        row.m = sum.m;
-        row.l = sum.l / exp2_fast(below_ref(sum.m, sum.m, sc.c));    // (exactly 1 where there is one token)
-        row.at = sum.at;
-        const bool any = row.l > 0.f;                  // (and not NaN)
-        const Row<KIND> of{row.m, row.l, sc.c};
-        const float px = any ? of.exact(value) : 0.f;
-        row.ok = i < n - 1 && any && inside && (sc.greedy ? sum.at == x : u * q < px);
-        row.logprob = of.log_of(value);
+    if (n > 0) {
+      stop = *(p.stop + s);
+      last = p.result[r0 + stop];
+      if (first && out_logprobs)
+        for (int i = tid; i < min(stop, p.out_stride); i += VERIFY_THREADS) out_logprobs[i] = p.result[r0 + i].logprob;
+    }
+  } else {
+    // rows until one accepts nothing: a warp a row
+    for (int i0 = 0; i0 < n && stop < 0; i0 += VERIFY_WARPS) {
+      const int i = i0 + warp;
+      const Draft d = draft_of<KIND>(p, r0 + i, i < n - 1, sc);
+      if (!waited) pdl_wait();
+      waited = true;
+      if (i < n) {
+        const RowResult row = judge<KIND>(p, r0 + i, d, sc);
+        if (lane == 0) s_row[warp] = row;
       }
-      if (i < n - 1 && !inside) row.ok = -1;
-      if (lane == 0) s_row[warp] = row;
+      __syncthreads();
+      const int count = min(VERIFY_WARPS, n - i0);
+      int good = 0;
+      while (good < count && s_row[good].ok > 0) ++good;
+      if (good < count) {
+        stop = i0 + good;
+        last = s_row[good];
+      }
+      if (first && out_logprobs && tid < good && i0 + tid < p.out_stride) out_logprobs[i0 + tid] = s_row[tid].logprob;
+      __syncthreads();
     }
-    __syncthreads();
-    const int count = min(VERIFY_WARPS, n - i0);
-    int good = 0;
-    while (good < count && s_row[good].ok > 0) ++good;
-    if (good < count) {
-      stop = i0 + good;
-      last = s_row[good];
-      if (last.ok < 0) status |= EFIM_DEV_BAD_TOKEN;
-    }
-    if (first && out_logprobs && tid < good && i0 + tid < p.out_stride) out_logprobs[i0 + tid] = s_row[tid].logprob;
-    __syncthreads();
   }
+  if (last.ok < 0) status |= EFIM_DEV_BAD_TOKEN;
   if (!waited) pdl_wait();
   pdl_launch();
   if (first) {
@@ -560,17 +626,38 @@ static Pieces pieces_of(long long rows, int vocab, int most) {
 }
 constexpr int MASS_MOST_BYTES = MASS_VECTORS * VERIFY_THREADS * 16, RACE_MOST = 8192;
 
-// The most that a call of at most these rows over at most this vocabulary cuts its rows into: one wave, or the largest pieces.
-static size_t part_bytes(long long rows, int vocab) {
+// The workspace, laid out one array behind the other.  Masses: the most that a call of at most these rows over at most this vocabulary
+// cuts them into is one wave, or the largest pieces.
+static size_t verify_layout(long long batch, long long rows, int vocab, char* ws, VerifyParams* p) {
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    char* x = ws + at;
+    at += (bytes + 255) / 256 * 256;
+    return x;
+  };
   const long long least = (vocab + MASS_MOST_BYTES / 4 - 1) / (MASS_MOST_BYTES / 4);
-  return ((size_t)std::max(4LL * sm_count() + rows, rows * least) * sizeof(uint4) + 255) / 256 * 256;
+  uint4* part = reinterpret_cast<uint4*>(take(std::max(4LL * sm_count() + rows, rows * least) * sizeof(uint4)));
+  RowResult* result = reinterpret_cast<RowResult*>(take(rows * sizeof(RowResult)));
+  unsigned long long* key = reinterpret_cast<unsigned long long*>(take(batch * 8));
+  int* done = reinterpret_cast<int*>(take(batch * 4));
+  int* stop = reinterpret_cast<int*>(take(batch * 4));
+  int* through = reinterpret_cast<int*>(take(rows * 4));
+  if (p) {
+    p->part = part;
+    p->result = result;
+    p->key = key;
+    p->done = done;
+    p->stop = stop;
+    p->through = through;
+  }
+  return at;
 }
 
 }  // namespace efim
 
 extern "C" size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab) {
   if (batch <= 0 || total_rows < 0 || vocab <= 0) return 0;
-  return efim::part_bytes(total_rows, vocab) + (size_t)batch * 16;
+  return efim::verify_layout(batch, total_rows, vocab, nullptr, nullptr);
 }
 
 extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_accepted, int32_t* d_next_token,
@@ -613,28 +700,36 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   p.total_rows = d->total_rows;
   p.vocab = d->vocab;
   p.out_stride = d_out_tokens || d_out_logprobs ? out_stride : 0;
-  char* ws = static_cast<char*>(d_workspace);
-  p.part = reinterpret_cast<uint4*>(ws);
-  p.key = reinterpret_cast<unsigned long long*>(ws + part_bytes(d->total_rows, d->vocab));
-  p.done = reinterpret_cast<int*>(p.key + d->batch);
+  verify_layout(d->batch, d->total_rows, d->vocab, static_cast<char*>(d_workspace), &p);
   const Pieces mass = pieces_of(d->total_rows, d->vocab, d->target_kind == EFIM_TARGET_LOGITS_BF16 ? MASS_MOST_BYTES / 2 : MASS_MOST_BYTES / 4);
-  const Pieces race = pieces_of(d->batch, d->vocab, RACE_MOST);
+  const bool logits = d->target_kind != EFIM_TARGET_PROBS_F32 && d->total_rows > 0;
+  const bool bf16 = d->target_kind == EFIM_TARGET_LOGITS_BF16;
+  const long long ctas = (long long)mass.count * d->total_rows;
+  bool ordered = logits && ctas >= 16LL * sm_count();
+  if (getenv("V_ORD")) ordered = logits && atoi(getenv("V_ORD"));
+  int most = RACE_MOST;
+  if (getenv("V_RACE")) most = atoi(getenv("V_RACE"));
+  const Pieces race = pieces_of(d->batch, d->vocab, most);
   p.piece = mass.size;
   p.pieces = mass.count;
   p.race_piece = race.size;
   p.race_pieces = race.count;
-  if ((long long)mass.count * d->total_rows > 0x7fffffffLL || (long long)race.count * d->batch > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  const long long places = std::max<long long>(1, (d->total_rows + d->batch - 1) / d->batch);      // rows of a sequence, on average
+  if (ctas > 0x7fffffffLL || places * d->batch * mass.count > 0x7fffffffLL || (long long)race.count * d->batch > 0x7fffffffLL)
+    return EFIM_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const dim3 block(VERIFY_THREADS), pick((unsigned)(race.count * d->batch));
-  if (d->target_kind == EFIM_TARGET_PROBS_F32 || d->total_rows == 0) {
-    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3(1), block, 0, s, p));
-  } else {
-    EFIM_CUDA_TRY(launch_pdl(d->target_kind == EFIM_TARGET_LOGITS_BF16 ? verify_mass_kernel<TARGET_BF16> : verify_mass_kernel<TARGET_F32>,
-                             dim3((unsigned)(mass.count * d->total_rows)), block, 0, s, p));
-  }
-  EFIM_CUDA_TRY(launch_pdl(d->target_kind == EFIM_TARGET_LOGITS_BF16  ? verify_pick_kernel<TARGET_BF16>
-                           : d->target_kind == EFIM_TARGET_LOGITS_F32 ? verify_pick_kernel<TARGET_F32>
-                                                                      : verify_pick_kernel<TARGET_PROBS>,
+  if (!logits || ordered)
+    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3((unsigned)((std::max(d->total_rows, d->batch) + VERIFY_THREADS - 1) / VERIFY_THREADS)),
+                             block, 0, s, p));
+  if (ordered)
+    EFIM_CUDA_TRY(launch_pdl(bf16 ? verify_ordered_kernel<TARGET_BF16> : verify_ordered_kernel<TARGET_F32>,
+                             dim3((unsigned)(places * d->batch * mass.count)), block, 0, s, p));
+  else if (logits)
+    EFIM_CUDA_TRY(launch_pdl(bf16 ? verify_mass_kernel<TARGET_BF16> : verify_mass_kernel<TARGET_F32>, dim3((unsigned)ctas), block, 0, s, p));
+  EFIM_CUDA_TRY(launch_pdl(d->target_kind == EFIM_TARGET_PROBS_F32 ? verify_pick_kernel<TARGET_PROBS, false>
+                           : bf16 ? (ordered ? verify_pick_kernel<TARGET_BF16, true> : verify_pick_kernel<TARGET_BF16, false>)
+                                  : (ordered ? verify_pick_kernel<TARGET_F32, true> : verify_pick_kernel<TARGET_F32, false>),
                            pick, block, 0, s, p));
   return EFIM_OK;
 }
