@@ -164,7 +164,7 @@ class _Calls:
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
         loader.exec_module(module)
         for m in ("kv_append", "append_prefill_attn", "append_prefill_step", "decode_attn", "decode_step",
-                  "qk_norm_append", "draft_lookup", "verify_drafts"):
+                  "qk_norm_append", "draft_lookup", "verify_workspace_bytes", "verify_drafts"):
             setattr(self, m, getattr(module, m))          # found directly from now on
         return self.__dict__[name]
 
@@ -313,45 +313,22 @@ def efim_kv_append(cache: Cache, batch: Batch, rope, q, k_new, v_new, status=Non
 def efim_qk_norm_append(cache: Cache, batch: Batch, norm: QkNorm, rope, q, k, v, q_out, status=None, stream=None):
     """efim_kv_append with a norm of every q and k head before the rotation.  q, k and v: bf16, one row per new token (of any rank
     past the first, packed), views of one buffer allowed; q_out: packed.  q and q_out may both be None."""
-    heads = cache.desc.num_kv_heads * cache.desc.head_dim
-    tokens = batch.desc.total_new_tokens
-    strides = [_row_stride(x, tokens, n) for x, n in ((q, cache.desc.num_q_heads * cache.desc.head_dim), (k, heads), (v, heads))]
     st = _calls.qk_norm_append(_addr(cache.desc), _addr(batch.desc), _addr(norm.desc),
-                               _addr(rope.desc) if rope is not None else None, q, strides[0], k, strides[1], v, strides[2], q_out,
-                               status, _stream_ptr(stream))
+                               _addr(rope.desc) if rope is not None else None, q, k, v, q_out, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_qk_norm_append")
-
-
-def _row_stride(x, rows, row):
-    """Elements from one row of x to the next; its rows are packed."""
-    if x is None:
-        return 0
-    shape, stride = x.shape, x.stride()
-    inner = 1
-    for n, step in zip(shape[:0:-1], stride[:0:-1]):
-        if step != inner and n != 1:
-            raise ValueError("the values of a token are packed")
-        inner *= n
-    if shape[0] != rows or inner != row:
-        raise ValueError(f"{rows} rows of {row} values are expected, not {tuple(shape)}")
-    return stride[0] if rows > 1 else row
 
 
 def efim_draft_lookup(history, lengths, min_ngram, max_ngram, drafts, draft_len, status=None, stream=None):
     """Drafts for each row of `history` (int32 [batch, max_len], rows may be further apart) from what followed its last tokens
     earlier on; drafts: int32 [batch, num_drafts]."""
-    batch, max_len = history.shape
-    if history.stride(1) != 1 or not drafts.is_contiguous():
-        raise ValueError("rows of the history, and the drafts, are packed")
-    st = _calls.draft_lookup(batch, history, history.stride(0) if batch > 1 else max_len, max_len, lengths, int(min_ngram),
-                             int(max_ngram), drafts.shape[1], drafts, draft_len, status, _stream_ptr(stream))
+    st = _calls.draft_lookup(history, lengths, min_ngram, max_ngram, drafts, draft_len, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_draft_lookup")
 
 
 def efim_verify_workspace_bytes(batch: int, total_rows: int, vocab: int) -> int:
-    return int(load_library().efim_verify_workspace_bytes(batch, total_rows, vocab))
+    return _calls.verify_workspace_bytes(batch, total_rows, vocab)
 
 
 def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform=None, noise=None, draft_probs=None,
@@ -361,30 +338,25 @@ def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform
     `target_is_probs` probabilities in fp32; draft_probs fp32 [rows, vocab]; noise fp32 [batch, vocab] (none: greedy);
     out_tokens and out_logprobs: packed [batch, n] of the same n.  Without a workspace one is taken from torch's allocator, on
     torch's current stream, which the call then has to run on."""
-    batch = row_indptr.shape[0] - 1
-    rows, vocab = target.shape
-    kind = 2 if target_is_probs else 0 if target.element_size() == 2 else 1
-    strides = [_matrix_stride(x, vocab) for x in (target, draft_probs, noise)]
-    out = out_tokens if out_tokens is not None else out_logprobs
+    batch = accepted.shape[0]
+    stream = _stream_ptr(stream)
     if workspace is None:
-        if stream is not None and _stream_ptr(stream) != _current_stream():
+        if stream != _current_stream():
             raise ValueError("a call on another stream than torch's current one brings its workspace along")
-        torch = _torch()
-        workspace = torch.empty(efim_verify_workspace_bytes(batch, rows, vocab), dtype=torch.uint8, device=target.device)
-    st = _calls.verify_drafts(batch, rows, vocab, kind, row_indptr, tokens, target, strides[0], draft_probs, strides[1], uniform,
-                              noise, strides[2], temperature, accepted, next_token, out_tokens, out_logprobs,
-                              out.shape[1] if out is not None else 0, workspace, status, _stream_ptr(stream))
+        workspace = _bytes_beside(target, _calls.verify_workspace_bytes(batch, *target.shape))
+    st = _calls.verify_drafts(batch, row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature, accepted,
+                              next_token, out_tokens, out_logprobs, workspace, status, stream)
     if st != 0:
         raise EfimError(st, "efim_verify_drafts")
 
 
-def _matrix_stride(x, columns):
-    if x is None:
-        return 0
-    step, unit = x.stride()
-    if unit != 1 or x.shape[1] != columns:
-        raise ValueError(f"rows of {columns} packed values are expected")
-    return step if x.shape[0] > 1 else columns
+def _bytes_beside(tensor, n):
+    global _bytes_beside
+    uint8 = _torch().uint8
+
+    def _bytes_beside(tensor, n):
+        return tensor.new_empty(n, dtype=uint8)
+    return _bytes_beside(tensor, n)
 
 
 def efim_prefill_workspace_bytes(cache: Cache, batch: Batch) -> int:

@@ -3,7 +3,8 @@
  * A decode step takes the GPU a few microseconds, and converting its seventeen arguments in Python and
  * ctypes took the host about as long.  Here a call is one C function: descriptors come as addresses,
  * device memory as anything with a data_ptr() (a torch tensor), as an integer address or None, a plan as a
- * numpy array.  Returns the efim_status as an int; nothing else happens here. */
+ * numpy array.  Calls whose tensors may be strided take shapes, types and strides from the tensors and check them.  Returns the
+ * efim_status as an int; nothing else happens here. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include "efim.h"
@@ -42,10 +43,6 @@ static int as_i32(PyObject* o, int32_t* out) {
   if (v == -1 && PyErr_Occurred()) return 0;
   *out = (int32_t)v;
   return 1;
-}
-static int as_i64(PyObject* o, int64_t* out) {
-  *out = PyLong_AsLongLong(o);
-  return !(*out == -1 && PyErr_Occurred());
 }
 static int as_float(PyObject* o, float* out) {
   const double v = PyFloat_AsDouble(o);
@@ -172,50 +169,147 @@ static PyObject* decode_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
                                           scale, p[13], ws, p[14], p[15]));
 }
 
-/* cache, batch, norm, rope, q, q_stride, k, k_stride, v, v_stride, q_out, status, stream */
+/* ---- calls that take shapes and row strides from the tensors themselves */
+static PyObject *s_shape, *s_stride, *s_dtype, *bf16, *f32, *i32; /* torch's types, looked up by the first such call */
+
+static int have_types(void) {
+  if (i32) return 1;
+  PyObject* torch = PyImport_ImportModule("torch");
+  if (!torch) return 0;
+  bf16 = PyObject_GetAttrString(torch, "bfloat16");
+  f32 = PyObject_GetAttrString(torch, "float32");
+  i32 = PyObject_GetAttrString(torch, "int32");
+  Py_DECREF(torch);
+  return bf16 && f32 && i32;
+}
+static int is_tensor(PyObject* o) { return o != Py_None && !PyLong_Check(o) && !PyObject_TypeCheck(o, ndarray); }
+static int is_type(PyObject* o, PyObject* type) { /* -1: no such attribute */
+  PyObject* t = PyObject_GetAttr(o, s_dtype);
+  Py_XDECREF(t); /* (the types live on) */
+  return t ? t == type : -1;
+}
+/* address of values of one type; an address without a type is taken at its word */
+static int as_typed(PyObject* o, PyObject* type, const char* what, void** out) {
+  if (is_tensor(o)) {
+    const int ok = is_type(o, type);
+    if (ok <= 0) {
+      if (!ok) PyErr_Format(PyExc_TypeError, "%s: a tensor of %S is expected", what, type);
+      return 0;
+    }
+  }
+  return as_ptr(o, out);
+}
+/* Rows of a tensor: their number, values (all dimensions but the first, packed) and the distance from one to the next.  None has none. */
+static int as_rows(PyObject* o, PyObject* type, const char* what, void** out, int64_t* rows, int64_t* row, int64_t* step) {
+  *out = NULL;
+  *rows = *row = *step = 0;
+  if (o == Py_None) return 1;
+  if (!as_typed(o, type, what, out)) return 0;
+  PyObject* shape = PyObject_GetAttr(o, s_shape);
+  PyObject* stride = shape ? PyObject_CallMethodNoArgs(o, s_stride) : NULL;
+  int ok = 0;
+  if (stride && PyTuple_Check(shape) && PyTuple_Check(stride) && PyTuple_GET_SIZE(shape) >= 2 &&
+      PyTuple_GET_SIZE(shape) == PyTuple_GET_SIZE(stride)) {
+    ok = 1;
+    *row = 1;
+    for (Py_ssize_t d = PyTuple_GET_SIZE(shape) - 1; d >= 0; --d) {
+      const int64_t n = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, d)), s = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, d));
+      if (d == 0) {
+        *rows = n;
+        *step = n > 1 ? s : *row; /* a single row may stand anywhere */
+      } else {
+        if (s != *row && n > 1) ok = 0;
+        *row *= n;
+      }
+    }
+  }
+  Py_XDECREF(shape);
+  Py_XDECREF(stride);
+  if (PyErr_Occurred()) return 0;
+  if (!ok) PyErr_Format(PyExc_ValueError, "%s: rows of packed values are expected", what);
+  return ok;
+}
+static int expect(int64_t got, int64_t wanted, const char* what) {
+  if (got == wanted) return 1;
+  PyErr_Format(PyExc_ValueError, "%s: %lld expected, got %lld", what, (long long)wanted, (long long)got);
+  return 0;
+}
+/* rows of what is given, of a known shape */
+static int as_matrix(PyObject* o, PyObject* type, const char* what, int64_t rows, int64_t row, void** out, int64_t* step) {
+  int64_t n, m;
+  return as_rows(o, type, what, out, &n, &m, step) && (o == Py_None || (expect(n, rows, what) && expect(m, row, what)));
+}
+
+/* cache, batch, norm, rope, q, k, v, q_out, status, stream */
 static PyObject* qk_norm_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[13];
-  int64_t q_stride, k_stride, v_stride;
-  if (!want(n, 13)) return NULL;
-  if (!PTR(0) || !PTR(1) || !PTR(2) || !PTR(3) || !PTR(4) || !as_i64(a[5], &q_stride) || !PTR(6) || !as_i64(a[7], &k_stride) ||
-      !PTR(8) || !as_i64(a[9], &v_stride) || !PTR(10) || !PTR(11) || !PTR(12))
+  void* p[10];
+  int64_t qs, ks, vs, os;
+  if (!want(n, 10) || !have_types()) return NULL;
+  if (!PTR(0) || !PTR(1) || !PTR(2) || !PTR(3) || !as_typed(a[8], i32, "status", &p[8]) || !PTR(9)) return NULL;
+  const efim_cache_desc* c = p[0];
+  const int64_t rows = ((const efim_batch_desc*)p[1])->total_new_tokens, q = (int64_t)c->num_q_heads * c->head_dim,
+                kv = (int64_t)c->num_kv_heads * c->head_dim;
+  if (!as_matrix(a[4], bf16, "q", rows, q, &p[4], &qs) || !as_matrix(a[5], bf16, "k", rows, kv, &p[5], &ks) ||
+      !as_matrix(a[6], bf16, "v", rows, kv, &p[6], &vs) || !as_matrix(a[7], bf16, "q_out", rows, q, &p[7], &os) ||
+      (p[7] && !expect(os, q, "q_out, values from one row to the next")))
     return NULL;
-  RETURN_STATUS(efim_qk_norm_append(p[0], p[1], p[2], p[3], p[4], q_stride, p[6], k_stride, p[8], v_stride, p[10], p[11], p[12]));
+  RETURN_STATUS(efim_qk_norm_append(p[0], p[1], p[2], p[3], p[4], qs, p[5], ks, p[6], vs, p[7], p[8], p[9]));
 }
 
-/* batch, history, stride, max_len, len, min_ngram, max_ngram, num_drafts, drafts, draft_len, status, stream */
+/* history, len, min_ngram, max_ngram, drafts, draft_len, status, stream */
 static PyObject* draft_lookup(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[12];
-  int64_t stride;
-  int32_t batch, max_len, lo, hi, num;
-  if (!want(n, 12)) return NULL;
-  if (!as_i32(a[0], &batch) || !PTR(1) || !as_i64(a[2], &stride) || !as_i32(a[3], &max_len) || !PTR(4) || !as_i32(a[5], &lo) ||
-      !as_i32(a[6], &hi) || !as_i32(a[7], &num) || !PTR(8) || !PTR(9) || !PTR(10) || !PTR(11))
+  void* p[8];
+  int64_t batch, max_len, stride, rows, num, step;
+  int32_t lo, hi;
+  if (!want(n, 8) || !have_types()) return NULL;
+  if (!as_rows(a[0], i32, "history", &p[0], &batch, &max_len, &stride) || !as_typed(a[1], i32, "lengths", &p[1]) ||
+      !as_i32(a[2], &lo) || !as_i32(a[3], &hi) || !as_rows(a[4], i32, "drafts", &p[4], &rows, &num, &step) ||
+      !expect(rows, batch, "drafts, rows") || !expect(step, num, "drafts, values from one row to the next") ||
+      !as_typed(a[5], i32, "draft_len", &p[5]) || !as_typed(a[6], i32, "status", &p[6]) || !PTR(7))
     return NULL;
-  RETURN_STATUS(efim_draft_lookup(batch, p[1], stride, max_len, p[4], lo, hi, num, p[8], p[9], p[10], p[11]));
+  RETURN_STATUS(efim_draft_lookup((int32_t)batch, p[0], stride, (int32_t)max_len, p[1], lo, hi, (int32_t)num, p[4], p[5], p[6], p[7]));
 }
 
-/* batch, rows, vocab, kind, row_indptr, tokens, target, stride, draft_probs, stride, uniform, noise, stride, temperature, accepted,
-   next_token, out_tokens, out_logprobs, out_stride, workspace, status, stream */
+/* batch, rows, vocab */
+static PyObject* verify_workspace_bytes(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  int32_t batch, rows, vocab;
+  if (!want(n, 3) || !as_i32(a[0], &batch) || !as_i32(a[1], &rows) || !as_i32(a[2], &vocab)) return NULL;
+  return PyLong_FromSize_t(efim_verify_workspace_bytes(batch, rows, vocab));
+}
+
+/* batch, row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature, accepted, next_token, out_tokens,
+   out_logprobs, workspace, status, stream */
 static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[22];
+  void* p[16];
   efim_verify_desc d;
-  int32_t out_stride;
+  int64_t rows, vocab, out_rows, step, width = 0, logs = 0;
   size_t ws;
-  if (!want(n, 22)) return NULL;
-  if (!as_i32(a[0], &d.batch) || !as_i32(a[1], &d.total_rows) || !as_i32(a[2], &d.vocab) || !as_i32(a[3], &d.target_kind) ||
-      !PTR(4) || !PTR(5) || !PTR(6) || !as_i64(a[7], &d.target_stride) || !PTR(8) || !as_i64(a[9], &d.draft_stride) || !PTR(10) ||
-      !PTR(11) || !as_i64(a[12], &d.noise_stride) || !PTR(13) || !PTR(14) || !PTR(15) || !PTR(16) || !PTR(17) ||
-      !as_i32(a[18], &out_stride) || !as_workspace(a[19], &p[19], &ws) || !PTR(20) || !PTR(21))
+  if (!want(n, 16) || !have_types()) return NULL;
+  const int probs = PyObject_IsTrue(a[4]), half = probs ? 0 : is_type(a[3], bf16);
+  if (probs < 0 || half < 0) return NULL;
+  if (!as_i32(a[0], &d.batch) || !as_typed(a[1], i32, "row_indptr", &p[1]) || !as_typed(a[2], i32, "tokens", &p[2]) ||
+      !as_rows(a[3], half ? bf16 : f32, "target", &p[3], &rows, &vocab, &d.target_stride) ||
+      !as_matrix(a[5], f32, "draft_probs", rows, vocab, &p[5], &d.draft_stride) || !as_typed(a[6], f32, "uniform", &p[6]) ||
+      !as_matrix(a[7], f32, "noise", d.batch, vocab, &p[7], &d.noise_stride) || !as_typed(a[8], f32, "temperature", &p[8]) ||
+      !as_typed(a[9], i32, "accepted", &p[9]) || !as_typed(a[10], i32, "next_token", &p[10]) ||
+      !as_rows(a[11], i32, "out_tokens", &p[11], &out_rows, &width, &step) ||
+      (p[11] && (!expect(out_rows, d.batch, "out_tokens, rows") || !expect(step, width, "out_tokens, values from one row to the next"))) ||
+      !as_rows(a[12], f32, "out_logprobs", &p[12], &out_rows, &logs, &step) ||
+      (p[12] && (!expect(out_rows, d.batch, "out_logprobs, rows") || !expect(step, logs, "out_logprobs, values from one row to the next"))) ||
+      (p[11] && p[12] && !expect(logs, width, "out_logprobs, values of a row")) || !as_workspace(a[13], &p[13], &ws) ||
+      !as_typed(a[14], i32, "status", &p[14]) || !PTR(15))
     return NULL;
-  d.d_row_indptr = p[4];
-  d.d_tokens = p[5];
-  d.d_target = p[6];
-  d.d_draft_probs = p[8];
-  d.d_uniform = p[10];
-  d.d_noise = p[11];
-  d.d_temperature = p[13];
-  RETURN_STATUS(efim_verify_drafts(&d, p[14], p[15], p[16], p[17], out_stride, p[19], ws, p[20], p[21]));
+  d.total_rows = (int32_t)rows;
+  d.vocab = (int32_t)vocab;
+  d.target_kind = probs ? EFIM_TARGET_PROBS_F32 : half ? EFIM_TARGET_LOGITS_BF16 : EFIM_TARGET_LOGITS_F32;
+  d.d_row_indptr = p[1];
+  d.d_tokens = p[2];
+  d.d_target = p[3];
+  d.d_draft_probs = p[5];
+  d.d_uniform = p[6];
+  d.d_noise = p[7];
+  d.d_temperature = p[8];
+  RETURN_STATUS(efim_verify_drafts(&d, p[9], p[10], p[11], p[12], (int32_t)(p[11] ? width : logs), p[13], ws, p[14], p[15]));
 }
 
 static PyMethodDef methods[] = {
@@ -226,6 +320,7 @@ static PyMethodDef methods[] = {
     {"decode_step", (PyCFunction)(void*)decode_step, METH_FASTCALL, NULL},
     {"qk_norm_append", (PyCFunction)(void*)qk_norm_append, METH_FASTCALL, NULL},
     {"draft_lookup", (PyCFunction)(void*)draft_lookup, METH_FASTCALL, NULL},
+    {"verify_workspace_bytes", (PyCFunction)(void*)verify_workspace_bytes, METH_FASTCALL, NULL},
     {"verify_drafts", (PyCFunction)(void*)verify_drafts, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -233,8 +328,11 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, m
 PyMODINIT_FUNC PyInit__calls(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_nbytes = PyUnicode_InternFromString("nbytes");
+  s_shape = PyUnicode_InternFromString("shape");
+  s_stride = PyUnicode_InternFromString("stride");
+  s_dtype = PyUnicode_InternFromString("dtype");
   PyObject* numpy = PyImport_ImportModule("numpy");
-  if (!s_data_ptr || !s_nbytes || !numpy) return NULL;
+  if (!s_data_ptr || !s_nbytes || !s_shape || !s_stride || !s_dtype || !numpy) return NULL;
   ndarray = (PyTypeObject*)PyObject_GetAttrString(numpy, "ndarray");
   Py_DECREF(numpy);
   if (!ndarray || !PyType_Check(ndarray)) return NULL;

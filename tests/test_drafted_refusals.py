@@ -89,16 +89,49 @@ def test_verify(lib):
     assert lib.efim_verify_workspace_bytes(0, 6, 1000) == lib.efim_verify_workspace_bytes(2, 6, 0) == 0
 
 
-def test_python_side():
-    """Shapes and strides that the binding can see."""
+def test_python_side(lib):
+    """Types, shapes and strides that the binding can see (tensors of the host, never read)."""
     torch = pytest.importorskip("torch")
-    x = torch.zeros(4, 24, dtype=torch.bfloat16)
-    assert B._row_stride(x, 4, 24) == 24 and B._row_stride(x[:, :8], 4, 8) == 24 and B._row_stride(x.view(4, 3, 8), 4, 24) == 24
-    assert B._row_stride(None, 4, 24) == 0 and B._row_stride(x[:1, :8], 1, 8) == 8
-    for bad in (lambda: B._row_stride(x[:, ::2], 4, 12), lambda: B._row_stride(x, 5, 24), lambda: B._row_stride(x, 4, 16),
-                lambda: B._row_stride(x.view(4, 3, 8).transpose(1, 2), 4, 24), lambda: B._matrix_stride(x.t(), 4),
-                lambda: B._matrix_stride(x, 23), lambda: efim.QkNorm(torch.zeros(8), torch.zeros(8, dtype=torch.bfloat16)),
-                lambda: efim.QkNorm(torch.zeros(16)[::2], None), lambda: efim.QkNorm(torch.zeros(8, dtype=torch.float16), None),
-                lambda: efim.Rope.from_table(torch.zeros(4, 8, dtype=torch.float64))):
+    half, whole = torch.bfloat16, torch.int32
+    pools = torch.zeros(4, 1, 16, 64, dtype=half)
+    cache = efim.Cache(pools, pools.clone(), 2)
+    batch = efim.Batch([0], [4], torch.zeros(1, 4, dtype=whole), device="cpu")
+    norm = efim.QkNorm(None, None)
+    x = torch.zeros(4, 300, dtype=half)
+    good = dict(q=x[:, :128], k=x[:, 128:192], v=x[:, 192:256], q_out=torch.zeros(4, 2, 64, dtype=half))
+
+    def append(**changed):
+        efim.efim_qk_norm_append(cache, batch, norm, None, **{**good, **changed}, stream=0)
+    for error, changed in [(ValueError, dict(q=x[:, :256:2])), (ValueError, dict(q=x[:3, :128])), (ValueError, dict(k=x[:, 128:200])),
+                           (ValueError, dict(v=x[:, :64].reshape(4, 8, 8).transpose(1, 2))), (ValueError, dict(q_out=x[:, :128])),
+                           (ValueError, dict(k=x[0, :64])), (TypeError, dict(k=x[:, :64].float())),
+                           (TypeError, dict(q_out=good["q_out"].half()))]:
+        with pytest.raises(error):
+            append(**changed)
+    for bad in (lambda: efim.QkNorm(torch.zeros(8), torch.zeros(8, dtype=half)), lambda: efim.QkNorm(torch.zeros(16)[::2], None),
+                lambda: efim.QkNorm(torch.zeros(8, dtype=torch.float16), None),
+                lambda: efim.Rope.from_table(torch.zeros(4, 8, dtype=torch.float64)), lambda: efim.Rope.from_table(torch.zeros(8, 8).t()[:, :4])):
         with pytest.raises(ValueError):
             bad()
+    hist, drafts, n = torch.zeros(2, 50, dtype=whole), torch.zeros(2, 3, dtype=whole), torch.zeros(2, dtype=whole)
+    for error, args in [(ValueError, (hist[:, ::2], n, 1, 2, drafts, n)), (ValueError, (hist, n, 1, 2, drafts[:, :2], n)),
+                        (ValueError, (hist, n, 1, 2, drafts[:1], n)), (TypeError, (hist.long(), n, 1, 2, drafts, n)),
+                        (TypeError, (hist, n.long(), 1, 2, drafts, n)), (TypeError, (hist, n, 1, 2.5, drafts, n))]:
+        with pytest.raises(error):
+            efim.efim_draft_lookup(*args, stream=0)
+    logits, ws = torch.zeros(5, 100, dtype=half), torch.zeros(1 << 16, dtype=torch.uint8)
+    r = dict(row_indptr=torch.zeros(3, dtype=whole), tokens=torch.zeros(5, dtype=whole), target=logits, accepted=n, next_token=n.clone(),
+             uniform=torch.zeros(5), noise=torch.zeros(2, 100), workspace=ws)
+    wide = torch.zeros(2, 6)
+    for error, changed in [(TypeError, dict(target=logits.half())), (TypeError, dict(target=logits, target_is_probs=True)),
+                           (TypeError, dict(noise=torch.zeros(2, 100, dtype=half))), (ValueError, dict(noise=torch.zeros(3, 100))),
+                           (ValueError, dict(noise=torch.zeros(2, 99))), (ValueError, dict(draft_probs=torch.zeros(4, 100))),
+                           (ValueError, dict(target=torch.zeros(100, 5, dtype=half).t())), (TypeError, dict(tokens=torch.zeros(5, dtype=torch.int64))),
+                           (ValueError, dict(out_tokens=torch.zeros(2, 6, dtype=whole), out_logprobs=wide[:, :5].contiguous())),
+                           (ValueError, dict(out_logprobs=wide[:, :5])), (ValueError, dict(out_tokens=torch.zeros(1, 6, dtype=whole))),
+                           (TypeError, dict(temperature=torch.zeros(2, dtype=torch.float64)))]:
+        with pytest.raises(error):
+            efim.efim_verify_drafts(**{**r, **changed}, stream=0)
+    with pytest.raises(efim.EfimError) as e:
+        efim.efim_verify_drafts(**{**r, "workspace": ws[:256]}, stream=0)
+    assert e.value.code == WORKSPACE
