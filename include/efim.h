@@ -378,7 +378,7 @@ typedef struct {
   int64_t noise_stride;
   const float* d_temperature;    /* [batch], or NULL: 1 */
 } efim_verify_desc;
-size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab);
+size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab, int32_t target_kind);
 efim_status efim_verify_drafts(const efim_verify_desc* desc, int32_t* d_accepted, int32_t* d_next_token,
                                int32_t* d_out_tokens, float* d_out_logprobs, int32_t out_stride,
                                void* d_workspace, size_t workspace_bytes, int32_t* d_status, void* stream);

@@ -112,7 +112,7 @@ def load_library():
     lib.efim_verify_drafts.argtypes = [POINTER(_VerifyDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
                                        c_size_t, c_void_p, c_void_p]
     lib.efim_verify_workspace_bytes.restype = c_size_t
-    lib.efim_verify_workspace_bytes.argtypes = [c_int32, c_int32, c_int32]
+    lib.efim_verify_workspace_bytes.argtypes = [c_int32, c_int32, c_int32, c_int32]
     lib.efim_selftest_bounded_wait.restype = ctypes.c_int
     lib.efim_selftest_bounded_wait.argtypes = [ctypes.c_uint64, c_void_p, c_void_p, c_void_p]
     lib.efim_decode_workspace_bytes.restype = c_size_t
@@ -327,8 +327,9 @@ def efim_draft_lookup(history, lengths, min_ngram, max_ngram, drafts, draft_len,
         raise EfimError(st, "efim_draft_lookup")
 
 
-def efim_verify_workspace_bytes(batch: int, total_rows: int, vocab: int) -> int:
-    return _calls.verify_workspace_bytes(batch, total_rows, vocab)
+def efim_verify_workspace_bytes(batch: int, target, target_is_probs=False) -> int:
+    """Bytes of workspace for target rows of this shape and type (0: none is needed)."""
+    return _calls.verify_workspace_bytes(batch, target, target_is_probs)
 
 
 def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform=None, noise=None, draft_probs=None,
@@ -341,9 +342,11 @@ def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform
     batch = accepted.shape[0]
     stream = _stream_ptr(stream)
     if workspace is None:
-        if stream != _current_stream():
-            raise ValueError("a call on another stream than torch's current one brings its workspace along")
-        workspace = _bytes_beside(target, _calls.verify_workspace_bytes(batch, *target.shape))
+        need = _calls.verify_workspace_bytes(batch, target, target_is_probs)
+        if need:
+            if stream != _current_stream():
+                raise ValueError("a call on another stream than torch's current one brings its workspace along")
+            workspace = _bytes_beside(target, need)
     st = _calls.verify_drafts(batch, row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature, accepted,
                               next_token, out_tokens, out_logprobs, workspace, status, stream)
     if st != 0:

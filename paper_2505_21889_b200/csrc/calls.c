@@ -270,11 +270,16 @@ static PyObject* draft_lookup(PyObject* self, PyObject* const* a, Py_ssize_t n) 
   RETURN_STATUS(efim_draft_lookup((int32_t)batch, p[0], stride, (int32_t)max_len, p[1], lo, hi, (int32_t)num, p[4], p[5], p[6], p[7]));
 }
 
-/* batch, rows, vocab */
+/* batch, target, target_is_probs */
 static PyObject* verify_workspace_bytes(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  int32_t batch, rows, vocab;
-  if (!want(n, 3) || !as_i32(a[0], &batch) || !as_i32(a[1], &rows) || !as_i32(a[2], &vocab)) return NULL;
-  return PyLong_FromSize_t(efim_verify_workspace_bytes(batch, rows, vocab));
+  void* p;
+  int32_t batch;
+  int64_t rows, vocab, step;
+  if (!want(n, 3) || !have_types() || !as_i32(a[0], &batch)) return NULL;
+  const int probs = PyObject_IsTrue(a[2]), half = probs ? 0 : is_type(a[1], bf16);
+  if (probs < 0 || half < 0 || !as_rows(a[1], half ? bf16 : f32, "target", &p, &rows, &vocab, &step)) return NULL;
+  const int kind = probs ? EFIM_TARGET_PROBS_F32 : half ? EFIM_TARGET_LOGITS_BF16 : EFIM_TARGET_LOGITS_F32;
+  return PyLong_FromSize_t(efim_verify_workspace_bytes(batch, (int32_t)rows, (int32_t)vocab, kind));
 }
 
 /* batch, row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature, accepted, next_token, out_tokens,

@@ -10,115 +10,13 @@
 // Two kernels.  The first takes every row's maximum and sum (its mass), a piece of a row per CTA.  The second has CTAs for pieces of the
 // vocabulary of every sequence: each joins the masses, finds the row at which its sequence stops and runs its piece of the race
 // for the next token there; the last of them to finish writes the result.
-#include "common.cuh"
-#include <float.h>
-#include <stdlib.h>
+#include "verify.cuh"
 #include <algorithm>
 
 namespace efim {
 
 constexpr int VERIFY_THREADS = 256;
 constexpr int VERIFY_WARPS = VERIFY_THREADS / 32;
-
-struct __align__(16) RowResult {
-  float m, l, logprob;      // maximum and sum of the row, log-probability of its draft
-  int at, ok;               // place of the maximum; draft accepted: 1, refused: 0, refused for what it is: -1
-  int unused[3];
-};
-
-struct VerifyParams {
-  const void* target;       // rows of [vocab], target_stride elements apart
-  const int32_t* row_indptr;
-  const int32_t* tokens;    // [total_rows]
-  const float* draft_probs; // rows of [vocab], or null: drafts that are certain
-  const float* uniform;     // [total_rows]
-  const float* noise;       // rows of [vocab], one per sequence, or null: every sequence greedy
-  const float* temperature; // [batch], or null: 1
-  int32_t* accepted;
-  int32_t* next_token;
-  int32_t* out_tokens;      // [batch][out_stride] or null
-  float* out_logprobs;      // the same
-  int32_t* status;
-  uint4* part;              // [total_rows][pieces]: maximum, sum, place of the maximum
-  RowResult* result;        // [total_rows], where rows are taken in order
-  unsigned long long* key;  // [batch] best of the race so far
-  int* done;                // [batch] pieces of the race that are through
-  int* stop;                // [batch] first row so far that accepts nothing, where rows are taken in order
-  int* through;             // [total_rows] pieces of the row that are through, the same
-  long long target_stride, draft_stride, noise_stride;
-  int batch, total_rows, vocab, out_stride;
-  int piece, pieces;        // places of a CTA of the first kernel, CTAs of a row
-  int race_piece, race_pieces;   // places of a CTA of the second, CTAs of a sequence
-};
-
-enum { TARGET_BF16 = EFIM_TARGET_LOGITS_BF16, TARGET_F32 = EFIM_TARGET_LOGITS_F32, TARGET_PROBS = EFIM_TARGET_PROBS_F32 };
-template <int KIND> struct TargetOf { using type = float; };
-template <> struct TargetOf<TARGET_BF16> { using type = uint16_t; };
-
-__device__ __forceinline__ float as_float(float x) { return x; }
-__device__ __forceinline__ float as_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float rcp_fast(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// maximum over the warp; NaN lanes do not count
-__device__ __forceinline__ float warp_max(float x) {
-  float y;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
-}
-// Mass of a row's values: the largest, m; the sum l of 2^(x c - ref(m)); and the first place of the largest (where asked for).
-// ref(m) is the whole number next to m c: x c - ref is then one fused product with one rounding, of what is left, and masses of
-// different m are joined by exact powers of two.  Where m c passes 2^30 (no fp32 logits there are closer than 2^6 in x c) it is m c
-// itself, by way of (x - m) c; so it is for infinite m.  A NaN among the values makes the sum NaN; values of -inf have no mass; at
-// +inf those values share all of it.
-struct Mass {
-  float m, l;
-  int at;
-};
-__device__ __forceinline__ Mass no_mass() { return {-INFINITY, 0.f, 0x7fffffff}; }
-__device__ __forceinline__ bool has_ref(float m, float c) { return fabsf(m * c) < 1073741824.f; }
-// x c - ref(m), x <= m
-__device__ __forceinline__ float below_ref(float x, float m, float c) {
-  if (has_ref(m, c)) return fmaf(x, c, -rintf(m * c));
-  if (x == m) return m == -INFINITY ? -INFINITY : 0.f;
-  return (x - m) * c;
-}
-// what a sum at `from` is worth at `to` >= from
-__device__ __forceinline__ float shift(float from, float to, float c) {
-  if (has_ref(from, c) && has_ref(to, c)) return exp2_fast(rintf(from * c) - rintf(to * c));
-  if (from == to) return 1.f;
-  return exp2_fast((from - to) * c);
-}
-// The lanes' masses together, in every lane.
-__device__ __forceinline__ Mass warp_join(Mass s, float c, bool want_at) {
-  Mass r{warp_max(s.m), 0.f, 0x7fffffff};
-  r.l = s.l * shift(s.m, r.m, c);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) r.l += __shfl_xor_sync(0xffffffffu, r.l, d);
-  if (want_at) r.at = (int)__reduce_min_sync(0xffffffffu, s.m == r.m ? (unsigned)s.at : 0x7fffffffu);
-  return r;
-}
-
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// Values 2 e and 2 e + 1 of the 16 bytes of a vector
-template <typename T>
-__device__ __forceinline__ float2 pair_of(const uint4& w, int e) {
-  const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-  if constexpr (sizeof(T) == 2) return make_float2(bf16lo(q[e]), bf16hi(q[e]));
-  else return make_float2(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1]));
-}
 
 // A thread's share of a piece of a row: up to MASS_VECTORS vectors of 16 bytes, a CTA's threads apart, and one value before and behind
 // the vectors of a piece that is not aligned.  All of it is on its way before anything is computed.
@@ -203,42 +101,18 @@ struct Share {
   }
 };
 
-// Probabilities of one row, from its logits or as they are: m, and l = sum of 2^((x - m) c).
-template <int KIND>
-struct Row {
-  float m, l, c;
-  // (x - m) c, where it is not 0 times or less infinity
-  __device__ __forceinline__ float below(float x) const { return x == m ? 0.f : (x - m) * c; }
-  __device__ __forceinline__ float exact(float x) const { return KIND == TARGET_PROBS ? x : exp2f(below(x)) / l; }
-  __device__ __forceinline__ float log_of(float x) const {
-    return KIND == TARGET_PROBS ? logf(x) : below(x) * 0.6931471805599453f - logf(l);
-  }
-};
-
-// The race for the next token over places [begin, end) of a row: the largest r / e, r = (p - q)^+ or p, the lowest place among
-// equals.  `gone` is a place that does not take part.  Returns (r / e, place) as one number to be compared, 0 if nobody ran.
-//
-// An exact result costs two divisions and an exponential.  So every place gets a bound from above first, by the fast instructions (in a
-// probability: the exponent's rounding 150 * 2^-24 * ln 2, ex2 2^-22, the factor 2^-23; rcp and the products 2^-22 more; the
-// bound is 2^-16 higher, twice), and only places whose bound reaches the best result known so far are computed: a few a warp.
-// `known` is a lower limit of the best, from other CTAs of the race: what it leaves out cannot win.  (Probabilities below 2^-126 are taken
-// for 0 here.)
-constexpr float RACE_ABOVE = 1.f + 1.f / 65536;
+// The race over places [begin, end) of a row.
 template <int KIND, bool VEC>
-__device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>::type* row, const float* noise, const float* q,
-                                                   int begin, int end, int gone, const Row<KIND>& of, float known) {
+__device__ __forceinline__ void race_over(Race<KIND>& race, const typename TargetOf<KIND>::type* row, const float* noise, const float* q,
+                                          int begin, int end) {
   constexpr int N = 8;                                // places of a thread in flight: two groups of four, or eight apart
   using T = typename TargetOf<KIND>::type;
   const int tid = threadIdx.x;
-  const bool plain = KIND == TARGET_PROBS || has_ref(of.m, of.c);
-  const float scale = KIND == TARGET_PROBS ? RACE_ABOVE : RACE_ABOVE / (of.l * exp2_fast(below_ref(of.m, of.m, of.c))), ref = KIND == TARGET_PROBS ? 0.f : rintf(of.m * of.c);
-  unsigned long long key = 0;
-  float best = known;                                 // the warp's
   auto place = [&](int a0, int i) { return VEC ? a0 + (i / 4) * 4 * VERIFY_THREADS + i % 4 : a0 + i * VERIFY_THREADS; };
   const int first = begin + (VEC ? 4 * tid : tid);
   // whole warps stay together: the first lane's place decides
   for (int a0 = first; a0 - (VEC ? 4 : 1) * (tid & 31) < end; a0 += N * VERIFY_THREADS) {
-    float x[N], e[N], qx[N];
+    float x[N], e[N], qx[N], bound[N];
     if constexpr (VEC) {
 #pragma unroll
       for (int g = 0; g < N / 4; ++g) {
@@ -253,8 +127,7 @@ __device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>
           } else {
             *reinterpret_cast<float4*>(x + 4 * g) = *reinterpret_cast<const float4*>(row + at);
           }
-          const uint4 w = ldg_stream(noise + at);
-          *reinterpret_cast<uint4*>(e + 4 * g) = w;
+          *reinterpret_cast<uint4*>(e + 4 * g) = ldg_stream(noise + at);
           if (q) *reinterpret_cast<uint4*>(qx + 4 * g) = ldg_stream(q + at);
         }
       }
@@ -269,94 +142,20 @@ __device__ __forceinline__ unsigned long long race(const typename TargetOf<KIND>
         }
       }
     }
-    float above[N], top = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      above[i] = 0.f;
-      if (place(a0, i) < end) {
-        const float p = KIND == TARGET_PROBS ? x[i] : exp2_fast(plain ? fmaf(x[i], of.c, -ref) : below_ref(x[i], of.m, of.c));
-        const float r = q ? fmaf(p, scale, -qx[i]) : p * scale;
-        above[i] = r * rcp_fast(e[i]) * RACE_ABOVE;
-      }
-      top = fmaxf(top, above[i]);
+      if (!q) qx[i] = 0.f;
+      bound[i] = place(a0, i) < end ? race.above(x[i], e[i], qx[i]) : 0.f;
     }
-    // from the highest bound down, as long as they reach the best result
-    for (float highest; (highest = warp_max(top)) > 0.f && highest >= best;) {
-      float t = 0.f;
-      if (top == highest) {
-        int at = 0;
-        float px = 0.f, ex = 1.f, qq = 0.f;
-        bool found = false;
-        top = 0.f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          if (!found && above[i] == highest) {
-            found = true;
-            at = place(a0, i);
-            px = x[i];
-            ex = e[i];
-            if (q) qq = qx[i];
-            above[i] = 0.f;
-          }
-          top = fmaxf(top, above[i]);
-        }
-        const float r = of.exact(px) - qq;
-        if (r > 0.f && at != gone) {
-          t = r / ex;
-          if (t > 0.f) key = max(key, (unsigned long long)__float_as_uint(t) << 32 | (0xffffffffu - (uint32_t)at));
-        }
-      }
-      best = fmaxf(best, warp_max(t));
-    }
+    race.template run<N>(x, e, qx, bound, [&](int i) { return place(a0, i); });
   }
-  return key;
 }
 
-// Temperature of a sequence, as a factor of its logits; greedy sequences take 1.
-struct Scale {
-  float c;                  // log2(e) / T
-  bool greedy;
-};
-__device__ __forceinline__ Scale scale_of(const VerifyParams& p, int s) {
-  Scale r{1.4426950408889634f, !p.noise};
-  if (p.noise && p.temperature) {
-    const float t = *(p.temperature + s);
-    r.greedy = !(t > 0.f);
-    if (!r.greedy) r.c = fminf(1.4426950408889634f / t, FLT_MAX);
-  }
-  return r;
-}
-
-// The draft that a row judges, and what it is judged by: inputs alone.
-struct Draft {
-  int x;
-  bool any, inside;         // the row has a draft; it is one of the vocabulary
-  float value, q, u;        // of the target's row, of its own distribution, uniform
-};
+// Row r's judgement by a warp, from the masses of the row's pieces.
 template <int KIND>
-__device__ __forceinline__ Draft draft_of(const VerifyParams& p, int r, bool any, const Scale& sc) {
-  Draft d{-1, any, false, -INFINITY, 1.f, 0.f};
-  if (!any) return d;
-  d.x = *(p.tokens + r + 1);
-  d.inside = d.x >= 0 && d.x < p.vocab;
-  if (d.inside) {
-    d.value = as_float(static_cast<const typename TargetOf<KIND>::type*>(p.target)[r * p.target_stride + d.x]);
-    if (!sc.greedy) {
-      d.u = *(p.uniform + r);
-      if (p.draft_probs) d.q = p.draft_probs[r * p.draft_stride + d.x];
-    }
-  }
-  return d;
-}
-// What row r makes of it, by a warp, from the masses of the row's pieces.
-template <int KIND>
-__device__ __forceinline__ RowResult judge(const VerifyParams& p, int r, const Draft& d, const Scale& sc) {
-  RowResult row{0.f, 1.f, 0.f, 0, 0};
-  if (KIND == TARGET_PROBS) {
-    row.ok = d.inside && d.u * d.q < d.value;
-    row.logprob = logf(d.value);
-  } else {
-    Mass sum = no_mass();
+__device__ __forceinline__ RowResult judge_row(const VerifyParams& p, int r, const Draft& d, const Scale& sc) {
+  Mass sum = no_mass();
+  if (KIND != TARGET_PROBS) {
     for (int k = threadIdx.x & 31; k < p.pieces; k += 32) {
       const uint4 w = __ldcg(p.part + (size_t)r * p.pieces + k);
       const Mass o{__uint_as_float(w.x), __uint_as_float(w.y), (int)w.z};
@@ -366,17 +165,8 @@ __device__ __forceinline__ RowResult judge(const VerifyParams& p, int r, const D
       sum.m = m;
     }
     sum = warp_join(sum, sc.c, sc.greedy);
-    row.m = sum.m;
-    row.l = sum.l / exp2_fast(below_ref(sum.m, sum.m, sc.c));    // (exactly 1 where there is one token)
-    row.at = sum.at;
-    const bool some = row.l > 0.f;                     // (and not NaN)
-    const Row<KIND> of{row.m, row.l, sc.c};
-    const float px = some ? of.exact(d.value) : 0.f;
-    row.ok = some && d.inside && (sc.greedy ? sum.at == d.x : d.u * d.q < px);
-    row.logprob = of.log_of(d.value);
   }
-  if (d.any && !d.inside) row.ok = -1;
-  return row;
+  return judge<KIND>(sum, d, sc);
 }
 
 // What the CTAs of the others meet in.
@@ -462,7 +252,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_ordered_kernel(const
         __threadfence();
       }
       if (__shfl_sync(0xffffffffu, before, 0) == p.pieces - 1) {
-        const RowResult row = judge<KIND>(p, r, draft_of<KIND>(p, r, i < n - 1, sc), sc);
+        const RowResult row = judge_row<KIND>(p, r, draft_of<KIND>(p, r, i < n - 1 ? *(p.tokens + r + 1) : -1, i < n - 1, sc), sc);
         if (lane == 0) {
           p.result[r] = row;
           if (row.ok <= 0) atomicMin(p.stop + s, i);
@@ -509,11 +299,11 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
     // rows until one accepts nothing: a warp a row
     for (int i0 = 0; i0 < n && stop < 0; i0 += VERIFY_WARPS) {
       const int i = i0 + warp;
-      const Draft d = draft_of<KIND>(p, r0 + i, i < n - 1, sc);
+      const Draft d = draft_of<KIND>(p, r0 + i, i < n - 1 ? *(p.tokens + r0 + i + 1) : -1, i < n - 1, sc);
       if (!waited) pdl_wait();
       waited = true;
       if (i < n) {
-        const RowResult row = judge<KIND>(p, r0 + i, d, sc);
+        const RowResult row = judge_row<KIND>(p, r0 + i, d, sc);
         if (lane == 0) s_row[warp] = row;
       }
       __syncthreads();
@@ -553,21 +343,19 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
     const T* row = target + (r0 + stop) * p.target_stride;
     const float* noise = p.noise + s * p.noise_stride;
     const float* q = judged && p.draft_probs ? p.draft_probs + (r0 + stop) * p.draft_stride : nullptr;
-    int gone = judged && !p.draft_probs ? *(p.tokens + r0 + stop + 1) : -1;
+    int gone = judged && !p.draft_probs ? last.draft : -1;
     const Row<KIND> of{last.m, last.l, sc.c};
     const bool aligned = !((reinterpret_cast<uintptr_t>(row) & (4 * sizeof(T) - 1)) | (reinterpret_cast<uintptr_t>(noise) & 15) |
                            (reinterpret_cast<uintptr_t>(q) & 15));
     auto run = [&](int a, int b, float known) {        // the whole CTA's best, in thread 0
       const int whole = aligned ? a + ((b - a) & ~3) : a;
-      unsigned long long k = race<KIND, true>(row, noise, q, a, whole, gone, of, known);
-      k = max(k, race<KIND, false>(row, noise, q, whole, b, gone, of, known));
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, d));
+      Race<KIND> r(of, gone, known);
+      race_over<KIND, true>(r, row, noise, q, a, whole);
+      race_over<KIND, false>(r, row, noise, q, whole, b);
+      unsigned long long k = warp_best(r.key);
       if (lane == 0) s_key[warp] = k;
       __syncthreads();
-      if (tid == 0)
-        for (int w = 1; w < VERIFY_WARPS; ++w) k = max(k, s_key[w]);
-      return k;
+      return warp == 0 ? warp_best(lane < VERIFY_WARPS ? s_key[lane] : 0) : k;
     };
     key = run(begin, end, __uint_as_float((uint32_t)(*(volatile unsigned long long*)(p.key + s) >> 32)));
     // the CTAs of a sequence meet: the last one through has the best of all
@@ -594,7 +382,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   if (tid != 0) return;
   int next = -1;
   if (sound && sc.greedy) next = last.at;
-  if (key) next = (int)(0xffffffffu - (uint32_t)key);
+  if (key) next = place_of(key);
   float logprob = 0.f;
   if (next >= 0) {
     const float x = as_float(target[(r0 + stop) * p.target_stride + next]);
@@ -624,7 +412,7 @@ static Pieces pieces_of(long long rows, int vocab, int most) {
   size = (size + 63) / 64 * 64;
   return {(int)size, (int)((vocab + size - 1) / size)};
 }
-constexpr int MASS_MOST_BYTES = MASS_VECTORS * VERIFY_THREADS * 16, RACE_MOST = 8192;
+constexpr int MASS_MOST_BYTES = MASS_VECTORS * VERIFY_THREADS * 16, RACE_MOST = 32768;
 
 // The workspace, laid out one array behind the other.  Masses: the most that a call of at most these rows over at most this vocabulary
 // cuts them into is one wave, or the largest pieces.
@@ -655,8 +443,8 @@ static size_t verify_layout(long long batch, long long rows, int vocab, char* ws
 
 }  // namespace efim
 
-extern "C" size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab) {
-  if (batch <= 0 || total_rows < 0 || vocab <= 0) return 0;
+extern "C" size_t efim_verify_workspace_bytes(int32_t batch, int32_t total_rows, int32_t vocab, int32_t target_kind) {
+  if (batch <= 0 || total_rows < 0 || vocab <= 0 || efim::verify_is_fused(batch, vocab, target_kind)) return 0;
   return efim::verify_layout(batch, total_rows, vocab, nullptr, nullptr);
 }
 
@@ -678,8 +466,9 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
     if (d->d_draft_probs && d->draft_stride < d->vocab) return EFIM_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(d->d_noise) | reinterpret_cast<uintptr_t>(d->d_draft_probs)) & 3) return EFIM_ERR_INVALID_ARG;
   }
-  if (!d_workspace || workspace_bytes < efim_verify_workspace_bytes(d->batch, d->total_rows, d->vocab)) return EFIM_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(d_workspace) & 255) return EFIM_ERR_INVALID_ARG;
+  const size_t need = efim_verify_workspace_bytes(d->batch, d->total_rows, d->vocab, d->target_kind);
+  if (need > 0 && (!d_workspace || workspace_bytes < need)) return EFIM_ERR_WORKSPACE;
+  if (need > 0 && reinterpret_cast<uintptr_t>(d_workspace) & 255) return EFIM_ERR_INVALID_ARG;
   VerifyParams p{};
   p.target = d->d_target;
   p.row_indptr = d->d_row_indptr;
@@ -700,16 +489,19 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   p.total_rows = d->total_rows;
   p.vocab = d->vocab;
   p.out_stride = d_out_tokens || d_out_logprobs ? out_stride : 0;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (need == 0) {
+    if (d->batch > 0x7fffffff / 8) return EFIM_ERR_UNSUPPORTED;
+    EFIM_CUDA_TRY(verify_fused_launch(p, d->target_kind, s));
+    return EFIM_OK;
+  }
   verify_layout(d->batch, d->total_rows, d->vocab, static_cast<char*>(d_workspace), &p);
   const Pieces mass = pieces_of(d->total_rows, d->vocab, d->target_kind == EFIM_TARGET_LOGITS_BF16 ? MASS_MOST_BYTES / 2 : MASS_MOST_BYTES / 4);
   const bool logits = d->target_kind != EFIM_TARGET_PROBS_F32 && d->total_rows > 0;
   const bool bf16 = d->target_kind == EFIM_TARGET_LOGITS_BF16;
   const long long ctas = (long long)mass.count * d->total_rows;
-  bool ordered = logits && ctas >= 16LL * sm_count();
-  if (getenv("V_ORD")) ordered = logits && atoi(getenv("V_ORD"));
-  int most = RACE_MOST;
-  if (getenv("V_RACE")) most = atoi(getenv("V_RACE"));
-  const Pieces race = pieces_of(d->batch, d->vocab, most);
+  const bool ordered = logits && ctas >= 16LL * sm_count();
+  const Pieces race = pieces_of(d->batch, d->vocab, RACE_MOST);
   p.piece = mass.size;
   p.pieces = mass.count;
   p.race_piece = race.size;
@@ -717,7 +509,6 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   const long long places = std::max<long long>(1, (d->total_rows + d->batch - 1) / d->batch);      // rows of a sequence, on average
   if (ctas > 0x7fffffffLL || places * d->batch * mass.count > 0x7fffffffLL || (long long)race.count * d->batch > 0x7fffffffLL)
     return EFIM_ERR_UNSUPPORTED;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
   const dim3 block(VERIFY_THREADS), pick((unsigned)(race.count * d->batch));
   if (!logits || ordered)
     EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3((unsigned)((std::max(d->total_rows, d->batch) + VERIFY_THREADS - 1) / VERIFY_THREADS)),

@@ -68,7 +68,7 @@ def _verify(lib, accepted=0x1000, nxt=0x2000, out=None, logs=None, out_stride=0,
                   d_temperature=0x9000)
     desc = B._VerifyDesc(**{**fields, **changed})
     if ws_bytes is None:
-        ws_bytes = lib.efim_verify_workspace_bytes(desc.batch, desc.total_rows, desc.vocab)
+        ws_bytes = lib.efim_verify_workspace_bytes(desc.batch, desc.total_rows, desc.vocab, desc.target_kind)
     return lib.efim_verify_drafts(ctypes.byref(desc), accepted, nxt, out, logs, out_stride, ws, ws_bytes, None, None)
 
 
@@ -81,12 +81,15 @@ def test_verify(lib):
                 dict(target_kind=2, d_target=0x5004), dict(target_kind=2, d_target=0x5004, d_temperature=None, d_noise=None)):
         assert _verify(lib, **bad) == INVALID_ARG, bad
     assert _verify(lib, batch=0, d_row_indptr=None) == OK
-    need = lib.efim_verify_workspace_bytes(2, 6, 1000)
-    assert need > 0 and _verify(lib, ws_bytes=need - 1) == _verify(lib, ws=None) == WORKSPACE
-    assert _verify(lib, ws=0x100010) == INVALID_ARG
-    for smaller in ((1, 6, 1000), (2, 1, 1000), (2, 6, 1), (2, 0, 1000)):
-        assert 0 < lib.efim_verify_workspace_bytes(*smaller) <= need
-    assert lib.efim_verify_workspace_bytes(0, 6, 1000) == lib.efim_verify_workspace_bytes(2, 6, 0) == 0
+    size = lib.efim_verify_workspace_bytes
+    wide = dict(vocab=100000, target_stride=100000, draft_stride=100000, noise_stride=100000)
+    need = size(2, 6, 100000, 0)
+    assert need > 0 and _verify(lib, ws_bytes=need - 1, **wide) == _verify(lib, ws=None, **wide) == WORKSPACE
+    assert _verify(lib, ws=0x100010, **wide) == INVALID_ARG
+    for smaller in ((1, 6, 100000), (2, 1, 100000), (2, 6, 40000), (2, 0, 100000)):
+        assert 0 < size(*smaller, 0) <= need
+    assert size(0, 6, 100000, 0) == size(2, 6, 0, 0) == 0
+    assert [size(2, 6, v, k) == 0 for v, k in ((32768, 0), (32769, 0), (16384, 1), (16385, 1), (16384, 2), (16385, 2))] == [True, False] * 3
 
 
 def test_python_side(lib):
@@ -119,7 +122,7 @@ def test_python_side(lib):
                         (TypeError, (hist, n.long(), 1, 2, drafts, n)), (TypeError, (hist, n, 1, 2.5, drafts, n))]:
         with pytest.raises(error):
             efim.efim_draft_lookup(*args, stream=0)
-    logits, ws = torch.zeros(5, 100, dtype=half), torch.zeros(1 << 16, dtype=torch.uint8)
+    logits, ws = torch.zeros(5, 100, dtype=half), None
     r = dict(row_indptr=torch.zeros(3, dtype=whole), tokens=torch.zeros(5, dtype=whole), target=logits, accepted=n, next_token=n.clone(),
              uniform=torch.zeros(5), noise=torch.zeros(2, 100), workspace=ws)
     wide = torch.zeros(2, 6)
@@ -132,6 +135,8 @@ def test_python_side(lib):
                            (TypeError, dict(temperature=torch.zeros(2, dtype=torch.float64)))]:
         with pytest.raises(error):
             efim.efim_verify_drafts(**{**r, **changed}, stream=0)
+    big = dict(target=torch.zeros(5, 40000, dtype=half), noise=torch.zeros(2, 40000))
+    assert efim.efim_verify_workspace_bytes(2, logits) == 0 < efim.efim_verify_workspace_bytes(2, big["target"])
     with pytest.raises(efim.EfimError) as e:
-        efim.efim_verify_drafts(**{**r, "workspace": ws[:256]}, stream=0)
+        efim.efim_verify_drafts(**{**r, **big, "workspace": torch.zeros(256, dtype=torch.uint8)}, stream=0)
     assert e.value.code == WORKSPACE
