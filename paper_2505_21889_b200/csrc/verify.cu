@@ -48,19 +48,7 @@ struct Share {
   }
   __device__ __forceinline__ Mass mass(float c, bool want_at) const {
     Mass s = no_mass();
-    if constexpr (sizeof(T) == 2) {
-      uint32_t m = w[0].x;
-#pragma unroll
-      for (int u = 0; u < MASS_VECTORS; ++u)
-        m = max_bf16x2(max_bf16x2(max_bf16x2(m, w[u].x), w[u].y), max_bf16x2(w[u].z, w[u].w));
-      s.m = fmaxf(bf16lo(m), bf16hi(m));
-    } else {
-      s.m = __uint_as_float(w[0].x);
-#pragma unroll
-      for (int u = 0; u < MASS_VECTORS; ++u)
-        s.m = fmaxf(fmaxf(fmaxf(s.m, __uint_as_float(w[u].x)), __uint_as_float(w[u].y)),
-                    fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
-    }
+    s.m = top_of<T, MASS_VECTORS>(w);
     s.m = fmaxf(fmaxf(s.m, -INFINITY), fmaxf(head, tail));                 // (not NaN where all values are)
     if (want_at) {
       // from the last place to the first
@@ -101,7 +89,8 @@ struct Share {
   }
 };
 
-// The race over places [begin, end) of a row.
+// The race over places [begin, end) of a row.  VEC: the operands are 16-byte aligned there (8 for bf16 logits) and end - begin is a
+// multiple of 4.
 template <int KIND, bool VEC>
 __device__ __forceinline__ void race_over(Race<KIND>& race, const typename TargetOf<KIND>::type* row, const float* noise, const float* q,
                                           int begin, int end) {
@@ -109,26 +98,31 @@ __device__ __forceinline__ void race_over(Race<KIND>& race, const typename Targe
   using T = typename TargetOf<KIND>::type;
   const int tid = threadIdx.x;
   auto place = [&](int a0, int i) { return VEC ? a0 + (i / 4) * 4 * VERIFY_THREADS + i % 4 : a0 + i * VERIFY_THREADS; };
-  const int first = begin + (VEC ? 4 * tid : tid);
-  // whole warps stay together: the first lane's place decides
-  for (int a0 = first; a0 - (VEC ? 4 : 1) * (tid & 31) < end; a0 += N * VERIFY_THREADS) {
-    float x[N], e[N], qx[N], bound[N];
+  // whole warps stay together: the first lane's place decides; places past the end take forever (e infinite)
+#pragma unroll 1
+  for (int a0 = begin + (VEC ? 4 * tid : tid); a0 - (VEC ? 4 : 1) * (tid & 31) < end; a0 += N * VERIFY_THREADS) {
+    __align__(16) float x[N], e[N], qx[N], estimate[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = qx[i] = 0.f;
+      e[i] = INFINITY;
+    }
     if constexpr (VEC) {
 #pragma unroll
-      for (int g = 0; g < N / 4; ++g) {
-        const int at = place(a0, 4 * g);
+      for (int g = 0; g < N; g += 4) {
+        const int at = place(a0, g);
         if (at < end) {
           if constexpr (sizeof(T) == 2) {
             const uint2 w = *reinterpret_cast<const uint2*>(row + at);
-            x[4 * g] = bf16lo(w.x);
-            x[4 * g + 1] = bf16hi(w.x);
-            x[4 * g + 2] = bf16lo(w.y);
-            x[4 * g + 3] = bf16hi(w.y);
+            x[g] = bf16lo(w.x);
+            x[g + 1] = bf16hi(w.x);
+            x[g + 2] = bf16lo(w.y);
+            x[g + 3] = bf16hi(w.y);
           } else {
-            *reinterpret_cast<float4*>(x + 4 * g) = *reinterpret_cast<const float4*>(row + at);
+            *reinterpret_cast<float4*>(x + g) = *reinterpret_cast<const float4*>(row + at);
           }
-          *reinterpret_cast<uint4*>(e + 4 * g) = ldg_stream(noise + at);
-          if (q) *reinterpret_cast<uint4*>(qx + 4 * g) = ldg_stream(q + at);
+          *reinterpret_cast<uint4*>(e + g) = ldg_stream(noise + at);
+          if (q) *reinterpret_cast<uint4*>(qx + g) = ldg_stream(q + at);
         }
       }
     } else {
@@ -143,11 +137,8 @@ __device__ __forceinline__ void race_over(Race<KIND>& race, const typename Targe
       }
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (!q) qx[i] = 0.f;
-      bound[i] = place(a0, i) < end ? race.above(x[i], e[i], qx[i]) : 0.f;
-    }
-    race.template run<N>(x, e, qx, bound, [&](int i) { return place(a0, i); });
+    for (int i = 0; i < N; ++i) estimate[i] = race.estimate(x[i], e[i], qx[i]);
+    race.template run<N>(x, e, qx, estimate, [&](int i) { return place(a0, i); });
   }
 }
 
@@ -176,9 +167,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_init_kernel(const Verif
   for (int s = blockIdx.x * VERIFY_THREADS + threadIdx.x; s < p.batch; s += gridDim.x * VERIFY_THREADS) {
     p.key[s] = 0;
     p.done[s] = 0;
-    p.stop[s] = 0x7fffffff;
   }
-  for (int r = blockIdx.x * VERIFY_THREADS + threadIdx.x; r < p.total_rows; r += gridDim.x * VERIFY_THREADS) p.through[r] = 0;
 }
 
 // The masses of all rows, a CTA a piece.
@@ -220,51 +209,8 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const Ve
   if (tid == 0) p.part[blockIdx.x] = packed(sum);
 }
 
-// The same, first rows first: all sequences' first rows, then their second ones, and so on.  The last piece of a row to be through judges
-// it, and rows behind one that has refused are left out by CTAs that start after that.
+// The end of every sequence: the row it stops at, and the race.
 template <int KIND>
-__global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_ordered_kernel(const VerifyParams p) {
-  using T = typename TargetOf<KIND>::type;
-  __shared__ Mass s_warp[VERIFY_WARPS];
-  __shared__ int s_stop;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per_place = p.batch * p.pieces, rest = blockIdx.x % per_place;
-  const int s = rest / p.pieces, piece = rest % p.pieces;
-  const int r0 = *(p.row_indptr + s), r1 = *(p.row_indptr + s + 1);
-  const int n = r0 >= 0 && r1 <= p.total_rows ? r1 - r0 : 0;
-  const Scale sc = scale_of(p, s);
-  pdl_wait();
-  pdl_launch();
-  for (int i = blockIdx.x / per_place; i < n; i += gridDim.x / per_place) {
-    if (tid == 0) s_stop = *reinterpret_cast<volatile int*>(p.stop + s);
-    __syncthreads();
-    if (s_stop < i) break;
-    const int r = r0 + i;
-    Share<T> share;
-    share.fetch(static_cast<const T*>(p.target) + r * p.target_stride, piece * p.piece, min(p.vocab, (piece + 1) * p.piece));
-    const Mass sum = piece_mass<KIND>(share, sc, s_warp);
-    if (warp == 0) {
-      int before = 0;
-      if (lane == 0) {
-        p.part[(size_t)r * p.pieces + piece] = packed(sum);
-        __threadfence();
-        before = atomicAdd(p.through + r, 1);
-        __threadfence();
-      }
-      if (__shfl_sync(0xffffffffu, before, 0) == p.pieces - 1) {
-        const RowResult row = judge_row<KIND>(p, r, draft_of<KIND>(p, r, i < n - 1 ? *(p.tokens + r + 1) : -1, i < n - 1, sc), sc);
-        if (lane == 0) {
-          p.result[r] = row;
-          if (row.ok <= 0) atomicMin(p.stop + s, i);
-        }
-      }
-    }
-    __syncthreads();
-  }
-}
-
-// The end of every sequence: the row it stops at (found here, or DECIDED already), and the race.
-template <int KIND, bool DECIDED>
 __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const VerifyParams p) {
   using T = typename TargetOf<KIND>::type;
   __shared__ RowResult s_row[VERIFY_WARPS];
@@ -282,41 +228,31 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   const int begin = piece * p.race_piece, end = min(p.vocab, begin + p.race_piece);
   int32_t* out_tokens = p.out_tokens ? p.out_tokens + (size_t)s * p.out_stride : nullptr;
   float* out_logprobs = p.out_logprobs ? p.out_logprobs + (size_t)s * p.out_stride : nullptr;
+  if (tid == 0 && n > 0 && !sc.greedy) prefetch_l2(p.noise + s * p.noise_stride + begin, (end - begin) * 4LL);
 
   int stop = -1, status = rows_ok ? 0 : EFIM_DEV_BAD_POSITION;
   RowResult last{};
   bool waited = false;
-  if constexpr (DECIDED) {
-    pdl_wait();
+  // rows until one accepts nothing: a warp a row
+  for (int i0 = 0; i0 < n && stop < 0; i0 += VERIFY_WARPS) {
+    const int i = i0 + warp;
+    const Draft d = draft_of<KIND>(p, r0 + i, i < n - 1 ? *(p.tokens + r0 + i + 1) : -1, i < n - 1, sc);
+    if (!waited) pdl_wait();
     waited = true;
-    if (n > 0) {
-      stop = *(p.stop + s);
-      last = p.result[r0 + stop];
-      if (first && out_logprobs)
-        for (int i = tid; i < min(stop, p.out_stride); i += VERIFY_THREADS) out_logprobs[i] = p.result[r0 + i].logprob;
+    if (i < n) {
+      const RowResult row = judge_row<KIND>(p, r0 + i, d, sc);
+      if (lane == 0) s_row[warp] = row;
     }
-  } else {
-    // rows until one accepts nothing: a warp a row
-    for (int i0 = 0; i0 < n && stop < 0; i0 += VERIFY_WARPS) {
-      const int i = i0 + warp;
-      const Draft d = draft_of<KIND>(p, r0 + i, i < n - 1 ? *(p.tokens + r0 + i + 1) : -1, i < n - 1, sc);
-      if (!waited) pdl_wait();
-      waited = true;
-      if (i < n) {
-        const RowResult row = judge_row<KIND>(p, r0 + i, d, sc);
-        if (lane == 0) s_row[warp] = row;
-      }
-      __syncthreads();
-      const int count = min(VERIFY_WARPS, n - i0);
-      int good = 0;
-      while (good < count && s_row[good].ok > 0) ++good;
-      if (good < count) {
-        stop = i0 + good;
-        last = s_row[good];
-      }
-      if (first && out_logprobs && tid < good && i0 + tid < p.out_stride) out_logprobs[i0 + tid] = s_row[tid].logprob;
-      __syncthreads();
+    __syncthreads();
+    const int count = min(VERIFY_WARPS, n - i0);
+    int good = 0;
+    while (good < count && s_row[good].ok > 0) ++good;
+    if (good < count) {
+      stop = i0 + good;
+      last = s_row[good];
     }
+    if (first && out_logprobs && tid < good && i0 + tid < p.out_stride) out_logprobs[i0 + tid] = s_row[tid].logprob;
+    __syncthreads();
   }
   if (last.ok < 0) status |= EFIM_DEV_BAD_TOKEN;
   if (!waited) pdl_wait();
@@ -344,14 +280,22 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
     const float* noise = p.noise + s * p.noise_stride;
     const float* q = judged && p.draft_probs ? p.draft_probs + (r0 + stop) * p.draft_stride : nullptr;
     int gone = judged && !p.draft_probs ? last.draft : -1;
+    if (tid == 0) {
+      prefetch_l2(row + begin, (end - begin) * (long long)sizeof(T));
+      if (q) prefetch_l2(q + begin, (end - begin) * 4LL);
+    }
     const Row<KIND> of{last.m, last.l, sc.c};
     const bool aligned = !((reinterpret_cast<uintptr_t>(row) & (4 * sizeof(T) - 1)) | (reinterpret_cast<uintptr_t>(noise) & 15) |
                            (reinterpret_cast<uintptr_t>(q) & 15));
     auto run = [&](int a, int b, float known) {        // the whole CTA's best, in thread 0
-      const int whole = aligned ? a + ((b - a) & ~3) : a;
       Race<KIND> r(of, gone, known);
-      race_over<KIND, true>(r, row, noise, q, a, whole);
-      race_over<KIND, false>(r, row, noise, q, whole, b);
+      int rest = a;                                    // what is left to be computed place by place
+      if (r.estimates()) {
+        rest = aligned ? a + ((b - a) & ~3) : b;
+        if (aligned) race_over<KIND, true>(r, row, noise, q, a, rest);
+        else race_over<KIND, false>(r, row, noise, q, a, b);
+      }
+      for (int at = rest + tid; at < b; at += VERIFY_THREADS) r.compute(as_float(row[at]), noise[at], q ? q[at] : 0.f, at);
       unsigned long long k = warp_best(r.key);
       if (lane == 0) s_key[warp] = k;
       __syncthreads();
@@ -412,7 +356,7 @@ static Pieces pieces_of(long long rows, int vocab, int most) {
   size = (size + 63) / 64 * 64;
   return {(int)size, (int)((vocab + size - 1) / size)};
 }
-constexpr int MASS_MOST_BYTES = MASS_VECTORS * VERIFY_THREADS * 16, RACE_MOST = 32768;
+constexpr int MASS_MOST_BYTES = MASS_VECTORS * VERIFY_THREADS * 16, RACE_MOST = 16384;
 
 // The workspace, laid out one array behind the other.  Masses: the most that a call of at most these rows over at most this vocabulary
 // cuts them into is one wave, or the largest pieces.
@@ -425,18 +369,12 @@ static size_t verify_layout(long long batch, long long rows, int vocab, char* ws
   };
   const long long least = (vocab + MASS_MOST_BYTES / 4 - 1) / (MASS_MOST_BYTES / 4);
   uint4* part = reinterpret_cast<uint4*>(take(std::max(4LL * sm_count() + rows, rows * least) * sizeof(uint4)));
-  RowResult* result = reinterpret_cast<RowResult*>(take(rows * sizeof(RowResult)));
   unsigned long long* key = reinterpret_cast<unsigned long long*>(take(batch * 8));
   int* done = reinterpret_cast<int*>(take(batch * 4));
-  int* stop = reinterpret_cast<int*>(take(batch * 4));
-  int* through = reinterpret_cast<int*>(take(rows * 4));
   if (p) {
     p->part = part;
-    p->result = result;
     p->key = key;
     p->done = done;
-    p->stop = stop;
-    p->through = through;
   }
   return at;
 }
@@ -499,28 +437,20 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   const Pieces mass = pieces_of(d->total_rows, d->vocab, d->target_kind == EFIM_TARGET_LOGITS_BF16 ? MASS_MOST_BYTES / 2 : MASS_MOST_BYTES / 4);
   const bool logits = d->target_kind != EFIM_TARGET_PROBS_F32 && d->total_rows > 0;
   const bool bf16 = d->target_kind == EFIM_TARGET_LOGITS_BF16;
-  const long long ctas = (long long)mass.count * d->total_rows;
-  const bool ordered = logits && ctas >= 16LL * sm_count();
   const Pieces race = pieces_of(d->batch, d->vocab, RACE_MOST);
   p.piece = mass.size;
   p.pieces = mass.count;
   p.race_piece = race.size;
   p.race_pieces = race.count;
-  const long long places = std::max<long long>(1, (d->total_rows + d->batch - 1) / d->batch);      // rows of a sequence, on average
-  if (ctas > 0x7fffffffLL || places * d->batch * mass.count > 0x7fffffffLL || (long long)race.count * d->batch > 0x7fffffffLL)
-    return EFIM_ERR_UNSUPPORTED;
+  const long long ctas = (long long)mass.count * d->total_rows;
+  if (ctas > 0x7fffffffLL || (long long)race.count * d->batch > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
   const dim3 block(VERIFY_THREADS), pick((unsigned)(race.count * d->batch));
-  if (!logits || ordered)
-    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3((unsigned)((std::max(d->total_rows, d->batch) + VERIFY_THREADS - 1) / VERIFY_THREADS)),
-                             block, 0, s, p));
-  if (ordered)
-    EFIM_CUDA_TRY(launch_pdl(bf16 ? verify_ordered_kernel<TARGET_BF16> : verify_ordered_kernel<TARGET_F32>,
-                             dim3((unsigned)(places * d->batch * mass.count)), block, 0, s, p));
-  else if (logits)
+  if (logits) {
     EFIM_CUDA_TRY(launch_pdl(bf16 ? verify_mass_kernel<TARGET_BF16> : verify_mass_kernel<TARGET_F32>, dim3((unsigned)ctas), block, 0, s, p));
-  EFIM_CUDA_TRY(launch_pdl(d->target_kind == EFIM_TARGET_PROBS_F32 ? verify_pick_kernel<TARGET_PROBS, false>
-                           : bf16 ? (ordered ? verify_pick_kernel<TARGET_BF16, true> : verify_pick_kernel<TARGET_BF16, false>)
-                                  : (ordered ? verify_pick_kernel<TARGET_F32, true> : verify_pick_kernel<TARGET_F32, false>),
+  } else {
+    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3((unsigned)((d->batch + VERIFY_THREADS - 1) / VERIFY_THREADS)), block, 0, s, p));
+  }
+  EFIM_CUDA_TRY(launch_pdl(!logits ? verify_pick_kernel<TARGET_PROBS> : bf16 ? verify_pick_kernel<TARGET_BF16> : verify_pick_kernel<TARGET_F32>,
                            pick, block, 0, s, p));
   return EFIM_OK;
 }

@@ -5,10 +5,10 @@
 
 namespace efim {
 
-struct __align__(16) RowResult {
+struct RowResult {
   float m, l, logprob;      // maximum and sum of the row, log-probability of its draft
   int at, ok;               // place of the maximum; draft accepted: 1, refused: 0, refused for what it is: -1
-  int draft, unused[2];     // its draft
+  int draft;
 };
 
 struct VerifyParams {
@@ -25,11 +25,8 @@ struct VerifyParams {
   float* out_logprobs;      // the same
   int32_t* status;
   uint4* part;              // [total_rows][pieces]: maximum, sum, place of the maximum
-  RowResult* result;        // [total_rows], where rows are taken in order
   unsigned long long* key;  // [batch] best of the race so far
   int* done;                // [batch] pieces of the race that are through
-  int* stop;                // [batch] first row so far that accepts nothing, where rows are taken in order
-  int* through;             // [total_rows] pieces of the row that are through, the same
   long long target_stride, draft_stride, noise_stride;
   int batch, total_rows, vocab, out_stride;
   int piece, pieces;        // places of a CTA of the first kernel, CTAs of a row
@@ -52,6 +49,11 @@ __device__ __forceinline__ float rcp_fast(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// Sends for [p, p + bytes) of global memory to be in L2 (whole 16-byte units of it).
+__device__ __forceinline__ void prefetch_l2(const void* p, long long bytes) {
+  const uintptr_t a = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, z = (reinterpret_cast<uintptr_t>(p) + bytes) & ~(uintptr_t)15;
+  if (a < z) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(z - a)) : "memory");
 }
 // maximum over the warp; NaN lanes do not count
 __device__ __forceinline__ float warp_max(float x) {
@@ -105,6 +107,23 @@ __device__ __forceinline__ float2 pair_of(const uint4& w, int e) {
   else return make_float2(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1]));
 }
 
+// The largest of N vectors' values; NaN does not count.
+template <typename T, int N>
+__device__ __forceinline__ float top_of(const uint4* w) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t m = w[0].x;
+#pragma unroll
+    for (int u = 0; u < N; ++u) m = max_bf16x2(max_bf16x2(max_bf16x2(m, w[u].x), w[u].y), max_bf16x2(w[u].z, w[u].w));
+    return fmaxf(bf16lo(m), bf16hi(m));
+  } else {
+    float m = __uint_as_float(w[0].x);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(w[u].x)), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
+    return m;
+  }
+}
+
 // Probabilities of one row, from its logits or as they are: m, and l = sum of 2^((x - m) c).
 template <int KIND>
 struct Row {
@@ -119,10 +138,10 @@ struct Row {
 
 // The race for the next token: the largest r / e, r = (p - q)^+ or p, the lowest place among equals.
 //
-// An exact result costs two divisions and an exponential.  So every place gets a bound from above first, by the fast instructions (in a
-// probability: the exponent's rounding 150 * 2^-24 * ln 2, ex2 2^-22, the factor 2^-23; rcp and the products 2^-22 more; the
-// bound is 2^-16 higher, twice), and only places whose bound reaches the best result known so far are computed: a few a warp.
-// (Probabilities below 2^-126 are taken for 0 here.)
+// An exact result costs two divisions and an exponential.  So every place gets an estimate first, by the fast instructions (in a
+// probability: the exponent's rounding 150 * 2^-24 * ln 2, ex2 2^-22, the factor 2^-23: `scale` makes up for them; rcp and the last
+// product 2^-22 more: RACE_ABOVE does), and only places whose estimate, a little increased, reaches the best result known so far are
+// computed: a few a warp.  (Probabilities below 2^-126 are taken for 0 there.)
 constexpr float RACE_ABOVE = 1.f + 1.f / 65536;
 template <int KIND>
 struct Race {
@@ -134,20 +153,27 @@ struct Race {
   __device__ __forceinline__ Race(const Row<KIND>& of_, int gone_, float known) : of(of_), gone(gone_), best(known), key(0) {
     const bool logits = KIND != TARGET_PROBS;
     scale = logits ? RACE_ABOVE / (of.l * exp2_fast(below_ref(of.m, of.m, of.c))) : RACE_ABOVE;
-    ref = logits && has_ref(of.m, of.c) ? rintf(of.m * of.c) : 0.f;
+    ref = logits && has_ref(of.m, of.c) ? -rintf(of.m * of.c) : 0.f;
   }
-  __device__ __forceinline__ float above(float x, float e, float q) const {
-    if (KIND == TARGET_PROBS) return fmaf(x, scale, -q) * rcp_fast(e) * RACE_ABOVE;
-    return fmaf(exp2_fast(has_ref(of.m, of.c) ? fmaf(x, of.c, -ref) : below_ref(x, of.m, of.c)), scale, -q) * rcp_fast(e) * RACE_ABOVE;
+  // Whether estimates can be made; else (logits beyond 2^30 or infinite) every place is computed.
+  __device__ __forceinline__ bool estimates() const { return KIND == TARGET_PROBS || has_ref(of.m, of.c); }
+  __device__ __forceinline__ float estimate(float x, float e, float q) const {
+    return fmaf(KIND == TARGET_PROBS ? x : exp2_fast(fmaf(x, of.c, ref)), scale, -q) * rcp_fast(e);
   }
-  // N places of every lane of the warp, of which those with a bound of 0 do not run.
+  // The result of one place, computed.
+  __device__ __forceinline__ float compute(float x, float e, float q, int at) {
+    const float r = of.exact(x) - q, t = r > 0.f && at != gone ? r / e : 0.f;
+    if (t > 0.f) key = max(key, (unsigned long long)__float_as_uint(t) << 32 | (0xffffffffu - (uint32_t)at));
+    return t;
+  }
+  // N places of every lane of the warp with their estimates; places with an estimate of 0 do not run.
   template <int N, typename Place>
-  __device__ __forceinline__ void run(const float* x, const float* e, const float* q, float* bound, Place place) {
+  __device__ __forceinline__ void run(const float* x, const float* e, const float* q, float* estimate, Place place) {
     float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, bound[i]);
-    // from the highest bound down, as long as they reach the best result
-    for (float highest; (highest = warp_max(top)) > 0.f && highest >= best;) {
+    for (int i = 0; i < N; ++i) top = fmaxf(top, estimate[i]);
+    // from the highest estimate down, as long as they reach the best result
+    for (float highest; (highest = warp_max(top)) > 0.f && highest * RACE_ABOVE >= best;) {
       float t = 0.f;
       if (top == highest) {
         int at = 0;
@@ -156,21 +182,17 @@ struct Race {
         top = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          if (!found && bound[i] == highest) {
+          if (!found && estimate[i] == highest) {
             found = true;
             at = place(i);
             px = x[i];
             ex = e[i];
             qx = q[i];
-            bound[i] = 0.f;
+            estimate[i] = 0.f;
           }
-          top = fmaxf(top, bound[i]);
+          top = fmaxf(top, estimate[i]);
         }
-        const float r = of.exact(px) - qx;
-        if (r > 0.f && at != gone) {
-          t = r / ex;
-          if (t > 0.f) key = max(key, (unsigned long long)__float_as_uint(t) << 32 | (0xffffffffu - (uint32_t)at));
-        }
+        t = compute(px, ex, qx, at);
       }
       best = fmaxf(best, warp_max(t));
     }

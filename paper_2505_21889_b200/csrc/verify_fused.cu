@@ -218,10 +218,17 @@ __global__ void __launch_bounds__(FUSED_THREADS, PER_SM) verify_fused_kernel(con
     // once, or, where the draft's distribution leaves nothing (rounding alone refused it), again over the target's own
     for (int round = 0; round < 2 && next < 0; ++round) {
       Race<KIND> race({last.m, last.l, sc.c}, gone, 0.f);
-      float bound[N];
+      if (race.estimates()) {
+        float estimate[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) bound[e] = e < count ? race.above(x[e], noise[e], q[e]) : 0.f;
-      race.template run<N>(x, noise, q, bound, [&](int e) { return begin + e; });
+        for (int e = 0; e < N; ++e) estimate[e] = e < count ? race.estimate(x[e], noise[e], q[e]) : 0.f;
+        race.template run<N>(x, noise, q, estimate, [&](int e) { return begin + e; });
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < count; ++e)
+          race.compute(as_float(target[(r0 + stop) * p.target_stride + begin + e]), p.noise[s * p.noise_stride + begin + e],
+                       dense && round == 0 ? p.draft_probs[(r0 + stop) * p.draft_stride + begin + e] : 0.f, begin + e);
+      }
       unsigned long long key = warp_best(race.key);
       if (lane == 0) s_key[warp] = key;
       __syncthreads();

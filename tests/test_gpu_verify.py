@@ -125,6 +125,29 @@ def test_rows_at_any_place(kind, vocab, stride, offset):
     Step([3, 1, 6], vocab, kind, False, seed=6, stride=stride, offset=offset).check()
 
 
+@pytest.mark.parametrize("kind,vocab,stride,offset,dense", [("bf16", 131072, 131072, 0, False), ("bf16", 131072, 131072, 0, True),
+                                                            ("f32", 70001, 70001, 0, False), ("bf16", 99999, 100001, 3, False)])
+def test_many_rows(kind, vocab, stride, offset, dense):
+    """Rows taken in order, those behind a refusal left out; some sequences of many more rows than the others, some of none."""
+    rng = np.random.default_rng(vocab)
+    rows = rng.integers(0, 6, 100).tolist() + [17, 0, 1, 40]
+    step = Step(rows, vocab, kind, dense, seed=29, stride=stride, offset=offset)
+    # a sequence that accepts everything, past the average number of rows
+    a = int(step.indptr[-2])
+    step.tokens[a + 1:] = step.target[a:-1].argmax(1)
+    step.uniform[a:] = 1e-7
+    if dense:
+        step.q[a:] = 1.0 / vocab
+    n = step.check()
+    assert n > 100 and int(step.accepted[-1]) == 39
+    first = [t.clone() for t in (step.accepted, step.next, step.out, step.logs)]
+    for _ in range(3):
+        step.again()
+    torch.cuda.synchronize()
+    for x, y in zip(first, (step.accepted, step.next, step.out, step.logs)):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_greedy(kind):
     """No noise at all: every sequence greedy, ties to the lowest place (bf16 logits have many)."""
