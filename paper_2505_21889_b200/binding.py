@@ -339,27 +339,13 @@ def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform
     `target_is_probs` probabilities in fp32; draft_probs fp32 [rows, vocab]; noise fp32 [batch, vocab] (none: greedy);
     out_tokens and out_logprobs: packed [batch, n] of the same n.  Without a workspace one is taken from torch's allocator, on
     torch's current stream, which the call then has to run on."""
-    batch = accepted.shape[0]
-    stream = _stream_ptr(stream)
-    if workspace is None:
-        need = _calls.verify_workspace_bytes(batch, target, target_is_probs)
-        if need:
-            if stream != _current_stream():
-                raise ValueError("a call on another stream than torch's current one brings its workspace along")
-            workspace = _bytes_beside(target, need)
-    st = _calls.verify_drafts(batch, row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature, accepted,
-                              next_token, out_tokens, out_logprobs, workspace, status, stream)
+    if workspace is None and stream is not None and _calls.verify_workspace_bytes(accepted.shape[0], target, target_is_probs) and \
+            _stream_ptr(stream) != _current_stream():
+        raise ValueError("a call on another stream than torch's current one brings its workspace along")
+    st = _calls.verify_drafts(accepted.shape[0], row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature,
+                              accepted, next_token, out_tokens, out_logprobs, workspace, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_verify_drafts")
-
-
-def _bytes_beside(tensor, n):
-    global _bytes_beside
-    uint8 = _torch().uint8
-
-    def _bytes_beside(tensor, n):
-        return tensor.new_empty(n, dtype=uint8)
-    return _bytes_beside(tensor, n)
 
 
 def efim_prefill_workspace_bytes(cache: Cache, batch: Batch) -> int:

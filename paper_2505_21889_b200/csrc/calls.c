@@ -170,7 +170,8 @@ static PyObject* decode_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 /* ---- calls that take shapes and row strides from the tensors themselves */
-static PyObject *s_shape, *s_stride, *s_dtype, *bf16, *f32, *i32; /* torch's types, looked up by the first such call */
+static PyObject *s_shape, *s_stride, *s_dtype, *s_new_empty, *kw_dtype;
+static PyObject *bf16, *f32, *i32, *u8; /* torch's types, looked up by the first such call */
 
 static int have_types(void) {
   if (i32) return 1;
@@ -178,9 +179,10 @@ static int have_types(void) {
   if (!torch) return 0;
   bf16 = PyObject_GetAttrString(torch, "bfloat16");
   f32 = PyObject_GetAttrString(torch, "float32");
+  u8 = PyObject_GetAttrString(torch, "uint8");
   i32 = PyObject_GetAttrString(torch, "int32");
   Py_DECREF(torch);
-  return bf16 && f32 && i32;
+  return bf16 && f32 && u8 && i32;
 }
 static int is_tensor(PyObject* o) { return o != Py_None && !PyLong_Check(o) && !PyObject_TypeCheck(o, ndarray); }
 static int is_type(PyObject* o, PyObject* type) { /* -1: no such attribute */
@@ -282,13 +284,24 @@ static PyObject* verify_workspace_bytes(PyObject* self, PyObject* const* a, Py_s
   return PyLong_FromSize_t(efim_verify_workspace_bytes(batch, (int32_t)rows, (int32_t)vocab, kind));
 }
 
+/* `n` bytes beside a tensor, of torch's allocator on torch's current stream */
+static PyObject* bytes_beside(PyObject* o, size_t n) {
+  PyObject* size = PyLong_FromSize_t(n);
+  if (!size) return NULL;
+  PyObject* args[3] = {o, size, u8};
+  PyObject* r = PyObject_VectorcallMethod(s_new_empty, args, 2 | PY_VECTORCALL_ARGUMENTS_OFFSET, kw_dtype);
+  Py_DECREF(size);
+  return r;
+}
+
 /* batch, row_indptr, tokens, target, target_is_probs, draft_probs, uniform, noise, temperature, accepted, next_token, out_tokens,
-   out_logprobs, workspace, status, stream */
+   out_logprobs, workspace or None (one is taken beside the target), status, stream */
 static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   void* p[16];
   efim_verify_desc d;
   int64_t rows, vocab, out_rows, step, width = 0, logs = 0;
   size_t ws;
+  PyObject* own = NULL;
   if (!want(n, 16) || !have_types()) return NULL;
   const int probs = PyObject_IsTrue(a[4]), half = probs ? 0 : is_type(a[3], bf16);
   if (probs < 0 || half < 0) return NULL;
@@ -314,7 +327,19 @@ static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n)
   d.d_uniform = p[6];
   d.d_noise = p[7];
   d.d_temperature = p[8];
-  RETURN_STATUS(efim_verify_drafts(&d, p[9], p[10], p[11], p[12], (int32_t)(p[11] ? width : logs), p[13], ws, p[14], p[15]));
+  if (a[13] == Py_None) {
+    ws = efim_verify_workspace_bytes(d.batch, d.total_rows, d.vocab, d.target_kind);
+    if (ws > 0 && (!(own = bytes_beside(a[3], ws)) || !as_ptr(own, &p[13]))) {
+      Py_XDECREF(own);
+      return NULL;
+    }
+  }
+  efim_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = efim_verify_drafts(&d, p[9], p[10], p[11], p[12], (int32_t)(p[11] ? width : logs), p[13], ws, p[14], p[15]);
+  Py_END_ALLOW_THREADS
+  Py_XDECREF(own); /* (whatever takes its place next comes behind the call on the stream) */
+  return PyLong_FromLong(st);
 }
 
 static PyMethodDef methods[] = {
@@ -336,8 +361,10 @@ PyMODINIT_FUNC PyInit__calls(void) {
   s_shape = PyUnicode_InternFromString("shape");
   s_stride = PyUnicode_InternFromString("stride");
   s_dtype = PyUnicode_InternFromString("dtype");
+  s_new_empty = PyUnicode_InternFromString("new_empty");
+  kw_dtype = s_dtype ? PyTuple_Pack(1, s_dtype) : NULL;
   PyObject* numpy = PyImport_ImportModule("numpy");
-  if (!s_data_ptr || !s_nbytes || !s_shape || !s_stride || !s_dtype || !numpy) return NULL;
+  if (!s_data_ptr || !s_nbytes || !s_shape || !s_stride || !s_dtype || !s_new_empty || !kw_dtype || !numpy) return NULL;
   ndarray = (PyTypeObject*)PyObject_GetAttrString(numpy, "ndarray");
   Py_DECREF(numpy);
   if (!ndarray || !PyType_Check(ndarray)) return NULL;

@@ -249,6 +249,21 @@ def test_other_streams_and_graphs():
     step = Step([4, 2, 6], 9000, "bf16", True, seed=19).run()
     want = [t.clone() for t in (step.accepted, step.next, step.out, step.logs)]
     step.out.fill_(-5)
+    # a call that needs a workspace takes one on torch's current stream, so it runs there or brings its own
+    wide = Step([2, 3], 50000, "bf16", False, seed=2).run()
+    other = torch.cuda.Stream()
+    was = wide.out.clone()
+    wide.args["stream"] = other
+    with pytest.raises(ValueError):
+        wide.again()
+    other.wait_stream(torch.cuda.current_stream())
+    wide.args["workspace"] = torch.empty(efim.efim_verify_workspace_bytes(2, wide.main[2]), dtype=torch.uint8, device="cuda")
+    other.wait_stream(torch.cuda.current_stream())
+    wide.out.fill_(-5)
+    other.wait_stream(torch.cuda.current_stream())
+    wide.again()
+    other.synchronize()
+    assert torch.equal(wide.out, was)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
