@@ -306,9 +306,9 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
     if (p.race_pieces > 1) {
       if (tid == 0) {
         if (key) atomicMax(p.key + s, key);
-        __threadfence();
-        s_last = atomicAdd(p.done + s, 1) == p.race_pieces - 1;
-        __threadfence();
+        int before;                                    // the keys of those before are seen with it
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.done + s) : "memory");
+        s_last = before == p.race_pieces - 1;
         if (s_last) key = *(volatile unsigned long long*)(p.key + s);
       }
       __syncthreads();
