@@ -67,7 +67,7 @@ __device__ __forceinline__ void load_weights(const void* weight, int f32, float 
 // values are loaded once.  A warp's first rows are on their way before its token's sequence is looked up, then the next group's while
 // one is computed.
 //
-// Bound: HBM with many tokens (25,600 at 32/8 heads x 128: 107 us, 6.0 TB/s), and close to it the instructions of a group: 64 registers and
+// Bound: HBM with many tokens (25,600 at 32/8 heads x 128: 105 us, 6.1 TB/s), and close to it the instructions (2.95 a clock): 64 registers and
 // four CTAs an SM even with a few bytes spilled (three CTAs 2-5 % longer with many tokens, two 16 %), weights taken from L1 when they are
 // needed (held in registers the kernel spilled and took 25 % longer, in shared memory as fp32 5 %), warp-wide values marked as such.
 // Not kept: a warp that walks several tokens in a row (code of one loop more: 40 % longer), two groups on their way (2-3 %),

@@ -9,7 +9,15 @@
 //
 // Two kernels.  The first takes every row's maximum and sum (its mass), a piece of a row per CTA.  The second has CTAs for pieces of the
 // vocabulary of every sequence: each joins the masses, finds the row at which its sequence stops and runs its piece of the race
-// for the next token there; the last of them to finish writes the result.
+// for the next token there; the last of them to finish writes the result.  (Few sequences of small vocabularies: verify_fused.cu.)
+//
+// Bound, 256 sequences x 5 rows x 131,072 bf16 with dense drafts, 120 us in all: the masses 66-70 us for 336 MB (5 TB/s; the exponentials keep
+// the special function units at 72 %, without them it is 58), the race 45 us for 274 MB (6 TB/s).  16 sequences, 14.9 us: 1.5 us of
+// dependent loads to the stop, 1.2 to count the race's CTAs, launches.
+// Not kept: every fourth exponential on the FMA pipe (the same, every second 12 us longer); copies through shared memory, four groups
+// on their way (the same; 16 sequences 1 us longer); rows taken first rows first, so that those behind a refusal are left out, which halves
+// the bytes here: with a count behind each piece 117 us, as a persistent kernel of 16 KB pieces 115-193, of whole rows 127; a cluster per
+// sequence that walks its rows 160-212.
 #include "verify.cuh"
 #include <algorithm>
 
@@ -344,6 +352,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   if (status && p.status) atomicOr(p.status, status);
 }
 
+// Pieces of the race of at most 16,384 places: 256 sequences x 131,072 118 us, 8,192 125, 32,768 127 (every CTA looks for the stop itself).
 // Places of a piece and pieces of a row (or a sequence) of `vocab` places, where there are `rows` of them: as many as fill the GPU once
 // (4 CTAs an SM), of 2,048 to `most` places.
 struct Pieces {
