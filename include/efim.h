@@ -348,16 +348,17 @@ efim_status efim_draft_lookup(int32_t batch, const int32_t* d_history, int64_t h
  * if the target had been sampled token by token.  With no drafts (one row) this is plain sampling.
  * Target rows, target_stride elements apart (at least vocab; any alignment of the type): logits in bf16 or fp32, of which
  * p_r = softmax(logits / temperature), or probabilities in fp32 (filtered, say; d_temperature is then NULL).  Logits of -inf have no
- * probability; those at +inf share all of it.  A row with a NaN, or with nothing but -inf, accepts and picks nothing: next is
- * -1 and EFIM_DEV_NO_TOKEN is set.  A draft outside [0, vocab) is refused and sets EFIM_DEV_BAD_TOKEN when its row is reached.
+ * probability; those at +inf share all of it.  A row of logits with a NaN, or with nothing but -inf, accepts and picks nothing: next is
+ * -1 and EFIM_DEV_NO_TOKEN is set; so it is where the next token would have to come from probabilities that are all 0 (NaN counts as 0).  A draft outside [0, vocab) is refused and sets EFIM_DEV_BAD_TOKEN when its row is reached.
  * temperature <= 0 (or no d_noise at all, with logits): greedy - a draft is accepted iff it is the row's largest logit (the lowest place
  * among equals), and that is the next token.  Softmax statistics and probabilities are held in fp32.
  * Results: d_accepted[s] drafts, d_next_token[s]; optionally out_stride entries a sequence of the tokens it goes on with (accepted drafts,
  * next, then -1) and their natural log-probabilities in p (at temperature 1 where greedy; 0 past the end).  A
  * sequence without rows accepts 0 and gets next -1.  The k/v of a sequence's first d_accepted[s] + 1 new tokens stay valid;
- * the next step's tokens overwrite the rest.  Two kernels; may be captured; the same inputs give the same bits.  Workspace: 256-byte
- * aligned, exclusively this call's until the stream has passed it; efim_verify_workspace_bytes() bytes serve every call with no more
- * sequences, rows and places.
+ * the next step's tokens overwrite the rest.  May be captured; the same inputs give the same bits.  vocab is at most 2^30.
+ * Rows of up to 64 KB, with few sequences: one kernel without a workspace (efim_verify_workspace_bytes() is 0, d_workspace may be NULL);
+ * else two.  Workspace: 256-byte aligned, exclusively this call's until the stream has passed it; its bytes serve every call of the same
+ * target_kind with no more sequences, rows and places.
  */
 #define EFIM_TARGET_LOGITS_BF16  0
 #define EFIM_TARGET_LOGITS_F32   1

@@ -215,7 +215,7 @@ __device__ __forceinline__ Scale scale_of(const VerifyParams& p, int s) {
   if (p.noise && p.temperature) {
     const float t = *(p.temperature + s);
     r.greedy = !(t > 0.f);
-    if (!r.greedy) r.c = fminf(1.4426950408889634f / t, FLT_MAX);
+    if (!r.greedy) r.c = fminf(fmaxf(1.4426950408889634f / t, FLT_MIN), FLT_MAX);   // (0 times -inf would be NaN)
   }
   return r;
 }

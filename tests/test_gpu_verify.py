@@ -13,6 +13,7 @@ from oracle import efim_drafts_oracle as orc
 pytestmark = pytest.mark.gpu
 BAD_POSITION, BAD_TOKEN, NO_TOKEN = 2, 8, 16
 LOG_TOL, MARGIN = 5e-5, 1e-5
+WIDE = 70000                                            # rows of more than 64 KB: two kernels
 
 
 class Step:
@@ -128,7 +129,7 @@ def test_rows_at_any_place(kind, vocab, stride, offset):
 @pytest.mark.parametrize("kind,vocab,stride,offset,dense", [("bf16", 131072, 131072, 0, False), ("bf16", 131072, 131072, 0, True),
                                                             ("f32", 70001, 70001, 0, False), ("bf16", 99999, 100001, 3, False)])
 def test_many_rows(kind, vocab, stride, offset, dense):
-    """Rows taken in order, those behind a refusal left out; some sequences of many more rows than the others, some of none."""
+    """Rows of more than 64 KB; some sequences of many more rows than the others, some of none."""
     rng = np.random.default_rng(vocab)
     rows = rng.integers(0, 6, 100).tolist() + [17, 0, 1, 40]
     step = Step(rows, vocab, kind, dense, seed=29, stride=stride, offset=offset)
@@ -148,10 +149,11 @@ def test_many_rows(kind, vocab, stride, offset, dense):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("vocab", [30000, WIDE])
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-def test_greedy(kind):
+def test_greedy(kind, vocab):
     """No noise at all: every sequence greedy, ties to the lowest place (bf16 logits have many)."""
-    step = Step([4, 1, 7, 2], 30000, kind, False, None, seed=9, greedy=True)
+    step = Step([4, 1, 7, 2], vocab, kind, False, None, seed=9, greedy=True)
     step.target = np.round(step.target)
     lowest = step.target.argmax(1)
     step.tokens[1:] = lowest[:-1]
@@ -159,14 +161,16 @@ def test_greedy(kind):
     assert step.check() == 3 + 1 + 1
 
 
-def test_statuses_and_rows_without_a_token():
-    step = Step([3, 3, 3, 2, 1], 2000, "f32", False, None, seed=2)
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab,place", [(2000, 7), (WIDE, WIDE - 3)])
+def test_statuses_and_rows_without_a_token(vocab, place, kind):
+    step = Step([3, 3, 3, 2, 1], vocab, kind, False, None, seed=2)
     step.tokens[[1, 2]] = step.target[[0, 1]].argmax(1)
     step.uniform[:] = 1e-6
     step.target[2] = -np.inf                            # sequence 0's last row
-    step.target[4, 7] = np.nan                          # sequence 1's second
+    step.target[4, place] = np.nan                          # sequence 1's second
     step.tokens[4] = step.target[3].argmax()
-    step.tokens[7] = 2000                               # sequence 2's first draft
+    step.tokens[7] = vocab                              # sequence 2's first draft
     step.target[10, 5] = np.inf                         # sequence 3's second
     step.target[10, 9] = np.inf
     step.tokens[10] = step.target[9].argmax()
@@ -182,22 +186,26 @@ def test_statuses_and_rows_without_a_token():
         assert np.abs(step.logs[s, :len(w[2])].cpu().numpy() - w[2]).max() <= LOG_TOL
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5000, WIDE])
 @pytest.mark.parametrize("value", [-3.0e38, -1e9])
-def test_masks_of_low_finite_values(value):
-    step = Step([2, 1], 5000, "f32", False, None, seed=4)
+def test_masks_of_low_finite_values(value, vocab, kind):
+    step = Step([2, 1], vocab, kind, False, None, seed=4)
     for row in range(3):
         keep = [11 + row, 17, 4000]
-        masked = np.full(5000, value, np.float32)
+        masked = np.full(vocab, value, np.float32)
         masked[keep] = [1.0, 2.0, 0.5]
         step.target[row] = masked
     step.check()
     step.target[:] = value                              # nothing but the mask: all equal
     step.run()
-    assert int(step.status.item()) == 0 and abs(float(step.logs[1, 0]) + np.log(5000)) < LOG_TOL
+    assert int(step.status.item()) == 0 and abs(float(step.logs[1, 0]) + np.log(vocab)) < LOG_TOL
 
 
-def test_small_temperatures_and_infinite_masks():
-    step = Step([3, 1, 2], 3000, "f32", False, None, seed=13)
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [3000, WIDE])
+def test_small_temperatures_and_infinite_masks(vocab, kind):
+    step = Step([3, 1, 2], vocab, kind, False, None, seed=13)
     step.target[:, 100:] = -np.inf
     step.tokens[1:] = step.target.argmax(1)[:-1]
     step.temperature = np.array([1e-30, 1e-6, 1e-39], np.float32)
@@ -207,9 +215,37 @@ def test_small_temperatures_and_infinite_masks():
     assert np.abs(step.logs.cpu().numpy()).max() < 1e-6
 
 
-def test_a_draft_that_leaves_nothing():
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [3000, WIDE])
+def test_infinite_temperature(vocab, kind):
+    """The limit: all that has a probability has the same."""
+    step = Step([2, 1], vocab, kind, False, None, seed=15)
+    step.target[:, 100:] = -np.inf
+    step.tokens[1] = 200                                # masked: refused
+    step.temperature = np.array([np.inf, np.inf], np.float32)
+    step.run()
+    assert int(step.status.item()) == 0 and step.accepted.tolist() == [0, 0]
+    assert step.next.tolist() == step.noise[:, :100].argmin(1).tolist()
+    assert np.abs(step.logs[:, 0].cpu().numpy() + np.log(100)).max() < LOG_TOL
+
+
+@pytest.mark.parametrize("vocab", [3000, WIDE])
+def test_probabilities_of_nothing(vocab):
+    """Rows of zeros; NaN has no probability."""
+    step = Step([2, 1, 1], vocab, "probs", False, seed=27)
+    step.target[:] = 0
+    step.target[2, [5, vocab - 1]] = [np.nan, 0.25]
+    step.target[3, 8] = 1.0
+    step.run()
+    assert int(step.status.item()) == NO_TOKEN and step.accepted.tolist() == [0, 0, 0]
+    assert step.next.tolist() == [-1, vocab - 1, 8]
+    assert np.abs(step.logs[:, 0].cpu().numpy() - [0, np.log(0.25), 0]).max() < 1e-6
+
+
+@pytest.mark.parametrize("vocab", [700, WIDE])
+def test_a_draft_that_leaves_nothing(vocab):
     """q = p: every draft below u = 1 is accepted; one that is refused all the same falls back on p."""
-    step = Step([2, 2], 700, "probs", True, seed=21)
+    step = Step([2, 2], vocab, "probs", True, seed=21)
     step.q = step.target.copy()
     step.uniform[:] = [1.0, 0, 0.999, 0]
     step.run()                                          # (1 * q < p is exact, so the margin of 0 is none)
@@ -217,8 +253,9 @@ def test_a_draft_that_leaves_nothing():
     assert step.next.tolist() == [step.want(s)[1] for s in (0, 1)] and int(step.status.item()) == 0
 
 
-def test_row_ranges_outside_the_rows():
-    step = Step([2, 3], 500, "f32", False, seed=1)
+@pytest.mark.parametrize("vocab", [500, WIDE])
+def test_row_ranges_outside_the_rows(vocab):
+    step = Step([2, 3], vocab, "f32", False, seed=1)
     step.run()
     step.indptr[:] = [0, 2, 9]
     step.run()
@@ -226,8 +263,9 @@ def test_row_ranges_outside_the_rows():
     assert step.out[1].tolist() == [-1] * step.out.shape[1]
 
 
-def test_optional_outputs_and_repeats():
-    step = Step([4, 1, 8], 20000, "bf16", True, seed=17).run()
+@pytest.mark.parametrize("vocab", [20000, WIDE])
+def test_optional_outputs_and_repeats(vocab):
+    step = Step([4, 1, 8], vocab, "bf16", True, seed=17).run()
     want = [t.clone() for t in (step.accepted, step.next, step.out, step.logs)]
     for _ in range(3):
         for t in (step.accepted, step.next, step.out):
@@ -236,7 +274,7 @@ def test_optional_outputs_and_repeats():
         torch.cuda.synchronize()
         for x, y in zip(want, (step.accepted, step.next, step.out, step.logs)):
             assert torch.equal(x, y)                    # the same bits
-    bare = Step([4, 1, 8], 20000, "bf16", True, seed=17).run(out=False)
+    bare = Step([4, 1, 8], vocab, "bf16", True, seed=17).run(out=False)
     assert torch.equal(bare.accepted, want[0]) and torch.equal(bare.next, want[1])
     narrow = torch.full((3, 2), -9, dtype=torch.int32, device="cuda")
     step.args.update(out_tokens=narrow, out_logprobs=None)
