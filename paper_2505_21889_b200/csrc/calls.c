@@ -170,7 +170,7 @@ static PyObject* decode_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 /* ---- calls that take shapes and row strides from the tensors themselves */
-static PyObject *s_shape, *s_stride, *s_dtype, *s_new_empty, *kw_dtype;
+static PyObject *s_shape, *s_stride, *s_numel, *s_is_contiguous, *s_dtype, *s_new_empty, *kw_dtype;
 static PyObject *bf16, *f32, *i32, *u8; /* torch's types, looked up by the first such call */
 
 static int have_types(void) {
@@ -201,6 +201,18 @@ static int as_typed(PyObject* o, PyObject* type, const char* what, void** out) {
   }
   return as_ptr(o, out);
 }
+/* at least n values of one type, packed */
+static int as_vector(PyObject* o, PyObject* type, const char* what, int64_t n, void** out) {
+  if (!as_typed(o, type, what, out)) return 0;
+  if (!is_tensor(o)) return 1;
+  PyObject* count = PyObject_CallMethodNoArgs(o, s_numel);
+  PyObject* packed = count ? PyObject_CallMethodNoArgs(o, s_is_contiguous) : NULL;
+  const int ok = packed ? packed == Py_True && PyLong_AsLongLong(count) >= n : -1;
+  Py_XDECREF(count);
+  Py_XDECREF(packed);
+  if (ok == 0) PyErr_Format(PyExc_ValueError, "%s: %lld packed values are expected", what, (long long)n);
+  return ok > 0;
+}
 /* Rows of a tensor: their number, values (all dimensions but the first, packed) and the distance from one to the next.  None has none. */
 static int as_rows(PyObject* o, PyObject* type, const char* what, void** out, int64_t* rows, int64_t* row, int64_t* step) {
   *out = NULL;
@@ -229,6 +241,10 @@ static int as_rows(PyObject* o, PyObject* type, const char* what, void** out, in
   Py_XDECREF(stride);
   if (PyErr_Occurred()) return 0;
   if (!ok) PyErr_Format(PyExc_ValueError, "%s: rows of packed values are expected", what);
+  if (ok && (*rows > INT32_MAX || *row > INT32_MAX)) {
+    PyErr_Format(PyExc_ValueError, "%s: more rows or values of a row than 32 bits count", what);
+    ok = 0;
+  }
   return ok;
 }
 static int expect(int64_t got, int64_t wanted, const char* what) {
@@ -264,10 +280,10 @@ static PyObject* draft_lookup(PyObject* self, PyObject* const* a, Py_ssize_t n) 
   int64_t batch, max_len, stride, rows, num, step;
   int32_t lo, hi;
   if (!want(n, 8) || !have_types()) return NULL;
-  if (!as_rows(a[0], i32, "history", &p[0], &batch, &max_len, &stride) || !as_typed(a[1], i32, "lengths", &p[1]) ||
+  if (!as_rows(a[0], i32, "history", &p[0], &batch, &max_len, &stride) || !as_vector(a[1], i32, "lengths", batch, &p[1]) ||
       !as_i32(a[2], &lo) || !as_i32(a[3], &hi) || !as_rows(a[4], i32, "drafts", &p[4], &rows, &num, &step) ||
       !expect(rows, batch, "drafts, rows") || !expect(step, num, "drafts, values from one row to the next") ||
-      !as_typed(a[5], i32, "draft_len", &p[5]) || !as_typed(a[6], i32, "status", &p[6]) || !PTR(7))
+      !as_vector(a[5], i32, "draft_len", batch, &p[5]) || !as_typed(a[6], i32, "status", &p[6]) || !PTR(7))
     return NULL;
   RETURN_STATUS(efim_draft_lookup((int32_t)batch, p[0], stride, (int32_t)max_len, p[1], lo, hi, (int32_t)num, p[4], p[5], p[6], p[7]));
 }
@@ -305,11 +321,12 @@ static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n)
   if (!want(n, 16) || !have_types()) return NULL;
   const int probs = PyObject_IsTrue(a[4]), half = probs ? 0 : is_type(a[3], bf16);
   if (probs < 0 || half < 0) return NULL;
-  if (!as_i32(a[0], &d.batch) || !as_typed(a[1], i32, "row_indptr", &p[1]) || !as_typed(a[2], i32, "tokens", &p[2]) ||
+  if (!as_i32(a[0], &d.batch) || !as_vector(a[1], i32, "row_indptr", (int64_t)d.batch + 1, &p[1]) ||
       !as_rows(a[3], half ? bf16 : f32, "target", &p[3], &rows, &vocab, &d.target_stride) ||
-      !as_matrix(a[5], f32, "draft_probs", rows, vocab, &p[5], &d.draft_stride) || !as_typed(a[6], f32, "uniform", &p[6]) ||
-      !as_matrix(a[7], f32, "noise", d.batch, vocab, &p[7], &d.noise_stride) || !as_typed(a[8], f32, "temperature", &p[8]) ||
-      !as_typed(a[9], i32, "accepted", &p[9]) || !as_typed(a[10], i32, "next_token", &p[10]) ||
+      !as_vector(a[2], i32, "tokens", rows, &p[2]) || !as_matrix(a[5], f32, "draft_probs", rows, vocab, &p[5], &d.draft_stride) ||
+      !as_vector(a[6], f32, "uniform", rows, &p[6]) || !as_matrix(a[7], f32, "noise", d.batch, vocab, &p[7], &d.noise_stride) ||
+      !as_vector(a[8], f32, "temperature", d.batch, &p[8]) || !as_vector(a[9], i32, "accepted", d.batch, &p[9]) ||
+      !as_vector(a[10], i32, "next_token", d.batch, &p[10]) ||
       !as_rows(a[11], i32, "out_tokens", &p[11], &out_rows, &width, &step) ||
       (p[11] && (!expect(out_rows, d.batch, "out_tokens, rows") || !expect(step, width, "out_tokens, values from one row to the next"))) ||
       !as_rows(a[12], f32, "out_logprobs", &p[12], &out_rows, &logs, &step) ||
@@ -360,11 +377,13 @@ PyMODINIT_FUNC PyInit__calls(void) {
   s_nbytes = PyUnicode_InternFromString("nbytes");
   s_shape = PyUnicode_InternFromString("shape");
   s_stride = PyUnicode_InternFromString("stride");
+  s_numel = PyUnicode_InternFromString("numel");
+  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   s_dtype = PyUnicode_InternFromString("dtype");
   s_new_empty = PyUnicode_InternFromString("new_empty");
   kw_dtype = s_dtype ? PyTuple_Pack(1, s_dtype) : NULL;
   PyObject* numpy = PyImport_ImportModule("numpy");
-  if (!s_data_ptr || !s_nbytes || !s_shape || !s_stride || !s_dtype || !s_new_empty || !kw_dtype || !numpy) return NULL;
+  if (!s_data_ptr || !s_nbytes || !s_shape || !s_stride || !s_numel || !s_is_contiguous || !s_dtype || !s_new_empty || !kw_dtype || !numpy) return NULL;
   ndarray = (PyTypeObject*)PyObject_GetAttrString(numpy, "ndarray");
   Py_DECREF(numpy);
   if (!ndarray || !PyType_Check(ndarray)) return NULL;

@@ -81,6 +81,8 @@ def test_verify(lib):
                 dict(target_kind=2, d_target=0x5004), dict(target_kind=2, d_target=0x5004, d_temperature=None, d_noise=None)):
         assert _verify(lib, **bad) == INVALID_ARG, bad
     assert _verify(lib, batch=0, d_row_indptr=None) == OK
+    huge = (1 << 30) + 1
+    assert _verify(lib, vocab=huge, target_stride=huge, draft_stride=huge, noise_stride=huge) == UNSUPPORTED
     size = lib.efim_verify_workspace_bytes
     wide = dict(vocab=100000, target_stride=100000, draft_stride=100000, noise_stride=100000)
     need = size(2, 6, 100000, 0)
@@ -111,6 +113,8 @@ def test_python_side(lib):
                            (TypeError, dict(q_out=good["q_out"].half()))]:
         with pytest.raises(error):
             append(**changed)
+    with pytest.raises(ValueError):                     # weights of heads of another size
+        efim.efim_qk_norm_append(cache, batch, efim.QkNorm(None, torch.zeros(32)), None, **good, stream=0)
     for bad in (lambda: efim.QkNorm(torch.zeros(8), torch.zeros(8, dtype=half)), lambda: efim.QkNorm(torch.zeros(16)[::2], None),
                 lambda: efim.QkNorm(torch.zeros(8, dtype=torch.float16), None),
                 lambda: efim.Rope.from_table(torch.zeros(4, 8, dtype=torch.float64)), lambda: efim.Rope.from_table(torch.zeros(8, 8).t()[:, :4])):
@@ -119,7 +123,8 @@ def test_python_side(lib):
     hist, drafts, n = torch.zeros(2, 50, dtype=whole), torch.zeros(2, 3, dtype=whole), torch.zeros(2, dtype=whole)
     for error, args in [(ValueError, (hist[:, ::2], n, 1, 2, drafts, n)), (ValueError, (hist, n, 1, 2, drafts[:, :2], n)),
                         (ValueError, (hist, n, 1, 2, drafts[:1], n)), (TypeError, (hist.long(), n, 1, 2, drafts, n)),
-                        (TypeError, (hist, n.long(), 1, 2, drafts, n)), (TypeError, (hist, n, 1, 2.5, drafts, n))]:
+                        (TypeError, (hist, n.long(), 1, 2, drafts, n)), (ValueError, (hist, n[:1], 1, 2, drafts, n)),
+                        (ValueError, (hist, hist[:, 0], 1, 2, drafts, n)), (ValueError, (hist, n, 1, 2, drafts, drafts[:, 1])), (TypeError, (hist, n, 1, 2.5, drafts, n))]:
         with pytest.raises(error):
             efim.efim_draft_lookup(*args, stream=0)
     logits, ws = torch.zeros(5, 100, dtype=half), None
@@ -132,7 +137,11 @@ def test_python_side(lib):
                            (ValueError, dict(target=torch.zeros(100, 5, dtype=half).t())), (TypeError, dict(tokens=torch.zeros(5, dtype=torch.int64))),
                            (ValueError, dict(out_tokens=torch.zeros(2, 6, dtype=whole), out_logprobs=wide[:, :5].contiguous())),
                            (ValueError, dict(out_logprobs=wide[:, :5])), (ValueError, dict(out_tokens=torch.zeros(1, 6, dtype=whole))),
-                           (TypeError, dict(temperature=torch.zeros(2, dtype=torch.float64)))]:
+                           (TypeError, dict(temperature=torch.zeros(2, dtype=torch.float64))),
+                           (ValueError, dict(row_indptr=torch.zeros(2, dtype=whole))), (ValueError, dict(tokens=torch.zeros(4, dtype=whole))),
+                           (ValueError, dict(uniform=torch.zeros(4))), (ValueError, dict(uniform=torch.zeros(5, 2)[:, 0])),
+                           (ValueError, dict(temperature=torch.zeros(1))), (ValueError, dict(accepted=hist[:, 0])),
+                           (ValueError, dict(next_token=n[:1]))]:
         with pytest.raises(error):
             efim.efim_verify_drafts(**{**r, **changed}, stream=0)
     big = dict(target=torch.zeros(5, 40000, dtype=half), noise=torch.zeros(2, 40000))
