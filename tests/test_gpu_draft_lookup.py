@@ -68,6 +68,20 @@ def test_repetitions():
     assert _check(hist, [400, 399, 400, 400], 1, 32, 9) == 3
 
 
+@pytest.mark.parametrize("hi", [1, 2, 3, 32])
+@pytest.mark.parametrize("batch", [2, 200])
+def test_long_repetitions(batch, hi):
+    """Every place agrees, or every second, or all but the newest; the longest agreement may be an old one."""
+    rows = np.zeros((batch, 9001), np.int32)
+    rows[1::4, 1::2] = 3
+    rows[2::4] = np.random.default_rng(5).integers(0, 2, rows[2::4].shape)
+    rows[3::4] = np.arange(9001)
+    rows[3::4, 40:45] = rows[3::4, 8990:8995] = 7, 8, 9, 8, 9
+    rows[3::4, 8996:] = 7, 8, 9, 8, 9
+    lens = [9001, 9000, 8999, 9001] * (batch // 4) + [9001, 8999, 9001][:batch % 4]
+    assert _check(rows, lens, 1, hi, 11, stride=9003, offset=1) == batch
+
+
 def test_lengths_outside_the_rows():
     hist = np.tile(np.array([[4, 5, 6, 4]], np.int32), (3, 1))
     drafts, n, status = _run(hist, [-3, 9, 4], 1, 2, 2)
