@@ -116,6 +116,12 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return r;
 }
 
+// Sends for [p, p + bytes) of global memory to be in L2 (whole 16-byte units of it).
+__device__ __forceinline__ void prefetch_l2(const void* p, long long bytes) {
+  const uintptr_t a = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, z = (reinterpret_cast<uintptr_t>(p) + bytes) & ~(uintptr_t)15;
+  if (a < z) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(z - a)) : "memory");
+}
+
 // maximum that is NaN if either operand is (fmaxf drops a NaN)
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;

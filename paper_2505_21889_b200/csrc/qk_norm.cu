@@ -28,6 +28,7 @@ struct QkNormParams {
   int batch, max_pages_per_seq, total_new_tokens;
   int num_pages, Hq, Hkv, max_position, interleaved, weight_f32;
   int warps;                // of a token
+  int ahead;                // a token's rows are sent for into L2 by its first and last warp
   int early_next;           // let the next kernel start its set-up while this one runs
 };
 
@@ -38,27 +39,27 @@ constexpr int QK_NORM_THREADS = 256;
 __device__ __forceinline__ int uniform(int x) { return __reduce_max_sync(0xffffffffu, x); }
 
 // 8 weights from position d on, as the products take them
-__device__ __forceinline__ void load_weights(const void* weight, int f32, float offset, int d, float* w) {
+__device__ __forceinline__ void load_weights(const void* weight, int f32, float offset, int d, float2* w) {
   if (!weight) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    for (int i = 0; i < 4; ++i) w[i] = make_float2(1.f, 1.f);
     return;
   }
   if (f32) {
     const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(weight) + d);
-    *reinterpret_cast<float4*>(w) = src[0];
-    *reinterpret_cast<float4*>(w + 4) = src[1];
+    const float4 u = src[0], v = src[1];
+    w[0] = make_float2(u.x, u.y);
+    w[1] = make_float2(u.z, u.w);
+    w[2] = make_float2(v.x, v.y);
+    w[3] = make_float2(v.z, v.w);
   } else {
     const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(weight) + d);
     const uint32_t p[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[2 * i] = bf16lo(p[i]);
-      w[2 * i + 1] = bf16hi(p[i]);
-    }
+    for (int i = 0; i < 4; ++i) w[i] = make_float2(bf16lo(p[i]), bf16hi(p[i]));
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] += offset;
+  for (int i = 0; i < 4; ++i) w[i] = add2(w[i], make_float2(offset, offset));
 }
 
 // A token's q and k heads go to its warps (WARPS, or p.warps where that is 0) in groups of HW = 512 / D, v's vectors, which are
@@ -67,9 +68,10 @@ __device__ __forceinline__ void load_weights(const void* weight, int f32, float 
 // values are loaded once.  A warp's first rows are on their way before its token's sequence is looked up, then the next group's while
 // one is computed.
 //
-// Bound: HBM with many tokens (25,600 at 32/8 heads x 128: 105 us, 6.1 TB/s), and close to it the instructions (2.95 a clock): 64 registers and
-// four CTAs an SM even with a few bytes spilled (three CTAs 2-5 % longer with many tokens, two 16 %), weights taken from L1 when they are
-// needed (held in registers the kernel spilled and took 25 % longer, in shared memory as fp32 5 %), warp-wide values marked as such.
+// Bound: HBM with many tokens (25,600 at 32/8 heads x 128: 99 us, 6.4 TB/s), and close to it the instructions (2.8 a clock, with the products
+// two at a time; one by one 15 % more of them and 1 us): 64 registers and four CTAs an SM even with a few bytes spilled (three CTAs 2-5 %
+// longer with many tokens, two 16 %), weights taken from L1 when they are needed (held in registers the kernel spilled and took 25 %
+// longer, in shared memory as fp32 5 %), warp-wide values marked as such.
 // Not kept: a warp that walks several tokens in a row (code of one loop more: 40 % longer), two groups on their way (2-3 %),
 // v's heads in the groups' loop (8 %), warps of v's alone (6 %).
 template <int D, int WARPS>
@@ -105,6 +107,13 @@ __global__ void __launch_bounds__(QK_NORM_THREADS, 4) qk_norm_append_kernel(cons
     for (int i = 0; i < COPIES; ++i)
       if (u0 + v_step * i < n_vec) v[i] = ldg_stream(vin + u0 + v_step * i);
   };
+  if (p.ahead && lane == 0) {
+    if (part == 0 && p.q) prefetch_l2(p.q + t * p.q_stride, nq * D * 2LL);
+    if (part == warps - 1) {
+      prefetch_l2(p.k + t * p.k_stride, p.Hkv * D * 2LL);
+      prefetch_l2(p.v + t * p.v_stride, p.Hkv * D * 2LL);
+    }
+  }
   fetch(base0 + sub);
   fetch_v(v0);
 
@@ -118,15 +127,20 @@ __global__ void __launch_bounds__(QK_NORM_THREADS, 4) qk_norm_append_kernel(cons
   } else {
     page = *(p.block_table + (size_t)at.seq * p.max_pages_per_seq + page_idx);
   }
-  float c[8], s[8];
+  float2 c[4], s[4];
   if (p.cos_sin && in_table && base0 < nh) {
     // 8 pairs: (f, f + D/2) from f = 8 j on, or the 4 + 4 neighbours of the two vectors
     const float* cs = p.cos_sin + (size_t)pos * D + j * (p.interleaved ? 4 : 8);
     const int second = p.interleaved ? D / 4 : 4;
-    *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(cs);
-    *reinterpret_cast<float4*>(c + 4) = *reinterpret_cast<const float4*>(cs + second);
-    *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(cs + D / 2);
-    *reinterpret_cast<float4*>(s + 4) = *reinterpret_cast<const float4*>(cs + D / 2 + second);
+    auto four = [](const float* src, float2* to) {
+      const float4 u = *reinterpret_cast<const float4*>(src);
+      to[0] = make_float2(u.x, u.y);
+      to[1] = make_float2(u.z, u.w);
+    };
+    four(cs, c);
+    four(cs + second, c + 2);
+    four(cs + D / 2, s);
+    four(cs + D / 2 + second, s + 2);
   }
   if (placed && (page < 0 || page >= p.num_pages)) {
     if (lane == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
@@ -147,20 +161,18 @@ __global__ void __launch_bounds__(QK_NORM_THREADS, 4) qk_norm_append_kernel(cons
 #pragma unroll 1
   for (int base = base0; base < nh; base += step) {    // (the same for a warp's lanes: the sums below are the whole warp's)
     const int h = base + sub;
-    float x[16];
+    float2 x[8];
     {
       const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[2 * e] = bf16lo(w[e]);
-        x[2 * e + 1] = bf16hi(w[e]);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = make_float2(bf16lo(w[e]), bf16hi(w[e]));
     }
     if (base + step < nh) fetch(h + step);
     auto squares = [&]() {
-      float ss = 0.f;
+      float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+      for (int e = 0; e < 8; ++e) s2 = fma2(x[e], x[e], s2);
+      float ss = s2.x + s2.y;
 #pragma unroll
       for (int d = HALF / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
       return ss;
@@ -171,38 +183,43 @@ __global__ void __launch_bounds__(QK_NORM_THREADS, 4) qk_norm_append_kernel(cons
       // them).  A row with an infinity or a NaN stays what the formula makes of it.
       const float down = ss <= FLT_MAX ? 1.f : 8.470329472543003e-22f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] *= down;
+      for (int e = 0; e < 8; ++e) x[e] = mul2(x[e], make_float2(down, down));
       if (down != 1.f) eps = 0.f;
       ss = squares();
     }
     if (h >= nh || (h >= nq && !placed)) continue;
     const float r = rsqrtf(fmaf(ss, 1.f / D, eps));
+    const float2 rr = make_float2(r, r);
     // (from L1 after a warp's first heads: in registers beside the rotary values they made the kernel spill)
     const void* weight = h < nq ? p.q_weight : p.k_weight;
-    float w[8];
+    float2 w[4];
     load_weights(weight, p.weight_f32, p.weight_offset, j * 8, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] * r * w[e];
+    for (int e = 0; e < 4; ++e) x[e] = mul2(mul2(x[e], rr), w[e]);
     load_weights(weight, p.weight_f32, p.weight_offset, (j + HALF) * 8, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[8 + e] = x[8 + e] * r * w[e];
+    for (int e = 0; e < 4; ++e) x[4 + e] = mul2(mul2(x[4 + e], rr), w[e]);
     uint32_t y[8];
     if (!p.cos_sin) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+      for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[e].x, x[e].y);
     } else if (!in_table) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = 0;     // no rotation for this row: a query of zeros
     } else if (!p.interleaved) {
+      const float2 minus = make_float2(-1.f, -1.f);
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        y[e / 2] = pack_bf16x2(fmaf(x[e], c[e], -(x[8 + e] * s[e])), fmaf(x[e + 1], c[e + 1], -(x[9 + e] * s[e + 1])));
-        y[4 + e / 2] = pack_bf16x2(fmaf(x[8 + e], c[e], x[e] * s[e]), fmaf(x[9 + e], c[e + 1], x[e + 1] * s[e + 1]));
+      for (int e = 0; e < 4; ++e) {
+        const float2 lo = fma2(x[e], c[e], mul2(mul2(x[4 + e], s[e]), minus)), hi = fma2(x[4 + e], c[e], mul2(x[e], s[e]));
+        y[e] = pack_bf16x2(lo.x, lo.y);
+        y[4 + e] = pack_bf16x2(hi.x, hi.y);
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        y[e] = pack_bf16x2(fmaf(x[2 * e], c[e], -(x[2 * e + 1] * s[e])), fmaf(x[2 * e + 1], c[e], x[2 * e] * s[e]));
+      for (int e = 0; e < 8; ++e) {
+        const float ce = e % 2 ? c[e / 2].y : c[e / 2].x, se = e % 2 ? s[e / 2].y : s[e / 2].x;
+        y[e] = pack_bf16x2(fmaf(x[e].x, ce, -(x[e].y * se)), fmaf(x[e].y, ce, x[e].x * se));
+      }
     }
     uint4* dst = reinterpret_cast<uint4*>(h < nq ? q_out + h * D : p.k_pool + pool_tok + (size_t)(h - nq) * 16 * D + j * 8);
     dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
@@ -272,15 +289,18 @@ extern "C" efim_status efim_qk_norm_append(const efim_cache_desc* cache, const e
   p.num_pages = cache->num_pages;
   p.Hq = cache->num_q_heads;
   p.Hkv = cache->num_kv_heads;
-  // Warps of a token: as many as are resident at once, up to one for every group of q's and k's heads; with more tokens one, or two
-  // from ten groups on.  Microseconds with 1 / 2 / 4 / a warp per group: 64 tokens at 32/8 heads x 128 8.3 / 5.5 / 4.3 / 2.7, 900 at 28/4 7.3 / 5.6 /
-  // 5.3 / 6.4, 2,336 at 32/8 14.3 / 12.8 / 13.7 / 16.4, at 32/32 25.5 / 22.0 / 22.7 / 25 or more, 20,000 at 28/4 64.1 / 66.8 / 73.5 / 91, at 32/8 84.5 /
-  // 83.4 / 93.6 / 116, at 32/32 171 / 166 / 167 / 180 or more, at 4/4 x 64 15.8 / 20.4.
+  // Warps of a token: as many as are resident at once, up to one for every group of q's and k's heads; with more tokens one, or from
+  // ten groups on one for every five.  Microseconds with 1 / 2 / 4 / 10 (or a warp per group): 64 tokens at 32/8 heads x 128 8.3 / 5.5 / 4.3 / 2.7,
+  // 2,304 at 28/4 10.2 / 9.4 / 9.7 / 11.7, at 32/8 13.8 / 12.1 / 12.8 / 15.4, at 32/32 25.3 / 22.1 / 21.3 / 23.0, 12,800 at 28/4 41.9 / 43.4 / 46.2 / 57,
+  // at 32/8 54.3 / 54.8 / 58.6 / 72, at 32/32 107 / 109 / 104 / 113.
   const int hw = 512 / D, heads = (d_q ? cache->num_q_heads : 0) + cache->num_kv_heads, groups = (heads + hw - 1) / hw;
   const long long resident = 4LL * (QK_NORM_THREADS / 32) * sm_count();
-  p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 10 ? 2 : 1, resident / T));
+  p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 10 ? (groups + 4) / 5 : 1, resident / T));
   const long long ctas = (T * p.warps + QK_NORM_THREADS / 32 - 1) / (QK_NORM_THREADS / 32);
   if (ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  // From several waves on, where a token has several warps: 9,600 tokens at 32/8 42.8 -> 42.0, 25,600 104 -> 99, at 32/32 206 -> 199, at 64/8 177 -> 164;
+  // but 3,200 at 32/32 28.9 -> 29.9, one wave of 2,304 21.8 -> 23.1, a warp a token 12,800 at 28/4 41.9 -> 44.1.
+  p.ahead = p.warps > 1 && T * p.warps > 4 * resident;
   p.early_next = ctas <= sm_count();
   auto launch = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)ctas), dim3(QK_NORM_THREADS), 0, static_cast<cudaStream_t>(stream), p);

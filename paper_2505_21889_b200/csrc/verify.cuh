@@ -50,11 +50,6 @@ __device__ __forceinline__ float rcp_fast(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Sends for [p, p + bytes) of global memory to be in L2 (whole 16-byte units of it).
-__device__ __forceinline__ void prefetch_l2(const void* p, long long bytes) {
-  const uintptr_t a = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15, z = (reinterpret_cast<uintptr_t>(p) + bytes) & ~(uintptr_t)15;
-  if (a < z) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(z - a)) : "memory");
-}
 // maximum over the warp; NaN lanes do not count
 __device__ __forceinline__ float warp_max(float x) {
   float y;
