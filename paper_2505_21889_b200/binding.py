@@ -291,7 +291,7 @@ class QkNorm:
         _check(all(w.dtype in (torch.bfloat16, torch.float32) and w.dim() == 1 and w.is_contiguous() for w in given)
                and len({(w.dtype, w.shape) for w in given}) <= 1, "the norms' weights are two bf16 or two fp32 vectors of one length")
         self.q_weight, self.k_weight = q_weight, k_weight
-        self.head_dim = given[0].shape[0] if given else None      # of any, without weights
+        self.head_dim = given[0].shape[0] if given else 0         # 0: of any
         self.desc = _QkNormDesc(_ptr(q_weight), _ptr(k_weight), 1 if given and given[0].dtype == torch.float32 else 0, eps,
                                 weight_offset)
 
@@ -314,8 +314,7 @@ def efim_kv_append(cache: Cache, batch: Batch, rope, q, k_new, v_new, status=Non
 def efim_qk_norm_append(cache: Cache, batch: Batch, norm: QkNorm, rope, q, k, v, q_out, status=None, stream=None):
     """efim_kv_append with a norm of every q and k head before the rotation.  q, k and v: bf16, one row per new token (of any rank
     past the first, packed), views of one buffer allowed; q_out: packed.  q and q_out may both be None."""
-    _check(norm.head_dim is None or norm.head_dim == cache.desc.head_dim, "the norm's weights are as long as a head")
-    st = _calls.qk_norm_append(_addr(cache.desc), _addr(batch.desc), _addr(norm.desc),
+    st = _calls.qk_norm_append(_addr(cache.desc), _addr(batch.desc), _addr(norm.desc), norm.head_dim,
                                _addr(rope.desc) if rope is not None else None, q, k, v, q_out, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_qk_norm_append")

@@ -258,20 +258,21 @@ static int as_matrix(PyObject* o, PyObject* type, const char* what, int64_t rows
   return as_rows(o, type, what, out, &n, &m, step) && (o == Py_None || (expect(n, rows, what) && expect(m, row, what)));
 }
 
-/* cache, batch, norm, rope, q, k, v, q_out, status, stream */
+/* cache, batch, norm, head_dim of its weights (or 0), rope, q, k, v, q_out, status, stream */
 static PyObject* qk_norm_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[10];
+  void* p[11];
+  int32_t weights;
   int64_t qs, ks, vs, os;
-  if (!want(n, 10) || !have_types()) return NULL;
-  if (!PTR(0) || !PTR(1) || !PTR(2) || !PTR(3) || !as_typed(a[8], i32, "status", &p[8]) || !PTR(9)) return NULL;
+  if (!want(n, 11) || !have_types()) return NULL;
+  if (!PTR(0) || !PTR(1) || !PTR(2) || !as_i32(a[3], &weights) || !PTR(4) || !as_typed(a[9], i32, "status", &p[9]) || !PTR(10)) return NULL;
   const efim_cache_desc* c = p[0];
   const int64_t rows = ((const efim_batch_desc*)p[1])->total_new_tokens, q = (int64_t)c->num_q_heads * c->head_dim,
                 kv = (int64_t)c->num_kv_heads * c->head_dim;
-  if (!as_matrix(a[4], bf16, "q", rows, q, &p[4], &qs) || !as_matrix(a[5], bf16, "k", rows, kv, &p[5], &ks) ||
-      !as_matrix(a[6], bf16, "v", rows, kv, &p[6], &vs) || !as_matrix(a[7], bf16, "q_out", rows, q, &p[7], &os) ||
-      (p[7] && !expect(os, q, "q_out, values from one row to the next")))
+  if ((weights && !expect(weights, c->head_dim, "the norm's weights, values")) || !as_matrix(a[5], bf16, "q", rows, q, &p[5], &qs) ||
+      !as_matrix(a[6], bf16, "k", rows, kv, &p[6], &ks) || !as_matrix(a[7], bf16, "v", rows, kv, &p[7], &vs) ||
+      !as_matrix(a[8], bf16, "q_out", rows, q, &p[8], &os) || (p[8] && !expect(os, q, "q_out, values from one row to the next")))
     return NULL;
-  RETURN_STATUS(efim_qk_norm_append(p[0], p[1], p[2], p[3], p[4], qs, p[5], ks, p[6], vs, p[7], p[8], p[9]));
+  RETURN_STATUS(efim_qk_norm_append(p[0], p[1], p[2], p[4], p[5], qs, p[6], ks, p[7], vs, p[8], p[9], p[10]));
 }
 
 /* history, len, min_ngram, max_ngram, drafts, draft_len, status, stream */
