@@ -121,9 +121,10 @@ def test_weights_and_pairings(weights, offset, interleaved, rope):
 
 
 @pytest.mark.parametrize("tokens,hq,hkv,d", [(444, 4, 4, 64), (445, 4, 4, 64), (900, 2, 1, 64), (1800, 4, 4, 64), (1790, 2, 2, 128),
-                                             (900, 32, 32, 128), (1777, 24, 4, 128)])
+                                             (900, 32, 32, 128), (1777, 24, 4, 128),
+                                             (9500, 32, 8, 128), (1500, 240, 16, 128), (9600, 72, 8, 64)])
 def test_numbers_of_tokens(tokens, hq, hkv, d):
-    """Every number of warps a token, ragged over sequences (one of them without new tokens)."""
+    """Every number of warps a token, one wave and several, ragged over sequences (one of them without new tokens)."""
     rng = np.random.default_rng(tokens)
     cut = np.sort(rng.integers(0, tokens + 1, 6))
     new = np.diff(np.concatenate([[0], cut, [tokens]])).tolist()
