@@ -169,14 +169,18 @@ __device__ __forceinline__ RowResult judge_row(const VerifyParams& p, int r, con
   return judge<KIND>(sum, d, sc);
 }
 
-// What the CTAs of the others meet in.
-__global__ void __launch_bounds__(VERIFY_THREADS) verify_init_kernel(const VerifyParams p) {
-  pdl_wait();
-  pdl_launch();
-  for (int s = blockIdx.x * VERIFY_THREADS + threadIdx.x; s < p.batch; s += gridDim.x * VERIFY_THREADS) {
+// What the CTAs of the second kernel meet in, cleared by all of a grid's threads together.  In 64 bits: a grid of rows and pieces may
+// have more than 2^31 threads.
+__device__ __forceinline__ void clear_meetings(const VerifyParams& p) {
+  for (long long s = (long long)blockIdx.x * VERIFY_THREADS + threadIdx.x; s < p.batch; s += (long long)gridDim.x * VERIFY_THREADS) {
     p.key[s] = 0;
     p.done[s] = 0;
   }
+}
+__global__ void __launch_bounds__(VERIFY_THREADS) verify_init_kernel(const VerifyParams p) {
+  pdl_wait();
+  pdl_launch();
+  clear_meetings(p);
 }
 
 // The masses of all rows, a CTA a piece.
@@ -198,10 +202,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_mass_kernel(const Ve
   const int r = blockIdx.x / p.pieces, piece = blockIdx.x % p.pieces;
   pdl_wait();
   pdl_launch();
-  for (int s = blockIdx.x * VERIFY_THREADS + tid; s < p.batch; s += gridDim.x * VERIFY_THREADS) {
-    p.key[s] = 0;
-    p.done[s] = 0;
-  }
+  clear_meetings(p);
   Share<T> share;
   share.fetch(static_cast<const T*>(p.target) + r * p.target_stride, piece * p.piece, min(p.vocab, (piece + 1) * p.piece));
   // the row's sequence: the last that starts at or before it
@@ -459,7 +460,7 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   if (logits) {
     EFIM_CUDA_TRY(launch_pdl(bf16 ? verify_mass_kernel<TARGET_BF16> : verify_mass_kernel<TARGET_F32>, dim3((unsigned)ctas), block, 0, s, p));
   } else {
-    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3((unsigned)((d->batch + VERIFY_THREADS - 1) / VERIFY_THREADS)), block, 0, s, p));
+    EFIM_CUDA_TRY(launch_pdl(verify_init_kernel, dim3((unsigned)((d->batch + (long long)VERIFY_THREADS - 1) / VERIFY_THREADS)), block, 0, s, p));
   }
   EFIM_CUDA_TRY(launch_pdl(!logits ? verify_pick_kernel<TARGET_PROBS> : bf16 ? verify_pick_kernel<TARGET_BF16> : verify_pick_kernel<TARGET_F32>,
                            pick, block, 0, s, p));
