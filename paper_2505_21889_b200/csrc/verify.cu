@@ -311,7 +311,10 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
       __syncthreads();
       return warp == 0 ? warp_best(lane < VERIFY_WARPS ? s_key[lane] : 0) : k;
     };
-    key = run(begin, end, __uint_as_float((uint32_t)(*(volatile unsigned long long*)(p.key + s) >> 32)));
+    // Other CTAs raise the key meanwhile, and the race's loops are a warp's together: one lane looks, for all of its warp.
+    float known = 0.f;
+    if (lane == 0) known = __uint_as_float((uint32_t)(*(volatile unsigned long long*)(p.key + s) >> 32));
+    key = run(begin, end, __shfl_sync(0xffffffffu, known, 0));
     // the CTAs of a sequence meet: the last one through has the best of all
     if (p.race_pieces > 1) {
       if (tid == 0) {

@@ -143,7 +143,7 @@ struct Race {
   Row<KIND> of;
   float scale, ref;
   int gone;                                           // a place that does not take part
-  float best;                                         // of the warp, or known to be reached by others: what it leaves out cannot win
+  float best;                                         // of the warp (the same in its lanes), or known to be reached by others: what it leaves out cannot win
   unsigned long long key;                             // of this lane: result and place as one number to be compared, 0 for none
   __device__ __forceinline__ Race(const Row<KIND>& of_, int gone_, float known) : of(of_), gone(gone_), best(known), key(0) {
     const bool logits = KIND != TARGET_PROBS;

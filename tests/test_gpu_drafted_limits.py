@@ -37,3 +37,28 @@ def test_more_than_2_to_31_threads():
     for x, y in zip(want, (accepted, following, step.out, step.logs)):
         assert torch.equal(x, y)
     assert bool((guard[:4096] == 255).all()) and bool((guard[4096 + need:] == 255).all())
+
+
+@pytest.mark.parametrize("vocab", [300000, 300001])
+@pytest.mark.parametrize("dense", [False, True])
+def test_races_that_others_raise(dense, vocab):
+    """One sequence, as many CTAs as there can be on one race, with results that rise along the row and fall along it: CTAs begin
+    while others have raised the best already.  Whatever each of them saw, the result is the definition's, every time."""
+    for flip in (False, True):
+        step = Step([1], vocab, "f32", False, None, seed=37)
+        if dense:                                       # two rows: the first refuses its draft
+            step = Step([2, 1], vocab, "f32", True, None, seed=37)
+            step.tokens[1] = step.target[0].argmin()
+            step.q[0] *= 0.5
+            step.q[0, step.tokens[1]] = 0.5
+            step.uniform[0] = 0.999
+        step.target[:] = np.random.default_rng(41).uniform(-1, 1, step.target.shape)
+        place = np.arange(vocab)[::-1] if flip else np.arange(vocab)
+        step.noise[:] = 1.0 / (1.0 + place) * np.random.default_rng(43).uniform(0.9, 1.1, step.noise.shape)
+        step.check()
+        want = [t.clone() for t in (step.accepted, step.next, step.out, step.logs)]
+        for _ in range(50):
+            step.again()
+        torch.cuda.synchronize()
+        for x, y in zip(want, (step.accepted, step.next, step.out, step.logs)):
+            assert torch.equal(x, y)
