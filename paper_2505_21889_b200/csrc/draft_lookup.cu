@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) draft_lookup_kernel(const Look
     const int n_vec = (n - lead) / 4, tail = lead + n_vec * 4;
     const int id = rank * LOOKUP_THREADS + tid, lanes = ctas * LOOKUP_THREADS;
     auto look_at = [&](int at) { look(T[at], at > 0 ? T[at - 1] : 0, at); };
-    if (tail + id < n) look_at(tail + id);
+    if (id < n - tail) look_at(tail + id);             // (tail + id may pass 2^31)
     const int4* vec = reinterpret_cast<const int4*>(T + lead);
     constexpr int U = 8;                               // vectors of four tokens in flight
     for (int v0 = n_vec - 1 - id; v0 + lane >= 0; v0 -= U * lanes) {       // (the same for a warp's lanes)
@@ -109,8 +109,9 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) draft_lookup_kernel(const Look
   key = s_keys[0];
   for (int k = 1; k < ctas; ++k) key = max(key, s_keys[k]);
   const int e = (int)(uint32_t)key;
-  for (int i = tid; i < p.num_drafts; i += LOOKUP_THREADS)
-    p.drafts[(size_t)s * p.num_drafts + i] = key ? T[e + i % (len - e)] : -1;
+  const unsigned period = max(1, len - e);             // (len - e >= 1 where there is a key)
+  for (unsigned i = tid; i < (unsigned)p.num_drafts; i += LOOKUP_THREADS)
+    p.drafts[(size_t)s * p.num_drafts + i] = key ? T[e + (int)(i % period)] : -1;
   if (tid == 0) p.draft_len[s] = key ? p.num_drafts : 0;
 }
 

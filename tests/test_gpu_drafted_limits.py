@@ -62,3 +62,38 @@ def test_races_that_others_raise(dense, vocab):
         torch.cuda.synchronize()
         for x, y in zip(want, (step.accepted, step.next, step.out, step.logs)):
             assert torch.equal(x, y)
+
+
+def _look(history, num_drafts, length=None, lo=1, hi=4):
+    drafts = torch.full((1, num_drafts), -9, dtype=torch.int32, device="cuda")
+    n = torch.full((1,), -9, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    length = torch.tensor([history.shape[1] if length is None else length], dtype=torch.int32, device="cuda")
+    efim.efim_draft_lookup(history, length, lo, hi, drafts, n, status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    return drafts, int(n.item())
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+def test_the_longest_history(offset):
+    """2^31 - 1 tokens, aligned and not; the place to be found is one of the first, or the last of all."""
+    size = (1 << 31) - 1
+    buf = torch.zeros(size + offset, dtype=torch.int32, device="cuda")
+    history = buf[offset:].view(1, size)
+    history[0, 3], history[0, 4], history[0, size - 1] = 5, 9, 5
+    drafts, n = _look(history, 4)
+    assert n == 4 and drafts.tolist() == [[9, 0, 0, 0]]
+    for back in (2, 3, 4):                              # of one to three tokens behind the last vector
+        history[0, size - back] = 5
+        drafts, n = _look(history, 4, hi=1)
+        assert n == 4 and drafts.tolist() == [(([0] * (back - 2) + [5]) * 4)[:4]]
+        history[0, size - back] = 0
+
+
+def test_the_most_drafts():
+    history = torch.tensor([[7, 8, 8, 8]], dtype=torch.int32, device="cuda")
+    drafts, n = _look(history, (1 << 31) - 1)
+    assert n == (1 << 31) - 1 and bool((drafts == 8).all())
+    drafts, n = _look(history, (1 << 31) - 1, length=1)
+    assert n == 0 and bool((drafts == -1).all())
