@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 4) verify_pick_kernel(const Ve
   if (!waited) pdl_wait();
   pdl_launch();
   if (first) {
-    for (int i = tid; i < p.out_stride; i += VERIFY_THREADS) {
+    for (long long i = tid; i < p.out_stride; i += VERIFY_THREADS) {
       if (i < stop) {
         if (out_tokens) out_tokens[i] = *(p.tokens + r0 + i + 1);
       } else if (i > max(stop, 0)) {

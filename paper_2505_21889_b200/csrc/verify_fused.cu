@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, PER_SM) verify_fused_kernel(con
     if (status && p.status) atomicOr(p.status, status);
   }
   if (rank == 0) {
-    for (int i = tid; i < p.out_stride; i += FUSED_THREADS) {
+    for (long long i = tid; i < p.out_stride; i += FUSED_THREADS) {
       if (i < stop) {
         if (out_tokens) out_tokens[i] = *(p.tokens + r0 + i + 1);
       } else if (i > acc) {

@@ -97,3 +97,16 @@ def test_the_most_drafts():
     assert n == (1 << 31) - 1 and bool((drafts == 8).all())
     drafts, n = _look(history, (1 << 31) - 1, length=1)
     assert n == 0 and bool((drafts == -1).all())
+
+
+@pytest.mark.parametrize("vocab", [2000, 70000])
+def test_the_longest_output(vocab):
+    """2^31 - 1 places for what a sequence goes on with, in both forms."""
+    step = Step([3], vocab, "bf16", False, seed=47).run()
+    width = (1 << 31) - 1
+    out = torch.full((1, width), -9, dtype=torch.int32, device="cuda")
+    step.args.update(out_tokens=out, out_logprobs=None)
+    step.again()
+    torch.cuda.synchronize()
+    n = int(step.accepted[0]) + 1
+    assert out[0, :n].tolist() == step.out[0, :n].tolist() and bool((out[0, n:] == -1).all())
