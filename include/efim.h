@@ -355,7 +355,7 @@ efim_status efim_draft_lookup(int32_t batch, const int32_t* d_history, int64_t h
  * Results: d_accepted[s] drafts, d_next_token[s]; optionally out_stride entries a sequence of the tokens it goes on with (accepted drafts,
  * next, then -1) and their natural log-probabilities in p (at temperature 1 where greedy; 0 past the end).  A
  * sequence without rows accepts 0 and gets next -1.  The k/v of a sequence's first d_accepted[s] + 1 new tokens stay valid;
- * the next step's tokens overwrite the rest.  May be captured; the same inputs give the same bits.  vocab is at most 2^30.
+ * the next step's tokens overwrite the rest.  May be captured; the same inputs give the same bits.  vocab and total_rows are at most 2^30.
  * Rows of up to 64 KB, with few sequences: one kernel without a workspace (efim_verify_workspace_bytes() is 0, d_workspace may be NULL);
  * else two.  Workspace: 256-byte aligned, exclusively this call's until the stream has passed it; its bytes serve every call of the same
  * target_kind with no more sequences, rows and places.

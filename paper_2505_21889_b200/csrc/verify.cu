@@ -25,7 +25,7 @@ namespace efim {
 
 constexpr int VERIFY_THREADS = 256;
 constexpr int VERIFY_WARPS = VERIFY_THREADS / 32;
-constexpr int VERIFY_MOST_VOCAB = 1 << 30;              // places, and those a piece or a step further on, are counted in 32 bits
+constexpr int VERIFY_MOST = 1 << 30;                    // places, rows, and those a piece or a step further on, are counted in 32 bits
 
 // A thread's share of a piece of a row: up to MASS_VECTORS vectors of 16 bytes, a CTA's threads apart, and one value before and behind
 // the vectors of a piece that is not aligned.  All of it is on its way before anything is computed.
@@ -405,7 +405,7 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
                                           size_t workspace_bytes, int32_t* d_status, void* stream) {
   using namespace efim;
   if (!d || d->batch < 0 || d->total_rows < 0 || d->vocab <= 0) return EFIM_ERR_INVALID_ARG;
-  if (d->vocab > VERIFY_MOST_VOCAB) return EFIM_ERR_UNSUPPORTED;
+  if (d->vocab > VERIFY_MOST || d->total_rows > VERIFY_MOST) return EFIM_ERR_UNSUPPORTED;
   if (d->target_kind < EFIM_TARGET_LOGITS_BF16 || d->target_kind > EFIM_TARGET_PROBS_F32) return EFIM_ERR_INVALID_ARG;
   if (d->batch == 0) return EFIM_OK;
   if (!d->d_row_indptr || !d_accepted || !d_next_token) return EFIM_ERR_INVALID_ARG;

@@ -1,0 +1,31 @@
+"""Sizes and arguments at the ends of what the calls of a drafted step take, on the host and before any launch (the addresses are
+never used)."""
+import ctypes
+
+import pytest
+
+import paper_2505_21889_b200 as efim
+from paper_2505_21889_b200 import binding as B
+from paper_2505_21889_b200 import build as efim_build
+
+UNSUPPORTED = 2
+
+
+@pytest.fixture(scope="module")
+def lib():
+    efim_build.build()
+    return efim.load_library()
+
+
+def _verify(lib, **changed):
+    fields = dict(batch=2, total_rows=6, vocab=1000, target_kind=0, d_row_indptr=0x3000, d_tokens=0x4000, d_target=0x5002,
+                  target_stride=1001, d_draft_probs=0x6004, draft_stride=1000, d_uniform=0x7000, d_noise=0x8000, noise_stride=1000,
+                  d_temperature=0x9000)
+    desc = B._VerifyDesc(**{**fields, **changed})
+    size = lib.efim_verify_workspace_bytes(desc.batch, desc.total_rows, desc.vocab, desc.target_kind)
+    return lib.efim_verify_drafts(ctypes.byref(desc), 0x1000, 0x2000, None, None, 0, 0x100000, size, None, None)
+
+
+def test_rows_are_counted_in_32_bits(lib):
+    assert _verify(lib, total_rows=(1 << 30) + 1) == _verify(lib, total_rows=(1 << 31) - 1) == UNSUPPORTED
+    assert _verify(lib, total_rows=(1 << 31) - 1, batch=1000, vocab=8, target_stride=8) == UNSUPPORTED
