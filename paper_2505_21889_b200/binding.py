@@ -236,6 +236,7 @@ class Cache:
         assert k_pool.shape == v_pool.shape and k_pool.is_contiguous() and v_pool.is_contiguous()
         self.k_pool, self.v_pool = k_pool, v_pool
         n, hkv, p, d = k_pool.shape
+        self.head_dim = d
         self.desc = _CacheDesc(k_pool.data_ptr(), v_pool.data_ptr(), n, p, num_q_heads, hkv, d)
 
 
@@ -269,6 +270,7 @@ class Rope:
         import torch
         host = efim_rope_table_build(base, head_dim, max_position)
         self.table = torch.from_numpy(host).to(device)
+        self.head_dim = head_dim
         self.desc = _RopeDesc(self.table.data_ptr(), max_position, 1 if interleaved else 0)
 
     @classmethod
@@ -277,9 +279,18 @@ class Rope:
         _check(table.dtype == _torch().float32 and table.dim() == 2 and table.is_contiguous(),
                "the rotary table is a contiguous fp32 matrix")
         rope = cls.__new__(cls)
-        rope.table = table
+        rope.table, rope.head_dim = table, table.shape[1]
         rope.desc = _RopeDesc(table.data_ptr(), table.shape[0], 1 if interleaved else 0)
         return rope
+
+
+def _rope_addr(cache, rope):
+    """The kernels know a table's rows but not its width."""
+    if rope is None:
+        return None
+    if rope.head_dim != cache.head_dim:
+        raise ValueError(f"the rotary table is for heads of {rope.head_dim}, the cache's have {cache.head_dim}")
+    return _addr(rope.desc)
 
 
 class QkNorm:
@@ -305,7 +316,7 @@ def efim_rope_table_build(base, head_dim, max_position) -> np.ndarray:
 
 
 def efim_kv_append(cache: Cache, batch: Batch, rope, q, k_new, v_new, status=None, stream=None):
-    st = _calls.kv_append(_addr(cache.desc), _addr(batch.desc), _addr(rope.desc) if rope is not None else None,
+    st = _calls.kv_append(_addr(cache.desc), _addr(batch.desc), _rope_addr(cache, rope),
                           q, k_new, v_new, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_kv_append")
@@ -315,7 +326,7 @@ def efim_qk_norm_append(cache: Cache, batch: Batch, norm: QkNorm, rope, q, k, v,
     """efim_kv_append with a norm of every q and k head before the rotation.  q, k and v: bf16, one row per new token (of any rank
     past the first, packed), views of one buffer allowed; q_out: packed.  q and q_out may both be None."""
     st = _calls.qk_norm_append(_addr(cache.desc), _addr(batch.desc), _addr(norm.desc), norm.head_dim,
-                               _addr(rope.desc) if rope is not None else None, q, k, v, q_out, status, _stream_ptr(stream))
+                               _rope_addr(cache, rope), q, k, v, q_out, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_qk_norm_append")
 
@@ -380,7 +391,7 @@ def efim_append_prefill_step(cache: Cache, batch: Batch, rope, q, k_new, v_new, 
     """kv_append of the new tokens' k/v, then append-prefill attention of q rotated by its positions.  q is not modified, unless
     out is q (which is allowed): the append may leave the rotated queries in out, where their outputs go afterwards.  A call that
     is refused has changed nothing."""
-    st = _calls.append_prefill_step(_addr(cache.desc), _addr(batch.desc), _addr(rope.desc) if rope is not None else None,
+    st = _calls.append_prefill_step(_addr(cache.desc), _addr(batch.desc), _rope_addr(cache, rope),
                                     q, k_new, v_new, out, lse, sm_scale, plan, 1 if lists_resident else 0, workspace,
                                     status, _stream_ptr(stream))
     if st != 0:
@@ -490,7 +501,7 @@ def efim_decode_step(cache: Cache, batch: int, d_ctx_len, max_ctx_len, d_block_t
                      lse=None, sm_scale=0.0, workspace=None, status=None, stream=None):
     """kv_append of one token per row and decode attention in one launch (q is not modified)."""
     st = _calls.decode_step(_addr(cache.desc), batch, d_ctx_len, int(max_ctx_len), d_block_table, d_block_table.shape[1],
-                            _addr(rope.desc) if rope is not None else None, q, k_new, v_new, out, lse, sm_scale,
+                            _rope_addr(cache, rope), q, k_new, v_new, out, lse, sm_scale,
                             workspace, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_decode_step")

@@ -29,3 +29,26 @@ def _verify(lib, **changed):
 def test_rows_are_counted_in_32_bits(lib):
     assert _verify(lib, total_rows=(1 << 30) + 1) == _verify(lib, total_rows=(1 << 31) - 1) == UNSUPPORTED
     assert _verify(lib, total_rows=(1 << 31) - 1, batch=1000, vocab=8, target_stride=8) == UNSUPPORTED
+
+
+def test_rotary_tables_of_another_width(lib):
+    """A table's rows are head_dim apart: one of another width would be read at other rows, and past its end."""
+    torch = pytest.importorskip("torch")
+    half, whole = torch.bfloat16, torch.int32
+    cache = efim.Cache(torch.zeros(4, 1, 16, 128, dtype=half), torch.zeros(4, 1, 16, 128, dtype=half), 2)
+    batch = efim.Batch([0], [4], torch.zeros(1, 4, dtype=whole), device="cpu")
+    q, k = torch.zeros(4, 2, 128, dtype=half), torch.zeros(4, 1, 128, dtype=half)
+    one = torch.ones(1, dtype=whole)
+    for rope in (efim.Rope.from_table(torch.zeros(64, 64)), efim.Rope.from_table(torch.zeros(64, 256)),
+                 efim.Rope(10000.0, 64, 64, False, "cpu")):
+        for call in (lambda: efim.efim_qk_norm_append(cache, batch, efim.QkNorm(None, None), rope, q, k, k, q.clone(), stream=0),
+                     lambda: efim.efim_kv_append(cache, batch, rope, q, k, k, stream=0),
+                     lambda: efim.efim_append_prefill_step(cache, batch, rope, q, k, k, q.clone(), stream=0),
+                     lambda: efim.efim_decode_step(cache, 1, one, 4, batch.d_block_table, rope, q[:1], k[:1], k[:1], q[:1].clone(),
+                                                   stream=0)):
+            with pytest.raises(ValueError, match="rotary"):
+                call()
+    # a table that fits goes on to the launch, which needs a GPU, or to the next refusal
+    fits = efim.Rope.from_table(torch.zeros(64, 128))
+    with pytest.raises(efim.EfimError):
+        efim.efim_append_prefill_step(cache, batch, fits, q, k, k, q.clone(), stream=0)
