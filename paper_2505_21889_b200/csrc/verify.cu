@@ -428,7 +428,7 @@ extern "C" efim_status efim_verify_drafts(const efim_verify_desc* d, int32_t* d_
   p.tokens = d->d_tokens;
   p.draft_probs = d->d_draft_probs;
   p.uniform = d->d_uniform;
-  p.noise = d->d_noise;
+  p.noise = d->total_rows > 0 ? d->d_noise : nullptr;   // (without rows nothing of it was checked, and nothing is read)
   p.temperature = d->d_temperature;
   p.accepted = d_accepted;
   p.next_token = d_next_token;

@@ -110,3 +110,25 @@ def test_the_longest_output(vocab):
     torch.cuda.synchronize()
     n = int(step.accepted[0]) + 1
     assert out[0, :n].tolist() == step.out[0, :n].tolist() and bool((out[0, n:] == -1).all())
+
+
+@pytest.mark.parametrize("vocab", [2000, 70000])
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_no_rows_at_all(kind, vocab):
+    """Nothing is read of a call without rows but the (empty) row ranges: not the random numbers, whose address and rows are not
+    looked at either."""
+    import ctypes
+    from paper_2505_21889_b200 import binding as B
+    indptr = torch.zeros(3, dtype=torch.int32, device="cuda")
+    accepted, following = torch.full((2, 2), -9, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    few = torch.ones(8, device="cuda")
+    lib = efim.load_library()
+    size = lib.efim_verify_workspace_bytes(2, 0, vocab, kind)
+    ws = torch.full((max(size, 1),), 255, dtype=torch.uint8, device="cuda")
+    desc = B._VerifyDesc(batch=2, total_rows=0, vocab=vocab, target_kind=kind, d_row_indptr=indptr.data_ptr(),
+                         d_noise=few.data_ptr() + 2, noise_stride=1 << 40)
+    assert lib.efim_verify_drafts(ctypes.byref(desc), accepted.data_ptr(), following.data_ptr(), None, None, 0,
+                                  ws.data_ptr() if size else None, size, status.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert accepted.tolist() == [0, 0] and following.tolist() == [-1, -1] and int(status.item()) == 0
