@@ -299,7 +299,7 @@ class QkNorm:
     def __init__(self, q_weight, k_weight, eps=1e-6, weight_offset=0.0):
         torch = _torch()
         given = [w for w in (q_weight, k_weight) if w is not None]
-        _check(all(w.dtype in (torch.bfloat16, torch.float32) and w.dim() == 1 and w.is_contiguous() for w in given)
+        _check(all(w.dtype in (torch.bfloat16, torch.float32) and w.dim() == 1 and w.numel() > 0 and w.is_contiguous() for w in given)
                and len({(w.dtype, w.shape) for w in given}) <= 1, "the norms' weights are two bf16 or two fp32 vectors of one length")
         self.q_weight, self.k_weight = q_weight, k_weight
         self.head_dim = given[0].shape[0] if given else 0         # 0: of any

@@ -52,3 +52,14 @@ def test_rotary_tables_of_another_width(lib):
     fits = efim.Rope.from_table(torch.zeros(64, 128))
     with pytest.raises(efim.EfimError):
         efim.efim_append_prefill_step(cache, batch, fits, q, k, k, q.clone(), stream=0)
+
+
+def test_norm_weights_of_no_values():
+    """None stands for weights of one; a vector without values does not, and is not read past its end."""
+    torch = pytest.importorskip("torch")
+    for dtype in (torch.bfloat16, torch.float32):
+        for empty in (torch.zeros(0, dtype=dtype), torch.zeros(128, dtype=dtype)[:0]):
+            with pytest.raises(ValueError):
+                efim.QkNorm(empty, empty)
+            with pytest.raises(ValueError):
+                efim.QkNorm(None, empty)
