@@ -213,8 +213,10 @@ static int as_vector(PyObject* o, PyObject* type, const char* what, int64_t n, v
   if (ok == 0) PyErr_Format(PyExc_ValueError, "%s: %lld packed values are expected", what, (long long)n);
   return ok > 0;
 }
-/* Rows of a tensor: their number, values (all dimensions but the first, packed) and the distance from one to the next.  None has none. */
-static int as_rows(PyObject* o, PyObject* type, const char* what, void** out, int64_t* rows, int64_t* row, int64_t* step) {
+/* Rows of a tensor: their number, values and the distance from one to the next.  None has none.  A row is all dimensions but the first,
+   packed, where it is HEADS; where it is a LINE it is the last, and any between are of size 1. */
+enum { HEADS, LINE };
+static int as_rows(PyObject* o, PyObject* type, const char* what, int form, void** out, int64_t* rows, int64_t* row, int64_t* step) {
   *out = NULL;
   *rows = *row = *step = 0;
   if (o == Py_None) return 1;
@@ -233,6 +235,7 @@ static int as_rows(PyObject* o, PyObject* type, const char* what, void** out, in
         *step = n > 1 ? s : *row; /* a single row may stand anywhere */
       } else {
         if (s != *row && n > 1) ok = 0;
+        if (form == LINE && n != 1 && d < PyTuple_GET_SIZE(shape) - 1) ok = 0;
         *row *= n;
       }
     }
@@ -253,9 +256,9 @@ static int expect(int64_t got, int64_t wanted, const char* what) {
   return 0;
 }
 /* rows of what is given, of a known shape */
-static int as_matrix(PyObject* o, PyObject* type, const char* what, int64_t rows, int64_t row, void** out, int64_t* step) {
+static int as_matrix(PyObject* o, PyObject* type, const char* what, int form, int64_t rows, int64_t row, void** out, int64_t* step) {
   int64_t n, m;
-  return as_rows(o, type, what, out, &n, &m, step) && (o == Py_None || (expect(n, rows, what) && expect(m, row, what)));
+  return as_rows(o, type, what, form, out, &n, &m, step) && (o == Py_None || (expect(n, rows, what) && expect(m, row, what)));
 }
 
 /* cache, batch, norm, head_dim of its weights (or 0), rope, q, k, v, q_out, status, stream */
@@ -268,9 +271,9 @@ static PyObject* qk_norm_append(PyObject* self, PyObject* const* a, Py_ssize_t n
   const efim_cache_desc* c = p[0];
   const int64_t rows = ((const efim_batch_desc*)p[1])->total_new_tokens, q = (int64_t)c->num_q_heads * c->head_dim,
                 kv = (int64_t)c->num_kv_heads * c->head_dim;
-  if ((weights && !expect(weights, c->head_dim, "the norm's weights, values")) || !as_matrix(a[5], bf16, "q", rows, q, &p[5], &qs) ||
-      !as_matrix(a[6], bf16, "k", rows, kv, &p[6], &ks) || !as_matrix(a[7], bf16, "v", rows, kv, &p[7], &vs) ||
-      !as_matrix(a[8], bf16, "q_out", rows, q, &p[8], &os) || (p[8] && !expect(os, q, "q_out, values from one row to the next")))
+  if ((weights && !expect(weights, c->head_dim, "the norm's weights, values")) || !as_matrix(a[5], bf16, "q", HEADS, rows, q, &p[5], &qs) ||
+      !as_matrix(a[6], bf16, "k", HEADS, rows, kv, &p[6], &ks) || !as_matrix(a[7], bf16, "v", HEADS, rows, kv, &p[7], &vs) ||
+      !as_matrix(a[8], bf16, "q_out", HEADS, rows, q, &p[8], &os) || (p[8] && !expect(os, q, "q_out, values from one row to the next")))
     return NULL;
   RETURN_STATUS(efim_qk_norm_append(p[0], p[1], p[2], p[4], p[5], qs, p[6], ks, p[7], vs, p[8], p[9], p[10]));
 }
@@ -281,8 +284,8 @@ static PyObject* draft_lookup(PyObject* self, PyObject* const* a, Py_ssize_t n) 
   int64_t batch, max_len, stride, rows, num, step;
   int32_t lo, hi;
   if (!want(n, 8) || !have_types()) return NULL;
-  if (!as_rows(a[0], i32, "history", &p[0], &batch, &max_len, &stride) || !as_vector(a[1], i32, "lengths", batch, &p[1]) ||
-      !as_i32(a[2], &lo) || !as_i32(a[3], &hi) || !as_rows(a[4], i32, "drafts", &p[4], &rows, &num, &step) ||
+  if (!as_rows(a[0], i32, "history", LINE, &p[0], &batch, &max_len, &stride) || !as_vector(a[1], i32, "lengths", batch, &p[1]) ||
+      !as_i32(a[2], &lo) || !as_i32(a[3], &hi) || !as_rows(a[4], i32, "drafts", HEADS, &p[4], &rows, &num, &step) ||
       !expect(rows, batch, "drafts, rows") || !expect(step, num, "drafts, values from one row to the next") ||
       !as_vector(a[5], i32, "draft_len", batch, &p[5]) || !as_typed(a[6], i32, "status", &p[6]) || !PTR(7))
     return NULL;
@@ -296,7 +299,7 @@ static PyObject* verify_workspace_bytes(PyObject* self, PyObject* const* a, Py_s
   int64_t rows, vocab, step;
   if (!want(n, 3) || !have_types() || !as_i32(a[0], &batch)) return NULL;
   const int probs = PyObject_IsTrue(a[2]), half = probs ? 0 : is_type(a[1], bf16);
-  if (probs < 0 || half < 0 || !as_rows(a[1], half ? bf16 : f32, "target", &p, &rows, &vocab, &step)) return NULL;
+  if (probs < 0 || half < 0 || !as_rows(a[1], half ? bf16 : f32, "target", LINE, &p, &rows, &vocab, &step)) return NULL;
   const int kind = probs ? EFIM_TARGET_PROBS_F32 : half ? EFIM_TARGET_LOGITS_BF16 : EFIM_TARGET_LOGITS_F32;
   return PyLong_FromSize_t(efim_verify_workspace_bytes(batch, (int32_t)rows, (int32_t)vocab, kind));
 }
@@ -323,14 +326,14 @@ static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n)
   const int probs = PyObject_IsTrue(a[4]), half = probs ? 0 : is_type(a[3], bf16);
   if (probs < 0 || half < 0) return NULL;
   if (!as_i32(a[0], &d.batch) || !as_vector(a[1], i32, "row_indptr", (int64_t)d.batch + 1, &p[1]) ||
-      !as_rows(a[3], half ? bf16 : f32, "target", &p[3], &rows, &vocab, &d.target_stride) ||
-      !as_vector(a[2], i32, "tokens", rows, &p[2]) || !as_matrix(a[5], f32, "draft_probs", rows, vocab, &p[5], &d.draft_stride) ||
-      !as_vector(a[6], f32, "uniform", rows, &p[6]) || !as_matrix(a[7], f32, "noise", d.batch, vocab, &p[7], &d.noise_stride) ||
+      !as_rows(a[3], half ? bf16 : f32, "target", LINE, &p[3], &rows, &vocab, &d.target_stride) ||
+      !as_vector(a[2], i32, "tokens", rows, &p[2]) || !as_matrix(a[5], f32, "draft_probs", LINE, rows, vocab, &p[5], &d.draft_stride) ||
+      !as_vector(a[6], f32, "uniform", rows, &p[6]) || !as_matrix(a[7], f32, "noise", LINE, d.batch, vocab, &p[7], &d.noise_stride) ||
       !as_vector(a[8], f32, "temperature", d.batch, &p[8]) || !as_vector(a[9], i32, "accepted", d.batch, &p[9]) ||
       !as_vector(a[10], i32, "next_token", d.batch, &p[10]) ||
-      !as_rows(a[11], i32, "out_tokens", &p[11], &out_rows, &width, &step) ||
+      !as_rows(a[11], i32, "out_tokens", HEADS, &p[11], &out_rows, &width, &step) ||
       (p[11] && (!expect(out_rows, d.batch, "out_tokens, rows") || !expect(step, width, "out_tokens, values from one row to the next"))) ||
-      !as_rows(a[12], f32, "out_logprobs", &p[12], &out_rows, &logs, &step) ||
+      !as_rows(a[12], f32, "out_logprobs", HEADS, &p[12], &out_rows, &logs, &step) ||
       (p[12] && (!expect(out_rows, d.batch, "out_logprobs, rows") || !expect(step, logs, "out_logprobs, values from one row to the next"))) ||
       (p[11] && p[12] && !expect(logs, width, "out_logprobs, values of a row")) || !as_workspace(a[13], &p[13], &ws) ||
       !as_typed(a[14], i32, "status", &p[14]) || !PTR(15))

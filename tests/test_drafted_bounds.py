@@ -63,3 +63,35 @@ def test_norm_weights_of_no_values():
                 efim.QkNorm(empty, empty)
             with pytest.raises(ValueError):
                 efim.QkNorm(None, empty)
+
+
+def test_rows_that_are_no_lines(lib):
+    """[batch, k + 1, vocab] is not [rows, vocab]: folded into rows of (k + 1) vocab it would be judged by wrong rows.  Dimensions of
+    size 1 between change nothing."""
+    torch = pytest.importorskip("torch")
+    whole = torch.int32
+    n = torch.zeros(2, dtype=whole)
+    tokens, indptr = torch.zeros(6, dtype=whole), torch.tensor([0, 3, 6], dtype=whole)
+    block = torch.zeros(2, 3, 40000)                                      # of a size that needs a workspace
+    rows, noise, small = block.view(6, 40000), torch.ones(2, 40000), torch.zeros(256, dtype=torch.uint8)
+
+    def verify(**changed):
+        efim.efim_verify_drafts(**{**dict(row_indptr=indptr, tokens=tokens, target=rows, accepted=n, next_token=n.clone(),
+                                          uniform=torch.zeros(6), noise=noise, workspace=small), **changed}, stream=0)
+    for changed in (dict(target=block, noise=None), dict(target=block, noise=torch.ones(2, 120000)), dict(noise=noise.view(2, 200, 200)),
+                    dict(draft_probs=rows.view(6, 2, 20000))):
+        with pytest.raises(ValueError):
+            verify(**changed)
+    with pytest.raises(ValueError):
+        efim.efim_verify_workspace_bytes(2, block)
+    assert efim.efim_verify_workspace_bytes(2, rows[:, None]) == efim.efim_verify_workspace_bytes(2, rows) > 0
+    for fits in (dict(), dict(target=rows[:, None], draft_probs=rows[:, None], noise=noise[:, None])):
+        with pytest.raises(efim.EfimError) as e:
+            verify(**fits)
+        assert e.value.code == 4                                          # the workspace is too small
+    drafts = torch.zeros(2, 3, dtype=whole)
+    with pytest.raises(ValueError):
+        efim.efim_draft_lookup(torch.zeros(2, 5, 8, dtype=whole), n, 1, 2, drafts, n.clone(), stream=0)
+    with pytest.raises(efim.EfimError) as e:                              # (no n-gram of 33)
+        efim.efim_draft_lookup(torch.zeros(2, 1, 8, dtype=whole), n, 1, 33, drafts, n.clone(), stream=0)
+    assert e.value.code == UNSUPPORTED
