@@ -41,6 +41,10 @@ static int as_ptr(PyObject* o, void** out) {
 static int as_i32(PyObject* o, int32_t* out) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) return 0;
+  if (v < INT32_MIN || v > INT32_MAX) {
+    PyErr_Format(PyExc_OverflowError, "%ld does not fit 32 bits", v);
+    return 0;
+  }
   *out = (int32_t)v;
   return 1;
 }

@@ -95,3 +95,22 @@ def test_rows_that_are_no_lines(lib):
     with pytest.raises(efim.EfimError) as e:                              # (no n-gram of 33)
         efim.efim_draft_lookup(torch.zeros(2, 1, 8, dtype=whole), n, 1, 33, drafts, n.clone(), stream=0)
     assert e.value.code == UNSUPPORTED
+
+
+def test_numbers_that_do_not_fit(lib):
+    """A number past 32 bits is an error, not its lowest bits."""
+    torch = pytest.importorskip("torch")
+    whole = torch.int32
+    history, n, drafts = torch.zeros(2, 8, dtype=whole), torch.zeros(2, dtype=whole), torch.zeros(2, 3, dtype=whole)
+    for lo, hi in (((1 << 32) + 1, 2), (1, (1 << 32) + 2), (1, 1 << 31), (-(1 << 31) - 1, 2), (1, 1 << 70)):
+        with pytest.raises(OverflowError):
+            efim.efim_draft_lookup(history, n, lo, hi, drafts, n.clone(), stream=0)
+    with pytest.raises(OverflowError):
+        efim.efim_verify_workspace_bytes((1 << 32) + 2, torch.zeros(6, 40000))
+    cache = efim.Cache(torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16), 2)
+    q = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(OverflowError):
+        efim.efim_decode_attn(cache, 1, n, (1 << 32) + 16, drafts, q, q.clone(), stream=0)
+    with pytest.raises(efim.EfimError) as e:                              # (the largest that fits; no n-gram of it)
+        efim.efim_draft_lookup(history, n, 1, (1 << 31) - 1, drafts, n.clone(), stream=0)
+    assert e.value.code == UNSUPPORTED
