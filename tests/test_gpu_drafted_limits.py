@@ -132,3 +132,27 @@ def test_no_rows_at_all(kind, vocab):
                                   ws.data_ptr() if size else None, size, status.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
     torch.cuda.synchronize()
     assert accepted.tolist() == [0, 0] and following.tolist() == [-1, -1] and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("vocab", [3000, 70000])
+@pytest.mark.parametrize("operand", ["target", "draft_probs", "noise"])
+def test_rows_far_apart(operand, vocab):
+    """2^30 elements from one row to the next, so that the third is past 2^31 of them, for one operand at a time: the same bits as
+    packed."""
+    step = Step([3, 1, 2, 3], vocab, "bf16", True, seed=23).run()
+    assert int(step.accepted.sum()) >= 2
+    want = [t.clone() for t in (step.accepted, step.next, step.out, step.logs)]
+    rows = step.main[2] if operand == "target" else step.args[operand]
+    buf = torch.empty((len(rows) - 1 << 30) + vocab, dtype=rows.dtype, device="cuda")
+    far = buf.as_strided(rows.shape, (1 << 30, 1))
+    far.copy_(rows)
+    if operand == "target":
+        step.main = step.main[:2] + (far,) + step.main[3:]
+    else:
+        step.args[operand] = far
+    for t in (step.accepted, step.next, step.out):
+        t.fill_(-5)
+    step.again()
+    torch.cuda.synchronize()
+    for x, y in zip(want, (step.accepted, step.next, step.out, step.logs)):
+        assert torch.equal(x, y)
