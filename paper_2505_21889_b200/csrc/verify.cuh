@@ -133,10 +133,12 @@ struct Row {
 
 // The race for the next token: the largest r / e, r = (p - q)^+ or p, the lowest place among equals.
 //
-// An exact result costs two divisions and an exponential.  So every place gets an estimate first, by the fast instructions (in a
-// probability: the exponent's rounding 150 * 2^-24 * ln 2, ex2 2^-22, the factor 2^-23: `scale` makes up for them; rcp and the last
-// product 2^-22 more: RACE_ABOVE does), and only places whose estimate, a little increased, reaches the best result known so far are
-// computed: a few a warp.  (Probabilities below 2^-126 are taken for 0 there.)
+// An exact result costs two divisions and an exponential.  So every place gets an estimate first, by the fast instructions, and only places
+// whose estimate, a little increased, reaches the best result known so far are computed: a few a warp.  What an estimate has to make up
+// for, in a probability of 2^-126 and more (smaller ones are taken for 0 here), whose exponents are below 128 and half an ulp of them at
+// most 2^-18: its own exponent's rounding, 2^-18, and those of the computed one's difference and product, 126 * 2^-24 + 2^-18, together
+// 254 * 2^-24 ln 2 = 1.05e-5; ex2 2^-22 in either and in the sum's reference, the exponential's and the division's few 2^-24: below 1.5e-6.
+// `scale` is 1.52e-5 more (before q is taken off); rcp and the last product are 2^-22, for which RACE_ABOVE comes in again.
 constexpr float RACE_ABOVE = 1.f + 1.f / 65536;
 template <int KIND>
 struct Race {

@@ -156,3 +156,28 @@ def test_rows_far_apart(operand, vocab):
     torch.cuda.synchronize()
     for x, y in zip(want, (step.accepted, step.next, step.out, step.logs)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [3000, 70000])
+def test_small_probabilities_that_are_left(vocab, kind):
+    """(p - q)+ leaves one place of a probability between 2^-124 and 2^-40, 2e-5 of which is more than its q.  An fp32 probability there is
+    within 1.1e-5 of p: two roundings of an exponent below 128 (126 * 2^-24 and 2^-18), times ln 2, and 1e-6 for the exponential, the
+    sum and the division."""
+    step = Step([2] * 40, vocab, kind, True, None, seed=53)
+    rng = np.random.default_rng(59)
+    step.target[:] = rng.uniform(-85.0, -28.0, step.target.shape)
+    step.target[:, [5, 9]] = 0.0
+    if kind == "bf16":
+        step.target = torch.from_numpy(step.target).bfloat16().float().numpy()
+    places = rng.integers(10, vocab, 40)
+    for s, j in enumerate(places):
+        p = np.exp(step.target[2 * s].astype(np.float64))
+        p /= p.sum()
+        step.q[2 * s] = 1.01 * p
+        step.q[2 * s, j] = p[j] * (1 - 2e-5)
+        step.q[2 * s, 5], step.q[2 * s, 9] = 1.0, 0.6
+        step.tokens[2 * s + 1], step.uniform[2 * s] = 5, 0.999
+    step.run()
+    assert int(step.status.item()) == 0 and step.accepted.tolist() == [0] * 40
+    assert step.next.tolist() == places.tolist()
