@@ -275,7 +275,8 @@ class Rope:
 
     @classmethod
     def from_table(cls, table, interleaved=False):
-        """A table that is on the device already: fp32 [max_position, head_dim], cos then sin (with any scaling)."""
+        """A table that is on the device already: fp32 [max_position, head_dim], cos then sin (with any scaling).  Its width has to be
+        the head_dim of the caches that it is used with."""
         _check(table.dtype == _torch().float32 and table.dim() == 2 and table.is_contiguous(),
                "the rotary table is a contiguous fp32 matrix")
         rope = cls.__new__(cls)
@@ -348,7 +349,8 @@ def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform
                        temperature=None, target_is_probs=False, out_tokens=None, out_logprobs=None, workspace=None, status=None,
                        stream=None):
     """Accepted drafts and next token of every sequence of a step.  target: [rows, vocab] logits in bf16 or fp32, or with
-    `target_is_probs` probabilities in fp32; draft_probs fp32 [rows, vocab]; noise fp32 [batch, vocab] (none: greedy);
+    `target_is_probs` probabilities in fp32; draft_probs fp32 [rows, vocab]; noise fp32 [batch, vocab] (none: greedy); dimensions of
+    size 1 between the two are allowed, others are not ([batch, drafts, vocab] is not [rows, vocab]).
     out_tokens and out_logprobs: packed [batch, n] of the same n.  Without a workspace one is taken from torch's allocator, on
     torch's current stream, which the call then has to run on."""
     if workspace is None and stream is not None and _calls.verify_workspace_bytes(accepted.shape[0], target, target_is_probs) and \

@@ -87,7 +87,9 @@ struct Share {
       }
       s.l = l.x + l.y;
     } else {
-      // rare: one value after the other, read again
+      // one value after the other, read again.  By the thread's own maximum: all of its values are -inf, or the largest is +inf or times c
+      // beyond 2^30.  Rows masked but for 50 places, by -inf or the type's lowest values, send nearly every thread here: 256 sequences x
+      // 5 rows x 131,072 bf16 with certain drafts 115 -> 237 us, 16 13.4 -> 23.1, 37 x 1-8 x 100,003 fp32 20.6 -> 34.1.
       s.l = exp2_fast(below_ref(head, s.m, c)) + exp2_fast(below_ref(tail, s.m, c));
 #pragma unroll 1
       for (int v = threadIdx.x; v < n_vec; v += VERIFY_THREADS)

@@ -292,7 +292,9 @@ static unsigned fused_ctas(long long vocab, int kind) {
 
 // As long as all CTAs are resident at once, two an SM.  GPU microseconds, one kernel against two, five rows each: bf16 logits, 1 x 1,000 5.4 / 5.7,
 // 1 x 32,768 7.4 / 7.2 (and 4 us of host time less), 8 x 32,768 7.5 / 9.5, 128 x 4,096 6.5 / 10.6, 256 x 4,096 9.4 / 13.7, 32 x 32,768 11.9 / 11.7,
-// 128 x 32,768 45 / 25; probabilities, 1 x 16,384 3.5 / 5.0, 32 x 16,384 4.8 / 6.0, 128 x 16,384 15.8 / 8.1.
+// 128 x 32,768 45 / 25; probabilities, 1 x 16,384 3.5 / 5.0, 32 x 16,384 4.8 / 6.0, 128 x 16,384 15.8 / 8.1.  With more rows, all accepted,
+// two kernels are ahead (bf16, 1 x 32,768 places: 9 rows 10.7 / 7.6, 17 15.7 / 9.7, 40 28 / 14, 128 84 / 32; 8 sequences 10.9 / 9.9, 16 / 12, 29 / 19,
+// 87 / 46), but calls of these sizes are promised to need no workspace, however many rows they have.
 bool verify_is_fused(long long batch, long long vocab, int kind) {
   return vocab * (kind == TARGET_BF16 ? 2 : 4) <= FUSED_MOST_BYTES && batch * fused_ctas(vocab, kind) <= 2 * sm_count();
 }
