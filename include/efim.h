@@ -385,6 +385,68 @@ efim_status efim_verify_drafts(const efim_verify_desc* desc, int32_t* d_accepted
                                void* d_workspace, size_t workspace_bytes, int32_t* d_status, void* stream);
 
 /*
+ * A KV cache held in 4 bits (the paper has no counterpart: more users' prefixes and suffixes stay in memory, and a decode step reads 3.6
+ * times fewer bytes).  Sixteen neighbouring values x of one token's head are held as sixteen 4-bit floats (e2m1: 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives) and one 8-bit scale (e4m3), 4.5 bits a value; with g the pool's scale (k_scale, v_scale)
+ *   s = e4m3(max |x| / (6 g)), at least 2^-9, at most 448;    c = e2m1(x / (s g));    held: c s g
+ * both rounded to nearest, ties to even; what is beyond the largest is held as the largest, infinities too; a NaN makes its sixteen
+ * values NaN.  g is a power of two from 2^-60 to 2^60, so that what is held is a bf16 number.
+ * Codes: dim 2i in the low four bits of byte i of a head's row, dim 2i + 1 in the high ones.  Pools 128-byte aligned; page_size 16,
+ * head_dim 64 or 128, block tables as for the bf16 cache.
+ */
+typedef struct {
+  void* d_k_codes;           /* [num_pages][num_kv_heads][page_size][head_dim / 2] bytes  */
+  void* d_v_codes;
+  void* d_k_scales;          /* [num_pages][num_kv_heads][page_size][head_dim / 16] bytes */
+  void* d_v_scales;
+  int32_t num_pages;
+  int32_t page_size;         /* 16 */
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  float k_scale, v_scale;
+} efim_cache4_desc;
+
+/*
+ * Step 1 over a 4-bit cache: q and k normalised if `norm` is not NULL (as efim_qk_norm_append does it), rotated by their positions if
+ * `rope` holds a table, rounded to bf16; q goes to d_q_out, k and v to their blocks.  Operands, strides, d_q_out (packed, d_q itself
+ * where that is packed, too) and errors as for efim_qk_norm_append.  total_new_tokens may be more than the device's q_indptr[batch]: the
+ * rows behind the last sequence's are left as they were.  One kernel; no workspace; may be captured.
+ */
+efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim_batch_desc* batch, const efim_qk_norm_desc* norm,
+                            const efim_rope_desc* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                            const void* d_v, int64_t v_stride, void* d_q_out, int32_t* d_status, void* stream);
+
+/*
+ * Pages of a 4-bit cache as bf16: page d_pages[i] to place i of d_k_out and d_v_out, [num][num_kv_heads][page_size][head_dim] (either may
+ * be NULL), exactly.  A page outside the pool sets EFIM_DEV_BAD_PAGE and leaves its place as it was.  The results must not overlap the pools.
+ */
+efim_status efim_kv4_unpack(const efim_cache4_desc* cache, const int32_t* d_pages, int32_t num, void* d_k_out, void* d_v_out,
+                            int32_t* d_status, void* stream);
+
+/*
+ * Steps 2 and 3 over a 4-bit cache for one or a few new tokens a sequence (a generated token, a pending token and its drafts),
+ * already appended; no host copy of any length is needed.  Sequence s has the q rows d_q_indptr[s] .. d_q_indptr[s+1]-1 (with d_q_indptr
+ * NULL row s alone: total_rows = batch, max_new_len = 1), n_s of them, and ctx_len[s] keys, theirs included; row i of it sees keys
+ * j < ctx_len[s] - n_s + i + 1:
+ *   out[t,h,:] = sum_j softmax_j(sm_scale * q[t,h,:].k[j,h/G,:]) v[j,h/G,:],   lse as for efim_append_prefill_attn
+ * on what the cache holds; queries are taken exactly, probabilities with 11 bits, everything else is fp32, the output bf16.
+ * sm_scale <= 0 selects 1/sqrt(head_dim).  max_ctx_len (<= 0: the table's capacity) and max_new_len bound the lengths and fix the plan; total_rows is
+ * how many rows d_q and d_out have.  What is beyond these bounds sets EFIM_DEV_BAD_POSITION: keys beyond are not seen, rows beyond
+ * are not computed.  Rows without keys get 0 and lse -inf; rows behind the last sequence's are left as they were.  Keys of a page outside the
+ * pool count as absent and set EFIM_DEV_BAD_PAGE.  A query row with an infinity or a NaN gives NaN; so does a value that is NaN, in its
+ * sixteen places, to the rows that see it, and to no others.
+ * d_out may be d_q, and overlaps nothing else that is read.  Workspace: 256-byte aligned, efim_kv4_decode_workspace_bytes() for exactly these arguments (0: none needed),
+ * exclusively this call's until the stream has passed it.  One kernel, two where the keys are split; may be captured; the same inputs
+ * give the same bits.
+ */
+size_t efim_kv4_decode_workspace_bytes(const efim_cache4_desc* cache, int32_t batch, int32_t max_new_len, int32_t max_ctx_len);
+efim_status efim_kv4_decode_attn(const efim_cache4_desc* cache, int32_t batch, const int32_t* d_ctx_len, int32_t max_ctx_len,
+                                 const int32_t* d_block_table, int32_t max_pages_per_seq, const int32_t* d_q_indptr, int32_t total_rows,
+                                 int32_t max_new_len, const void* d_q, void* d_out, float* d_lse, float sm_scale, void* d_workspace,
+                                 size_t workspace_bytes, int32_t* d_status, void* stream);
+
+/*
  * Self-test of the bounded device wait (the paper has no counterpart).  Every wait inside
  * the kernels - on a bulk copy, on a tensor-core commit - gives up after a limit, sets
  * EFIM_DEV_TIMEOUT in *d_status and lets the kernel end normally.  This call runs that code

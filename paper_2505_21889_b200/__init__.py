@@ -10,5 +10,6 @@ from .binding import (  # noqa: F401
     efim_strerror, efim_version, efim_decode_attn_static, efim_decode_static_scratch_bytes,
     efim_prefill_launch_count, efim_decode_launch_count, Frontend, efim_prefill_plan, efim_decode_step,
     efim_append_prefill_step, efim_selftest_bounded_wait, QkNorm, efim_qk_norm_append, efim_draft_lookup,
-    efim_verify_workspace_bytes, efim_verify_drafts,
+    efim_verify_workspace_bytes, efim_verify_drafts, Cache4, efim_kv4_append, efim_kv4_unpack, efim_kv4_decode_workspace_bytes,
+    efim_kv4_decode_attn,
 )

@@ -42,6 +42,12 @@ class _QkNormDesc(Structure):
                 ("weight_offset", c_float)]
 
 
+class _Cache4Desc(Structure):
+    _fields_ = [("d_k_codes", c_void_p), ("d_v_codes", c_void_p), ("d_k_scales", c_void_p), ("d_v_scales", c_void_p),
+                ("num_pages", c_int32), ("page_size", c_int32), ("num_q_heads", c_int32), ("num_kv_heads", c_int32),
+                ("head_dim", c_int32), ("k_scale", c_float), ("v_scale", c_float)]
+
+
 class _VerifyDesc(Structure):
     _fields_ = [("batch", c_int32), ("total_rows", c_int32), ("vocab", c_int32), ("target_kind", c_int32),
                 ("d_row_indptr", c_void_p), ("d_tokens", c_void_p), ("d_target", c_void_p), ("target_stride", c_int64),
@@ -57,6 +63,7 @@ EXPORTS = ("efim_last_cuda_error", "efim_strerror", "efim_version", "efim_rope_t
            "efim_prefill_plan_bytes", "efim_prefill_plan", "efim_append_prefill_attn_planned", "efim_decode_step",
            "efim_append_prefill_step", "efim_selftest_bounded_wait",
            "efim_qk_norm_append", "efim_draft_lookup", "efim_verify_workspace_bytes", "efim_verify_drafts",
+           "efim_kv4_append", "efim_kv4_unpack", "efim_kv4_decode_workspace_bytes", "efim_kv4_decode_attn",
            "efim_fragment_cuts", "efim_fim_split", "efim_fim_fragment_spans",
            "efim_frontend_create", "efim_frontend_destroy", "efim_frontend_transform", "efim_frontend_admit",
            "efim_frontend_finish", "efim_frontend_stats")
@@ -113,6 +120,16 @@ def load_library():
                                        c_size_t, c_void_p, c_void_p]
     lib.efim_verify_workspace_bytes.restype = c_size_t
     lib.efim_verify_workspace_bytes.argtypes = [c_int32, c_int32, c_int32, c_int32]
+    lib.efim_kv4_append.restype = ctypes.c_int
+    lib.efim_kv4_append.argtypes = [POINTER(_Cache4Desc), POINTER(_BatchDesc), POINTER(_QkNormDesc), POINTER(_RopeDesc),
+                                    c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
+    lib.efim_kv4_unpack.restype = ctypes.c_int
+    lib.efim_kv4_unpack.argtypes = [POINTER(_Cache4Desc), c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.efim_kv4_decode_workspace_bytes.restype = c_size_t
+    lib.efim_kv4_decode_workspace_bytes.argtypes = [POINTER(_Cache4Desc), c_int32, c_int32, c_int32]
+    lib.efim_kv4_decode_attn.restype = ctypes.c_int
+    lib.efim_kv4_decode_attn.argtypes = [POINTER(_Cache4Desc), c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int32,
+                                         c_int32, c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_size_t, c_void_p, c_void_p]
     lib.efim_selftest_bounded_wait.restype = ctypes.c_int
     lib.efim_selftest_bounded_wait.argtypes = [ctypes.c_uint64, c_void_p, c_void_p, c_void_p]
     lib.efim_decode_workspace_bytes.restype = c_size_t
@@ -164,7 +181,8 @@ class _Calls:
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
         loader.exec_module(module)
         for m in ("kv_append", "append_prefill_attn", "append_prefill_step", "decode_attn", "decode_step",
-                  "qk_norm_append", "draft_lookup", "verify_workspace_bytes", "verify_drafts"):
+                  "qk_norm_append", "draft_lookup", "verify_workspace_bytes", "verify_drafts",
+                  "kv4_append", "kv4_unpack", "kv4_decode_attn"):
             setattr(self, m, getattr(module, m))          # found directly from now on
         return self.__dict__[name]
 
@@ -360,6 +378,60 @@ def efim_verify_drafts(row_indptr, tokens, target, accepted, next_token, uniform
                               accepted, next_token, out_tokens, out_logprobs, workspace, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_verify_drafts")
+
+
+class Cache4:
+    """KV cache of one layer in 4 bits: torch.uint8 CUDA tensors owned by the caller, codes [num_pages, num_kv_heads, 16, head_dim / 2] and
+    scales [num_pages, num_kv_heads, 16, head_dim / 16] of keys and of values; k_scale and v_scale, powers of two, say how large they
+    are: about the largest values over 2,688, or a little less where few are that large."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales, num_q_heads, k_scale=1.0, v_scale=1.0):
+        torch = _torch()
+        pools = (k_codes, v_codes, k_scales, v_scales)
+        _check(all(x.dtype == torch.uint8 and x.dim() == 4 and x.is_contiguous() for x in pools), "codes and scales are packed uint8 tensors")
+        n, hkv, page, half = k_codes.shape
+        _check(v_codes.shape == k_codes.shape and k_scales.shape == v_scales.shape == (n, hkv, page, half // 8),
+               "codes are [pages, kv heads, 16, head_dim / 2], scales [pages, kv heads, 16, head_dim / 16]")
+        _check(len({x.device for x in pools}) == 1, "codes and scales are on one device")
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = pools
+        self.head_dim = 2 * half
+        self.desc = _Cache4Desc(*(x.data_ptr() for x in pools), n, page, num_q_heads, hkv, 2 * half, k_scale, v_scale)
+
+    @classmethod
+    def empty(cls, num_pages, num_kv_heads, head_dim, num_q_heads, k_scale=1.0, v_scale=1.0, device="cuda"):
+        """A cache with pools of its own, all zeros."""
+        torch = _torch()
+        codes, scales = ((num_pages, num_kv_heads, 16, head_dim // n) for n in (2, 16))
+        return cls(*(torch.zeros(s, dtype=torch.uint8, device=device) for s in (codes, codes, scales, scales)), num_q_heads, k_scale, v_scale)
+
+
+def efim_kv4_append(cache: Cache4, batch: Batch, norm, rope, q, k, v, q_out, status=None, stream=None):
+    """Norm (a QkNorm, or None), rotation (a Rope, or None) and append to a 4-bit cache; operands as for efim_qk_norm_append."""
+    st = _calls.kv4_append(_addr(cache.desc), _addr(batch.desc), None if norm is None else _addr(norm.desc), 0 if norm is None else norm.head_dim,
+                           _rope_addr(cache, rope), q, k, v, q_out, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_kv4_append")
+
+
+def efim_kv4_unpack(cache: Cache4, pages, k_out, v_out, status=None, stream=None):
+    """The int32 `pages` of a 4-bit cache as bf16 pages [n, num_kv_heads, 16, head_dim]; k_out or v_out may be None."""
+    st = _calls.kv4_unpack(_addr(cache.desc), pages, k_out, v_out, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_kv4_unpack")
+
+
+def efim_kv4_decode_workspace_bytes(cache: Cache4, batch: int, max_new_len: int, max_ctx_len: int) -> int:
+    return int(load_library().efim_kv4_decode_workspace_bytes(ctypes.byref(cache.desc), batch, max_new_len, max_ctx_len))
+
+
+def efim_kv4_decode_attn(cache: Cache4, batch: int, d_ctx_len, max_ctx_len, d_block_table, q, out, lse=None, sm_scale=0.0, q_indptr=None,
+                         max_new_len=1, workspace=None, status=None, stream=None):
+    """Attention of the new tokens (one a sequence; with q_indptr up to max_new_len) over a 4-bit cache that holds them already.  ctx_len
+    counts all of a sequence's keys.  q and out: packed [rows, num_q_heads, head_dim]."""
+    st = _calls.kv4_decode_attn(_addr(cache.desc), batch, d_ctx_len, int(max_ctx_len), d_block_table, q_indptr, max_new_len, q, out, lse,
+                                sm_scale, workspace, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_kv4_decode_attn")
 
 
 def efim_prefill_workspace_bytes(cache: Cache, batch: Batch) -> int:

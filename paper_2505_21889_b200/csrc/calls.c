@@ -367,6 +367,67 @@ static PyObject* verify_drafts(PyObject* self, PyObject* const* a, Py_ssize_t n)
   return PyLong_FromLong(st);
 }
 
+/* ---- the 4-bit cache */
+/* cache, batch, norm or None, head_dim of its weights (or 0), rope, q, k, v, q_out, status, stream */
+static PyObject* kv4_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[11];
+  int32_t weights;
+  int64_t qs, ks, vs, os;
+  if (!want(n, 11) || !have_types()) return NULL;
+  if (!PTR(0) || !PTR(1) || !PTR(2) || !as_i32(a[3], &weights) || !PTR(4) || !as_typed(a[9], i32, "status", &p[9]) || !PTR(10)) return NULL;
+  const efim_cache4_desc* c = p[0];
+  const int64_t rows = ((const efim_batch_desc*)p[1])->total_new_tokens, q = (int64_t)c->num_q_heads * c->head_dim,
+                kv = (int64_t)c->num_kv_heads * c->head_dim;
+  if ((weights && !expect(weights, c->head_dim, "the norm's weights, values")) || !as_matrix(a[5], bf16, "q", HEADS, rows, q, &p[5], &qs) ||
+      !as_matrix(a[6], bf16, "k", HEADS, rows, kv, &p[6], &ks) || !as_matrix(a[7], bf16, "v", HEADS, rows, kv, &p[7], &vs) ||
+      !as_matrix(a[8], bf16, "q_out", HEADS, rows, q, &p[8], &os) || (p[8] && !expect(os, q, "q_out, values from one row to the next")))
+    return NULL;
+  RETURN_STATUS(efim_kv4_append(p[0], p[1], p[2], p[4], p[5], qs, p[6], ks, p[7], vs, p[8], p[9], p[10]));
+}
+
+/* cache, pages, k_out, v_out, status, stream */
+static PyObject* kv4_unpack(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[6];
+  int64_t rows[2], row, step;
+  if (!want(n, 6) || !have_types() || !PTR(0) || !as_typed(a[4], i32, "status", &p[4]) || !PTR(5)) return NULL;
+  const efim_cache4_desc* c = p[0];
+  const int64_t page = (int64_t)c->num_kv_heads * c->page_size * c->head_dim;
+  for (int i = 0; i < 2; ++i)
+    if (!as_rows(a[2 + i], bf16, i ? "v_out" : "k_out", HEADS, &p[2 + i], &rows[i], &row, &step) ||
+        (p[2 + i] && (!expect(row, page, "a page's values") || !expect(step, page, "values from one page to the next"))))
+      return NULL;
+  if (p[2] && p[3] && !expect(rows[1], rows[0], "v_out, pages")) return NULL;
+  const int64_t num = p[2] ? rows[0] : rows[1];
+  if (!as_vector(a[1], i32, "pages", num, &p[1])) return NULL;
+  RETURN_STATUS(efim_kv4_unpack(p[0], p[1], (int32_t)num, p[2], p[3], p[4], p[5]));
+}
+
+/* cache, batch, ctx_len, max_ctx_len, block_table, q_indptr or None, max_new_len, q, out, lse, sm_scale, workspace, status, stream */
+static PyObject* kv4_decode_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[14];
+  int32_t batch, max_ctx, max_new;
+  int64_t rows, row, width, step;
+  float scale;
+  size_t ws;
+  if (!want(n, 14) || !have_types()) return NULL;
+  if (!PTR(0) || !as_i32(a[1], &batch) || !as_vector(a[2], i32, "ctx_len", batch, &p[2]) || !as_i32(a[3], &max_ctx) ||
+      !as_rows(a[4], i32, "block_table", LINE, &p[4], &rows, &width, &step) || !expect(rows, batch, "block_table, rows") ||
+      !expect(step, width, "block_table, values from one row to the next"))
+    return NULL;
+  const efim_cache4_desc* c = p[0];
+  row = (int64_t)c->num_q_heads * c->head_dim;
+  int64_t given, values;
+  if ((a[5] == Py_None ? (p[5] = NULL, 0) : !as_vector(a[5], i32, "q_indptr", (int64_t)batch + 1, &p[5])) || !as_i32(a[6], &max_new) ||
+      !as_rows(a[7], bf16, "q", HEADS, &p[7], &given, &values, &step) || !expect(values, row, "q, values of a row") ||
+      !expect(step, row, "q, values from one row to the next") || !as_matrix(a[8], bf16, "out", HEADS, given, row, &p[8], &step) ||
+      !expect(step, row, "out, values from one row to the next") ||
+      (a[9] == Py_None ? (p[9] = NULL, 0) : !as_vector(a[9], f32, "lse", given * c->num_q_heads, &p[9])) || !as_float(a[10], &scale) ||
+      !as_workspace(a[11], &p[11], &ws) || !as_typed(a[12], i32, "status", &p[12]) || !PTR(13))
+    return NULL;
+  RETURN_STATUS(efim_kv4_decode_attn(p[0], batch, p[2], max_ctx, p[4], (int32_t)width, p[5], (int32_t)given, max_new, p[7], p[8], p[9], scale,
+                                     p[11], ws, p[12], p[13]));
+}
+
 static PyMethodDef methods[] = {
     {"kv_append", (PyCFunction)(void*)kv_append, METH_FASTCALL, NULL},
     {"append_prefill_attn", (PyCFunction)(void*)append_prefill_attn, METH_FASTCALL, NULL},
@@ -377,6 +438,9 @@ static PyMethodDef methods[] = {
     {"draft_lookup", (PyCFunction)(void*)draft_lookup, METH_FASTCALL, NULL},
     {"verify_workspace_bytes", (PyCFunction)(void*)verify_workspace_bytes, METH_FASTCALL, NULL},
     {"verify_drafts", (PyCFunction)(void*)verify_drafts, METH_FASTCALL, NULL},
+    {"kv4_append", (PyCFunction)(void*)kv4_append, METH_FASTCALL, NULL},
+    {"kv4_unpack", (PyCFunction)(void*)kv4_unpack, METH_FASTCALL, NULL},
+    {"kv4_decode_attn", (PyCFunction)(void*)kv4_decode_attn, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

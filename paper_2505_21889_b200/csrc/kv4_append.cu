@@ -1,0 +1,389 @@
+// efim_kv4_append: the new tokens' q and k normalised (where the model does that) and rotated, k and v put into the pages of a 4-bit
+// cache; efim_kv4_unpack: pages of such a cache as bf16.
+#include "kv4.cuh"
+#include "token_place.cuh"
+#include <float.h>
+#include <algorithm>
+
+namespace efim {
+
+struct Kv4AppendParams {
+  const uint16_t* q;        // rows of [Hq][D], q_stride elements apart; may be null
+  const uint16_t* k;        // rows of [Hkv][D]
+  const uint16_t* v;
+  long long q_stride, k_stride, v_stride;
+  uint16_t* q_out;          // [T][Hq][D]
+  uint8_t *k_codes, *v_codes;       // [pages][Hkv][16][D/2]
+  uint8_t *k_scales, *v_scales;     // [pages][Hkv][16][D/16]
+  const void* q_weight;     // [D] bf16 or fp32, or null
+  const void* k_weight;
+  const int32_t* cached_len;
+  const int32_t* q_indptr;
+  const int32_t* block_table;
+  const float* cos_sin;     // [max_position][D] or null
+  int32_t* status;
+  float eps, weight_offset, k_inv, v_inv;   // the pools' scales, inverted
+  int batch, max_pages_per_seq, total_new_tokens;
+  int num_pages, Hq, Hkv, max_position, interleaved, weight_f32, normed;
+  int warps;                // of a token
+  int early_next;           // let the next kernel start its set-up while this one runs
+};
+
+constexpr int KV4_APPEND_THREADS = 256;
+
+// 8 weights from position d on
+__device__ __forceinline__ void kv4_load_weights(const void* weight, int f32, float offset, int d, float* w) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = 1.f;
+  if (!weight) return;
+  if (f32) {
+    const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(weight) + d);
+    *reinterpret_cast<float4*>(w) = src[0];
+    *reinterpret_cast<float4*>(w + 4) = src[1];
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(weight) + d);
+    const uint32_t p[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[2 * i] = bf16lo(p[i]);
+      w[2 * i + 1] = bf16hi(p[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] += offset;
+}
+
+// Eight of a block's sixteen values (bf16 numbers; the other eight are the neighbour lane's) to a word of codes and the block's scale.
+// Rounding x / s without a division: x and every border t s between two codes are numbers of at most 8 significant bits, so
+// they are equal or at least 2^-8 of them apart.  y = x (1 / s) is within 2^-22 of x / s, and rounded to a multiple of 2^-12 (by the
+// sum with 3072) it is the border itself where x is, else on the right side of it.
+__device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g, uint32_t* scale) {
+  float x[8], top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = bf16lo(w[i]) * inv_g;
+    x[2 * i + 1] = bf16hi(w[i]) * inv_g;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(x[i]));
+  top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = __fdiv_rn(top, 6.f);
+  if (top < 0.001953125f) top = 0.001953125f;       // (a NaN stays: the block is NaN)
+  uint32_t s8, sf;
+  asm("{\n.reg .b16 h;\ncvt.rn.satfinite.e4m3x2.f32 h, %2, %3;\ncvt.u32.u16 %0, h;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}"
+      : "=r"(s8), "=r"(sf) : "f"(0.f), "f"(top));
+  *scale = s8 & 0xff;
+  const float inv_s = __frcp_rn(__half2float(__ushort_as_half((unsigned short)sf)));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = copysignf(__fadd_rn(__fadd_rn(__fmul_rn(x[i], inv_s), 3072.f), -3072.f), x[i]);
+  uint32_t codes;
+  asm("{\n.reg .b8 a, b, c, d;\ncvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\ncvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\ncvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\nmov.b32 %0, {a, b, c, d};\n}"
+      : "=r"(codes) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  return codes;
+}
+
+// A token's q, k and v heads go to its warps in groups of 512 / D heads.  A lane holds vector j of a head row and its partner
+// j + D/16, as in efim_qk_norm_append, so either pairing of the rotation stays inside the lane; two neighbours hold a block of sixteen.
+template <int D>
+__global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
+  constexpr int HALF = D / 16;                  // lanes that have a head
+  constexpr int HW = 32 / HALF;
+  const int lane = threadIdx.x & 31;
+  const int flat = blockIdx.x * (KV4_APPEND_THREADS / 32) + (threadIdx.x >> 5);
+  const int t = flat / p.warps, part = flat % p.warps;
+  pdl_wait();
+  if (p.early_next) pdl_launch();
+  if (t >= p.total_new_tokens || t >= *(p.q_indptr + p.batch)) return;
+  const int nq = p.q ? p.Hq : 0, nk = nq + p.Hkv, nh = nk + p.Hkv;
+  const int j = lane % HALF, sub = lane / HALF, step = p.warps * HW;
+  const uint4* qin = reinterpret_cast<const uint4*>(p.q + (p.q ? t * p.q_stride : 0)) + j;
+  const uint4* kin = reinterpret_cast<const uint4*>(p.k + t * p.k_stride) + j;
+  const uint4* vin = reinterpret_cast<const uint4*>(p.v + t * p.v_stride) + j;
+  uint4 a, b;
+  auto fetch = [&](int h) {
+    a = b = make_uint4(0, 0, 0, 0);
+    if (h < nh) {
+      const uint4* row = h < nq ? qin + h * (D / 8) : h < nk ? kin + (h - nq) * (D / 8) : vin + (h - nk) * (D / 8);
+      a = ldg_stream(row);
+      b = ldg_stream(row + HALF);
+    }
+  };
+  const int base0 = part * HW;
+  fetch(base0 + sub);
+  const TokenPlace at = find_token(p.q_indptr, p.cached_len, p.batch, t, lane);
+  const int pos = at.pos, page_idx = pos >> 4;
+  const bool in_table = !p.cos_sin || (pos >= 0 && pos < p.max_position);
+  bool placed = pos >= 0 && page_idx < p.max_pages_per_seq && in_table;   // k and v have a place in the cache
+  int page = 0;
+  if (!placed) {
+    if (lane == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_POSITION);
+  } else {
+    page = *(p.block_table + (size_t)at.seq * p.max_pages_per_seq + page_idx);
+  }
+  float c[8], s[8];
+  if (p.cos_sin && in_table) {
+    // 8 pairs: (f, f + D/2) from f = 8 j on, or the 4 + 4 neighbours of the two vectors
+    const float* cs = p.cos_sin + (size_t)pos * D + j * (p.interleaved ? 4 : 8);
+    const int second = p.interleaved ? D / 4 : 4;
+    *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(cs);
+    *reinterpret_cast<float4*>(c + 4) = *reinterpret_cast<const float4*>(cs + second);
+    *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(cs + D / 2);
+    *reinterpret_cast<float4*>(s + 4) = *reinterpret_cast<const float4*>(cs + D / 2 + second);
+  }
+  if (placed && (page < 0 || page >= p.num_pages)) {
+    if (lane == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
+    placed = false;
+  }
+  const size_t row0 = (size_t)page * p.Hkv * 16 + (pos & 15);              // + h * 16: rows of the pools
+  for (int base = base0; base < nh; base += step) {    // (the same for a warp's lanes: the sums below are the whole warp's)
+    const int h = base + sub;
+    uint32_t y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (base + step < nh) fetch(h + step);
+    if (base < nk) {
+      float x[16];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[2 * e] = bf16lo(y[e]);
+        x[2 * e + 1] = bf16hi(y[e]);
+      }
+      if (p.normed) {
+        auto squares = [&]() {
+          float s2[2] = {0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s2[e & 1] = fmaf(x[e], x[e], s2[e & 1]);
+          float ss = s2[0] + s2[1];
+#pragma unroll
+          for (int d = HALF / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+          return ss;
+        };
+        float ss = squares(), eps = p.eps;
+        if (__any_sync(0xffffffffu, !(ss <= FLT_MAX))) {
+          // Squares of values beyond 1e18 leave fp32: such heads are taken 2^-70 as large (exact, and eps no longer counts beside
+          // them).  A row with an infinity or a NaN stays what the formula makes of it.
+          const float down = ss <= FLT_MAX ? 1.f : 8.470329472543003e-22f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] *= down;
+          if (down != 1.f) eps = 0.f;
+          ss = squares();
+        }
+        const float r = rsqrtf(fmaf(ss, 1.f / D, eps));
+        const void* weight = h < nq ? p.q_weight : p.k_weight;
+        float w[8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          kv4_load_weights(weight, p.weight_f32, p.weight_offset, (j + half * HALF) * 8, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[8 * half + e] = x[8 * half + e] * r * w[e];
+        }
+      }
+      if (h < nk) {
+        if (!p.cos_sin) {
+          if (p.normed) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+          }
+        } else if (!in_table) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = 0;     // no rotation for this row: a query of zeros
+        } else if (!p.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int f = 2 * e;
+            y[e] = pack_bf16x2(fmaf(x[f], c[f], -(x[8 + f] * s[f])), fmaf(x[f + 1], c[f + 1], -(x[9 + f] * s[f + 1])));
+            y[4 + e] = pack_bf16x2(fmaf(x[8 + f], c[f], x[f] * s[f]), fmaf(x[9 + f], c[f + 1], x[f + 1] * s[f + 1]));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            y[e] = pack_bf16x2(fmaf(x[2 * e], c[e], -(x[2 * e + 1] * s[e])), fmaf(x[2 * e + 1], c[e], x[2 * e] * s[e]));
+        }
+        if (h < nq) {
+          uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)t * p.Hq + h) * D + j * 8);
+          dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+          dst[HALF] = make_uint4(y[4], y[5], y[6], y[7]);
+        }
+      }
+    }
+    if (base + HW <= nq) continue;                 // query heads alone
+    const bool key = h < nk;
+    const float inv = key ? p.k_inv : p.v_inv;
+    uint32_t s0, s1;
+    const uint32_t c0 = kv4_quantize(y, inv, &s0), c1 = kv4_quantize(y + 4, inv, &s1);
+    if (h >= nq && h < nh && placed) {
+      const size_t row = row0 + (size_t)(h - (key ? nq : nk)) * 16;
+      uint8_t* codes = (key ? p.k_codes : p.v_codes) + row * (D / 2) + j * 4;
+      *reinterpret_cast<uint32_t*>(codes) = c0;
+      *reinterpret_cast<uint32_t*>(codes + D / 4) = c1;
+      if ((j & 1) == 0) {
+        uint8_t* scales = (key ? p.k_scales : p.v_scales) + row * (D / 16) + j / 2;
+        scales[0] = (uint8_t)s0;
+        scales[D / 32] = (uint8_t)s1;
+      }
+    }
+  }
+}
+
+// ---- pages read back
+struct Kv4UnpackParams {
+  const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+  uint16_t *k_out, *v_out;          // [n][Hkv][16][D] bf16; either may be null
+  // The pages: d_pages[i], or those of a ragged batch's sequences one after another (out_table: where each went, -1 for bad ones)
+  const int32_t* pages;
+  const int32_t *cached_len, *new_len, *block_table;
+  int32_t* out_table;
+  int32_t* status;
+  float k_scale, v_scale;
+  int n, batch, max_pages_per_seq, out_pages_per_seq, num_pages, Hkv;
+};
+
+constexpr int KV4_UNPACK_THREADS = 256;
+
+// A thread has 16 bytes of codes (32 values, 64 bytes of the result); the threads of a CTA walk one page's heads, K then V.
+template <int D>
+__global__ void __launch_bounds__(KV4_UNPACK_THREADS) kv4_unpack_kernel(const Kv4UnpackParams p) {
+  constexpr int PER_HEAD = 16 * D / 32;             // 16-byte pieces of codes of one (page, head)
+  pdl_wait();
+  pdl_launch();
+  const int i = blockIdx.x;
+  const int page = p.pages[i];
+  if (page < 0 || page >= p.num_pages) {
+    if (threadIdx.x == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
+    return;
+  }
+  const int per_pool = p.Hkv * PER_HEAD;
+  for (int u = threadIdx.x; u < 2 * per_pool; u += KV4_UNPACK_THREADS) {
+    const bool key = u < per_pool;
+    const int w = key ? u : u - per_pool;
+    uint16_t* out = key ? p.k_out : p.v_out;
+    if (!out) continue;
+    const size_t at = (size_t)page * per_pool + w;
+    const uint4 codes = *reinterpret_cast<const uint4*>((key ? p.k_codes : p.v_codes) + at * 16);
+    const uint32_t two = *reinterpret_cast<const uint16_t*>((key ? p.k_scales : p.v_scales) + at * 2);
+    const uint32_t s2 = scales_to_half2(two);
+    const float g = key ? p.k_scale : p.v_scale;
+    const float s[2] = {__half2float(__ushort_as_half((unsigned short)s2)) * g, __half2float(__ushort_as_half((unsigned short)(s2 >> 16))) * g};
+    const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};
+    uint4* dst = reinterpret_cast<uint4*>(out) + ((size_t)i * per_pool + w) * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t h[4], r[4];
+      codes_to_half2(word[q], h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
+        r[e] = pack_bf16x2(f.x * s[q / 2], f.y * s[q / 2]);
+      }
+      dst[q] = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+  }
+}
+
+}  // namespace efim
+
+extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim_batch_desc* batch, const efim_qk_norm_desc* norm,
+                                       const efim_rope_desc* rope, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                                       const void* d_v, int64_t v_stride, void* d_q_out, int32_t* d_status, void* stream) {
+  using namespace efim;
+  efim_status st = check_cache4(cache);
+  if (st != EFIM_OK) return st;
+  if (!batch) return EFIM_ERR_INVALID_ARG;
+  st = check_batch(nullptr, batch, false);
+  if (st != EFIM_OK) return st;
+  if (norm && (!(norm->eps > 0.f) || !(norm->eps <= FLT_MAX) || (norm->weight_f32 != 0 && norm->weight_f32 != 1))) return EFIM_ERR_INVALID_ARG;
+  if (batch->batch == 0 || batch->total_new_tokens == 0) return EFIM_OK;
+  const long long D = cache->head_dim, q_row = cache->num_q_heads * D, kv_row = cache->num_kv_heads * D, T = batch->total_new_tokens;
+  auto address = [](const void* x) { return reinterpret_cast<uintptr_t>(x); };
+  if (!d_k || !d_v || !d_q != !d_q_out) return EFIM_ERR_INVALID_ARG;
+  if ((address(d_q) | address(d_k) | address(d_v) | address(d_q_out)) & 15) return EFIM_ERR_INVALID_ARG;
+  if (norm && ((address(norm->d_q_weight) | address(norm->d_k_weight)) & 15)) return EFIM_ERR_INVALID_ARG;
+  if ((d_q && (q_stride < q_row || q_stride % 8)) || k_stride < kv_row || k_stride % 8 || v_stride < kv_row || v_stride % 8)
+    return EFIM_ERR_INVALID_ARG;
+  if (rope && rope->d_cos_sin && (rope->max_position <= 0 || (address(rope->d_cos_sin) & 15))) return EFIM_ERR_INVALID_ARG;
+  if (d_q) {
+    // Rows of the result must not lie where another token's are still to be read: in place (packed rows), or apart.
+    const uintptr_t lo = address(d_q_out), hi = lo + T * q_row * 2;
+    auto meets = [&](const void* x, long long stride, long long row) {
+      return address(x) < hi && lo < address(x) + ((T - 1) * stride + row) * 2;
+    };
+    const bool in_place = d_q_out == d_q && q_stride == q_row;
+    if ((!in_place && meets(d_q, q_stride, q_row)) || meets(d_k, k_stride, kv_row) || meets(d_v, v_stride, kv_row))
+      return EFIM_ERR_INVALID_ARG;
+  }
+  Kv4AppendParams p{};
+  p.q = static_cast<const uint16_t*>(d_q);
+  p.k = static_cast<const uint16_t*>(d_k);
+  p.v = static_cast<const uint16_t*>(d_v);
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.q_out = static_cast<uint16_t*>(d_q_out);
+  p.k_codes = static_cast<uint8_t*>(cache->d_k_codes);
+  p.v_codes = static_cast<uint8_t*>(cache->d_v_codes);
+  p.k_scales = static_cast<uint8_t*>(cache->d_k_scales);
+  p.v_scales = static_cast<uint8_t*>(cache->d_v_scales);
+  p.k_inv = 1.f / cache->k_scale;
+  p.v_inv = 1.f / cache->v_scale;
+  if (norm) {
+    p.normed = 1;
+    p.q_weight = norm->d_q_weight;
+    p.k_weight = norm->d_k_weight;
+    p.weight_f32 = norm->weight_f32;
+    p.weight_offset = norm->weight_offset;
+    p.eps = norm->eps;
+  }
+  p.cached_len = batch->d_cached_len;
+  p.q_indptr = batch->d_q_indptr;
+  p.block_table = batch->d_block_table;
+  if (rope && rope->d_cos_sin) {
+    p.cos_sin = rope->d_cos_sin;
+    p.max_position = rope->max_position;
+    p.interleaved = rope->interleaved;
+  }
+  p.status = d_status;
+  p.batch = batch->batch;
+  p.max_pages_per_seq = batch->max_pages_per_seq;
+  p.total_new_tokens = batch->total_new_tokens;
+  p.num_pages = cache->num_pages;
+  p.Hq = cache->num_q_heads;
+  p.Hkv = cache->num_kv_heads;
+  const int hw = 512 / D, heads = (d_q ? cache->num_q_heads : 0) + 2 * cache->num_kv_heads, groups = (heads + hw - 1) / hw;
+  const long long resident = 4LL * (KV4_APPEND_THREADS / 32) * sm_count();
+  p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 10 ? (groups + 4) / 5 : 1, resident / T));
+  const long long ctas = (T * p.warps + KV4_APPEND_THREADS / 32 - 1) / (KV4_APPEND_THREADS / 32);
+  if (ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  p.early_next = ctas <= sm_count();
+  auto launch = [&](auto kernel) {
+    return launch_pdl(kernel, dim3((unsigned)ctas), dim3(KV4_APPEND_THREADS), 0, static_cast<cudaStream_t>(stream), p);
+  };
+  EFIM_CUDA_TRY(D == 128 ? launch(kv4_append_kernel<128>) : launch(kv4_append_kernel<64>));
+  return EFIM_OK;
+}
+
+extern "C" efim_status efim_kv4_unpack(const efim_cache4_desc* cache, const int32_t* d_pages, int32_t num, void* d_k_out, void* d_v_out,
+                                       int32_t* d_status, void* stream) {
+  using namespace efim;
+  const efim_status st = check_cache4(cache);
+  if (st != EFIM_OK) return st;
+  if (num < 0) return EFIM_ERR_INVALID_ARG;
+  if (num == 0) return EFIM_OK;
+  if (!d_pages || (!d_k_out && !d_v_out) || ((reinterpret_cast<uintptr_t>(d_k_out) | reinterpret_cast<uintptr_t>(d_v_out)) & 15))
+    return EFIM_ERR_INVALID_ARG;
+  Kv4UnpackParams p{};
+  p.k_codes = static_cast<const uint8_t*>(cache->d_k_codes);
+  p.v_codes = static_cast<const uint8_t*>(cache->d_v_codes);
+  p.k_scales = static_cast<const uint8_t*>(cache->d_k_scales);
+  p.v_scales = static_cast<const uint8_t*>(cache->d_v_scales);
+  p.k_out = static_cast<uint16_t*>(d_k_out);
+  p.v_out = static_cast<uint16_t*>(d_v_out);
+  p.pages = d_pages;
+  p.status = d_status;
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.n = num;
+  p.num_pages = cache->num_pages;
+  p.Hkv = cache->num_kv_heads;
+  EFIM_CUDA_TRY(cache->head_dim == 128 ? launch_pdl(kv4_unpack_kernel<128>, dim3(num), dim3(KV4_UNPACK_THREADS), 0, static_cast<cudaStream_t>(stream), p)
+                                       : launch_pdl(kv4_unpack_kernel<64>, dim3(num), dim3(KV4_UNPACK_THREADS), 0, static_cast<cudaStream_t>(stream), p));
+  return EFIM_OK;
+}

@@ -1,0 +1,619 @@
+// efim_kv4_decode_attn: attention of one or a few new tokens a sequence over a 4-bit cache, with keys split over CTAs and a
+// log-sum-exp merge.
+//
+// One CTA = (sequence, kv head, tile of 8 NT rows, key chunk); a row is a (new token, query head of the group) pair.  Its 4 warps walk
+// pages (16 tokens) round-robin, each with a ring of its own that cp.async fills.  A page is one 16-token tile of mma.sync m16n8k16
+// (fp16 in, fp32 accumulation), rows along n:
+//   S^T [16 tokens][rows]  = K [16][D] Q^T [D][rows]
+//   O^T [D][rows]         += V^T [D][16] P^T [16][rows]
+// The operands K and V are made in registers: a code times its block's scale is exact in fp16 (cvt from 4-bit floats, one product), and
+// the order of a contraction's index is free, so each lane takes neighbouring codes as they lie:
+//   K: lane (g, t) = (lane / 4, lane % 4) has tokens g, g + 8 and dims [t D/4, (t+1) D/4): a 16-byte (D = 64: 8-byte) piece of each row
+//   V: tokens 2t, 2t+1, 2t+8, 2t+9 and dims [g D/8, (g+1) D/8): 8 (4) bytes of four rows; nibbles of two tokens are put side by
+//      side, so that a conversion gives a pair of tokens
+// with the page's tokens numbered such that neither read meets a bank twice (kv4_token, kv4_v_piece).
+// Queries enter as fp16 after a shift by a power of two per row that takes the row's largest value to [2^14, 2^15): exact for
+// values down to 2^-28 of it.  P = 2^(s - m + 11) enters as fp16 (a rounding of 2^-12 of each, between 2^15 and, at full precision, 2^-25 of
+// the largest); the sums that it is divided by are the unrounded fp32 values.
+#include "kv4_attn.cuh"
+#include "token_place.cuh"
+#include <algorithm>
+#include <cfloat>
+
+namespace efim {
+
+constexpr int KV4_WARPS = 4;
+constexpr int KV4_THREADS = 32 * KV4_WARPS;
+constexpr float KV4_P_SHIFT = 11.f;     // P's largest value, log2, with the reference right; the reference may be 4 behind
+constexpr float KV4_LAG = 4.f;
+
+__host__ __device__ constexpr int kv4_page_bytes(int D) { return 2 * (kv4_code_bytes(D) + kv4_scale_bytes(D)); }
+__host__ __device__ constexpr int kv4_stages(int NT) { return NT == 4 ? 6 : 4; }
+__host__ __device__ constexpr int kv4_ctas_per_sm(int NT) { return NT == 4 ? 2 : 4; }
+__host__ __device__ constexpr int kv4_smem_bytes(int D, int NT) {
+  const int ring = KV4_WARPS * kv4_stages(NT) * kv4_page_bytes(D), exchange = KV4_WARPS * 8 * NT * (D + 4) * 4;
+  return ring > exchange ? ring : exchange;
+}
+
+// The token of a page that is the products' token 2t + e + 8h
+__device__ __forceinline__ int kv4_token(int t, int e, int h) { return (e ^ (t & 1)) | (t & 1) << 1 | (t >> 1) << 2 | h << 3; }
+// Where 16-byte piece c of a token's V codes stands in a staged page
+template <int D>
+__device__ __forceinline__ int kv4_v_piece(int token, int c) {
+  const int odd = (token >> 2) & 1;
+  return D == 128 ? token * 64 + ((c ^ (odd << 1)) << 4) : (token ^ odd) * 32 + (c << 4);
+}
+
+__device__ __forceinline__ uint32_t kv4_movm_t(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// c += a b, a 16 x 16 (row), b 16 x 8 (col), fp16 in, fp32 accumulation
+__device__ __forceinline__ void kv4_mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float kv4_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t kv4_pack_half2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void kv4_cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint32_t kv4_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// What a CTA works on.
+struct Kv4Work {
+  int ctx;        // keys of the sequence, clamped to what the launch covers
+  int first_row;  // the sequence's first row of q
+  int new_len;    // its rows of q that are computed
+  int cached;     // keys before its first new token
+};
+__device__ __forceinline__ Kv4Work kv4_work(const Kv4AttnParams& p, int s, int* err) {
+  Kv4Work w;
+  w.first_row = s;
+  w.new_len = 1;
+  if (p.q_indptr) {
+    w.first_row = *(p.q_indptr + s);
+    w.new_len = *(p.q_indptr + s + 1) - w.first_row;
+  }
+  int ctx = *(p.len + s);
+  if (p.len_is_cached) ctx += w.new_len;
+  w.cached = ctx - w.new_len;
+  w.ctx = ctx;
+  *err = 0;
+  if (w.first_row < 0 || w.new_len < 0 || w.new_len > p.total_rows - w.first_row) {   // rows that were not given
+    *err = EFIM_DEV_BAD_POSITION;
+    w.new_len = 0;
+  }
+  if (w.new_len > p.max_new) {
+    *err = EFIM_DEV_BAD_POSITION;
+    w.new_len = p.max_new;
+  }
+  if (w.ctx > p.key_cap) {
+    *err = EFIM_DEV_BAD_POSITION;
+    w.ctx = p.key_cap;
+  }
+  return w;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_kernel(const Kv4AttnParams p) {
+  constexpr int ST = kv4_stages(NT), ROWS = 8 * NT;
+  constexpr int CODES = kv4_code_bytes(D), SCALES = kv4_scale_bytes(D), PAGE = kv4_page_bytes(D);
+  constexpr int KS = D / 16;              // k-steps of S^T, m-tiles of O^T
+  constexpr int XD = D + 4;               // floats per row of the warps' exchange buffer
+  constexpr bool Q_IN_REGS = NT <= 2;
+  extern __shared__ __align__(128) uint8_t kv4_smem_raw[];
+  __shared__ __align__(16) uint16_t s_q[ROWS][D + 16];    // fp16, shifted; dim t D/4 + 4k + x at 16k + 4t + x
+  __shared__ float s_m[KV4_WARPS][ROWS], s_l[KV4_WARPS][ROWS], s_scale[ROWS];
+  __shared__ uint8_t s_nan[ROWS][8];      // rows that see a NaN value in dims [g D/8, (g+1) D/8)
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int tiles = p.row_tiles, s = blockIdx.x / tiles, tile = blockIdx.x % tiles, kvh = blockIdx.y, c = blockIdx.z;
+  const int G = p.Hq / p.Hkv;
+  pdl_wait();
+  pdl_launch();
+  const int32_t* bt = p.block_table + (size_t)s * p.max_pages_per_seq;
+  const int begin = c * p.chunk_tokens, first_pg = (begin >> 4) + warp;
+  int err;
+  const int my_pg = first_pg + KV4_WARPS * lane;
+  int pid_cache = my_pg < p.max_pages_per_seq ? *(bt + my_pg) : -1;      // (any entry of the row may be read)
+  const Kv4Work w = kv4_work(p, s, &err);
+  if (err && tid == 0 && p.status) atomicOr(p.status, err);
+  const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
+  if (n_rows <= 0) return;
+  const int len = max(w.ctx, 0);
+  if (begin >= len && !(len == 0 && c == 0)) return;
+  // keys that the tile's last row sees
+  const int last_limit = min(len, w.cached + (row0 + n_rows - 1) / G + 1);
+  const int end = min(last_limit, begin + p.chunk_tokens);
+  const int last_pg = (end - 1) >> 4;
+  const int n_pages = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / KV4_WARPS + 1 : 0;
+
+  const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * PAGE);
+  const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * PAGE);
+  uint32_t ok_bits = 0;                   // which of the in-flight pages are valid (bit = stage)
+  auto issue = [&](int i, int sg) {       // send for this warp's i-th page into stage sg
+    if (i < n_pages) {
+      const int pid = __shfl_sync(0xffffffffu, pid_cache, i & 31);
+      const bool ok = pid >= 0 && pid < p.num_pages;
+      ok_bits = (ok_bits & ~(1u << sg)) | (ok ? 1u << sg : 0u);
+      if (ok) {
+        const size_t at = (size_t)pid * p.Hkv + kvh;
+        const uint32_t dst = ring + sg * PAGE;
+        const uint8_t *k = p.k_codes + at * CODES, *v = p.v_codes + at * CODES;
+#pragma unroll
+        for (int u = lane; u < CODES / 16; u += 32) {
+          kv4_cp16(dst + u * 16, k + u * 16);
+          kv4_cp16(dst + CODES + kv4_v_piece<D>(u / (D / 32), u % (D / 32)), v + u * 16);
+        }
+        constexpr int PS = SCALES / 16;
+        if (lane < 2 * PS) {
+          const uint8_t* sc = lane < PS ? p.k_scales + at * SCALES + lane * 16 : p.v_scales + at * SCALES + (lane - PS) * 16;
+          kv4_cp16(dst + 2 * CODES + lane * 16, sc);
+        }
+      } else if (lane == 0 && p.status) {
+        atomicOr(p.status, EFIM_DEV_BAD_PAGE);
+      }
+      if (((i + 1) & 31) == 0) {          // the next 32 of this warp's pages
+        const int pg = first_pg + KV4_WARPS * (i + 1 + lane);
+        pid_cache = pg <= last_pg ? *(bt + pg) : -1;
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i) issue(i, i);
+
+  // ---- query rows as fp16, shifted: a warp a row
+  for (int r = warp; r < ROWS; r += KV4_WARPS) {
+    float x[D / 32];
+    float top = 0.f;
+    if (r < n_rows) {
+      const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
+      const uint16_t* q = p.q + ((size_t)(w.first_row + i) * p.Hq + h) * D + lane * (D / 32);
+      if constexpr (D == 128) {
+        const uint2 u = *reinterpret_cast<const uint2*>(q);
+        x[0] = bf16lo(u.x), x[1] = bf16hi(u.x), x[2] = bf16lo(u.y), x[3] = bf16hi(u.y);
+      } else {
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(q);
+        x[0] = bf16lo(u), x[1] = bf16hi(u);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) x[e] = 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) top = max_nan(top, fabsf(x[e]));
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
+    // 2^-(exponent of the largest) and back; a row with an infinity or a NaN becomes NaN
+    const int ex = (int)(__float_as_uint(top) >> 23);                    // biased; subnormal rows count as 2^-126
+    const bool bad = ex >= 255;
+    const float down = __uint_as_float((uint32_t)min(254, max(1, 268 - max(ex, 1))) << 23);    // 2^(14 - exponent), 2^127 at most
+#pragma unroll
+    for (int e = 0; e < D / 32; e += 2) {
+      const float lo = bad ? NAN : x[e] * down, hi = bad ? NAN : x[e + 1] * down;
+      const int d = lane * (D / 32) + e;
+      *reinterpret_cast<uint32_t*>(&s_q[r][d % (D / 4) / 4 * 16 + d / (D / 4) * 4 + d % 4]) = kv4_pack_half2(lo, hi);
+    }
+    if (lane == 0) s_scale[r] = fminf(p.scale_log2 / down, FLT_MAX);     // (a power of two: exact)
+    if (lane < 8) s_nan[r][lane] = 0;
+  }
+  __syncthreads();
+  // B fragments of row g: the dims that the K fragments have, D/4 from t D/4 on
+  uint32_t qf[Q_IN_REGS ? NT : 1][KS][2];
+  if constexpr (Q_IN_REGS) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint2 u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * k + 4 * t]);
+        qf[n][k][0] = u.x;
+        qf[n][k][1] = u.y;
+      }
+  }
+  float o[NT][KS][4];                     // O^T: dims g D/8 + 2 k + (e / 2), rows 8 n + 2 t + (e % 2)
+  float m_ref[NT][2], l_part[NT][2], sc[NT][2];
+  int limit[NT][2];                       // keys that rows 8 n + 2 t + {0, 1} see
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[n][k][e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = n * 8 + 2 * t + e;
+      m_ref[n][e] = -FLT_MAX;
+      l_part[n][e] = 0.f;
+      sc[n][e] = s_scale[r];
+      limit[n][e] = min(end, w.cached + (row0 + min(r, n_rows - 1)) / G + 1);
+    }
+  }
+  const int first_limit = min(end, w.cached + row0 / G + 1);
+  const int tok0 = kv4_token(g >> 1, g & 1, 0);             // this lane's key in S^T; the other is 8 on
+
+  for (int i = 0; i < n_pages; ++i) {
+    const int sg = i % ST;
+    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
+    __syncwarp();
+    issue(i + ST - 1, (i + ST - 1) % ST);                   // into the stage that the last trip has left
+    if (!((ok_bits >> sg) & 1u)) continue;
+    const uint8_t* page = ring_ptr + sg * PAGE;
+    const int key0 = (first_pg + KV4_WARPS * i) << 4;
+    // ---- S^T
+    float sx[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sx[n][e] = 0.f;
+    {
+      uint32_t scale[2][D / 64];           // of the two tokens, per block of 16 dims: the pair (s, s)
+      uint32_t kw[2][D / 32];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int token = tok0 + 8 * h;
+        if constexpr (D == 128) {
+          const uint4 u = *reinterpret_cast<const uint4*>(page + token * 64 + t * 16);
+          kw[h][0] = u.x, kw[h][1] = u.y, kw[h][2] = u.z, kw[h][3] = u.w;
+          const uint32_t two = scales_to_half2(*reinterpret_cast<const uint16_t*>(page + 2 * CODES + token * 8 + 2 * t));
+          scale[h][0] = __byte_perm(two, 0, 0x1010);
+          scale[h][1] = __byte_perm(two, 0, 0x3232);
+        } else {
+          const uint2 u = *reinterpret_cast<const uint2*>(page + token * 32 + t * 8);
+          kw[h][0] = u.x, kw[h][1] = u.y;
+          scale[h][0] = __byte_perm(scales_to_half2(page[2 * CODES + token * 4 + t]), 0, 0x1010);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < D / 32; ++q) {   // 8 dims of each token: two k-steps
+        uint32_t x[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          codes_to_half2(kw[h][q], x[h]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[h][e] = mul_half2(x[h][e], scale[h][q / 2]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t a[4] = {x[0][2 * k], x[1][2 * k], x[0][2 * k + 1], x[1][2 * k + 1]};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (Q_IN_REGS) {
+              kv4_mma(sx[n], a, qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
+            } else {
+              const uint2 u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
+              kv4_mma(sx[n], a, u.x, u.y);
+            }
+          }
+        }
+      }
+    }
+    // ---- scores, in log2, and the reference
+    const bool border = key0 + 16 > first_limit;            // some row does not see the whole page
+    bool grow = false;
+    float mx[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sx[n][e] *= sc[n][e & 1];
+        if (border && key0 + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[n][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        mx[n][e] = fmaxf(sx[n][e], sx[n][e + 2]);
+        grow |= mx[n][e] > m_ref[n][e] + KV4_LAG;
+      }
+    }
+    // Lazy rescale: the reference of a row only moves when a score exceeds it by more than 2^4 (always on the first page)
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x = mx[n][e];
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+          const float m_new = x > m_ref[n][e] + KV4_LAG ? x : m_ref[n][e];     // (each row by its own scores: its bits do not depend on the others')
+          const float alpha = kv4_ex2(m_ref[n][e] - m_new);
+          m_ref[n][e] = m_new;
+          l_part[n][e] *= alpha;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            o[n][k][e] *= alpha;
+            o[n][k][e + 2] *= alpha;
+          }
+        }
+    }
+    uint32_t pb[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float x0 = kv4_ex2(sx[n][2 * h] - m_ref[n][0] + KV4_P_SHIFT), x1 = kv4_ex2(sx[n][2 * h + 1] - m_ref[n][1] + KV4_P_SHIFT);
+        l_part[n][0] += x0;
+        l_part[n][1] += x1;
+        pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
+      }
+    // ---- O^T
+    uint32_t scale[2];                     // of tokens (2t, 2t+1) and (2t+8, 2t+9)
+    uint32_t vw[2][2][D / 64];
+    const uint8_t* vp = page + CODES;
+    uint32_t bytes = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int token = kv4_token(t, e, h);
+        uint32_t b;
+        if constexpr (D == 128) {
+          const uint2 u = *reinterpret_cast<const uint2*>(vp + kv4_v_piece<D>(token, g >> 1) + (g & 1) * 8);
+          vw[h][e][0] = u.x, vw[h][e][1] = u.y;
+          b = page[2 * CODES + SCALES + token * 8 + g];
+        } else {
+          vw[h][e][0] = *reinterpret_cast<const uint32_t*>(vp + kv4_v_piece<D>(token, g >> 2) + (g & 3) * 4);
+          b = page[2 * CODES + SCALES + token * 4 + (g >> 1)];
+        }
+        // what stands behind the last key is anything, a NaN's scale too: P is 0 there, 0 times NaN is not
+        if (border && key0 + token >= end) b = 0;
+        bytes |= b << (16 * h + 8 * e);
+      }
+    // Values that are NaN: rows that see them are marked and get their NaN at the end; in the products they are zeros, since rows that
+    // do not see them have a P of 0 there.
+    if (__any_sync(0xffffffffu, __vcmpeq4(bytes & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0)) {
+#pragma unroll 1
+      for (int q = 0; q < 4; ++q) {
+        if (((bytes >> (8 * q)) & 0x7f) != 0x7f) continue;
+        bytes &= ~(0xffu << (8 * q));
+        const int key = key0 + kv4_token(t, q & 1, q >> 1);
+        for (int r = 0; r < n_rows; ++r)
+          if (key < min(end, w.cached + (row0 + r) / G + 1)) s_nan[r][g] = 1;
+      }
+    }
+    scale[0] = scales_to_half2(bytes & 0xffff);
+    scale[1] = scales_to_half2(bytes >> 16);
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) {
+      // lo: even dims of the two tokens side by side, hi: odd dims
+      uint32_t lo[2][4], hi[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t a = vw[h][0][q], b = vw[h][1][q];
+        codes_to_half2((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), lo[h]);
+        codes_to_half2(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), hi[h]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          lo[h][e] = mul_half2(lo[h][e], scale[h]);
+          hi[h][e] = mul_half2(hi[h][e], scale[h]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t a[4] = {lo[0][e], hi[0][e], lo[1][e], hi[1][e]};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
+      }
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  // ---- fold the lanes' sums, then the 4 warps (the exchange buffer takes their rings' place)
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) l_part[n][e] += __shfl_xor_sync(0xffffffffu, l_part[n][e], off);
+      if (lane < 4) {
+        s_l[warp][n * 8 + 2 * lane + e] = l_part[n][e];
+        s_m[warp][n * 8 + 2 * lane + e] = m_ref[n][e];
+      }
+    }
+  __syncthreads();
+  float* xo = reinterpret_cast<float*>(kv4_smem_raw);       // [warp][row][XD]
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        *reinterpret_cast<float2*>(&xo[(warp * ROWS + n * 8 + 2 * t + e) * XD + g * (D / 8) + 2 * k]) = make_float2(o[n][k][e], o[n][k][e + 2]);
+  __syncthreads();
+  for (int idx = tid; idx < n_rows * (D / 4); idx += KV4_THREADS) {
+    const int r = idx / (D / 4), d = (idx % (D / 4)) * 4;
+    float M = s_m[0][r];
+#pragma unroll
+    for (int x = 1; x < KV4_WARPS; ++x) M = fmaxf(M, s_m[x][r]);
+    float L = 0.f;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < KV4_WARPS; ++x) {
+      const float f = exp2f(s_m[x][r] - M);
+      const float4 y = *reinterpret_cast<const float4*>(xo + (x * ROWS + r) * XD + d);
+      L = fmaf(s_l[x][r], f, L);
+      O.x = fmaf(y.x, f, O.x);
+      O.y = fmaf(y.y, f, O.y);
+      O.z = fmaf(y.z, f, O.z);
+      O.w = fmaf(y.w, f, O.w);
+    }
+    float inv = L == 0.f ? 0.f : p.v_scale / L;
+    if (s_nan[r][d / (D / 8)]) inv = NAN;
+    const float lse2 = L == 0.f ? -INFINITY : M - KV4_P_SHIFT + log2f(L);      // (a sum of NaN stays NaN)
+    const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
+    const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
+    if (p.n_chunks == 1) {
+      *reinterpret_cast<uint2*>(p.out + row_head * D + d) =
+          make_uint2(pack_bf16x2(O.x * inv, O.y * inv), pack_bf16x2(O.z * inv, O.w * inv));
+      if (p.lse && d == 0) p.lse[row_head] = lse2 * 0.6931471805599453f;
+    } else {
+      // partials of (sequence, row of it, chunk): rows are counted by sequence, max_new of them each
+      const size_t part = (((size_t)s * p.max_new + i) * p.Hq + h) * p.n_chunks + c;
+      *reinterpret_cast<float4*>(p.part_o + part * D + d) = make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
+      if (d == 0) p.part_lse[part] = lse2;
+    }
+  }
+}
+
+// Merge of a row's chunks: lse = log2 sum 2^lse_c, o = sum 2^(lse_c - lse) o_c.  A warp has one (row, head), lanes over head_dim.
+template <int D>
+__global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4AttnParams p) {
+  constexpr int EPL = D / 32;
+  const int lane = threadIdx.x & 31;
+  const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);       // (sequence, row, head)
+  pdl_wait();
+  pdl_launch();
+  if (unit >= (long long)p.batch * p.max_new * p.Hq) return;
+  const int h = (int)(unit % p.Hq), i = (int)(unit / p.Hq % p.max_new), s = (int)(unit / p.Hq / p.max_new);
+  int err;
+  const Kv4Work w = kv4_work(p, s, &err);
+  if (i >= w.new_len) return;
+  const int nc = max(1, (w.ctx + p.chunk_tokens - 1) / p.chunk_tokens);
+  const float* pl = p.part_lse + unit * p.n_chunks;
+  const float* po = p.part_o + unit * p.n_chunks * D + lane * EPL;
+  float M = -INFINITY;
+  for (int c = lane; c < nc; c += 32) M = max_nan(M, pl[c]);                  // a NaN chunk makes the row NaN
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, d));
+  float L = 0.f, acc[EPL];
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+  if (!(M == -INFINITY)) {                         // else a row without keys
+    for (int c = 0; c < nc; ++c) {
+      const float wi = exp2f(pl[c] - M);
+      L += wi;
+      if (pl[c] == -INFINITY) continue;            // (a chunk that the row sees nothing of)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) acc[e] = fmaf(wi, po[(size_t)c * D + e], acc[e]);
+    }
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
+  uint16_t* out = p.out + row_head * D + lane * EPL;
+  if constexpr (EPL == 4)
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+  else
+    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  if (p.lse && lane == 0) p.lse[row_head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
+// How the keys are cut.  As in efim_decode_attn: one wave of CTAs where that gives chunks of 256 to 1024 keys, else 2048.
+Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_ctx) {
+  Kv4Plan pl;
+  const int G = cache->num_q_heads / cache->num_kv_heads;
+  const long long rows = (long long)max_new * G;
+  pl.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+  pl.row_tiles = (rows + 8 * pl.nt - 1) / (8 * pl.nt);
+  if (max_ctx < 1) max_ctx = 1;
+  const long long slots = (long long)sm_count() * kv4_ctas_per_sm(pl.nt);
+  const long long units = (long long)batch * cache->num_kv_heads * pl.row_tiles;
+  long long chunk = 2048;
+  if (units * ((max_ctx + 2047) / 2048) < 4 * slots) {
+    const long long n = std::max<long long>(1, slots / units);
+    chunk = std::min<long long>(1024, std::max<long long>(256, (max_ctx + n - 1) / n));
+  }
+  chunk = (chunk + 63) / 64 * 64;
+  pl.chunk_tokens = (int)chunk;
+  pl.n_chunks = (int)((max_ctx + chunk - 1) / chunk);
+  const size_t parts = pl.n_chunks > 1 ? (size_t)batch * max_new * cache->num_q_heads * pl.n_chunks : 0;
+  pl.lse_bytes = (parts * 4 + 255) / 256 * 256;
+  pl.bytes = pl.lse_bytes + parts * cache->head_dim * 4;
+  return pl;
+}
+
+template <int D, int NT>
+static efim_status kv4_launch_nt(const Kv4AttnParams& p, const Kv4Plan& pl, cudaStream_t s) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<bool> done[kMaxDevices];
+  constexpr int smem = kv4_smem_bytes(D, NT);
+  int dev = 0;
+  EFIM_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices || !done[dev].load(std::memory_order_acquire)) {
+    EFIM_CUDA_TRY(cudaFuncSetAttribute(kv4_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if (dev >= 0 && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
+  }
+  EFIM_CUDA_TRY(launch_pdl(kv4_attn_kernel<D, NT>, dim3((unsigned)(p.batch * pl.row_tiles), p.Hkv, pl.n_chunks), dim3(KV4_THREADS), smem, s, p));
+  return EFIM_OK;
+}
+template <int D>
+static efim_status kv4_launch(const Kv4AttnParams& p, const Kv4Plan& pl, cudaStream_t s) {
+  const efim_status st = pl.nt == 1 ? kv4_launch_nt<D, 1>(p, pl, s) : pl.nt == 2 ? kv4_launch_nt<D, 2>(p, pl, s) : kv4_launch_nt<D, 4>(p, pl, s);
+  if (st != EFIM_OK || pl.n_chunks == 1) return st;
+  const long long warps = (long long)p.batch * p.max_new * p.Hq;
+  EFIM_CUDA_TRY(launch_pdl(kv4_merge_kernel<D>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, s, p));
+  return EFIM_OK;
+}
+
+efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max_ctx, float sm_scale, void* ws, size_t ws_bytes, void* stream) {
+  const long long cap = (long long)p.max_pages_per_seq * cache->page_size;
+  if (max_ctx <= 0) max_ctx = (int)std::min<long long>(cap, 0x7fffffff);
+  if (max_ctx > cap) return EFIM_ERR_OUT_OF_RANGE;
+  const long long G = cache->num_q_heads / cache->num_kv_heads;
+  if ((long long)p.max_new * G > 0x3fffffff || (long long)p.batch * p.max_new * p.Hq > 0x7fffffff) return EFIM_ERR_UNSUPPORTED;
+  const Kv4Plan pl = kv4_plan(cache, p.batch, p.max_new, max_ctx);
+  if (pl.n_chunks > 65535 || (long long)p.batch * pl.row_tiles > 0x7fffffff) return EFIM_ERR_UNSUPPORTED;
+  if (pl.bytes > 0) {
+    if (!ws || ws_bytes < pl.bytes) return EFIM_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) & 255) return EFIM_ERR_INVALID_ARG;
+    p.part_lse = static_cast<float*>(ws);
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.lse_bytes);
+  }
+  p.k_codes = static_cast<const uint8_t*>(cache->d_k_codes);
+  p.v_codes = static_cast<const uint8_t*>(cache->d_v_codes);
+  p.k_scales = static_cast<const uint8_t*>(cache->d_k_scales);
+  p.v_scales = static_cast<const uint8_t*>(cache->d_v_scales);
+  p.v_scale = cache->v_scale;
+  const float scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)cache->head_dim);
+  p.scale_log2 = scale * 1.4426950408889634f * cache->k_scale;
+  p.Hkv = cache->num_kv_heads;
+  p.num_pages = cache->num_pages;
+  p.row_tiles = (int)pl.row_tiles;
+  p.chunk_tokens = pl.chunk_tokens;
+  p.n_chunks = pl.n_chunks;
+  p.key_cap = (int)std::min<long long>((long long)pl.n_chunks * pl.chunk_tokens, cap);
+  return cache->head_dim == 128 ? kv4_launch<128>(p, pl, static_cast<cudaStream_t>(stream)) : kv4_launch<64>(p, pl, static_cast<cudaStream_t>(stream));
+}
+
+}  // namespace efim
+
+extern "C" size_t efim_kv4_decode_workspace_bytes(const efim_cache4_desc* cache, int32_t batch, int32_t max_new_len, int32_t max_ctx_len) {
+  if (efim::check_cache4(cache) != EFIM_OK || batch <= 0 || max_new_len <= 0) return 0;
+  return efim::kv4_plan(cache, batch, max_new_len, max_ctx_len).bytes;
+}
+
+extern "C" efim_status efim_kv4_decode_attn(const efim_cache4_desc* cache, int32_t batch, const int32_t* d_ctx_len, int32_t max_ctx_len,
+                                            const int32_t* d_block_table, int32_t max_pages_per_seq, const int32_t* d_q_indptr,
+                                            int32_t total_rows, int32_t max_new_len, const void* d_q, void* d_out, float* d_lse,
+                                            float sm_scale, void* d_workspace, size_t workspace_bytes, int32_t* d_status, void* stream) {
+  using namespace efim;
+  const efim_status st = check_cache4(cache);
+  if (st != EFIM_OK) return st;
+  if (batch < 0 || max_pages_per_seq <= 0 || total_rows < 0 || max_new_len <= 0) return EFIM_ERR_INVALID_ARG;
+  if (!d_q_indptr && (max_new_len != 1 || total_rows != batch)) return EFIM_ERR_INVALID_ARG;
+  if (batch == 0 || total_rows == 0) return EFIM_OK;
+  if (!d_ctx_len || !d_block_table || !d_q || !d_out) return EFIM_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out)) & 15) return EFIM_ERR_INVALID_ARG;
+  Kv4AttnParams p{};
+  p.q = static_cast<const uint16_t*>(d_q);
+  p.len = d_ctx_len;
+  p.q_indptr = d_q_indptr;
+  p.block_table = d_block_table;
+  p.out = static_cast<uint16_t*>(d_out);
+  p.lse = d_lse;
+  p.status = d_status;
+  p.batch = batch;
+  p.total_rows = total_rows;
+  p.max_new = max_new_len;
+  p.Hq = cache->num_q_heads;
+  p.max_pages_per_seq = max_pages_per_seq;
+  return kv4_attn_run(cache, p, max_ctx_len, sm_scale, d_workspace, workspace_bytes, stream);
+}

@@ -1,0 +1,36 @@
+// Internal interface of the attention over a 4-bit cache.
+#pragma once
+#include "kv4.cuh"
+#include <atomic>
+
+namespace efim {
+
+struct Kv4AttnParams {
+  const uint16_t* q;          // rows of [Hq][D] bf16
+  const int32_t* len;         // [batch] keys of each sequence, its new tokens included, or (len_is_cached) those before them
+  const int32_t* q_indptr;    // [batch + 1], or null: one row a sequence
+  const int32_t* block_table; // [batch][max_pages_per_seq]
+  const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+  uint16_t* out;
+  float* lse;                 // natural log, or null
+  float* part_o;              // [batch][max_new][Hq][n_chunks][D]   (n_chunks > 1)
+  float* part_lse;            // [batch][max_new][Hq][n_chunks]      base-2 log
+  int32_t* status;
+  int batch, total_rows, max_new, Hq, Hkv, max_pages_per_seq, num_pages, row_tiles, chunk_tokens, n_chunks, len_is_cached;
+  int key_cap;                // keys the launch can cover
+  float scale_log2;           // sm_scale * log2(e) * the key pool's scale
+  float v_scale;
+};
+
+struct Kv4Plan {
+  int nt;                     // 8-row tiles of a CTA
+  long long row_tiles;        // CTAs over a sequence's (new token, head of the group) rows
+  int chunk_tokens, n_chunks;
+  size_t lse_bytes, bytes;
+};
+Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_ctx);
+
+// Plans, checks the workspace and launches; `p` holds what the caller's arguments say.
+efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max_ctx, float sm_scale, void* ws, size_t ws_bytes, void* stream);
+
+}  // namespace efim
