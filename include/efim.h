@@ -73,6 +73,7 @@ typedef enum {
 #define EFIM_DEV_TIMEOUT       0x4   /* a bounded wait inside a kernel expired               */
 #define EFIM_DEV_BAD_TOKEN     0x8   /* a drafted token id outside [0, vocab)                */
 #define EFIM_DEV_NO_TOKEN      0x10  /* a distribution without a token to pick (all masked, or NaN) */
+#define EFIM_DEV_NO_PAGE       0x20  /* no free page left to give, or no room to take one back */
 
 const char* efim_strerror(efim_status s);
 /* Text of the CUDA error behind the calling thread's most recent EFIM_ERR_CUDA. */
@@ -445,6 +446,94 @@ efim_status efim_kv4_decode_attn(const efim_cache4_desc* cache, int32_t batch, c
                                  const int32_t* d_block_table, int32_t max_pages_per_seq, const int32_t* d_q_indptr, int32_t total_rows,
                                  int32_t max_new_len, const void* d_q, void* d_out, float* d_lse, float sm_scale, void* d_workspace,
                                  size_t workspace_bytes, int32_t* d_status, void* stream);
+
+/*
+ * Step 2 over a 4-bit cache for a turn's increments, whatever their length: efim_append_prefill_attn on what the cache holds, the new tokens
+ * appended already.  Few rows (new tokens times heads of a group) a sequence go through the kernel of efim_kv4_decode_attn; for more the
+ * batch's pages are unpacked to bf16 in the workspace, exactly, and the tensor-core kernel of efim_append_prefill_attn runs on them.
+ * Arguments, results and errors as for efim_append_prefill_attn (the host mirrors are read during the call, stream capture as
+ * there); rows that see a value that is NaN are NaN there, and may be NaN where a row of the same sequence sees one.
+ * Workspace: efim_kv4_prefill_workspace_bytes() for exactly these lengths, 256-byte aligned.  d_out may be d_q.
+ */
+size_t efim_kv4_prefill_workspace_bytes(const efim_cache4_desc* cache, const efim_batch_desc* batch);
+efim_status efim_kv4_append_prefill_attn(const efim_cache4_desc* cache, const efim_batch_desc* batch, const void* d_q, void* d_out,
+                                         float* d_lse, float sm_scale, void* d_workspace, size_t workspace_bytes, int32_t* d_status,
+                                         void* stream);
+
+/*
+ * Rows and pages of a step from lengths on the device (the paper has no counterpart): what a serving loop needs that goes on from
+ * accepted tokens without asking the host.  Sequence s holds cached_len[s] tokens and gets new_len[s] more:
+ *   q_indptr = exclusive prefix sum of new_len
+ *   places ceil(cached_len[s] / 16) .. ceil((cached_len[s] + new_len[s]) / 16) - 1 of its block-table row that are negative get pages
+ *     free_pages[n - 1], free_pages[n - 2], ..., n = *d_num_free, in the order of sequences and places; pages that are there already (of
+ *     a refused draft) stay.  Without a free page left a place becomes -1 and EFIM_DEV_NO_PAGE is set.
+ *   for new token i of sequence s, at row r = q_indptr[s] + i:  positions[r] = cached_len[s] + i,  sequences[r] = s,
+ *     slots[r] = 16 page + position % 16 (-1 where there is no page);  all three -1 for rows from q_indptr[batch] to rows - 1
+ * d_block_table_out (all other places are copied) and d_num_free_out may be d_block_table and d_num_free; they overlap nothing otherwise.
+ * d_positions, d_slots and d_sequences may each be NULL; new tokens past `rows` have none of them and set EFIM_DEV_BAD_POSITION.
+ * Lengths that are negative count as 0 tokens; those, lengths beyond the table (its places are filled, the tokens beyond get slot -1) and a
+ * number of free pages outside [0, free_capacity], which is clamped, set EFIM_DEV_BAD_POSITION.
+ * Two kernels; may be captured.  Workspace: efim_step_tables_workspace_bytes(batch) bytes (enough for fewer sequences, too), 4-byte
+ * aligned, exclusively this call's until the stream has passed it.
+ */
+size_t efim_step_tables_workspace_bytes(int32_t batch);
+efim_status efim_step_tables(int32_t batch, const int32_t* d_cached_len, const int32_t* d_new_len, const int32_t* d_block_table,
+                             int32_t max_pages_per_seq, const int32_t* d_free_pages, int32_t free_capacity, const int32_t* d_num_free,
+                             int32_t* d_block_table_out, int32_t* d_num_free_out, int32_t* d_q_indptr, int32_t rows, int32_t* d_positions,
+                             int64_t* d_slots, int32_t* d_sequences, void* d_workspace, size_t workspace_bytes, int32_t* d_status,
+                             void* stream);
+/*
+ * The way back: pages of row s from place ceil(keep_len[s] / 16) on (keep_len 0: all of a sequence that is over) go to the end of the
+ * free pages, in the order of sequences and places, and the places become -1.  What free_capacity has no room for stays in the
+ * table and sets EFIM_DEV_NO_PAGE; a row with a negative keep_len is left as it is and sets EFIM_DEV_BAD_POSITION.  Pages that
+ * other rows share are the caller's to keep out.  Workspace as for efim_step_tables.
+ */
+efim_status efim_release_pages(int32_t batch, const int32_t* d_keep_len, int32_t* d_block_table, int32_t max_pages_per_seq,
+                               int32_t* d_free_pages, int32_t free_capacity, int32_t* d_num_free, void* d_workspace,
+                               size_t workspace_bytes, int32_t* d_status, void* stream);
+
+/*
+ * Logits of a step before efim_verify_drafts judges them (the paper has no counterpart).  Row r of sequence s (d_row_indptr, as
+ * there) comes after the sequence's history and its tokens d_tokens[d_row_indptr[s] + 1 .. r] (the drafts before it; the history holds the
+ * pending token already).  Of tokens j that occur there n_j times behind the prompt (the history's first prompt_len[s]):
+ *   x = x > 0 ? x / repetition[s] : x * repetition[s]     for tokens that occur, in the prompt or behind it
+ *   x = x - frequency[s] * n_j - presence[s]              for tokens with n_j > 0
+ *   x = x + bias of the token                             (of a sequence's entries for one token the last one counts)
+ *   x = -inf                                              for tokens whose bit of the mask is 0
+ * in this order, in fp32, rounded once.  Everything but d_row_indptr and d_logits may be NULL: no history, no penalties and no counts; no
+ * d_tokens, no drafts counted; no d_prompt_len, a prompt of 0 tokens; no repetition, 1; no presence or frequency, 0.
+ * The mask: for row r from word r * mask_stride on, token j is allowed iff bit j % 32 of word j / 32 is 1.
+ * Rows of logits and results start logits_stride and out_stride elements apart (at least vocab; any alignment of the type); d_out is d_logits
+ * with the same stride, or overlaps nothing.  Rows outside every sequence's range are left as they were.
+ * Token ids outside [0, vocab) are passed over and set EFIM_DEV_BAD_TOKEN; lengths outside [0, max_len], a prompt longer than its
+ * history, rows and entries beyond total_rows and bias_entries are clamped or passed over and set EFIM_DEV_BAD_POSITION.
+ * One kernel; no workspace; may be captured; the same inputs give the same bits.  vocab and total_rows are at most 2^30.
+ */
+typedef struct {
+  int32_t batch;
+  int32_t total_rows;            /* rows of d_logits, d_tokens, d_mask */
+  int32_t vocab;
+  int32_t logits_f32;            /* 0: bf16 logits, 1: fp32 */
+  const int32_t* d_row_indptr;   /* [batch+1] */
+  const void* d_logits;          /* rows of [vocab] */
+  int64_t logits_stride;
+  const int32_t* d_tokens;       /* [total_rows] */
+  const int32_t* d_history;      /* rows of up to max_len token ids, history_stride elements apart */
+  int64_t history_stride;
+  int32_t max_len;
+  int32_t bias_entries;          /* of d_bias_tokens and d_bias */
+  const int32_t* d_len;          /* [batch] */
+  const int32_t* d_prompt_len;   /* [batch] */
+  const float* d_repetition;     /* [batch], > 0 */
+  const float* d_presence;       /* [batch] */
+  const float* d_frequency;      /* [batch] */
+  const int32_t* d_bias_indptr;  /* [batch+1]: sequence s has entries d_bias_indptr[s] .. d_bias_indptr[s+1]-1 */
+  const int32_t* d_bias_tokens;
+  const float* d_bias;
+  const void* d_mask;            /* 32-bit words */
+  int64_t mask_stride;           /* words */
+} efim_adjust_desc;
+efim_status efim_adjust_logits(const efim_adjust_desc* desc, void* d_out, int64_t out_stride, int32_t* d_status, void* stream);
 
 /*
  * Self-test of the bounded device wait (the paper has no counterpart).  Every wait inside

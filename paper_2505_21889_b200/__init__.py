@@ -11,5 +11,6 @@ from .binding import (  # noqa: F401
     efim_prefill_launch_count, efim_decode_launch_count, Frontend, efim_prefill_plan, efim_decode_step,
     efim_append_prefill_step, efim_selftest_bounded_wait, QkNorm, efim_qk_norm_append, efim_draft_lookup,
     efim_verify_workspace_bytes, efim_verify_drafts, Cache4, efim_kv4_append, efim_kv4_unpack, efim_kv4_decode_workspace_bytes,
-    efim_kv4_decode_attn,
+    efim_kv4_decode_attn, efim_kv4_prefill_workspace_bytes, efim_kv4_append_prefill_attn, efim_step_tables_workspace_bytes,
+    efim_step_tables, efim_release_pages, efim_adjust_logits,
 )

@@ -48,6 +48,15 @@ class _Cache4Desc(Structure):
                 ("head_dim", c_int32), ("k_scale", c_float), ("v_scale", c_float)]
 
 
+class _AdjustDesc(Structure):
+    _fields_ = [("batch", c_int32), ("total_rows", c_int32), ("vocab", c_int32), ("logits_f32", c_int32), ("d_row_indptr", c_void_p),
+                ("d_logits", c_void_p), ("logits_stride", c_int64), ("d_tokens", c_void_p), ("d_history", c_void_p),
+                ("history_stride", c_int64), ("max_len", c_int32), ("bias_entries", c_int32), ("d_len", c_void_p),
+                ("d_prompt_len", c_void_p), ("d_repetition", c_void_p), ("d_presence", c_void_p), ("d_frequency", c_void_p),
+                ("d_bias_indptr", c_void_p), ("d_bias_tokens", c_void_p), ("d_bias", c_void_p), ("d_mask", c_void_p),
+                ("mask_stride", c_int64)]
+
+
 class _VerifyDesc(Structure):
     _fields_ = [("batch", c_int32), ("total_rows", c_int32), ("vocab", c_int32), ("target_kind", c_int32),
                 ("d_row_indptr", c_void_p), ("d_tokens", c_void_p), ("d_target", c_void_p), ("target_stride", c_int64),
@@ -64,6 +73,8 @@ EXPORTS = ("efim_last_cuda_error", "efim_strerror", "efim_version", "efim_rope_t
            "efim_append_prefill_step", "efim_selftest_bounded_wait",
            "efim_qk_norm_append", "efim_draft_lookup", "efim_verify_workspace_bytes", "efim_verify_drafts",
            "efim_kv4_append", "efim_kv4_unpack", "efim_kv4_decode_workspace_bytes", "efim_kv4_decode_attn",
+           "efim_kv4_prefill_workspace_bytes", "efim_kv4_append_prefill_attn",
+           "efim_step_tables_workspace_bytes", "efim_step_tables", "efim_release_pages", "efim_adjust_logits",
            "efim_fragment_cuts", "efim_fim_split", "efim_fim_fragment_spans",
            "efim_frontend_create", "efim_frontend_destroy", "efim_frontend_transform", "efim_frontend_admit",
            "efim_frontend_finish", "efim_frontend_stats")
@@ -130,6 +141,21 @@ def load_library():
     lib.efim_kv4_decode_attn.restype = ctypes.c_int
     lib.efim_kv4_decode_attn.argtypes = [POINTER(_Cache4Desc), c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int32,
                                          c_int32, c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.efim_kv4_prefill_workspace_bytes.restype = c_size_t
+    lib.efim_kv4_prefill_workspace_bytes.argtypes = [POINTER(_Cache4Desc), POINTER(_BatchDesc)]
+    lib.efim_kv4_append_prefill_attn.restype = ctypes.c_int
+    lib.efim_kv4_append_prefill_attn.argtypes = [POINTER(_Cache4Desc), POINTER(_BatchDesc), c_void_p, c_void_p, c_void_p, c_float,
+                                                 c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.efim_step_tables_workspace_bytes.restype = c_size_t
+    lib.efim_step_tables_workspace_bytes.argtypes = [c_int32]
+    lib.efim_step_tables.restype = ctypes.c_int
+    lib.efim_step_tables.argtypes = [c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.efim_release_pages.restype = ctypes.c_int
+    lib.efim_release_pages.argtypes = [c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p,
+                                       c_void_p]
+    lib.efim_adjust_logits.restype = ctypes.c_int
+    lib.efim_adjust_logits.argtypes = [POINTER(_AdjustDesc), c_void_p, c_int64, c_void_p, c_void_p]
     lib.efim_selftest_bounded_wait.restype = ctypes.c_int
     lib.efim_selftest_bounded_wait.argtypes = [ctypes.c_uint64, c_void_p, c_void_p, c_void_p]
     lib.efim_decode_workspace_bytes.restype = c_size_t
@@ -182,7 +208,7 @@ class _Calls:
         loader.exec_module(module)
         for m in ("kv_append", "append_prefill_attn", "append_prefill_step", "decode_attn", "decode_step",
                   "qk_norm_append", "draft_lookup", "verify_workspace_bytes", "verify_drafts",
-                  "kv4_append", "kv4_unpack", "kv4_decode_attn"):
+                  "kv4_append", "kv4_unpack", "kv4_decode_attn", "kv4_append_prefill_attn", "step_tables", "release_pages", "adjust_logits"):
             setattr(self, m, getattr(module, m))          # found directly from now on
         return self.__dict__[name]
 
@@ -432,6 +458,59 @@ def efim_kv4_decode_attn(cache: Cache4, batch: int, d_ctx_len, max_ctx_len, d_bl
                                 sm_scale, workspace, status, _stream_ptr(stream))
     if st != 0:
         raise EfimError(st, "efim_kv4_decode_attn")
+
+
+def efim_kv4_prefill_workspace_bytes(cache: Cache4, batch: Batch) -> int:
+    return int(load_library().efim_kv4_prefill_workspace_bytes(ctypes.byref(cache.desc), ctypes.byref(batch.desc)))
+
+
+def efim_kv4_append_prefill_attn(cache: Cache4, batch: Batch, q, out, lse=None, sm_scale=0.0, workspace=None, status=None, stream=None):
+    """Attention of a turn's new tokens, appended already, over a 4-bit cache."""
+    st = _calls.kv4_append_prefill_attn(_addr(cache.desc), _addr(batch.desc), q, out, lse, sm_scale, workspace, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_kv4_append_prefill_attn")
+
+
+def efim_step_tables_workspace_bytes(batch: int) -> int:
+    return int(load_library().efim_step_tables_workspace_bytes(batch))
+
+
+def _own_workspace(workspace, stream):
+    """A workspace that the call takes itself comes from torch's allocator on torch's current stream."""
+    if workspace is None and stream is not None and _stream_ptr(stream) != _current_stream():
+        raise ValueError("a call on another stream than torch's current one brings its workspace along")
+
+
+def efim_step_tables(cached_len, new_len, block_table, free_pages, num_free, q_indptr, positions=None, slots=None, sequences=None,
+                     block_table_out=None, num_free_out=None, workspace=None, status=None, stream=None):
+    """Row offsets, positions, slots and sequences of a step's new tokens, and pages for them from a stack of free ones, all from
+    lengths on the device.  Without block_table_out and num_free_out those are changed in place; slots are int64, all else int32."""
+    _own_workspace(workspace, stream)
+    st = _calls.step_tables(cached_len, new_len, block_table, free_pages, num_free, q_indptr, positions, slots, sequences, block_table_out,
+                            num_free_out, workspace, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_step_tables")
+
+
+def efim_release_pages(keep_len, block_table, free_pages, num_free, workspace=None, status=None, stream=None):
+    """Pages behind each row's first keep_len tokens back to the stack of free ones."""
+    _own_workspace(workspace, stream)
+    st = _calls.release_pages(keep_len, block_table, free_pages, num_free, workspace, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_release_pages")
+
+
+def efim_adjust_logits(row_indptr, logits, out=None, history=None, lengths=None, prompt_len=None, tokens=None, repetition=None,
+                       presence=None, frequency=None, bias=None, mask=None, status=None, stream=None):
+    """Penalties, biases and grammar masks on a step's rows of logits (bf16 or fp32 [rows, vocab]), in place without `out`.  history: int32
+    [batch, max_len] of `lengths` tokens, the first `prompt_len` of them the prompt; tokens: the step's, whose drafts count for the rows
+    behind them; bias: (entries' offsets by sequence, tokens, values); mask: int32 [rows, ceil(vocab / 32)], a bit per allowed token."""
+    bias_indptr, bias_tokens, bias_values = bias if bias is not None else (None, None, None)
+    _check(bias is None or (bias_tokens.numel() == bias_values.numel()), "the bias has as many tokens as values")
+    st = _calls.adjust_logits(row_indptr, logits, out, row_indptr.shape[0] - 1, history, lengths, prompt_len, tokens, repetition, presence,
+                              frequency, bias_indptr, bias_tokens, bias_values, mask, status, _stream_ptr(stream))
+    if st != 0:
+        raise EfimError(st, "efim_adjust_logits")
 
 
 def efim_prefill_workspace_bytes(cache: Cache, batch: Batch) -> int:

@@ -1,0 +1,217 @@
+// efim_adjust_logits: penalties for tokens that occurred, biases and grammar masks on the rows of a step, before they are judged or sampled.
+//
+// A CTA has one sequence's slice of the vocabulary in shared memory, a word per token: how often it was generated, whether the prompt
+// holds it, and which entry of the bias list it has.  It reads the sequence's history once, then walks the sequence's rows,
+// counting each row's own draft before it (a row's distribution comes after that token).
+#include "common.cuh"
+#include <algorithm>
+#include <atomic>
+
+namespace efim {
+
+struct AdjustParams {
+  const void* logits;           // rows of [vocab], stride elements apart
+  void* out;
+  long long stride, out_stride, history_stride, mask_stride;
+  const int32_t* row_indptr;
+  const int32_t* tokens;        // [total_rows] or null
+  const int32_t* history;       // or null
+  const int32_t *len, *prompt_len;
+  const float *repetition, *presence, *frequency;
+  const int32_t *bias_indptr, *bias_tokens;
+  const float* bias;
+  const uint32_t* mask;
+  int32_t* status;
+  int batch, total_rows, vocab, max_len, bias_entries, entry_shift, slice, slices, vector;
+};
+
+constexpr int ADJUST_THREADS = 512;
+
+// A word of the counts, W: the prompt's bit on top, then the bias entry + 1, from bit p.entry_shift on, then the count.
+template <typename W> constexpr int PROMPT_BIT = sizeof(W) * 8 - 1;
+
+template <typename T> __device__ __forceinline__ float adjust_load(T x);
+template <> __device__ __forceinline__ float adjust_load(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+template <> __device__ __forceinline__ float adjust_load(float x) { return x; }
+template <typename T> __device__ __forceinline__ T adjust_store(float x);
+template <> __device__ __forceinline__ uint16_t adjust_store(float x) { return (uint16_t)pack_bf16x2(x, 0.f); }
+template <> __device__ __forceinline__ float adjust_store(float x) { return x; }
+
+struct Penalties {
+  float repetition, presence, frequency;
+  const float* bias;
+  int entry_shift;
+};
+template <typename W>
+__device__ __forceinline__ float adjusted(float x, W w, bool allowed, const Penalties& q) {
+  if (w) {
+    const W n = w & (((W)1 << q.entry_shift) - 1);
+    if (n || (w >> PROMPT_BIT<W>)) x = x > 0.f ? __fdiv_rn(x, q.repetition) : x * q.repetition;
+    if (n) x = x - q.frequency * (float)n - q.presence;
+    const W entry = (w & (((W)1 << PROMPT_BIT<W>) - 1)) >> q.entry_shift;
+    if (entry) x += *(q.bias + (entry - 1));
+  }
+  return allowed ? x : -INFINITY;
+}
+
+template <typename T, typename W>
+__global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const AdjustParams p) {
+  extern __shared__ __align__(16) uint8_t adjust_smem[];
+  W* slot = reinterpret_cast<W*>(adjust_smem);
+  const int tid = threadIdx.x, s = blockIdx.x / p.slices, part = blockIdx.x % p.slices;
+  const int v0 = part * p.slice, n_slot = min(p.slice, p.vocab - v0);
+  const bool tells = part == 0 && p.status;              // one slice reports what is wrong with the sequence
+  for (int i = tid; i < n_slot; i += ADJUST_THREADS) slot[i] = 0;
+  pdl_wait();
+  pdl_launch();
+  int row0 = *(p.row_indptr + s), row1 = *(p.row_indptr + s + 1), err = 0;
+  if (row0 < 0 || row1 > p.total_rows || row1 < row0) {
+    if (row0 < 0 || row0 > p.total_rows || row1 < row0) row1 = row0 = 0;
+    row1 = min(row1, p.total_rows);
+    err = EFIM_DEV_BAD_POSITION;
+  }
+  Penalties q{p.repetition ? *(p.repetition + s) : 1.f, p.presence ? *(p.presence + s) : 0.f, p.frequency ? *(p.frequency + s) : 0.f, nullptr, p.entry_shift};
+  __syncthreads();
+  if (p.bias) {
+    int b0 = *(p.bias_indptr + s), b1 = *(p.bias_indptr + s + 1);
+    if (b0 < 0 || b1 > p.bias_entries || b1 < b0) {
+      err = EFIM_DEV_BAD_POSITION;
+      b0 = b1 = 0;
+    }
+    q.bias = p.bias + b0;
+    for (int i = tid; i < b1 - b0; i += ADJUST_THREADS) {
+      const int x = *(p.bias_tokens + b0 + i);
+      if (x >= v0 && x < v0 + n_slot) atomicMax(&slot[x - v0], (W)(i + 1) << p.entry_shift);   // the last entry of a token counts
+      if (x < 0 || x >= p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+    }
+    __syncthreads();
+  }
+  if (p.history) {
+    int len = *(p.len + s), prompt = p.prompt_len ? *(p.prompt_len + s) : 0;
+    if (len < 0 || len > p.max_len || prompt < 0 || prompt > len) err |= EFIM_DEV_BAD_POSITION;
+    len = min(max(len, 0), p.max_len);
+    prompt = min(max(prompt, 0), len);
+    const int32_t* history = p.history + s * p.history_stride;
+    for (int i = tid; i < len; i += ADJUST_THREADS) {
+      const int x = *(history + i);
+      if (x >= v0 && x < v0 + n_slot) {
+        if (i < prompt) atomicOr(&slot[x - v0], (W)1 << PROMPT_BIT<W>);
+        else atomicAdd(&slot[x - v0], (W)1);
+      }
+      if (x < 0 || x >= p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+    }
+  }
+  for (int row = row0; row < row1; ++row) {
+    __syncthreads();
+    if (row > row0 && p.history && p.tokens) {
+      if (tid == 0) {
+        const int x = *(p.tokens + row);
+        if (x >= v0 && x < v0 + n_slot) slot[x - v0] += 1;
+        if (x < 0 || x >= p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+      }
+      __syncthreads();
+    }
+    const T* in = static_cast<const T*>(p.logits) + row * p.stride + v0;
+    T* out = static_cast<T*>(p.out) + row * p.out_stride + v0;
+    const uint8_t* mask = p.mask ? reinterpret_cast<const uint8_t*>(p.mask + row * p.mask_stride) + v0 / 8 : nullptr;
+    for (int i = tid * 8; i < n_slot; i += ADJUST_THREADS * 8) {
+      const uint32_t allowed = mask ? *(mask + i / 8) : 0xffu;
+      if (p.vector && i + 8 <= n_slot) {
+        constexpr int WORDS = sizeof(T) / 2;
+        uint4 u[WORDS];
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) u[e] = *(reinterpret_cast<const uint4*>(in + i) + e);
+        T* x = reinterpret_cast<T*>(u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = adjust_store<T>(adjusted<W>(adjust_load<T>(x[e]), slot[i + e], allowed >> e & 1, q));
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) *(reinterpret_cast<uint4*>(out + i) + e) = u[e];
+      } else {
+        for (int e = 0; e < 8 && i + e < n_slot; ++e)
+          out[i + e] = adjust_store<T>(adjusted<W>(adjust_load<T>(in[i + e]), slot[i + e], allowed >> e & 1, q));
+      }
+    }
+  }
+  if (err && tells) atomicOr(p.status, err);
+}
+
+template <typename T, typename W>
+static efim_status adjust_launch(const AdjustParams& p, cudaStream_t stream) {
+  constexpr int kMaxDevices = 64, kMost = 16384 * (int)sizeof(W);
+  static std::atomic<bool> done[kMaxDevices];
+  int dev = 0;
+  EFIM_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices || !done[dev].load(std::memory_order_acquire)) {
+    EFIM_CUDA_TRY(cudaFuncSetAttribute(adjust_logits_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
+    if (dev >= 0 && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
+  }
+  EFIM_CUDA_TRY(launch_pdl(adjust_logits_kernel<T, W>, dim3((unsigned)((long long)p.batch * p.slices)), dim3(ADJUST_THREADS),
+                           p.slice * sizeof(W), stream, p));
+  return EFIM_OK;
+}
+
+}  // namespace efim
+
+extern "C" efim_status efim_adjust_logits(const efim_adjust_desc* d, void* d_out, int64_t out_stride, int32_t* d_status, void* stream) {
+  using namespace efim;
+  if (!d || d->batch < 0 || d->total_rows < 0 || d->vocab <= 0 || (d->logits_f32 != 0 && d->logits_f32 != 1)) return EFIM_ERR_INVALID_ARG;
+  if (d->batch == 0 || d->total_rows == 0) return EFIM_OK;
+  if (d->vocab > 1 << 30 || d->total_rows > 1 << 30) return EFIM_ERR_UNSUPPORTED;
+  auto address = [](const void* x) { return reinterpret_cast<uintptr_t>(x); };
+  const int size = d->logits_f32 ? 4 : 2;
+  if (!d->d_row_indptr || !d->d_logits || !d_out || d->logits_stride < d->vocab || out_stride < d->vocab ||
+      ((address(d->d_logits) | address(d_out)) & (size - 1)))
+    return EFIM_ERR_INVALID_ARG;
+  if (d->d_history && (!d->d_len || d->max_len <= 0 || d->history_stride < d->max_len)) return EFIM_ERR_INVALID_ARG;
+  if (!d->d_history && (d->d_repetition || d->d_presence || d->d_frequency)) return EFIM_ERR_INVALID_ARG;
+  if (d->d_bias && (!d->d_bias_indptr || !d->d_bias_tokens || d->bias_entries < 0)) return EFIM_ERR_INVALID_ARG;
+  if (d->d_mask && d->mask_stride < ((long long)d->vocab + 31) / 32) return EFIM_ERR_INVALID_ARG;
+  if ((address(d->d_row_indptr) | address(d->d_tokens) | address(d->d_history) | address(d->d_len) | address(d->d_prompt_len) |
+       address(d->d_repetition) | address(d->d_presence) | address(d->d_frequency) | address(d->d_bias_indptr) |
+       address(d->d_bias_tokens) | address(d->d_bias) | address(d->d_mask)) & 3)
+    return EFIM_ERR_INVALID_ARG;
+  // in place, or apart: a row of the result must not lie where another one is still to be read
+  const bool in_place = d_out == d->d_logits && out_stride == d->logits_stride;
+  auto span = [&](long long stride) { return (uintptr_t)(((d->total_rows - 1LL) * stride + d->vocab) * size); };
+  if (!in_place && address(d_out) < address(d->d_logits) + span(d->logits_stride) && address(d->d_logits) < address(d_out) + span(out_stride))
+    return EFIM_ERR_INVALID_ARG;
+  AdjustParams p{};
+  p.logits = d->d_logits;
+  p.out = d_out;
+  p.stride = d->logits_stride;
+  p.out_stride = out_stride;
+  p.row_indptr = d->d_row_indptr;
+  p.tokens = d->d_tokens;
+  p.history = d->d_history;
+  p.history_stride = d->history_stride;
+  p.len = d->d_len;
+  p.prompt_len = d->d_prompt_len;
+  p.repetition = d->d_repetition;
+  p.presence = d->d_presence;
+  p.frequency = d->d_frequency;
+  p.bias_indptr = d->d_bias_indptr;
+  p.bias_tokens = d->d_bias_tokens;
+  p.bias = d->d_bias;
+  p.bias_entries = d->bias_entries;
+  p.mask = static_cast<const uint32_t*>(d->d_mask);
+  p.mask_stride = d->mask_stride;
+  p.status = d_status;
+  p.batch = d->batch;
+  p.total_rows = d->total_rows;
+  p.vocab = d->vocab;
+  p.max_len = d->max_len;
+  // whole 16-byte vectors where every row starts on one
+  p.vector = ((address(d->d_logits) | address(d_out) | (uintptr_t)(d->logits_stride * size) | (uintptr_t)(out_stride * size)) & 15) == 0;
+  // 32 bits a word where they hold the largest count, the longest bias list and the prompt's bit, else 64
+  auto bits = [](long long most) { int n = 0; while (most >> n) ++n; return n; };
+  p.entry_shift = bits((long long)d->max_len + d->total_rows);
+  const bool narrow = p.entry_shift + bits(d->d_bias ? d->bias_entries : 0) <= 31;
+  if (!narrow) p.entry_shift = 32;
+  p.slice = narrow ? 16384 : 8192;
+  while (p.slice > 2048 && (long long)d->batch * ((d->vocab + p.slice - 1) / p.slice) < 2LL * sm_count()) p.slice /= 2;
+  p.slices = (d->vocab + p.slice - 1) / p.slice;
+  if ((long long)p.batch * p.slices > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (d->logits_f32) return narrow ? adjust_launch<float, uint32_t>(p, s) : adjust_launch<float, unsigned long long>(p, s);
+  return narrow ? adjust_launch<uint16_t, uint32_t>(p, s) : adjust_launch<uint16_t, unsigned long long>(p, s);
+}

@@ -175,7 +175,7 @@ static PyObject* decode_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 
 /* ---- calls that take shapes and row strides from the tensors themselves */
 static PyObject *s_shape, *s_stride, *s_numel, *s_is_contiguous, *s_dtype, *s_new_empty, *kw_dtype;
-static PyObject *bf16, *f32, *i32, *u8; /* torch's types, looked up by the first such call */
+static PyObject *bf16, *f32, *i32, *i64, *u8; /* torch's types, looked up by the first such call */
 
 static int have_types(void) {
   if (i32) return 1;
@@ -184,9 +184,10 @@ static int have_types(void) {
   bf16 = PyObject_GetAttrString(torch, "bfloat16");
   f32 = PyObject_GetAttrString(torch, "float32");
   u8 = PyObject_GetAttrString(torch, "uint8");
+  i64 = PyObject_GetAttrString(torch, "int64");
   i32 = PyObject_GetAttrString(torch, "int32");
   Py_DECREF(torch);
-  return bf16 && f32 && u8 && i32;
+  return bf16 && f32 && u8 && i64 && i32;
 }
 static int is_tensor(PyObject* o) { return o != Py_None && !PyLong_Check(o) && !PyObject_TypeCheck(o, ndarray); }
 static int is_type(PyObject* o, PyObject* type) { /* -1: no such attribute */
@@ -428,6 +429,170 @@ static PyObject* kv4_decode_attn(PyObject* self, PyObject* const* a, Py_ssize_t 
                                      p[11], ws, p[12], p[13]));
 }
 
+/* cache, batch, q, out, lse, sm_scale, workspace, status, stream */
+static PyObject* kv4_append_prefill_attn(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[9];
+  int64_t rows, row, step;
+  float scale;
+  size_t ws;
+  if (!want(n, 9) || !have_types() || !PTR(0) || !PTR(1)) return NULL;
+  const efim_cache4_desc* c = p[0];
+  rows = ((const efim_batch_desc*)p[1])->total_new_tokens;
+  row = (int64_t)c->num_q_heads * c->head_dim;
+  for (int i = 2; i < 4; ++i)
+    if (!as_matrix(a[i], bf16, i == 2 ? "q" : "out", HEADS, rows, row, &p[i], &step) || !expect(step, row, "q and out, values from one row to the next"))
+      return NULL;
+  if ((a[4] == Py_None ? (p[4] = NULL, 0) : !as_vector(a[4], f32, "lse", rows * c->num_q_heads, &p[4])) || !as_float(a[5], &scale) ||
+      !as_workspace(a[6], &p[6], &ws) || !as_typed(a[7], i32, "status", &p[7]) || !PTR(8))
+    return NULL;
+  RETURN_STATUS(efim_kv4_append_prefill_attn(p[0], p[1], p[2], p[3], p[4], scale, p[6], ws, p[7], p[8]));
+}
+
+/* a vector or None: at least n values */
+static int as_optional(PyObject* o, PyObject* type, const char* what, int64_t n, void** out) {
+  *out = NULL;
+  return o == Py_None || as_vector(o, type, what, n, out);
+}
+static int numel(PyObject* o, int64_t* out) {
+  PyObject* r = PyObject_CallMethodNoArgs(o, s_numel);
+  if (!r) return 0;
+  *out = PyLong_AsLongLong(r);
+  Py_DECREF(r);
+  return !PyErr_Occurred();
+}
+
+/* cached_len, new_len, block_table, free_pages, num_free, q_indptr, positions, slots, sequences, block_table_out or None, num_free_out or
+   None, workspace or None, status, stream */
+static PyObject* step_tables(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[14];
+  int64_t batch, width, step, capacity, rows = -1;
+  size_t ws;
+  PyObject* own = NULL;
+  if (!want(n, 14) || !have_types()) return NULL;
+  if (!as_rows(a[2], i32, "block_table", LINE, &p[2], &batch, &width, &step) || !expect(step, width, "block_table, values from one row to the next") ||
+      !as_vector(a[0], i32, "cached_len", batch, &p[0]) || !as_vector(a[1], i32, "new_len", batch, &p[1]) || !numel(a[3], &capacity) ||
+      !as_vector(a[3], i32, "free_pages", 0, &p[3]) || !as_vector(a[4], i32, "num_free", 1, &p[4]) ||
+      !as_vector(a[5], i32, "q_indptr", batch + 1, &p[5]))
+    return NULL;
+  for (int i = 6; i < 9; ++i) { /* of one length */
+    int64_t m = 0;
+    p[i] = NULL;
+    if (a[i] == Py_None) continue;
+    if (!numel(a[i], &m) || !as_vector(a[i], i == 7 ? i64 : i32, i == 6 ? "positions" : i == 7 ? "slots" : "sequences", m, &p[i]) ||
+        (rows >= 0 && !expect(m, rows, "positions, slots and sequences, values")))
+      return NULL;
+    rows = m;
+  }
+  if (rows < 0) rows = 0;
+  if (rows > INT32_MAX || capacity > INT32_MAX) {
+    PyErr_SetString(PyExc_ValueError, "more rows or free pages than 32 bits count");
+    return NULL;
+  }
+  p[9] = p[2];
+  if (a[9] != Py_None && (!as_matrix(a[9], i32, "block_table_out", LINE, batch, width, &p[9], &step) ||
+                          !expect(step, width, "block_table_out, values from one row to the next")))
+    return NULL;
+  p[10] = p[4];
+  if ((a[10] != Py_None && !as_vector(a[10], i32, "num_free_out", 1, &p[10])) || !as_workspace(a[11], &p[11], &ws) ||
+      !as_typed(a[12], i32, "status", &p[12]) || !PTR(13))
+    return NULL;
+  if (a[11] == Py_None && batch > 0) {
+    ws = efim_step_tables_workspace_bytes((int32_t)batch);
+    if (!(own = bytes_beside(a[0], ws)) || !as_ptr(own, &p[11])) {
+      Py_XDECREF(own);
+      return NULL;
+    }
+  }
+  efim_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = efim_step_tables((int32_t)batch, p[0], p[1], p[2], (int32_t)width, p[3], (int32_t)capacity, p[4], p[9], p[10], p[5], (int32_t)rows, p[6],
+                        p[7], p[8], p[11], ws, p[12], p[13]);
+  Py_END_ALLOW_THREADS
+  Py_XDECREF(own);
+  return PyLong_FromLong(st);
+}
+
+/* keep_len, block_table, free_pages, num_free, workspace or None, status, stream */
+static PyObject* release_pages(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* p[7];
+  int64_t batch, width, step, capacity;
+  size_t ws;
+  PyObject* own = NULL;
+  if (!want(n, 7) || !have_types()) return NULL;
+  if (!as_rows(a[1], i32, "block_table", LINE, &p[1], &batch, &width, &step) || !expect(step, width, "block_table, values from one row to the next") ||
+      !as_vector(a[0], i32, "keep_len", batch, &p[0]) || !numel(a[2], &capacity) || !as_vector(a[2], i32, "free_pages", 0, &p[2]) ||
+      !as_vector(a[3], i32, "num_free", 1, &p[3]) || !as_workspace(a[4], &p[4], &ws) || !as_typed(a[5], i32, "status", &p[5]) || !PTR(6))
+    return NULL;
+  if (capacity > INT32_MAX) {
+    PyErr_SetString(PyExc_ValueError, "more free pages than 32 bits count");
+    return NULL;
+  }
+  if (a[4] == Py_None && batch > 0) {
+    ws = efim_step_tables_workspace_bytes((int32_t)batch);
+    if (!(own = bytes_beside(a[0], ws)) || !as_ptr(own, &p[4])) {
+      Py_XDECREF(own);
+      return NULL;
+    }
+  }
+  efim_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = efim_release_pages((int32_t)batch, p[0], p[1], (int32_t)width, p[2], (int32_t)capacity, p[3], p[4], ws, p[5], p[6]);
+  Py_END_ALLOW_THREADS
+  Py_XDECREF(own);
+  return PyLong_FromLong(st);
+}
+
+/* row_indptr, logits, out or None, batch, history, lengths, prompt_len, tokens, repetition, presence, frequency, bias_indptr, bias_tokens,
+   bias, mask, status, stream */
+static PyObject* adjust_logits(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *out = NULL, *p[17];
+  efim_adjust_desc d;
+  int64_t rows, vocab, histories, max_len = 0, mask_rows, words, entries = 0, out_step;
+  if (!want(n, 17) || !have_types()) return NULL;
+  const int half = is_type(a[1], bf16);
+  if (half < 0 || !as_i32(a[3], &d.batch) || !as_vector(a[0], i32, "row_indptr", (int64_t)d.batch + 1, &p[0]) ||
+      !as_rows(a[1], half ? bf16 : f32, "logits", LINE, &p[1], &rows, &vocab, &d.logits_stride))
+    return NULL;
+  out = p[1];
+  out_step = d.logits_stride;
+  d.history_stride = d.mask_stride = 0;
+  if (a[2] != Py_None && !as_matrix(a[2], half ? bf16 : f32, "out", LINE, rows, vocab, &out, &out_step)) return NULL;
+  if (!as_rows(a[4], i32, "history", LINE, &p[4], &histories, &max_len, &d.history_stride) ||
+      (p[4] && !expect(histories, d.batch, "history, rows")) || !as_optional(a[5], i32, "lengths", d.batch, &p[5]) ||
+      !as_optional(a[6], i32, "prompt_len", d.batch, &p[6]) || !as_optional(a[7], i32, "tokens", rows, &p[7]) ||
+      !as_optional(a[8], f32, "repetition", d.batch, &p[8]) || !as_optional(a[9], f32, "presence", d.batch, &p[9]) ||
+      !as_optional(a[10], f32, "frequency", d.batch, &p[10]) || !as_optional(a[11], i32, "the bias, sequences", (int64_t)d.batch + 1, &p[11]) ||
+      (a[13] != Py_None && !numel(a[13], &entries)) || !as_optional(a[12], i32, "the bias, tokens", entries, &p[12]) ||
+      !as_optional(a[13], f32, "the bias, values", entries, &p[13]) ||
+      !as_rows(a[14], i32, "mask", LINE, &p[14], &mask_rows, &words, &d.mask_stride) ||
+      (p[14] && (!expect(mask_rows, rows, "mask, rows") || !expect(words, (vocab + 31) / 32, "mask, words of a row"))) ||
+      !as_typed(a[15], i32, "status", &p[15]) || !PTR(16))
+    return NULL;
+  if (entries > INT32_MAX) {
+    PyErr_SetString(PyExc_ValueError, "more bias entries than 32 bits count");
+    return NULL;
+  }
+  d.total_rows = (int32_t)rows;
+  d.vocab = (int32_t)vocab;
+  d.logits_f32 = !half;
+  d.d_row_indptr = p[0];
+  d.d_logits = p[1];
+  d.d_tokens = p[7];
+  d.d_history = p[4];
+  d.max_len = (int32_t)max_len;
+  d.bias_entries = (int32_t)entries;
+  d.d_len = p[5];
+  d.d_prompt_len = p[6];
+  d.d_repetition = p[8];
+  d.d_presence = p[9];
+  d.d_frequency = p[10];
+  d.d_bias_indptr = p[11];
+  d.d_bias_tokens = p[12];
+  d.d_bias = p[13];
+  d.d_mask = p[14];
+  RETURN_STATUS(efim_adjust_logits(&d, out, out_step, p[15], p[16]));
+}
+
 static PyMethodDef methods[] = {
     {"kv_append", (PyCFunction)(void*)kv_append, METH_FASTCALL, NULL},
     {"append_prefill_attn", (PyCFunction)(void*)append_prefill_attn, METH_FASTCALL, NULL},
@@ -441,6 +606,10 @@ static PyMethodDef methods[] = {
     {"kv4_append", (PyCFunction)(void*)kv4_append, METH_FASTCALL, NULL},
     {"kv4_unpack", (PyCFunction)(void*)kv4_unpack, METH_FASTCALL, NULL},
     {"kv4_decode_attn", (PyCFunction)(void*)kv4_decode_attn, METH_FASTCALL, NULL},
+    {"kv4_append_prefill_attn", (PyCFunction)(void*)kv4_append_prefill_attn, METH_FASTCALL, NULL},
+    {"step_tables", (PyCFunction)(void*)step_tables, METH_FASTCALL, NULL},
+    {"release_pages", (PyCFunction)(void*)release_pages, METH_FASTCALL, NULL},
+    {"adjust_logits", (PyCFunction)(void*)adjust_logits, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

@@ -53,4 +53,22 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   return r;
 }
 
+// 16 bytes of codes (32 values, two scales) as bf16
+__device__ __forceinline__ void kv4_to_bf16(const uint4& codes, uint32_t two_scales, float g, uint4* dst) {
+  const uint32_t s2 = scales_to_half2(two_scales);
+  const float s[2] = {__half2float(__ushort_as_half((unsigned short)s2)) * g, __half2float(__ushort_as_half((unsigned short)(s2 >> 16))) * g};
+  const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t h[4], r[4];
+    codes_to_half2(word[q], h);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
+      r[e] = pack_bf16x2(f.x * s[q / 2], f.y * s[q / 2]);
+    }
+    dst[q] = make_uint4(r[0], r[1], r[2], r[3]);
+  }
+}
+
 }  // namespace efim

@@ -228,13 +228,10 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
 struct Kv4UnpackParams {
   const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
   uint16_t *k_out, *v_out;          // [n][Hkv][16][D] bf16; either may be null
-  // The pages: d_pages[i], or those of a ragged batch's sequences one after another (out_table: where each went, -1 for bad ones)
   const int32_t* pages;
-  const int32_t *cached_len, *new_len, *block_table;
-  int32_t* out_table;
   int32_t* status;
   float k_scale, v_scale;
-  int n, batch, max_pages_per_seq, out_pages_per_seq, num_pages, Hkv;
+  int num_pages, Hkv;
 };
 
 constexpr int KV4_UNPACK_THREADS = 256;
@@ -260,22 +257,7 @@ __global__ void __launch_bounds__(KV4_UNPACK_THREADS) kv4_unpack_kernel(const Kv
     const size_t at = (size_t)page * per_pool + w;
     const uint4 codes = *reinterpret_cast<const uint4*>((key ? p.k_codes : p.v_codes) + at * 16);
     const uint32_t two = *reinterpret_cast<const uint16_t*>((key ? p.k_scales : p.v_scales) + at * 2);
-    const uint32_t s2 = scales_to_half2(two);
-    const float g = key ? p.k_scale : p.v_scale;
-    const float s[2] = {__half2float(__ushort_as_half((unsigned short)s2)) * g, __half2float(__ushort_as_half((unsigned short)(s2 >> 16))) * g};
-    const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};
-    uint4* dst = reinterpret_cast<uint4*>(out) + ((size_t)i * per_pool + w) * 4;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      uint32_t h[4], r[4];
-      codes_to_half2(word[q], h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
-        r[e] = pack_bf16x2(f.x * s[q / 2], f.y * s[q / 2]);
-      }
-      dst[q] = make_uint4(r[0], r[1], r[2], r[3]);
-    }
+    kv4_to_bf16(codes, two, key ? p.k_scale : p.v_scale, reinterpret_cast<uint4*>(out) + ((size_t)i * per_pool + w) * 4);
   }
 }
 
@@ -380,7 +362,6 @@ extern "C" efim_status efim_kv4_unpack(const efim_cache4_desc* cache, const int3
   p.status = d_status;
   p.k_scale = cache->k_scale;
   p.v_scale = cache->v_scale;
-  p.n = num;
   p.num_pages = cache->num_pages;
   p.Hkv = cache->num_kv_heads;
   EFIM_CUDA_TRY(cache->head_dim == 128 ? launch_pdl(kv4_unpack_kernel<128>, dim3(num), dim3(KV4_UNPACK_THREADS), 0, static_cast<cudaStream_t>(stream), p)
