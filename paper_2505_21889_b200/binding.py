@@ -307,6 +307,23 @@ class Batch:
                                self.h_cached_len.ctypes.data, self.h_new_len.ctypes.data)
 
 
+    @classmethod
+    def from_device(cls, cached_len, new_len, q_indptr, block_table, rows):
+        """A batch whose lengths only the device knows (what efim_step_tables leaves): int32 CUDA tensors, `rows` rows of q, k and v, of which
+        those behind q_indptr's last are not used.  For calls that read no lengths on the host: efim_kv4_append."""
+        torch = _torch()
+        given = (cached_len, new_len, q_indptr, block_table)
+        _check(all(x.dtype == torch.int32 and x.is_contiguous() for x in given) and block_table.dim() == 2,
+               "lengths, row offsets and the block table are packed int32 tensors")
+        n = block_table.shape[0]
+        _check(cached_len.numel() >= n and new_len.numel() >= n and q_indptr.numel() >= n + 1, "a length per sequence, and one more row offset")
+        batch = cls.__new__(cls)
+        batch.d_cached_len, batch.d_new_len, batch.d_q_indptr, batch.d_block_table = given
+        batch.h_cached_len = batch.h_new_len = batch.h_q_indptr = None
+        batch.desc = _BatchDesc(n, block_table.shape[1], rows, *(x.data_ptr() for x in given), None, None)
+        return batch
+
+
 class Rope:
     """Rotary table on the device (built on the host by the library in double)."""
 
@@ -360,7 +377,14 @@ def efim_rope_table_build(base, head_dim, max_position) -> np.ndarray:
     return out
 
 
+def _exact(batch):
+    """Calls that take every row for a new token have no use for rows behind the last sequence."""
+    if batch.h_new_len is None:
+        raise ValueError("a batch whose lengths only the device knows goes to the calls over a 4-bit cache")
+
+
 def efim_kv_append(cache: Cache, batch: Batch, rope, q, k_new, v_new, status=None, stream=None):
+    _exact(batch)
     st = _calls.kv_append(_addr(cache.desc), _addr(batch.desc), _rope_addr(cache, rope),
                           q, k_new, v_new, status, _stream_ptr(stream))
     if st != 0:
@@ -370,6 +394,7 @@ def efim_kv_append(cache: Cache, batch: Batch, rope, q, k_new, v_new, status=Non
 def efim_qk_norm_append(cache: Cache, batch: Batch, norm: QkNorm, rope, q, k, v, q_out, status=None, stream=None):
     """efim_kv_append with a norm of every q and k head before the rotation.  q, k and v: bf16, one row per new token (of any rank
     past the first, packed), views of one buffer allowed; q_out: packed.  q and q_out may both be None."""
+    _exact(batch)
     st = _calls.qk_norm_append(_addr(cache.desc), _addr(batch.desc), _addr(norm.desc), norm.head_dim,
                                _rope_addr(cache, rope), q, k, v, q_out, status, _stream_ptr(stream))
     if st != 0:
