@@ -19,6 +19,7 @@
 #include "token_place.cuh"
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 
 namespace efim {
 
@@ -28,10 +29,12 @@ constexpr float KV4_P_SHIFT = 11.f;     // P's largest value, log2, with the ref
 constexpr float KV4_LAG = 4.f;
 
 __host__ __device__ constexpr int kv4_page_bytes(int D) { return 2 * (kv4_code_bytes(D) + kv4_scale_bytes(D)); }
-__host__ __device__ constexpr int kv4_stages(int NT) { return NT == 4 ? 6 : 4; }
-__host__ __device__ constexpr int kv4_ctas_per_sm(int NT) { return NT == 4 ? 2 : 4; }
+// pages that a warp takes at a time, and sets of them in its ring
+__host__ __device__ constexpr int kv4_pages(int NT) { return NT == 1 ? 2 : 1; }
+__host__ __device__ constexpr int kv4_stages(int NT) { return NT == 1 ? 2 : NT == 2 ? 4 : 6; }
+__host__ __device__ constexpr int kv4_ctas_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
 __host__ __device__ constexpr int kv4_smem_bytes(int D, int NT) {
-  const int ring = KV4_WARPS * kv4_stages(NT) * kv4_page_bytes(D), exchange = KV4_WARPS * 8 * NT * (D + 4) * 4;
+  const int ring = KV4_WARPS * kv4_stages(NT) * kv4_pages(NT) * kv4_page_bytes(D), exchange = KV4_WARPS * 8 * NT * (D + 4) * 4;
   return ring > exchange ? ring : exchange;
 }
 
@@ -107,7 +110,7 @@ __device__ __forceinline__ Kv4Work kv4_work(const Kv4AttnParams& p, int s, int* 
 
 template <int D, int NT>
 __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_kernel(const Kv4AttnParams p) {
-  constexpr int ST = kv4_stages(NT), ROWS = 8 * NT;
+  constexpr int ST = kv4_stages(NT), PG = kv4_pages(NT), ROWS = 8 * NT;
   constexpr int CODES = kv4_code_bytes(D), SCALES = kv4_scale_bytes(D), PAGE = kv4_page_bytes(D);
   constexpr int KS = D / 16;              // k-steps of S^T, m-tiles of O^T
   constexpr int XD = D + 4;               // floats per row of the warps' exchange buffer
@@ -123,9 +126,11 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   pdl_wait();
   pdl_launch();
   const int32_t* bt = p.block_table + (size_t)s * p.max_pages_per_seq;
-  const int begin = c * p.chunk_tokens, first_pg = (begin >> 4) + warp;
+  // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the chunk; lane l holds the id of the l-th of them (then of the next 32)
+  const int begin = c * p.chunk_tokens, first_pg = (begin >> 4) + PG * warp;
+  auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
   int err;
-  const int my_pg = first_pg + KV4_WARPS * lane;
+  const int my_pg = page_of(lane);
   int pid_cache = my_pg < p.max_pages_per_seq ? *(bt + my_pg) : -1;      // (any entry of the row may be read)
   const Kv4Work w = kv4_work(p, s, &err);
   if (err && tid == 0 && p.status) atomicOr(p.status, err);
@@ -137,35 +142,40 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   const int last_limit = min(len, w.cached + (row0 + n_rows - 1) / G + 1);
   const int end = min(last_limit, begin + p.chunk_tokens);
   const int last_pg = (end - 1) >> 4;
-  const int n_pages = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / KV4_WARPS + 1 : 0;
+  const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
 
-  const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * PAGE);
-  const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * PAGE);
-  uint32_t ok_bits = 0;                   // which of the in-flight pages are valid (bit = stage)
-  auto issue = [&](int i, int sg) {       // send for this warp's i-th page into stage sg
-    if (i < n_pages) {
-      const int pid = __shfl_sync(0xffffffffu, pid_cache, i & 31);
-      const bool ok = pid >= 0 && pid < p.num_pages;
-      ok_bits = (ok_bits & ~(1u << sg)) | (ok ? 1u << sg : 0u);
-      if (ok) {
-        const size_t at = (size_t)pid * p.Hkv + kvh;
-        const uint32_t dst = ring + sg * PAGE;
-        const uint8_t *k = p.k_codes + at * CODES, *v = p.v_codes + at * CODES;
+  const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * PG * PAGE);
+  const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * PG * PAGE);
+  constexpr int PIECES = CODES / 16, PS = SCALES / 16;                    // 16-byte pieces of a page's codes, of its scales
+  // where this lane's pieces come from and go to (a lane below 2 PS also has one of K's or V's scales)
+  const uint8_t *k_src = p.k_codes + lane * 16, *v_src = p.v_codes + lane * 16;
+  const uint8_t* s_src = lane < PS ? p.k_scales + lane * 16 : p.v_scales + (lane - PS) * 16;
+  const uint32_t k_dst = ring + lane * 16, v_dst = ring + CODES + kv4_v_piece<D>(lane / (D / 32), lane % (D / 32)), s_dst = k_dst + 2 * CODES;
+  uint32_t ok_bits = 0;                   // which of the in-flight pages are valid (bit = stage * PG + page)
+  auto issue = [&](int i, int sg) {       // send for the pages of this warp's i-th trip into stage sg
+    if (i < n_trips) {
 #pragma unroll
-        for (int u = lane; u < CODES / 16; u += 32) {
-          kv4_cp16(dst + u * 16, k + u * 16);
-          kv4_cp16(dst + CODES + kv4_v_piece<D>(u / (D / 32), u % (D / 32)), v + u * 16);
+      for (int x = 0; x < PG; ++x) {
+        const int pid = __shfl_sync(0xffffffffu, pid_cache, (i * PG + x) & 31);
+        const bool ok = (uint32_t)pid < (uint32_t)p.num_pages;
+        const uint32_t bit = 1u << (sg * PG + x), to = (sg * PG + x) * PAGE;
+        ok_bits &= ~bit;
+        if (ok) {
+          ok_bits |= bit;
+          const uint32_t at = (uint32_t)pid * p.Hkv + kvh;
+          const uint8_t *k = k_src + (uint64_t)at * CODES, *v = v_src + (uint64_t)at * CODES;
+#pragma unroll
+          for (int u = 0; u < PIECES; u += 32) {
+            kv4_cp16(k_dst + to + u * 16, k + u * 16);
+            kv4_cp16(v_dst + to + u * 16, v + u * 16);
+          }
+          if (lane < 2 * PS) kv4_cp16(s_dst + to, s_src + (uint64_t)at * SCALES);
+        } else if (page_of(i * PG + x) <= last_pg && lane == 0 && p.status) {
+          atomicOr(p.status, EFIM_DEV_BAD_PAGE);
         }
-        constexpr int PS = SCALES / 16;
-        if (lane < 2 * PS) {
-          const uint8_t* sc = lane < PS ? p.k_scales + at * SCALES + lane * 16 : p.v_scales + at * SCALES + (lane - PS) * 16;
-          kv4_cp16(dst + 2 * CODES + lane * 16, sc);
-        }
-      } else if (lane == 0 && p.status) {
-        atomicOr(p.status, EFIM_DEV_BAD_PAGE);
       }
-      if (((i + 1) & 31) == 0) {          // the next 32 of this warp's pages
-        const int pg = first_pg + KV4_WARPS * (i + 1 + lane);
+      if (((i * PG + PG) & 31) == 0) {    // the next 32 of this warp's pages
+        const int pg = page_of(i * PG + PG + lane);
         pid_cache = pg <= last_pg ? *(bt + pg) : -1;
       }
     }
@@ -206,7 +216,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       const int d = lane * (D / 32) + e;
       *reinterpret_cast<uint32_t*>(&s_q[r][d % (D / 4) / 4 * 16 + d / (D / 4) * 4 + d % 4]) = kv4_pack_half2(lo, hi);
     }
-    if (lane == 0) s_scale[r] = fminf(p.scale_log2 / down, FLT_MAX);     // (a power of two: exact)
+    if (lane == 0) s_scale[r] = fmaxf(fminf(p.scale_log2 / down, FLT_MAX), FLT_MIN);   // (by a power of two: exact)
     if (lane < 8) s_nan[r][lane] = 0;
   }
   __syncthreads();
@@ -223,7 +233,9 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       }
   }
   float o[NT][KS][4];                     // O^T: dims g D/8 + 2 k + (e / 2), rows 8 n + 2 t + (e % 2)
-  float m_ref[NT][2], l_part[NT][2], sc[NT][2];
+  // Scores stay as the products leave them; times sc they are in log2.  Per row: the score that the reference stands at, the one from which
+  // on it moves, and what is taken off a score (in log2, KV4_P_SHIFT less than the reference).  Before any score: p = 2^(-inf) = 0.
+  float m_next[NT][2], m_off[NT][2], l_part[NT][2], sc[NT][2];
   int limit[NT][2];                       // keys that rows 8 n + 2 t + {0, 1} see
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -234,7 +246,8 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int r = n * 8 + 2 * t + e;
-      m_ref[n][e] = -FLT_MAX;
+      m_next[n][e] = -FLT_MAX;
+      m_off[n][e] = -KV4_P_SHIFT;
       l_part[n][e] = 0.f;
       sc[n][e] = s_scale[r];
       limit[n][e] = min(end, w.cached + (row0 + min(r, n_rows - 1)) / G + 1);
@@ -242,81 +255,103 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   }
   const int first_limit = min(end, w.cached + row0 / G + 1);
   const int tok0 = kv4_token(g >> 1, g & 1, 0);             // this lane's key in S^T; the other is 8 on
+  // this lane's places in a staged page
+  const uint8_t* k_at = ring_ptr + (D == 128 ? tok0 * 64 + t * 16 : tok0 * 32 + t * 8);
+  const uint8_t* ks_at = ring_ptr + 2 * CODES + (D == 128 ? tok0 * 8 + 2 * t : tok0 * 4 + t);
+  const uint8_t *v_at[2], *vs_at[2];                        // of tokens 2t, 2t+1 (the others are 8 rows on)
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int token = kv4_token(t, e, 0);
+    v_at[e] = ring_ptr + CODES + (D == 128 ? kv4_v_piece<D>(token, g >> 1) + (g & 1) * 8 : kv4_v_piece<D>(token, g >> 2) + (g & 3) * 4);
+    vs_at[e] = ring_ptr + 2 * CODES + SCALES + (D == 128 ? token * 8 + g : token * 4 + (g >> 1));
+  }
 
-  for (int i = 0; i < n_pages; ++i) {
-    const int sg = i % ST;
+  int sg = 0;
+  for (int i = 0; i < n_trips; ++i) {
     asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
     __syncwarp();
-    issue(i + ST - 1, (i + ST - 1) % ST);                   // into the stage that the last trip has left
-    if (!((ok_bits >> sg) & 1u)) continue;
-    const uint8_t* page = ring_ptr + sg * PAGE;
-    const int key0 = (first_pg + KV4_WARPS * i) << 4;
+    issue(i + ST - 1, sg == 0 ? ST - 1 : sg - 1);           // into the stage that the last trip has left
+    int key0[PG];                                           // first keys; past every limit where there is no page
+    bool border = false;                                    // some row does not see all of the pages
+#pragma unroll
+    for (int x = 0; x < PG; ++x) {
+      key0[x] = (ok_bits >> (sg * PG + x)) & 1u ? page_of(i * PG + x) << 4 : INT_MAX - 16;
+      border |= key0[x] + 16 > first_limit;
+    }
+    const uint32_t at = sg * PG * PAGE;
+    if (++sg == ST) sg = 0;
+    if (PG == 1 && key0[0] == INT_MAX - 16) continue;
     // ---- S^T
-    float sx[NT][4];
+    float sx[PG][NT][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int x = 0; x < PG; ++x) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sx[n][e] = 0.f;
-    {
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sx[x][n][e] = 0.f;
       uint32_t scale[2][D / 64];           // of the two tokens, per block of 16 dims: the pair (s, s)
       uint32_t kw[2][D / 32];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int token = tok0 + 8 * h;
         if constexpr (D == 128) {
-          const uint4 u = *reinterpret_cast<const uint4*>(page + token * 64 + t * 16);
+          const uint4 u = *reinterpret_cast<const uint4*>(k_at + at + x * PAGE + h * 512);
           kw[h][0] = u.x, kw[h][1] = u.y, kw[h][2] = u.z, kw[h][3] = u.w;
-          const uint32_t two = scales_to_half2(*reinterpret_cast<const uint16_t*>(page + 2 * CODES + token * 8 + 2 * t));
+          const uint32_t two = scales_to_half2(*reinterpret_cast<const uint16_t*>(ks_at + at + x * PAGE + h * 64));
           scale[h][0] = __byte_perm(two, 0, 0x1010);
           scale[h][1] = __byte_perm(two, 0, 0x3232);
         } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(page + token * 32 + t * 8);
+          const uint2 u = *reinterpret_cast<const uint2*>(k_at + at + x * PAGE + h * 256);
           kw[h][0] = u.x, kw[h][1] = u.y;
-          scale[h][0] = __byte_perm(scales_to_half2(page[2 * CODES + token * 4 + t]), 0, 0x1010);
+          scale[h][0] = __byte_perm(scales_to_half2(ks_at[at + x * PAGE + h * 32]), 0, 0x1010);
         }
       }
 #pragma unroll
       for (int q = 0; q < D / 32; ++q) {   // 8 dims of each token: two k-steps
-        uint32_t x[2][4];
+        uint32_t kx[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          codes_to_half2(kw[h][q], x[h]);
+          codes_to_half2(kw[h][q], kx[h]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[h][e] = mul_half2(x[h][e], scale[h][q / 2]);
+          for (int e = 0; e < 4; ++e) kx[h][e] = mul_half2(kx[h][e], scale[h][q / 2]);
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t a[4] = {x[0][2 * k], x[1][2 * k], x[0][2 * k + 1], x[1][2 * k + 1]};
+          const uint32_t a[4] = {kx[0][2 * k], kx[1][2 * k], kx[0][2 * k + 1], kx[1][2 * k + 1]};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             if constexpr (Q_IN_REGS) {
-              kv4_mma(sx[n], a, qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
+              kv4_mma(sx[x][n], a, qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
             } else {
               const uint2 u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
-              kv4_mma(sx[n], a, u.x, u.y);
+              kv4_mma(sx[x][n], a, u.x, u.y);
             }
           }
         }
       }
     }
-    // ---- scores, in log2, and the reference
-    const bool border = key0 + 16 > first_limit;            // some row does not see the whole page
+    if (border) {
+#pragma unroll
+      for (int x = 0; x < PG; ++x)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key0[x] + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[x][n][e] = -INFINITY;
+    }
+    // ---- the reference
     bool grow = false;
     float mx[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        sx[n][e] *= sc[n][e & 1];
-        if (border && key0 + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[n][e] = -INFINITY;
-      }
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        mx[n][e] = fmaxf(sx[n][e], sx[n][e + 2]);
-        grow |= mx[n][e] > m_ref[n][e] + KV4_LAG;
+        mx[n][e] = fmaxf(sx[0][n][e], sx[0][n][e + 2]);
+#pragma unroll
+        for (int x = 1; x < PG; ++x) mx[n][e] = fmaxf(mx[n][e], fmaxf(sx[x][n][e], sx[x][n][e + 2]));
+        grow |= mx[n][e] > m_next[n][e];
       }
-    }
-    // Lazy rescale: the reference of a row only moves when a score exceeds it by more than 2^4 (always on the first page)
+    // Lazy rescale: the reference of a row only moves when a score exceeds it by more than 2^4 (always at the first), and each row's by its
+    // own scores: its bits do not depend on the other rows.
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -325,84 +360,90 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
           float x = mx[n][e];
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
-          const float m_new = x > m_ref[n][e] + KV4_LAG ? x : m_ref[n][e];     // (each row by its own scores: its bits do not depend on the others')
-          const float alpha = kv4_ex2(m_ref[n][e] - m_new);
-          m_ref[n][e] = m_new;
-          l_part[n][e] *= alpha;
+          if (x > m_next[n][e]) {
+            float off = fmaf(x, sc[n][e], -KV4_P_SHIFT);
+            if (!(fabsf(off) <= FLT_MAX)) off = NAN;        // scores that leave fp32
+            const float alpha = m_next[n][e] == -FLT_MAX ? 0.f : kv4_ex2(m_off[n][e] - off);
+            m_next[n][e] = x + KV4_LAG / sc[n][e];
+            m_off[n][e] = off;
+            l_part[n][e] *= alpha;
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            o[n][k][e] *= alpha;
-            o[n][k][e + 2] *= alpha;
+            for (int k = 0; k < KS; ++k) {
+              o[n][k][e] *= alpha;
+              o[n][k][e + 2] *= alpha;
+            }
           }
         }
     }
-    uint32_t pb[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int x = 0; x < PG; ++x) {
+      uint32_t pb[NT][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float x0 = kv4_ex2(sx[n][2 * h] - m_ref[n][0] + KV4_P_SHIFT), x1 = kv4_ex2(sx[n][2 * h + 1] - m_ref[n][1] + KV4_P_SHIFT);
-        l_part[n][0] += x0;
-        l_part[n][1] += x1;
-        pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
-      }
-    // ---- O^T
-    uint32_t scale[2];                     // of tokens (2t, 2t+1) and (2t+8, 2t+9)
-    uint32_t vw[2][2][D / 64];
-    const uint8_t* vp = page + CODES;
-    uint32_t bytes = 0;
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int token = kv4_token(t, e, h);
-        uint32_t b;
-        if constexpr (D == 128) {
-          const uint2 u = *reinterpret_cast<const uint2*>(vp + kv4_v_piece<D>(token, g >> 1) + (g & 1) * 8);
-          vw[h][e][0] = u.x, vw[h][e][1] = u.y;
-          b = page[2 * CODES + SCALES + token * 8 + g];
-        } else {
-          vw[h][e][0] = *reinterpret_cast<const uint32_t*>(vp + kv4_v_piece<D>(token, g >> 2) + (g & 3) * 4);
-          b = page[2 * CODES + SCALES + token * 4 + (g >> 1)];
+        for (int h = 0; h < 2; ++h) {
+          const float x0 = kv4_ex2(fmaf(sx[x][n][2 * h], sc[n][0], -m_off[n][0])), x1 = kv4_ex2(fmaf(sx[x][n][2 * h + 1], sc[n][1], -m_off[n][1]));
+          l_part[n][0] += x0;
+          l_part[n][1] += x1;
+          pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
         }
+      // ---- O^T
+      uint32_t vw[2][2][D / 64], b[2][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if constexpr (D == 128) {
+            const uint2 u = *reinterpret_cast<const uint2*>(v_at[e] + at + x * PAGE + h * 512);
+            vw[h][e][0] = u.x, vw[h][e][1] = u.y;
+            b[h][e] = vs_at[e][at + x * PAGE + h * 64];
+          } else {
+            vw[h][e][0] = *reinterpret_cast<const uint32_t*>(v_at[e] + at + x * PAGE + h * 256);
+            b[h][e] = vs_at[e][at + x * PAGE + h * 32];
+          }
+        }
+      // scales of tokens (2t, 2t+1) and (2t+8, 2t+9)
+      uint32_t bytes = __byte_perm(__byte_perm(b[0][0], b[0][1], 0x5540), __byte_perm(b[1][0], b[1][1], 0x5540), 0x5410);
+      if (border) {
         // what stands behind the last key is anything, a NaN's scale too: P is 0 there, 0 times NaN is not
-        if (border && key0 + token >= end) b = 0;
-        bytes |= b << (16 * h + 8 * e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (key0[x] + kv4_token(t, q & 1, q >> 1) >= end) bytes &= ~(0xffu << (8 * q));
       }
-    // Values that are NaN: rows that see them are marked and get their NaN at the end; in the products they are zeros, since rows that
-    // do not see them have a P of 0 there.
-    if (__any_sync(0xffffffffu, __vcmpeq4(bytes & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0)) {
+      // Values that are NaN: rows that see them are marked and get their NaN at the end; in the products they are zeros, since rows that
+      // do not see them have a P of 0 there.
+      if (__any_sync(0xffffffffu, ((bytes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) {
 #pragma unroll 1
-      for (int q = 0; q < 4; ++q) {
-        if (((bytes >> (8 * q)) & 0x7f) != 0x7f) continue;
-        bytes &= ~(0xffu << (8 * q));
-        const int key = key0 + kv4_token(t, q & 1, q >> 1);
-        for (int r = 0; r < n_rows; ++r)
-          if (key < min(end, w.cached + (row0 + r) / G + 1)) s_nan[r][g] = 1;
+        for (int q = 0; q < 4; ++q) {
+          if (((bytes >> (8 * q)) & 0x7f) != 0x7f) continue;
+          bytes &= ~(0xffu << (8 * q));
+          const int key = key0[x] + kv4_token(t, q & 1, q >> 1);
+          for (int r = 0; r < n_rows; ++r)
+            if (key < min(end, w.cached + (row0 + r) / G + 1)) s_nan[r][g] = 1;
+        }
       }
-    }
-    scale[0] = scales_to_half2(bytes & 0xffff);
-    scale[1] = scales_to_half2(bytes >> 16);
+      const uint32_t scale[2] = {scales_to_half2(bytes & 0xffff), scales_to_half2(bytes >> 16)};
 #pragma unroll
-    for (int q = 0; q < D / 64; ++q) {
-      // lo: even dims of the two tokens side by side, hi: odd dims
-      uint32_t lo[2][4], hi[2][4];
+      for (int q = 0; q < D / 64; ++q) {
+        // lo: even dims of the two tokens side by side, hi: odd dims
+        uint32_t lo[2][4], hi[2][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t a = vw[h][0][q], b = vw[h][1][q];
-        codes_to_half2((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), lo[h]);
-        codes_to_half2(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), hi[h]);
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t a0 = vw[h][0][q], a1 = vw[h][1][q];
+          codes_to_half2((a0 & 0x0f0f0f0fu) | ((a1 << 4) & 0xf0f0f0f0u), lo[h]);
+          codes_to_half2(((a0 >> 4) & 0x0f0f0f0fu) | (a1 & 0xf0f0f0f0u), hi[h]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            lo[h][e] = mul_half2(lo[h][e], scale[h]);
+            hi[h][e] = mul_half2(hi[h][e], scale[h]);
+          }
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          lo[h][e] = mul_half2(lo[h][e], scale[h]);
-          hi[h][e] = mul_half2(hi[h][e], scale[h]);
+          const uint32_t a[4] = {lo[0][e], hi[0][e], lo[1][e], hi[1][e]};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
         }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t a[4] = {lo[0][e], hi[0][e], lo[1][e], hi[1][e]};
-#pragma unroll
-        for (int n = 0; n < NT; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
       }
     }
   }
@@ -416,7 +457,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       for (int off = 4; off < 32; off <<= 1) l_part[n][e] += __shfl_xor_sync(0xffffffffu, l_part[n][e], off);
       if (lane < 4) {
         s_l[warp][n * 8 + 2 * lane + e] = l_part[n][e];
-        s_m[warp][n * 8 + 2 * lane + e] = m_ref[n][e];
+        s_m[warp][n * 8 + 2 * lane + e] = m_next[n][e] == -FLT_MAX ? -FLT_MAX : m_off[n][e];   // (of a warp that saw nothing: no weight)
       }
     }
   __syncthreads();
@@ -448,7 +489,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     }
     float inv = L == 0.f ? 0.f : p.v_scale / L;
     if (s_nan[r][d / (D / 8)]) inv = NAN;
-    const float lse2 = L == 0.f ? -INFINITY : M - KV4_P_SHIFT + log2f(L);      // (a sum of NaN stays NaN)
+    const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);      // (a sum of NaN stays NaN)
     const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
     const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
     if (p.n_chunks == 1) {
