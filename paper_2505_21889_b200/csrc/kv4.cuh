@@ -47,10 +47,10 @@ __device__ __forceinline__ void codes_to_half2(uint32_t word, uint32_t* r) {
       "cvt.rn.f16x2.e2m1x2 %2, c;\ncvt.rn.f16x2.e2m1x2 %3, d;\n}"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(word));
 }
-__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, __half2 b) {
+  const __half2 r = __hmul2(as_half2(a), b);
+  return *reinterpret_cast<const uint32_t*>(&r);
 }
 
 // 16 bytes of codes (32 values, two scales) as bf16

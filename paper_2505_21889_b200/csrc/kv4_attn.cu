@@ -58,6 +58,12 @@ __device__ __forceinline__ void kv4_mma(float* c, const uint32_t* a, uint32_t b0
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// c = a b
+__device__ __forceinline__ void kv4_mma_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ float kv4_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -73,15 +79,16 @@ __device__ __forceinline__ void kv4_cp16(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ uint32_t kv4_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// What a CTA works on.
-struct Kv4Work {
-  int ctx;        // keys of the sequence, clamped to what the launch covers
-  int first_row;  // the sequence's first row of q
+// A sequence's part of the call.
+struct Kv4Seq {
+  int ctx;        // keys, clamped to what the launch covers
+  int first_row;  // its first row of q
   int new_len;    // its rows of q that are computed
   int cached;     // keys before its first new token
+  int err;
 };
-__device__ __forceinline__ Kv4Work kv4_work(const Kv4AttnParams& p, int s, int* err) {
-  Kv4Work w;
+__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4AttnParams& p, int s) {
+  Kv4Seq w;
   w.first_row = s;
   w.new_len = 1;
   if (p.q_indptr) {
@@ -92,24 +99,42 @@ __device__ __forceinline__ Kv4Work kv4_work(const Kv4AttnParams& p, int s, int* 
   if (p.len_is_cached) ctx += w.new_len;
   w.cached = ctx - w.new_len;
   w.ctx = ctx;
-  *err = 0;
+  w.err = 0;
   if (w.first_row < 0 || w.new_len < 0 || w.new_len > p.total_rows - w.first_row) {   // rows that were not given
-    *err = EFIM_DEV_BAD_POSITION;
+    w.err = EFIM_DEV_BAD_POSITION;
     w.new_len = 0;
   }
   if (w.new_len > p.max_new) {
-    *err = EFIM_DEV_BAD_POSITION;
+    w.err = EFIM_DEV_BAD_POSITION;
     w.new_len = p.max_new;
   }
   if (w.ctx > p.key_cap) {
-    *err = EFIM_DEV_BAD_POSITION;
+    w.err = EFIM_DEV_BAD_POSITION;
     w.ctx = p.key_cap;
   }
+  w.ctx = max(w.ctx, 0);
   return w;
 }
 
+// The work of a call is a line of trips (a trip: PG pages by each of a CTA's warps), unit after unit: (sequence, kv head, tile of rows).  Each CTA has
+// an equal piece of the line, so all end together whatever the lengths are; a unit that lies in one piece is finished
+// there, the pieces of the others leave partial results, which a second kernel joins.  A piece has at most two such: of a unit that began before it
+// (kept in the CTA's first place), and of one that goes on behind it (second place).
+template <int NT>
+struct Kv4Line {
+  static constexpr int TRIP = 16 * KV4_WARPS * kv4_pages(NT);              // keys of a trip
+  static __device__ __forceinline__ int trips(const Kv4Seq& w) { return max(1, (w.ctx + TRIP - 1) / TRIP); }
+  static __device__ __forceinline__ int tiles(const Kv4Seq& w, int G) { return (w.new_len * G + 8 * NT - 1) / (8 * NT); }
+};
+// what a CTA leaves for the joining kernel
+struct Kv4Piece {
+  int seq, head, tile;    // of the unit that goes on behind it; seq -1: none
+  int first_ends;         // the unit that began before it ends in it
+};
+
 template <int D, int NT>
 __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_kernel(const Kv4AttnParams p) {
+  using Line = Kv4Line<NT>;
   constexpr int ST = kv4_stages(NT), PG = kv4_pages(NT), ROWS = 8 * NT;
   constexpr int CODES = kv4_code_bytes(D), SCALES = kv4_scale_bytes(D), PAGE = kv4_page_bytes(D);
   constexpr int KS = D / 16;              // k-steps of S^T, m-tiles of O^T
@@ -119,30 +144,104 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   __shared__ __align__(16) uint16_t s_q[ROWS][D + 16];    // fp16, shifted; dim t D/4 + 4k + x at 16k + 4t + x
   __shared__ float s_m[KV4_WARPS][ROWS], s_l[KV4_WARPS][ROWS], s_scale[ROWS];
   __shared__ uint8_t s_nan[ROWS][8];      // rows that see a NaN value in dims [g D/8, (g+1) D/8)
+  __shared__ long long s_sum[KV4_WARPS];
+  __shared__ long long s_at;              // trips of the line before the sequence that this CTA begins with
+  __shared__ int s_seq;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int tiles = p.row_tiles, s = blockIdx.x / tiles, tile = blockIdx.x % tiles, kvh = blockIdx.y, c = blockIdx.z;
   const int G = p.Hq / p.Hkv;
   pdl_wait();
   pdl_launch();
-  const int32_t* bt = p.block_table + (size_t)s * p.max_pages_per_seq;
-  // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the chunk; lane l holds the id of the l-th of them (then of the next 32)
-  const int begin = c * p.chunk_tokens, first_pg = (begin >> 4) + PG * warp;
+  // ---- this CTA's piece of the line
+  long long x0, x1;                       // in trips
+  int seq, off;                           // its first sequence, and the trips of that one before it
+  if (p.whole) {                          // units that are never cut, one a CTA
+    seq = blockIdx.x / p.units_per_seq;
+    x0 = x1 = off = 0;
+  } else {
+    const int per = (p.batch + KV4_THREADS - 1) / KV4_THREADS, first = min(p.batch, tid * per), last = min(p.batch, first + per);
+    auto weight = [&](int i) {
+      const Kv4Seq w = kv4_seq(p, i);
+      return (long long)Line::trips(w) * Line::tiles(w, G) * p.Hkv;
+    };
+    long long mine = 0;
+    for (int i = first; i < last; ++i) mine += weight(i);
+    long long upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += y;
+    }
+    if (lane == 31) s_sum[warp] = upto;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int i = 0; i < KV4_WARPS; ++i) {
+      if (i < warp) upto += s_sum[i];
+      total += s_sum[i];
+    }
+    const long long share = max((long long)p.least_trips, (total + gridDim.x - 1) / gridDim.x);
+    x0 = blockIdx.x * share;
+    x1 = min(total, x0 + share);
+    if (x0 >= total) {
+      if (tid == 0) p.pieces[blockIdx.x] = Kv4Piece{-1, 0, 0, 1};
+      return;
+    }
+    if (x0 >= upto - mine && x0 < upto) {
+      long long at = upto - mine;
+      int i = first;
+      for (; i < last - 1; ++i) {
+        const long long y = weight(i);
+        if (x0 < at + y) break;
+        at += y;
+      }
+      s_seq = i;
+      s_at = at;
+    }
+    __syncthreads();
+    seq = s_seq;
+    off = (int)min(x0 - s_at, 0x7fffffffLL);
+  }
+  Kv4Seq w = kv4_seq(p, seq);
+  int unit, trip0;                        // of the sequence's units (kv head, tile): the one at hand, and its trips that are done
+  if (p.whole) {
+    unit = blockIdx.x % p.units_per_seq;
+    trip0 = 0;
+    const int tiles = Line::tiles(w, G);
+    if (w.err && unit == 0 && tid == 0 && p.status) atomicOr(p.status, w.err);
+    if (unit / p.row_tiles >= p.Hkv || unit % p.row_tiles >= tiles) return;
+    unit = unit / p.row_tiles * tiles + unit % p.row_tiles;
+    x1 = Line::trips(w);
+  } else {
+    const int n = Line::trips(w);
+    unit = off / n;
+    trip0 = off % n;
+  }
+  Kv4Piece left{-1, 0, 0, 0};
+  bool first_part = trip0 != 0;           // the unit at hand began before this piece
+  if (!p.whole && blockIdx.x == 0)        // one CTA reports the lengths that do not fit
+    for (int i = tid; i < p.batch; i += KV4_THREADS)
+      if (const int err = kv4_seq(p, i).err; err && p.status) atomicOr(p.status, err);
+
+  while (x0 < x1) {
+  const int tiles = Line::tiles(w, G);
+  const int kvh = unit / tiles, tile = unit % tiles;
+  const int unit_trips = Line::trips(w), here = (int)min((long long)(unit_trips - trip0), x1 - x0);   // trips of the unit in this piece
+  const bool ends = trip0 + here == unit_trips;
+  const int32_t* bt = p.block_table + (size_t)seq * p.max_pages_per_seq;
+  // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece; lane l holds the id of the l-th of them (then of the next 32)
+  const int begin = trip0 * Line::TRIP, first_pg = (begin >> 4) + PG * warp;
   auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
-  int err;
-  const int my_pg = page_of(lane);
-  int pid_cache = my_pg < p.max_pages_per_seq ? *(bt + my_pg) : -1;      // (any entry of the row may be read)
-  const Kv4Work w = kv4_work(p, s, &err);
-  if (err && tid == 0 && p.status) atomicOr(p.status, err);
   const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
-  if (n_rows <= 0) return;
-  const int len = max(w.ctx, 0);
-  if (begin >= len && !(len == 0 && c == 0)) return;
-  // keys that the tile's last row sees
-  const int last_limit = min(len, w.cached + (row0 + n_rows - 1) / G + 1);
-  const int end = min(last_limit, begin + p.chunk_tokens);
+  // keys that the tile's last row sees, of this piece
+  const int end = min(min(w.ctx, w.cached + (row0 + n_rows - 1) / G + 1), begin + here * Line::TRIP);
   const int last_pg = (end - 1) >> 4;
   const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
+  int pid_cache = -1;
+  {
+    const int pg = page_of(lane);
+    if (pg <= last_pg) pid_cache = *(bt + pg);
+  }
 
   const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * PG * PAGE);
   const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * PG * PAGE);
@@ -268,9 +367,10 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 
   int sg = 0;
   for (int i = 0; i < n_trips; ++i) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
+    __syncwarp();                                           // everyone is done with the stage of the last trip
+    issue(i + ST - 1, sg == 0 ? ST - 1 : sg - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
     __syncwarp();
-    issue(i + ST - 1, sg == 0 ? ST - 1 : sg - 1);           // into the stage that the last trip has left
     int key0[PG];                                           // first keys; past every limit where there is no page
     bool border = false;                                    // some row does not see all of the pages
 #pragma unroll
@@ -285,24 +385,18 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     float sx[PG][NT][4];
 #pragma unroll
     for (int x = 0; x < PG; ++x) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sx[x][n][e] = 0.f;
-      uint32_t scale[2][D / 64];           // of the two tokens, per block of 16 dims: the pair (s, s)
+      __half2 scale[2];                    // of the two tokens: the lane's blocks of 16 dims, D / 64 of them
       uint32_t kw[2][D / 32];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if constexpr (D == 128) {
           const uint4 u = *reinterpret_cast<const uint4*>(k_at + at + x * PAGE + h * 512);
           kw[h][0] = u.x, kw[h][1] = u.y, kw[h][2] = u.z, kw[h][3] = u.w;
-          const uint32_t two = scales_to_half2(*reinterpret_cast<const uint16_t*>(ks_at + at + x * PAGE + h * 64));
-          scale[h][0] = __byte_perm(two, 0, 0x1010);
-          scale[h][1] = __byte_perm(two, 0, 0x3232);
+          scale[h] = as_half2(scales_to_half2(*reinterpret_cast<const uint16_t*>(ks_at + at + x * PAGE + h * 64)));
         } else {
           const uint2 u = *reinterpret_cast<const uint2*>(k_at + at + x * PAGE + h * 256);
           kw[h][0] = u.x, kw[h][1] = u.y;
-          scale[h][0] = __byte_perm(scales_to_half2(ks_at[at + x * PAGE + h * 32]), 0, 0x1010);
+          scale[h] = as_half2(scales_to_half2(ks_at[at + x * PAGE + h * 32]));
         }
       }
 #pragma unroll
@@ -312,19 +406,18 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
         for (int h = 0; h < 2; ++h) {
           codes_to_half2(kw[h][q], kx[h]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kx[h][e] = mul_half2(kx[h][e], scale[h][q / 2]);
+          for (int e = 0; e < 4; ++e) kx[h][e] = mul_half2(kx[h][e], q / 2 ? __high2half2(scale[h]) : __low2half2(scale[h]));
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const uint32_t a[4] = {kx[0][2 * k], kx[1][2 * k], kx[0][2 * k + 1], kx[1][2 * k + 1]};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            if constexpr (Q_IN_REGS) {
-              kv4_mma(sx[x][n], a, qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
-            } else {
-              const uint2 u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
-              kv4_mma(sx[x][n], a, u.x, u.y);
-            }
+            uint2 u;
+            if constexpr (Q_IN_REGS) u = make_uint2(qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
+            else u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
+            if (q == 0 && k == 0) kv4_mma_first(sx[x][n], a, u.x, u.y);
+            else kv4_mma(sx[x][n], a, u.x, u.y);
           }
         }
       }
@@ -338,8 +431,22 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
           for (int e = 0; e < 4; ++e)
             if (key0[x] + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[x][n][e] = -INFINITY;
     }
-    // ---- the reference
-    bool grow = false;
+    // ---- the values' scales: of tokens 2t, 2t+1, 2t+8, 2t+9
+    uint32_t vs[PG];
+#pragma unroll
+    for (int x = 0; x < PG; ++x) {
+      constexpr int H = D == 128 ? 64 : 32;
+      const uint32_t b00 = vs_at[0][at + x * PAGE], b01 = vs_at[1][at + x * PAGE], b10 = vs_at[0][at + x * PAGE + H], b11 = vs_at[1][at + x * PAGE + H];
+      vs[x] = __byte_perm(__byte_perm(b00, b01, 0x5540), __byte_perm(b10, b11, 0x5540), 0x5410);
+      if (border) {
+        // what stands behind the last key is anything, a NaN's scale too: P is 0 there, 0 times NaN is not
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (key0[x] + kv4_token(t, q & 1, q >> 1) >= end) vs[x] &= ~(0xffu << (8 * q));
+      }
+    }
+    // ---- the reference; values that are NaN
+    bool grow = false, nan = false;
     float mx[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -347,12 +454,14 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       for (int e = 0; e < 2; ++e) {
         mx[n][e] = fmaxf(sx[0][n][e], sx[0][n][e + 2]);
 #pragma unroll
-        for (int x = 1; x < PG; ++x) mx[n][e] = fmaxf(mx[n][e], fmaxf(sx[x][n][e], sx[x][n][e + 2]));
+        for (int x = 1; x < PG; ++x) mx[n][e] = fmaxf(fmaxf(mx[n][e], sx[x][n][e]), sx[x][n][e + 2]);
         grow |= mx[n][e] > m_next[n][e];
       }
+#pragma unroll
+    for (int x = 0; x < PG; ++x) nan |= (((vs[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
     // Lazy rescale: the reference of a row only moves when a score exceeds it by more than 2^4 (always at the first), and each row's by its
     // own scores: its bits do not depend on the other rows.
-    if (__any_sync(0xffffffffu, grow)) {
+    if (__any_sync(0xffffffffu, grow | nan)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -374,6 +483,18 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
             }
           }
         }
+      // Rows that see a value that is NaN are marked and get their NaN at the end; in the products such values are zeros, since rows that
+      // do not see them have a P of 0 there.
+#pragma unroll
+      for (int x = 0; x < PG; ++x)
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          if (((vs[x] >> (8 * q)) & 0x7f) != 0x7f) continue;
+          vs[x] &= ~(0xffu << (8 * q));
+          const int key = key0[x] + kv4_token(t, q & 1, q >> 1);
+          for (int r = 0; r < n_rows; ++r)
+            if (key < min(end, w.cached + (row0 + r) / G + 1)) s_nan[r][g] = 1;
+        }
     }
 #pragma unroll
     for (int x = 0; x < PG; ++x) {
@@ -388,7 +509,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
           pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
         }
       // ---- O^T
-      uint32_t vw[2][2][D / 64], b[2][2];
+      uint32_t vw[2][2][D / 64];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -396,33 +517,11 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
           if constexpr (D == 128) {
             const uint2 u = *reinterpret_cast<const uint2*>(v_at[e] + at + x * PAGE + h * 512);
             vw[h][e][0] = u.x, vw[h][e][1] = u.y;
-            b[h][e] = vs_at[e][at + x * PAGE + h * 64];
           } else {
             vw[h][e][0] = *reinterpret_cast<const uint32_t*>(v_at[e] + at + x * PAGE + h * 256);
-            b[h][e] = vs_at[e][at + x * PAGE + h * 32];
           }
         }
-      // scales of tokens (2t, 2t+1) and (2t+8, 2t+9)
-      uint32_t bytes = __byte_perm(__byte_perm(b[0][0], b[0][1], 0x5540), __byte_perm(b[1][0], b[1][1], 0x5540), 0x5410);
-      if (border) {
-        // what stands behind the last key is anything, a NaN's scale too: P is 0 there, 0 times NaN is not
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (key0[x] + kv4_token(t, q & 1, q >> 1) >= end) bytes &= ~(0xffu << (8 * q));
-      }
-      // Values that are NaN: rows that see them are marked and get their NaN at the end; in the products they are zeros, since rows that
-      // do not see them have a P of 0 there.
-      if (__any_sync(0xffffffffu, ((bytes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) {
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          if (((bytes >> (8 * q)) & 0x7f) != 0x7f) continue;
-          bytes &= ~(0xffu << (8 * q));
-          const int key = key0[x] + kv4_token(t, q & 1, q >> 1);
-          for (int r = 0; r < n_rows; ++r)
-            if (key < min(end, w.cached + (row0 + r) / G + 1)) s_nan[r][g] = 1;
-        }
-      }
-      const uint32_t scale[2] = {scales_to_half2(bytes & 0xffff), scales_to_half2(bytes >> 16)};
+      const __half2 scale[2] = {as_half2(scales_to_half2(vs[x] & 0xffff)), as_half2(scales_to_half2(vs[x] >> 16))};
 #pragma unroll
       for (int q = 0; q < D / 64; ++q) {
         // lo: even dims of the two tokens side by side, hi: odd dims
@@ -489,65 +588,92 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     }
     float inv = L == 0.f ? 0.f : p.v_scale / L;
     if (s_nan[r][d / (D / 8)]) inv = NAN;
-    const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);      // (a sum of NaN stays NaN)
-    const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
-    const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
-    if (p.n_chunks == 1) {
+    const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);                    // (a sum of NaN stays NaN)
+    if (!first_part && ends) {
+      const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
+      const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
       *reinterpret_cast<uint2*>(p.out + row_head * D + d) =
           make_uint2(pack_bf16x2(O.x * inv, O.y * inv), pack_bf16x2(O.z * inv, O.w * inv));
       if (p.lse && d == 0) p.lse[row_head] = lse2 * 0.6931471805599453f;
     } else {
-      // partials of (sequence, row of it, chunk): rows are counted by sequence, max_new of them each
-      const size_t part = (((size_t)s * p.max_new + i) * p.Hq + h) * p.n_chunks + c;
+      const size_t part = ((size_t)blockIdx.x * 2 + (first_part ? 0 : 1)) * ROWS + r;
       *reinterpret_cast<float4*>(p.part_o + part * D + d) = make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
       if (d == 0) p.part_lse[part] = lse2;
     }
   }
+  // ---- on along the line
+  if (first_part) left.first_ends = ends;
+  else if (!ends) left = Kv4Piece{seq, kvh, tile, left.first_ends};
+  first_part = false;
+  x0 += here;
+  trip0 = 0;
+  if (x0 < x1) {
+    if (++unit == tiles * p.Hkv) {
+      unit = 0;
+      do w = kv4_seq(p, ++seq);
+      while (w.new_len == 0);                       // (the line goes on, so there is one)
+    }
+    __syncthreads();                                // the exchange buffer becomes the rings again
+  }
+  }
+  if (!p.whole && tid == 0) p.pieces[blockIdx.x] = left;
 }
 
-// Merge of a row's chunks: lse = log2 sum 2^lse_c, o = sum 2^(lse_c - lse) o_c.  A warp has one (row, head), lanes over head_dim.
-template <int D>
-__global__ void __launch_bounds__(128) kv4_merge_kernel(const Kv4AttnParams p) {
-  constexpr int EPL = D / 32;
-  const int lane = threadIdx.x & 31;
-  const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);       // (sequence, row, head)
+// Joins a unit's partial results: lse = log2 sum 2^lse_c, o = sum 2^(lse_c - lse) o_c.  The CTA of the piece that the unit begins in: its second place, then
+// the first places of those behind it until the unit ends.  A warp has a row, lanes over head_dim.
+template <int D, int NT>
+__global__ void __launch_bounds__(KV4_THREADS) kv4_join_kernel(const Kv4AttnParams p) {
+  constexpr int EPL = D / 32, ROWS = 8 * NT;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_launch();
-  if (unit >= (long long)p.batch * p.max_new * p.Hq) return;
-  const int h = (int)(unit % p.Hq), i = (int)(unit / p.Hq % p.max_new), s = (int)(unit / p.Hq / p.max_new);
-  int err;
-  const Kv4Work w = kv4_work(p, s, &err);
-  if (i >= w.new_len) return;
-  const int nc = max(1, (w.ctx + p.chunk_tokens - 1) / p.chunk_tokens);
-  const float* pl = p.part_lse + unit * p.n_chunks;
-  const float* po = p.part_o + unit * p.n_chunks * D + lane * EPL;
-  float M = -INFINITY;
-  for (int c = lane; c < nc; c += 32) M = max_nan(M, pl[c]);                  // a NaN chunk makes the row NaN
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, d));
-  float L = 0.f, acc[EPL];
-#pragma unroll
-  for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
-  if (!(M == -INFINITY)) {                         // else a row without keys
-    for (int c = 0; c < nc; ++c) {
-      const float wi = exp2f(pl[c] - M);
-      L += wi;
-      if (pl[c] == -INFINITY) continue;            // (a chunk that the row sees nothing of)
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) acc[e] = fmaf(wi, po[(size_t)c * D + e], acc[e]);
+  const Kv4Piece me = p.pieces[blockIdx.x];
+  if (me.seq < 0) return;
+  int n = 1;                                        // pieces that it has
+  for (int c0 = blockIdx.x + 1;; c0 += 32) {
+    const int c = c0 + lane;
+    const unsigned ends = __ballot_sync(0xffffffffu, c >= (int)gridDim.x || p.pieces[c].first_ends);
+    if (ends) {
+      n = min(c0 + __ffs(ends), (int)gridDim.x) - (int)blockIdx.x;
+      break;
     }
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
-  uint16_t* out = p.out + row_head * D + lane * EPL;
-  if constexpr (EPL == 4)
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-  else
-    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-  if (p.lse && lane == 0) p.lse[row_head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  const Kv4Seq w = kv4_seq(p, me.seq);
+  const int G = p.Hq / p.Hkv, row0 = me.tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
+  for (int r = warp; r < n_rows; r += KV4_WARPS) {
+    const size_t first = ((size_t)blockIdx.x * 2 + 1) * ROWS + r;              // the c-th one: ROWS places on, then every 2 ROWS
+    auto place = [&](int c) { return first + (c == 0 ? 0 : (size_t)(2 * c - 1) * ROWS); };
+    float M = -INFINITY;
+    for (int c = lane; c < n; c += 32) M = max_nan(M, p.part_lse[place(c)]);   // a NaN piece makes the row NaN
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, d));
+    float L = 0.f, acc[EPL];
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+    if (!(M == -INFINITY)) {                        // else a row without keys
+      for (int c = 0; c < n; ++c) {
+        const float lse = p.part_lse[place(c)];
+        if (lse == -INFINITY) continue;             // (a piece that the row sees nothing of)
+        const float wi = exp2f(lse - M);
+        L += wi;
+        const float* po = p.part_o + place(c) * D + lane * EPL;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) acc[e] = fmaf(wi, po[e], acc[e]);
+      }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const size_t row_head = (size_t)(w.first_row + (row0 + r) / G) * p.Hq + me.head * G + (row0 + r) % G;
+    uint16_t* out = p.out + row_head * D + lane * EPL;
+    if constexpr (EPL == 4)
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    if (p.lse && lane == 0) p.lse[row_head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  }
 }
 
-// How the keys are cut.  As in efim_decode_attn: one wave of CTAs where that gives chunks of 256 to 1024 keys, else 2048.
+// One wave of CTAs, fewer where their pieces would fall below KV4_LEAST keys.  Units that fit KV4_WHOLE keys are not cut.
+constexpr int KV4_LEAST = 256, KV4_WHOLE = 512;
 Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_ctx) {
   Kv4Plan pl;
   const int G = cache->num_q_heads / cache->num_kv_heads;
@@ -555,19 +681,16 @@ Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_
   pl.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   pl.row_tiles = (rows + 8 * pl.nt - 1) / (8 * pl.nt);
   if (max_ctx < 1) max_ctx = 1;
-  const long long slots = (long long)sm_count() * kv4_ctas_per_sm(pl.nt);
-  const long long units = (long long)batch * cache->num_kv_heads * pl.row_tiles;
-  long long chunk = 2048;
-  if (units * ((max_ctx + 2047) / 2048) < 4 * slots) {
-    const long long n = std::max<long long>(1, slots / units);
-    chunk = std::min<long long>(1024, std::max<long long>(256, (max_ctx + n - 1) / n));
-  }
-  chunk = (chunk + 63) / 64 * 64;
-  pl.chunk_tokens = (int)chunk;
-  pl.n_chunks = (int)((max_ctx + chunk - 1) / chunk);
-  const size_t parts = pl.n_chunks > 1 ? (size_t)batch * max_new * cache->num_q_heads * pl.n_chunks : 0;
-  pl.lse_bytes = (parts * 4 + 255) / 256 * 256;
-  pl.bytes = pl.lse_bytes + parts * cache->head_dim * 4;
+  const int trip = 16 * KV4_WARPS * kv4_pages(pl.nt);
+  const long long trips = (max_ctx + (long long)trip - 1) / trip, units = batch * cache->num_kv_heads * pl.row_tiles;
+  pl.whole = max_ctx <= KV4_WHOLE;
+  pl.least_trips = KV4_LEAST / trip;
+  pl.ctas = pl.whole ? units : std::min<long long>((long long)sm_count() * kv4_ctas_per_sm(pl.nt), (units * trips + pl.least_trips - 1) / pl.least_trips);
+  const size_t parts = pl.whole ? 0 : (size_t)pl.ctas * 2 * 8 * pl.nt;
+  auto round = [](size_t n) { return (n + 255) / 256 * 256; };
+  pl.lse_bytes = round(parts * 4);
+  pl.piece_bytes = pl.whole ? 0 : round((size_t)pl.ctas * sizeof(Kv4Piece));
+  pl.bytes = pl.lse_bytes + pl.piece_bytes + parts * cache->head_dim * 4;
   return pl;
 }
 
@@ -582,16 +705,13 @@ static efim_status kv4_launch_nt(const Kv4AttnParams& p, const Kv4Plan& pl, cuda
     EFIM_CUDA_TRY(cudaFuncSetAttribute(kv4_attn_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     if (dev >= 0 && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
   }
-  EFIM_CUDA_TRY(launch_pdl(kv4_attn_kernel<D, NT>, dim3((unsigned)(p.batch * pl.row_tiles), p.Hkv, pl.n_chunks), dim3(KV4_THREADS), smem, s, p));
+  EFIM_CUDA_TRY(launch_pdl(kv4_attn_kernel<D, NT>, dim3((unsigned)pl.ctas), dim3(KV4_THREADS), smem, s, p));
+  if (!pl.whole) EFIM_CUDA_TRY(launch_pdl(kv4_join_kernel<D, NT>, dim3((unsigned)pl.ctas), dim3(KV4_THREADS), 0, s, p));
   return EFIM_OK;
 }
 template <int D>
 static efim_status kv4_launch(const Kv4AttnParams& p, const Kv4Plan& pl, cudaStream_t s) {
-  const efim_status st = pl.nt == 1 ? kv4_launch_nt<D, 1>(p, pl, s) : pl.nt == 2 ? kv4_launch_nt<D, 2>(p, pl, s) : kv4_launch_nt<D, 4>(p, pl, s);
-  if (st != EFIM_OK || pl.n_chunks == 1) return st;
-  const long long warps = (long long)p.batch * p.max_new * p.Hq;
-  EFIM_CUDA_TRY(launch_pdl(kv4_merge_kernel<D>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, s, p));
-  return EFIM_OK;
+  return pl.nt == 1 ? kv4_launch_nt<D, 1>(p, pl, s) : pl.nt == 2 ? kv4_launch_nt<D, 2>(p, pl, s) : kv4_launch_nt<D, 4>(p, pl, s);
 }
 
 efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max_ctx, float sm_scale, void* ws, size_t ws_bytes, void* stream) {
@@ -601,12 +721,13 @@ efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max
   const long long G = cache->num_q_heads / cache->num_kv_heads;
   if ((long long)p.max_new * G > 0x3fffffff || (long long)p.batch * p.max_new * p.Hq > 0x7fffffff) return EFIM_ERR_UNSUPPORTED;
   const Kv4Plan pl = kv4_plan(cache, p.batch, p.max_new, max_ctx);
-  if (pl.n_chunks > 65535 || (long long)p.batch * pl.row_tiles > 0x7fffffff) return EFIM_ERR_UNSUPPORTED;
+  if (pl.ctas > 0x7fffffff || pl.row_tiles * cache->num_kv_heads > 0x7fffffff) return EFIM_ERR_UNSUPPORTED;
   if (pl.bytes > 0) {
     if (!ws || ws_bytes < pl.bytes) return EFIM_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(ws) & 255) return EFIM_ERR_INVALID_ARG;
     p.part_lse = static_cast<float*>(ws);
-    p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.lse_bytes);
+    p.pieces = reinterpret_cast<Kv4Piece*>(static_cast<char*>(ws) + pl.lse_bytes);
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.lse_bytes + pl.piece_bytes);
   }
   p.k_codes = static_cast<const uint8_t*>(cache->d_k_codes);
   p.v_codes = static_cast<const uint8_t*>(cache->d_v_codes);
@@ -618,9 +739,10 @@ efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max
   p.Hkv = cache->num_kv_heads;
   p.num_pages = cache->num_pages;
   p.row_tiles = (int)pl.row_tiles;
-  p.chunk_tokens = pl.chunk_tokens;
-  p.n_chunks = pl.n_chunks;
-  p.key_cap = (int)std::min<long long>((long long)pl.n_chunks * pl.chunk_tokens, cap);
+  p.units_per_seq = (int)(pl.row_tiles * cache->num_kv_heads);
+  p.whole = pl.whole;
+  p.least_trips = pl.least_trips;
+  p.key_cap = max_ctx;
   return cache->head_dim == 128 ? kv4_launch<128>(p, pl, static_cast<cudaStream_t>(stream)) : kv4_launch<64>(p, pl, static_cast<cudaStream_t>(stream));
 }
 

@@ -13,10 +13,11 @@ struct Kv4AttnParams {
   const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
   uint16_t* out;
   float* lse;                 // natural log, or null
-  float* part_o;              // [batch][max_new][Hq][n_chunks][D]   (n_chunks > 1)
-  float* part_lse;            // [batch][max_new][Hq][n_chunks]      base-2 log
+  float* part_o;              // [CTAs][2][rows of a tile][D]
+  float* part_lse;            // [CTAs][2][rows of a tile], base-2 log
+  struct Kv4Piece* pieces;    // [CTAs]
   int32_t* status;
-  int batch, total_rows, max_new, Hq, Hkv, max_pages_per_seq, num_pages, row_tiles, chunk_tokens, n_chunks, len_is_cached;
+  int batch, total_rows, max_new, Hq, Hkv, max_pages_per_seq, num_pages, row_tiles, units_per_seq, whole, least_trips, len_is_cached;
   int key_cap;                // keys the launch can cover
   float scale_log2;           // sm_scale * log2(e) * the key pool's scale
   float v_scale;
@@ -24,9 +25,10 @@ struct Kv4AttnParams {
 
 struct Kv4Plan {
   int nt;                     // 8-row tiles of a CTA
-  long long row_tiles;        // CTAs over a sequence's (new token, head of the group) rows
-  int chunk_tokens, n_chunks;
-  size_t lse_bytes, bytes;
+  long long row_tiles;        // tiles of a sequence's (new token, head of the group) rows
+  long long ctas;
+  int whole, least_trips;
+  size_t lse_bytes, piece_bytes, bytes;
 };
 Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_ctx);
 
