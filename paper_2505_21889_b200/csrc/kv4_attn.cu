@@ -119,10 +119,11 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4AttnParams& p, int s) {
 // The work of a call is a line of trips (a trip: PG pages by each of a CTA's warps), unit after unit: (sequence, kv head, tile of rows).  Each CTA has
 // an equal piece of the line, so all end together whatever the lengths are; a unit that lies in one piece is finished
 // there, the pieces of the others leave partial results, which a second kernel joins.  A piece has at most two such: of a unit that began before it
-// (kept in the CTA's first place), and of one that goes on behind it (second place).
+// (kept in the CTA's first place), and of one that goes on behind it (second place).  A unit's start (queries, first pages, results)
+// costs about as much as START trips and, where pieces are a good deal longer than that, stands in the line as that many before its own.
 template <int NT>
 struct Kv4Line {
-  static constexpr int TRIP = 16 * KV4_WARPS * kv4_pages(NT);              // keys of a trip
+  static constexpr int TRIP = 16 * KV4_WARPS * kv4_pages(NT), START = NT == 4 ? 5 : 3;     // (TRIP: keys of a trip)
   static __device__ __forceinline__ int trips(const Kv4Seq& w) { return max(1, (w.ctx + TRIP - 1) / TRIP); }
   static __device__ __forceinline__ int tiles(const Kv4Seq& w, int G) { return (w.new_len * G + 8 * NT - 1) / (8 * NT); }
 };
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   __shared__ __align__(16) uint16_t s_q[ROWS][D + 16];    // fp16, shifted; dim t D/4 + 4k + x at 16k + 4t + x
   __shared__ float s_m[KV4_WARPS][ROWS], s_l[KV4_WARPS][ROWS], s_scale[ROWS];
   __shared__ uint8_t s_nan[ROWS][8];      // rows that see a NaN value in dims [g D/8, (g+1) D/8)
-  __shared__ long long s_sum[KV4_WARPS];
+  __shared__ long long s_sum[KV4_WARPS][2];
   __shared__ long long s_at;              // trips of the line before the sequence that this CTA begins with
   __shared__ int s_seq;
 
@@ -154,44 +155,53 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   pdl_launch();
   // ---- this CTA's piece of the line
   long long x0, x1;                       // in trips
-  int seq, off;                           // its first sequence, and the trips of that one before it
+  int seq, off;                           // its first sequence, and what of that one lies before it
+  int start = 0;                          // what a unit's start counts
   if (p.whole) {                          // units that are never cut, one a CTA
     seq = blockIdx.x / p.units_per_seq;
     x0 = x1 = off = 0;
   } else {
     const int per = (p.batch + KV4_THREADS - 1) / KV4_THREADS, first = min(p.batch, tid * per), last = min(p.batch, first + per);
-    auto weight = [&](int i) {
-      const Kv4Seq w = kv4_seq(p, i);
-      return (long long)Line::trips(w) * Line::tiles(w, G) * p.Hkv;
-    };
-    long long mine = 0;
-    for (int i = first; i < last; ++i) mine += weight(i);
-    long long upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += y;
+    auto units_of = [&](const Kv4Seq& q) { return (long long)Line::tiles(q, G) * p.Hkv; };
+    long long mine[2] = {0, 0};           // trips, units
+    for (int i = first; i < last; ++i) {
+      const Kv4Seq q = kv4_seq(p, i);
+      mine[0] += units_of(q) * Line::trips(q);
+      mine[1] += units_of(q);
     }
-    if (lane == 31) s_sum[warp] = upto;
+    long long upto[2] = {mine[0], mine[1]}, total[2] = {0, 0};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, upto[k], d);
+        if (lane >= d) upto[k] += y;
+      }
+      if (lane == 31) s_sum[warp][k] = upto[k];
+    }
     __syncthreads();
-    long long total = 0;
 #pragma unroll
-    for (int i = 0; i < KV4_WARPS; ++i) {
-      if (i < warp) upto += s_sum[i];
-      total += s_sum[i];
-    }
-    const long long share = max((long long)p.least_trips, (total + gridDim.x - 1) / gridDim.x);
+    for (int i = 0; i < KV4_WARPS; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (i < warp) upto[k] += s_sum[i][k];
+        total[k] += s_sum[i][k];
+      }
+    start = total[0] >= 4LL * Line::START * gridDim.x ? Line::START : 0;
+    const long long all = total[0] + start * total[1], before = upto[0] - mine[0] + start * (upto[1] - mine[1]);
+    const long long share = max((long long)p.least_trips, (all + gridDim.x - 1) / gridDim.x);
     x0 = blockIdx.x * share;
-    x1 = min(total, x0 + share);
-    if (x0 >= total) {
+    x1 = min(all, x0 + share);
+    if (x0 >= all) {
       if (tid == 0) p.pieces[blockIdx.x] = Kv4Piece{-1, 0, 0, 1};
       return;
     }
-    if (x0 >= upto - mine && x0 < upto) {
-      long long at = upto - mine;
+    if (x0 >= before && x0 < upto[0] + start * upto[1]) {
+      long long at = before;
       int i = first;
       for (; i < last - 1; ++i) {
-        const long long y = weight(i);
+        const Kv4Seq q = kv4_seq(p, i);
+        const long long y = units_of(q) * (start + Line::trips(q));
         if (x0 < at + y) break;
         at += y;
       }
@@ -203,44 +213,58 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     off = (int)min(x0 - s_at, 0x7fffffffLL);
   }
   Kv4Seq w = kv4_seq(p, seq);
-  int unit, trip0;                        // of the sequence's units (kv head, tile): the one at hand, and its trips that are done
+  int unit;                               // of the sequence's units (kv head, tile): the one at hand, `off` of it done
   if (p.whole) {
     unit = blockIdx.x % p.units_per_seq;
-    trip0 = 0;
     const int tiles = Line::tiles(w, G);
     if (w.err && unit == 0 && tid == 0 && p.status) atomicOr(p.status, w.err);
     if (unit / p.row_tiles >= p.Hkv || unit % p.row_tiles >= tiles) return;
     unit = unit / p.row_tiles * tiles + unit % p.row_tiles;
     x1 = Line::trips(w);
   } else {
-    const int n = Line::trips(w);
+    const int n = start + Line::trips(w);
     unit = off / n;
-    trip0 = off % n;
+    off %= n;
   }
   Kv4Piece left{-1, 0, 0, 0};
-  bool first_part = trip0 != 0;           // the unit at hand began before this piece
   if (!p.whole && blockIdx.x == 0)        // one CTA reports the lengths that do not fit
     for (int i = tid; i < p.batch; i += KV4_THREADS)
       if (const int err = kv4_seq(p, i).err; err && p.status) atomicOr(p.status, err);
 
+  auto token_of = [&](int row) { return p.max_new == 1 ? 0 : row / G; };
   while (x0 < x1) {
   const int tiles = Line::tiles(w, G);
   const int kvh = unit / tiles, tile = unit % tiles;
-  const int unit_trips = Line::trips(w), here = (int)min((long long)(unit_trips - trip0), x1 - x0);   // trips of the unit in this piece
-  const bool ends = trip0 + here == unit_trips;
+  const int unit_len = start + Line::trips(w), here = (int)min((long long)(unit_len - off), x1 - x0);   // of the unit in this piece
+  const int trip0 = max(off - start, 0), trip1 = off + here - start;
+  const bool first_part = trip0 > 0, ends = off + here == unit_len;        // the unit began before this piece; it ends in it
+  if (trip1 <= 0) break;                  // (the piece ends before the unit's first trip: it begins in the next one)
   const int32_t* bt = p.block_table + (size_t)seq * p.max_pages_per_seq;
   // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece; lane l holds the id of the l-th of them (then of the next 32)
   const int begin = trip0 * Line::TRIP, first_pg = (begin >> 4) + PG * warp;
   auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
   const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
   // keys that the tile's last row sees, of this piece
-  const int end = min(min(w.ctx, w.cached + (row0 + n_rows - 1) / G + 1), begin + here * Line::TRIP);
+  const int end = min(min(w.ctx, w.cached + token_of(row0 + n_rows - 1) + 1), trip1 * Line::TRIP);
   const int last_pg = (end - 1) >> 4;
   const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
   int pid_cache = -1;
   {
     const int pg = page_of(lane);
     if (pg <= last_pg) pid_cache = *(bt + pg);
+  }
+  // query rows, a warp a row: on their way before the pages are
+  uint2 q_raw[ROWS / KV4_WARPS];
+#pragma unroll
+  for (int i = 0; i < ROWS / KV4_WARPS; ++i) {
+    const int r = i * KV4_WARPS + warp;
+    q_raw[i] = make_uint2(0, 0);
+    if (r < n_rows) {
+      const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
+      const uint16_t* q = p.q + ((size_t)(w.first_row + token) * p.Hq + h) * D + lane * (D / 32);
+      if constexpr (D == 128) q_raw[i] = *reinterpret_cast<const uint2*>(q);
+      else q_raw[i].x = *reinterpret_cast<const uint32_t*>(q);
+    }
   }
 
   const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * PG * PAGE);
@@ -283,24 +307,12 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i) issue(i, i);
 
-  // ---- query rows as fp16, shifted: a warp a row
-  for (int r = warp; r < ROWS; r += KV4_WARPS) {
-    float x[D / 32];
-    float top = 0.f;
-    if (r < n_rows) {
-      const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
-      const uint16_t* q = p.q + ((size_t)(w.first_row + i) * p.Hq + h) * D + lane * (D / 32);
-      if constexpr (D == 128) {
-        const uint2 u = *reinterpret_cast<const uint2*>(q);
-        x[0] = bf16lo(u.x), x[1] = bf16hi(u.x), x[2] = bf16lo(u.y), x[3] = bf16hi(u.y);
-      } else {
-        const uint32_t u = *reinterpret_cast<const uint32_t*>(q);
-        x[0] = bf16lo(u), x[1] = bf16hi(u);
-      }
-    } else {
+  // ---- query rows as fp16, shifted
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) x[e] = 0.f;
-    }
+  for (int i = 0; i < ROWS / KV4_WARPS; ++i) {
+    const int r = i * KV4_WARPS + warp;
+    const float x[4] = {bf16lo(q_raw[i].x), bf16hi(q_raw[i].x), bf16lo(q_raw[i].y), bf16hi(q_raw[i].y)};
+    float top = 0.f;
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) top = max_nan(top, fabsf(x[e]));
 #pragma unroll
@@ -349,10 +361,10 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       m_off[n][e] = -KV4_P_SHIFT;
       l_part[n][e] = 0.f;
       sc[n][e] = s_scale[r];
-      limit[n][e] = min(end, w.cached + (row0 + min(r, n_rows - 1)) / G + 1);
+      limit[n][e] = min(end, w.cached + token_of(row0 + min(r, n_rows - 1)) + 1);
     }
   }
-  const int first_limit = min(end, w.cached + row0 / G + 1);
+  const int first_limit = min(end, w.cached + token_of(row0) + 1);
   const int tok0 = kv4_token(g >> 1, g & 1, 0);             // this lane's key in S^T; the other is 8 on
   // this lane's places in a staged page
   const uint8_t* k_at = ring_ptr + (D == 128 ? tok0 * 64 + t * 16 : tok0 * 32 + t * 8);
@@ -493,7 +505,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
           vs[x] &= ~(0xffu << (8 * q));
           const int key = key0[x] + kv4_token(t, q & 1, q >> 1);
           for (int r = 0; r < n_rows; ++r)
-            if (key < min(end, w.cached + (row0 + r) / G + 1)) s_nan[r][g] = 1;
+            if (key < min(end, w.cached + token_of(row0 + r) + 1)) s_nan[r][g] = 1;
         }
     }
 #pragma unroll
@@ -590,8 +602,8 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     if (s_nan[r][d / (D / 8)]) inv = NAN;
     const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);                    // (a sum of NaN stays NaN)
     if (!first_part && ends) {
-      const int i = (row0 + r) / G, h = kvh * G + (row0 + r) % G;
-      const size_t row_head = (size_t)(w.first_row + i) * p.Hq + h;
+      const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
+      const size_t row_head = (size_t)(w.first_row + token) * p.Hq + h;
       *reinterpret_cast<uint2*>(p.out + row_head * D + d) =
           make_uint2(pack_bf16x2(O.x * inv, O.y * inv), pack_bf16x2(O.z * inv, O.w * inv));
       if (p.lse && d == 0) p.lse[row_head] = lse2 * 0.6931471805599453f;
@@ -604,9 +616,8 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   // ---- on along the line
   if (first_part) left.first_ends = ends;
   else if (!ends) left = Kv4Piece{seq, kvh, tile, left.first_ends};
-  first_part = false;
   x0 += here;
-  trip0 = 0;
+  off = 0;
   if (x0 < x1) {
     if (++unit == tiles * p.Hkv) {
       unit = 0;
