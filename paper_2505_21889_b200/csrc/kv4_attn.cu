@@ -138,6 +138,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   using Line = Kv4Line<NT>;
   constexpr int ST = kv4_stages(NT), PG = kv4_pages(NT), ROWS = 8 * NT;
   constexpr int CODES = kv4_code_bytes(D), SCALES = kv4_scale_bytes(D), PAGE = kv4_page_bytes(D);
+  constexpr int STAGE = PG * PAGE;        // bytes of the ring that a trip's pages take
   constexpr int KS = D / 16;              // k-steps of S^T, m-tiles of O^T
   constexpr int XD = D + 4;               // floats per row of the warps' exchange buffer
   constexpr bool Q_IN_REGS = NT <= 2;
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   const bool first_part = trip0 > 0, ends = off + here == unit_len;        // the unit began before this piece; it ends in it
   if (trip1 <= 0) break;                  // (the piece ends before the unit's first trip: it begins in the next one)
   const int32_t* bt = p.block_table + (size_t)seq * p.max_pages_per_seq;
-  // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece; lane l holds the id of the l-th of them (then of the next 32)
+  // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece
   const int begin = trip0 * Line::TRIP, first_pg = (begin >> 4) + PG * warp;
   auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
   const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
@@ -248,11 +249,20 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   const int end = min(min(w.ctx, w.cached + token_of(row0 + n_rows - 1) + 1), trip1 * Line::TRIP);
   const int last_pg = (end - 1) >> 4;
   const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
-  int pid_cache = -1;
-  {
-    const int pg = page_of(lane);
-    if (pg <= last_pg) pid_cache = *(bt + pg);
-  }
+  // Lane l holds where the l-th of this warp's pages is (then of the next 32): (page, kv head) in the pools, -1 for no page.
+  int at_cache;
+  bool hole = false;                      // some pages are missing: every trip looks at its own
+  auto look_up = [&](int i) {
+    const int pg = page_of(i + lane);
+    at_cache = -1;
+    if (pg <= last_pg) {
+      const int pid = *(bt + pg);
+      if ((uint32_t)pid < (uint32_t)p.num_pages) at_cache = pid * p.Hkv + kvh;
+      else if (p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
+    }
+    hole |= __any_sync(0xffffffffu, pg <= last_pg && at_cache < 0);
+  };
+  look_up(0);
   // query rows, a warp a row: on their way before the pages are
   uint2 q_raw[ROWS / KV4_WARPS];
 #pragma unroll
@@ -267,45 +277,41 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     }
   }
 
-  const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * PG * PAGE);
-  const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * PG * PAGE);
-  constexpr int PIECES = CODES / 16, PS = SCALES / 16;                    // 16-byte pieces of a page's codes, of its scales
-  // where this lane's pieces come from and go to (a lane below 2 PS also has one of K's or V's scales)
+  const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * STAGE);
+  const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * STAGE);
+  constexpr int PIECES = CODES / 16, PS = 2 * SCALES / 16;                // 16-byte pieces of a page's codes (K or V), of its scales
+  // where this lane's pieces come from and go to: of every page's codes, of one page's scales
   const uint8_t *k_src = p.k_codes + lane * 16, *v_src = p.v_codes + lane * 16;
-  const uint8_t* s_src = lane < PS ? p.k_scales + lane * 16 : p.v_scales + (lane - PS) * 16;
-  const uint32_t k_dst = ring + lane * 16, v_dst = ring + CODES + kv4_v_piece<D>(lane / (D / 32), lane % (D / 32)), s_dst = k_dst + 2 * CODES;
-  uint32_t ok_bits = 0;                   // which of the in-flight pages are valid (bit = stage * PG + page)
-  auto issue = [&](int i, int sg) {       // send for the pages of this warp's i-th trip into stage sg
+  const uint8_t* s_src = lane % PS < PS / 2 ? p.k_scales + lane % PS * 16 : p.v_scales + (lane % PS - PS / 2) * 16;
+  const uint32_t k_dst = ring + lane * 16, v_dst = ring + CODES + kv4_v_piece<D>(lane / (D / 32), lane % (D / 32));
+  const uint32_t s_dst = ring + lane / PS * PAGE + 2 * CODES + lane % PS * 16;
+  uint32_t missing = 0;                   // a bit per page, the last one sent for lowest: not there
+  auto issue = [&](int i, uint32_t to) {  // send for the pages of this warp's i-th trip, to `to` bytes into the ring
+    missing <<= PG;
     if (i < n_trips) {
+      int at[PG];
 #pragma unroll
       for (int x = 0; x < PG; ++x) {
-        const int pid = __shfl_sync(0xffffffffu, pid_cache, (i * PG + x) & 31);
-        const bool ok = (uint32_t)pid < (uint32_t)p.num_pages;
-        const uint32_t bit = 1u << (sg * PG + x), to = (sg * PG + x) * PAGE;
-        ok_bits &= ~bit;
-        if (ok) {
-          ok_bits |= bit;
-          const uint32_t at = (uint32_t)pid * p.Hkv + kvh;
-          const uint8_t *k = k_src + (uint64_t)at * CODES, *v = v_src + (uint64_t)at * CODES;
+        at[x] = __shfl_sync(0xffffffffu, at_cache, (i * PG + x) & 31);
+        if (at[x] >= 0) {
+          const uint8_t *k = k_src + (uint64_t)at[x] * CODES, *v = v_src + (uint64_t)at[x] * CODES;
 #pragma unroll
           for (int u = 0; u < PIECES; u += 32) {
-            kv4_cp16(k_dst + to + u * 16, k + u * 16);
-            kv4_cp16(v_dst + to + u * 16, v + u * 16);
+            kv4_cp16(k_dst + to + x * PAGE + u * 16, k + u * 16);
+            kv4_cp16(v_dst + to + x * PAGE + u * 16, v + u * 16);
           }
-          if (lane < 2 * PS) kv4_cp16(s_dst + to, s_src + (uint64_t)at * SCALES);
-        } else if (page_of(i * PG + x) <= last_pg && lane == 0 && p.status) {
-          atomicOr(p.status, EFIM_DEV_BAD_PAGE);
+        } else {
+          missing |= 1u << x;
         }
       }
-      if (((i * PG + PG) & 31) == 0) {    // the next 32 of this warp's pages
-        const int pg = page_of(i * PG + PG + lane);
-        pid_cache = pg <= last_pg ? *(bt + pg) : -1;
-      }
+      const int mine = lane < PS ? at[0] : at[PG - 1];
+      if (lane < PG * PS && mine >= 0) kv4_cp16(s_dst + to, s_src + (uint64_t)mine * SCALES);
+      if (((i * PG + PG) & 31) == 0) look_up(i * PG + PG);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
-  for (int i = 0; i < ST - 1; ++i) issue(i, i);
+  for (int i = 0; i < ST - 1; ++i) issue(i, i * STAGE);
 
   // ---- query rows as fp16, shifted
 #pragma unroll
@@ -377,22 +383,19 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     vs_at[e] = ring_ptr + 2 * CODES + SCALES + (D == 128 ? token * 8 + g : token * 4 + (g >> 1));
   }
 
-  int sg = 0;
+  // trips whose pages every row sees in full
+  const int seen = max(first_limit, 0) >> 4, n_full = seen >= first_pg + PG ? (seen - first_pg - PG) / (KV4_WARPS * PG) + 1 : 0;
+
+  int at = 0;                             // where in the ring the trip's pages are
   for (int i = 0; i < n_trips; ++i) {
-    __syncwarp();                                           // everyone is done with the stage of the last trip
-    issue(i + ST - 1, sg == 0 ? ST - 1 : sg - 1);
+    __syncwarp();                         // everyone is done with the stage of the last trip
+    issue(i + ST - 1, at == 0 ? (ST - 1) * STAGE : at - STAGE);
     asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
     __syncwarp();
-    int key0[PG];                                           // first keys; past every limit where there is no page
-    bool border = false;                                    // some row does not see all of the pages
+    const bool border = i >= n_full || hole;
+    int key0[PG];                         // first keys; past every limit where there is no page (looked at where border is)
 #pragma unroll
-    for (int x = 0; x < PG; ++x) {
-      key0[x] = (ok_bits >> (sg * PG + x)) & 1u ? page_of(i * PG + x) << 4 : INT_MAX - 16;
-      border |= key0[x] + 16 > first_limit;
-    }
-    const uint32_t at = sg * PG * PAGE;
-    if (++sg == ST) sg = 0;
-    if (PG == 1 && key0[0] == INT_MAX - 16) continue;
+    for (int x = 0; x < PG; ++x) key0[x] = (missing >> ((ST - 1) * PG + x)) & 1u ? INT_MAX - 16 : page_of(i * PG + x) << 4;
     // ---- S^T
     float sx[PG][NT][4];
 #pragma unroll
@@ -557,6 +560,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
         }
       }
     }
+    at = at == (ST - 1) * STAGE ? 0 : at + STAGE;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   // ---- fold the lanes' sums, then the 4 warps (the exchange buffer takes their rings' place)
