@@ -285,28 +285,27 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   const uint8_t* s_src = lane % PS < PS / 2 ? p.k_scales + lane % PS * 16 : p.v_scales + (lane % PS - PS / 2) * 16;
   const uint32_t k_dst = ring + lane * 16, v_dst = ring + CODES + kv4_v_piece<D>(lane / (D / 32), lane % (D / 32));
   const uint32_t s_dst = ring + lane / PS * PAGE + 2 * CODES + lane % PS * 16;
-  uint32_t missing = 0;                   // a bit per page, the last one sent for lowest: not there
+  uint32_t missing = 0;                   // a bit per page, the last one sent for lowest: not there (kept where there is a hole)
   auto issue = [&](int i, uint32_t to) {  // send for the pages of this warp's i-th trip, to `to` bytes into the ring
-    missing <<= PG;
     if (i < n_trips) {
       int at[PG];
 #pragma unroll
       for (int x = 0; x < PG; ++x) {
         at[x] = __shfl_sync(0xffffffffu, at_cache, (i * PG + x) & 31);
-        if (at[x] >= 0) {
-          const uint8_t *k = k_src + (uint64_t)at[x] * CODES, *v = v_src + (uint64_t)at[x] * CODES;
+        if (hole) missing = missing << 1 | (uint32_t)at[x] >> 31;
+        at[x] = max(at[x], 0);            // (a page of the pool stands in for one that is not there)
+        const uint8_t *k = k_src + (uint64_t)at[x] * CODES, *v = v_src + (uint64_t)at[x] * CODES;
 #pragma unroll
-          for (int u = 0; u < PIECES; u += 32) {
-            kv4_cp16(k_dst + to + x * PAGE + u * 16, k + u * 16);
-            kv4_cp16(v_dst + to + x * PAGE + u * 16, v + u * 16);
-          }
-        } else {
-          missing |= 1u << x;
+        for (int u = 0; u < PIECES; u += 32) {
+          kv4_cp16(k_dst + to + x * PAGE + u * 16, k + u * 16);
+          kv4_cp16(v_dst + to + x * PAGE + u * 16, v + u * 16);
         }
       }
       const int mine = lane < PS ? at[0] : at[PG - 1];
-      if (lane < PG * PS && mine >= 0) kv4_cp16(s_dst + to, s_src + (uint64_t)mine * SCALES);
+      if (lane < PG * PS) kv4_cp16(s_dst + to, s_src + (uint64_t)mine * SCALES);
       if (((i * PG + PG) & 31) == 0) look_up(i * PG + PG);
+    } else {
+      missing <<= PG;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -395,7 +394,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     const bool border = i >= n_full || hole;
     int key0[PG];                         // first keys; past every limit where there is no page (looked at where border is)
 #pragma unroll
-    for (int x = 0; x < PG; ++x) key0[x] = (missing >> ((ST - 1) * PG + x)) & 1u ? INT_MAX - 16 : page_of(i * PG + x) << 4;
+    for (int x = 0; x < PG; ++x) key0[x] = (missing >> (ST * PG - 1 - x)) & 1u ? INT_MAX - 16 : page_of(i * PG + x) << 4;
     // ---- S^T
     float sx[PG][NT][4];
 #pragma unroll
