@@ -1,8 +1,9 @@
 // efim_adjust_logits: penalties for tokens that occurred, biases and grammar masks on the rows of a step, before they are judged or sampled.
 //
 // A CTA has one sequence's slice of the vocabulary in shared memory, a word per token: how often it was generated, whether the prompt
-// holds it, and which entry of the bias list it has.  It reads the sequence's history once, then walks the sequence's rows,
-// counting each row's own draft before it (a row's distribution comes after that token).
+// holds it, and which entry of the bias list it has.  It reads the sequence's history once; then each thread takes eight tokens' words into
+// registers and walks the sequence's rows, counting each row's own draft before it (a row's distribution comes after that token).
+// Most words are 0 and most masks whole: such logits are only copied, or left alone in place.
 #include "common.cuh"
 #include <algorithm>
 #include <atomic>
@@ -30,106 +31,203 @@ constexpr int ADJUST_THREADS = 512;
 // A word of the counts, W: the prompt's bit on top, then the bias entry + 1, from bit p.entry_shift on, then the count.
 template <typename W> constexpr int PROMPT_BIT = sizeof(W) * 8 - 1;
 
-template <typename T> __device__ __forceinline__ float adjust_load(T x);
-template <> __device__ __forceinline__ float adjust_load(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-template <> __device__ __forceinline__ float adjust_load(float x) { return x; }
-template <typename T> __device__ __forceinline__ T adjust_store(float x);
-template <> __device__ __forceinline__ uint16_t adjust_store(float x) { return (uint16_t)pack_bf16x2(x, 0.f); }
-template <> __device__ __forceinline__ float adjust_store(float x) { return x; }
-
 struct Penalties {
   float repetition, presence, frequency;
   const float* bias;
   int entry_shift;
 };
+// a logit of a token whose word is not 0
 template <typename W>
-__device__ __forceinline__ float adjusted(float x, W w, bool allowed, const Penalties& q) {
-  if (w) {
-    const W n = w & (((W)1 << q.entry_shift) - 1);
-    if (n || (w >> PROMPT_BIT<W>)) x = x > 0.f ? __fdiv_rn(x, q.repetition) : x * q.repetition;
-    if (n) x = x - q.frequency * (float)n - q.presence;
-    const W entry = (w & (((W)1 << PROMPT_BIT<W>) - 1)) >> q.entry_shift;
-    if (entry) x += *(q.bias + (entry - 1));
-  }
-  return allowed ? x : -INFINITY;
+__device__ __forceinline__ float adjusted(float x, W w, const Penalties& q) {
+  const W n = w & (((W)1 << q.entry_shift) - 1);
+  if (n || (w >> PROMPT_BIT<W>)) x = x > 0.f ? __fdiv_rn(x, q.repetition) : x * q.repetition;
+  if (n) x = x - q.frequency * (float)n - q.presence;
+  const W entry = (w & (((W)1 << PROMPT_BIT<W>) - 1)) >> q.entry_shift;
+  if (entry) x += *(q.bias + (entry - 1));
+  return x;
 }
+
+// Eight logits of neighbouring tokens, as they lie: 16 bytes of bf16 or 32 of fp32.
+template <typename T> struct Eight;
+template <> struct Eight<uint16_t> {
+  uint32_t x[4];
+  __device__ __forceinline__ float get(int e) const { return e & 1 ? bf16hi(x[e / 2]) : bf16lo(x[e / 2]); }
+  __device__ __forceinline__ void set(int e, float y) {
+    const uint32_t b = pack_bf16x2(y, 0.f);
+    x[e / 2] = e & 1 ? __byte_perm(x[e / 2], b, 0x5410) : __byte_perm(x[e / 2], b, 0x3254);
+  }
+  __device__ __forceinline__ void mask(uint32_t allowed) {                    // -inf where the bit is 0
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t keep = (allowed >> (2 * i) & 1 ? 0xffffu : 0u) | (allowed >> (2 * i) & 2 ? 0xffff0000u : 0u);
+      x[i] = (x[i] & keep) | (0xff80ff80u & ~keep);
+    }
+  }
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    const uint4 u = ldg_stream(p);
+    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+  }
+  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<uint4*>(p) = make_uint4(x[0], x[1], x[2], x[3]); }
+  __device__ __forceinline__ void load(const uint16_t* p, int n) {            // the first n, one by one
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (2 * i < n ? p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+  }
+  __device__ __forceinline__ void store(uint16_t* p, int n) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = (uint16_t)(x[e / 2] >> (16 * (e & 1)));
+  }
+};
+template <> struct Eight<float> {
+  float x[8];
+  __device__ __forceinline__ float get(int e) const { return x[e]; }
+  __device__ __forceinline__ void set(int e, float y) { x[e] = y; }
+  __device__ __forceinline__ void mask(uint32_t allowed) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = allowed >> e & 1 ? x[e] : -INFINITY;
+  }
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 u = ldg_stream(p + 4 * i);
+      x[4 * i] = __uint_as_float(u.x), x[4 * i + 1] = __uint_as_float(u.y), x[4 * i + 2] = __uint_as_float(u.z), x[4 * i + 3] = __uint_as_float(u.w);
+    }
+  }
+  __device__ __forceinline__ void store(float* p) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(p + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+  }
+  __device__ __forceinline__ void load(const float* p, int n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e < n ? p[e] : 0.f;
+  }
+  __device__ __forceinline__ void store(float* p, int n) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = x[e];
+  }
+};
 
 template <typename T, typename W>
 __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const AdjustParams p) {
+  constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;          // rows on their way
   extern __shared__ __align__(16) uint8_t adjust_smem[];
   W* slot = reinterpret_cast<W*>(adjust_smem);
   const int tid = threadIdx.x, s = blockIdx.x / p.slices, part = blockIdx.x % p.slices;
   const int v0 = part * p.slice, n_slot = min(p.slice, p.vocab - v0);
   const bool tells = part == 0 && p.status;              // one slice reports what is wrong with the sequence
-  for (int i = tid; i < n_slot; i += ADJUST_THREADS) slot[i] = 0;
+  for (int i = tid * 16 / (int)sizeof(W); i < p.slice; i += ADJUST_THREADS * 16 / (int)sizeof(W))
+    *reinterpret_cast<uint4*>(slot + i) = make_uint4(0, 0, 0, 0);
   pdl_wait();
   pdl_launch();
   int row0 = *(p.row_indptr + s), row1 = *(p.row_indptr + s + 1), err = 0;
+  int len = p.history ? *(p.len + s) : 0, prompt = p.history && p.prompt_len ? *(p.prompt_len + s) : 0;
+  Penalties q{p.repetition ? *(p.repetition + s) : 1.f, p.presence ? *(p.presence + s) : 0.f, p.frequency ? *(p.frequency + s) : 0.f, nullptr,
+              p.entry_shift};
   if (row0 < 0 || row1 > p.total_rows || row1 < row0) {
     if (row0 < 0 || row0 > p.total_rows || row1 < row0) row1 = row0 = 0;
     row1 = min(row1, p.total_rows);
     err = EFIM_DEV_BAD_POSITION;
   }
-  Penalties q{p.repetition ? *(p.repetition + s) : 1.f, p.presence ? *(p.presence + s) : 0.f, p.frequency ? *(p.frequency + s) : 0.f, nullptr, p.entry_shift};
+  if (len < 0 || len > p.max_len || prompt < 0 || prompt > len) err |= EFIM_DEV_BAD_POSITION;
+  len = min(max(len, 0), p.max_len);
+  prompt = min(max(prompt, 0), len);
   __syncthreads();
   if (p.bias) {
     int b0 = *(p.bias_indptr + s), b1 = *(p.bias_indptr + s + 1);
     if (b0 < 0 || b1 > p.bias_entries || b1 < b0) {
-      err = EFIM_DEV_BAD_POSITION;
+      err |= EFIM_DEV_BAD_POSITION;
       b0 = b1 = 0;
     }
     q.bias = p.bias + b0;
     for (int i = tid; i < b1 - b0; i += ADJUST_THREADS) {
       const int x = *(p.bias_tokens + b0 + i);
-      if (x >= v0 && x < v0 + n_slot) atomicMax(&slot[x - v0], (W)(i + 1) << p.entry_shift);   // the last entry of a token counts
-      if (x < 0 || x >= p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+      if ((uint32_t)(x - v0) < (uint32_t)n_slot) atomicMax(&slot[x - v0], (W)(i + 1) << p.entry_shift);   // the last entry of a token counts
+      if ((uint32_t)x >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
     }
     __syncthreads();
   }
-  if (p.history) {
-    int len = *(p.len + s), prompt = p.prompt_len ? *(p.prompt_len + s) : 0;
-    if (len < 0 || len > p.max_len || prompt < 0 || prompt > len) err |= EFIM_DEV_BAD_POSITION;
-    len = min(max(len, 0), p.max_len);
-    prompt = min(max(prompt, 0), len);
+  {
     const int32_t* history = p.history + s * p.history_stride;
-    for (int i = tid; i < len; i += ADJUST_THREADS) {
-      const int x = *(history + i);
-      if (x >= v0 && x < v0 + n_slot) {
+    auto count = [&](int i, int x) {
+      if ((uint32_t)(x - v0) < (uint32_t)n_slot) {
         if (i < prompt) atomicOr(&slot[x - v0], (W)1 << PROMPT_BIT<W>);
         else atomicAdd(&slot[x - v0], (W)1);
       }
-      if (x < 0 || x >= p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+      if ((uint32_t)x >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+    };
+    // four tokens at a time from where the row is 16-byte aligned on, four such vectors on their way
+    const int head = min(len, (int)((16 - (reinterpret_cast<uintptr_t>(history) & 15)) & 15) / 4), vectors = (len - head) / 4;
+    for (int i0 = tid; i0 < vectors; i0 += 4 * ADJUST_THREADS) {
+      int4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i0 + k * ADJUST_THREADS < vectors) x[k] = *reinterpret_cast<const int4*>(history + head + 4 * (i0 + k * ADJUST_THREADS));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * ADJUST_THREADS, at = head + 4 * i;
+        if (i < vectors) {
+          count(at, x[k].x);
+          count(at + 1, x[k].y);
+          count(at + 2, x[k].z);
+          count(at + 3, x[k].w);
+        }
+      }
+    }
+    const int rest = len - head - 4 * vectors;           // before and behind them
+    if (tid < head + rest) {
+      const int i = tid < head ? tid : len - rest + (tid - head);
+      count(i, *(history + i));
     }
   }
-  for (int row = row0; row < row1; ++row) {
-    __syncthreads();
-    if (row > row0 && p.history && p.tokens) {
-      if (tid == 0) {
-        const int x = *(p.tokens + row);
-        if (x >= v0 && x < v0 + n_slot) slot[x - v0] += 1;
-        if (x < 0 || x >= p.vocab) err |= EFIM_DEV_BAD_TOKEN;
-      }
-      __syncthreads();
+  __syncthreads();
+  const bool drafts = p.history && p.tokens, in_place = p.logits == p.out;
+  // A thread has eight neighbouring tokens and walks the sequence's rows with their words in registers.
+  for (int i = tid * 8; i < n_slot; i += ADJUST_THREADS * 8) {
+    const int n = min(8, n_slot - i);
+    const bool whole = p.vector && n == 8;
+    const T* in = static_cast<const T*>(p.logits) + v0 + i;
+    T* out = static_cast<T*>(p.out) + v0 + i;
+    const uint8_t* mask = p.mask ? reinterpret_cast<const uint8_t*>(p.mask) + (v0 + i) / 8 : nullptr;
+    W w[8], any = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = i + e < n_slot ? slot[i + e] : (W)0;
+      any |= w[e];
     }
-    const T* in = static_cast<const T*>(p.logits) + row * p.stride + v0;
-    T* out = static_cast<T*>(p.out) + row * p.out_stride + v0;
-    const uint8_t* mask = p.mask ? reinterpret_cast<const uint8_t*>(p.mask + row * p.mask_stride) + v0 / 8 : nullptr;
-    for (int i = tid * 8; i < n_slot; i += ADJUST_THREADS * 8) {
-      const uint32_t allowed = mask ? *(mask + i / 8) : 0xffu;
-      if (p.vector && i + 8 <= n_slot) {
-        constexpr int WORDS = sizeof(T) / 2;
-        uint4 u[WORDS];
+    for (int r0 = row0; r0 < row1; r0 += AHEAD) {
+      Eight<T> x[AHEAD];
+      uint32_t allowed[AHEAD];
 #pragma unroll
-        for (int e = 0; e < WORDS; ++e) u[e] = *(reinterpret_cast<const uint4*>(in + i) + e);
-        T* x = reinterpret_cast<T*>(u);
+      for (int k = 0; k < AHEAD; ++k)
+        if (r0 + k < row1) {
+          if (whole) x[k].load(in + (r0 + k) * p.stride);
+          else x[k].load(in + (r0 + k) * p.stride, n);
+          allowed[k] = mask ? *(mask + 4 * (r0 + k) * p.mask_stride) : 0xffu;
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = adjust_store<T>(adjusted<W>(adjust_load<T>(x[e]), slot[i + e], allowed >> e & 1, q));
+      for (int k = 0; k < AHEAD; ++k)
+        if (r0 + k < row1) {
+          const int row = r0 + k;
+          if (drafts && row > row0) {                    // the row's own token comes before it
+            const int token = *(p.tokens + row);
+            if ((uint32_t)(token - v0 - i) < (uint32_t)n) {
 #pragma unroll
-        for (int e = 0; e < WORDS; ++e) *(reinterpret_cast<uint4*>(out + i) + e) = u[e];
-      } else {
-        for (int e = 0; e < 8 && i + e < n_slot; ++e)
-          out[i + e] = adjust_store<T>(adjusted<W>(adjust_load<T>(in[i + e]), slot[i + e], allowed >> e & 1, q));
-      }
+              for (int e = 0; e < 8; ++e) w[e] += token - v0 - i == e;
+              any |= 1;
+            }
+            if ((uint32_t)token >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+          }
+          if (any) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (w[e]) x[k].set(e, adjusted<W>(x[k].get(e), w[e], q));
+          }
+          if (allowed[k] != 0xffu) x[k].mask(allowed[k]);
+          if (in_place && !any && allowed[k] == 0xffu) continue;
+          if (whole) x[k].store(out + row * p.out_stride);
+          else x[k].store(out + row * p.out_stride, n);
+        }
     }
   }
   if (err && tells) atomicOr(p.status, err);

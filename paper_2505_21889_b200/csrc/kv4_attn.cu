@@ -32,7 +32,7 @@ __host__ __device__ constexpr int kv4_page_bytes(int D) { return 2 * (kv4_code_b
 // pages that a warp takes at a time, and sets of them in its ring
 __host__ __device__ constexpr int kv4_pages(int NT) { return NT == 1 ? 2 : 1; }
 __host__ __device__ constexpr int kv4_stages(int NT) { return NT == 1 ? 2 : NT == 2 ? 4 : 6; }
-__host__ __device__ constexpr int kv4_ctas_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
+__host__ __device__ constexpr int kv4_ctas_per_sm(int NT) { return NT == 1 ? 3 : 2; }
 __host__ __device__ constexpr int kv4_smem_bytes(int D, int NT) {
   const int ring = KV4_WARPS * kv4_stages(NT) * kv4_pages(NT) * kv4_page_bytes(D), exchange = KV4_WARPS * 8 * NT * (D + 4) * 4;
   return ring > exchange ? ring : exchange;
