@@ -1,9 +1,9 @@
 // efim_adjust_logits: penalties for tokens that occurred, biases and grammar masks on the rows of a step, before they are judged or sampled.
 //
 // A CTA has one sequence's slice of the vocabulary in shared memory, a word per token: how often it was generated, whether the prompt
-// holds it, and which entry of the bias list it has.  It reads the sequence's history once; then each thread takes eight tokens' words into
-// registers and walks the sequence's rows, counting each row's own draft before it (a row's distribution comes after that token).
-// Most words are 0 and most masks whole: such logits are only copied, or left alone in place.
+// holds it, and which entry of the bias list it has.  Few tokens are touched by any of that, so the rows are copied first (with the
+// mask, in place only where it takes something away); then the touched tokens, listed, are computed over it, a thread a token, walking
+// the sequence's rows and counting each row's own draft before it (a row's distribution comes after that token).
 #include "common.cuh"
 #include <algorithm>
 #include <atomic>
@@ -47,15 +47,15 @@ __device__ __forceinline__ float adjusted(float x, W w, const Penalties& q) {
   return x;
 }
 
+__device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ void round_to(float x, uint16_t* y) { *y = (uint16_t)pack_bf16x2(x, 0.f); }
+__device__ __forceinline__ void round_to(float x, float* y) { *y = x; }
+
 // Eight logits of neighbouring tokens, as they lie: 16 bytes of bf16 or 32 of fp32.
 template <typename T> struct Eight;
 template <> struct Eight<uint16_t> {
   uint32_t x[4];
-  __device__ __forceinline__ float get(int e) const { return e & 1 ? bf16hi(x[e / 2]) : bf16lo(x[e / 2]); }
-  __device__ __forceinline__ void set(int e, float y) {
-    const uint32_t b = pack_bf16x2(y, 0.f);
-    x[e / 2] = e & 1 ? __byte_perm(x[e / 2], b, 0x5410) : __byte_perm(x[e / 2], b, 0x3254);
-  }
   __device__ __forceinline__ void mask(uint32_t allowed) {                    // -inf where the bit is 0
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -80,8 +80,6 @@ template <> struct Eight<uint16_t> {
 };
 template <> struct Eight<float> {
   float x[8];
-  __device__ __forceinline__ float get(int e) const { return x[e]; }
-  __device__ __forceinline__ void set(int e, float y) { x[e] = y; }
   __device__ __forceinline__ void mask(uint32_t allowed) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = allowed >> e & 1 ? x[e] : -INFINITY;
@@ -108,16 +106,22 @@ template <> struct Eight<float> {
   }
 };
 
+// places of the list of a slice's touched tokens
+constexpr int ADJUST_LIST = 4096;
+
 template <typename T, typename W>
 __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const AdjustParams p) {
-  constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;          // rows on their way
+  constexpr int AHEAD = 4;                               // loads on their way
   extern __shared__ __align__(16) uint8_t adjust_smem[];
   W* slot = reinterpret_cast<W*>(adjust_smem);
+  __shared__ uint16_t s_list[ADJUST_LIST];
+  __shared__ int s_listed;
   const int tid = threadIdx.x, s = blockIdx.x / p.slices, part = blockIdx.x % p.slices;
   const int v0 = part * p.slice, n_slot = min(p.slice, p.vocab - v0);
   const bool tells = part == 0 && p.status;              // one slice reports what is wrong with the sequence
   for (int i = tid * 16 / (int)sizeof(W); i < p.slice; i += ADJUST_THREADS * 16 / (int)sizeof(W))
     *reinterpret_cast<uint4*>(slot + i) = make_uint4(0, 0, 0, 0);
+  if (tid == 0) s_listed = 0;
   pdl_wait();
   pdl_launch();
   int row0 = *(p.row_indptr + s), row1 = *(p.row_indptr + s + 1), err = 0;
@@ -133,6 +137,42 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
   len = min(max(len, 0), p.max_len);
   prompt = min(max(prompt, 0), len);
   __syncthreads();
+  // ---- every logit: copied, or -inf where the mask says so; in place only the latter
+  {
+    const T* in = static_cast<const T*>(p.logits) + v0;
+    T* out = static_cast<T*>(p.out) + v0;
+    const bool in_place = p.logits == p.out;
+    const int groups = (n_slot + 7) / 8, whole = p.vector ? n_slot / 8 : 0;
+    const uint8_t* mask = reinterpret_cast<const uint8_t*>(p.mask) + v0 / 8;
+    const long long mask_stride = 4 * p.mask_stride;
+    for (int row = row0; row < row1 && !(in_place && !p.mask); ++row) {
+      const T* from = in + row * p.stride;
+      T* to = out + row * p.out_stride;
+      for (int i0 = tid; i0 < groups; i0 += AHEAD * ADJUST_THREADS) {
+        Eight<T> x[AHEAD];
+        uint32_t allowed[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const int i = i0 + k * ADJUST_THREADS;
+          if (i < groups) {
+            allowed[k] = p.mask ? *(mask + row * mask_stride + i) : 0xffu;
+            if (i < whole) x[k].load(from + 8 * i);
+            else x[k].load(from + 8 * i, n_slot - 8 * i);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const int i = i0 + k * ADJUST_THREADS;
+          if (i < groups) {
+            if (allowed[k] != 0xffu) x[k].mask(allowed[k]);
+            else if (in_place) continue;
+            if (i < whole) x[k].store(to + 8 * i);
+            else x[k].store(to + 8 * i, n_slot - 8 * i);
+          }
+        }
+      }
+    }
+  }
   if (p.bias) {
     int b0 = *(p.bias_indptr + s), b1 = *(p.bias_indptr + s + 1);
     if (b0 < 0 || b1 > p.bias_entries || b1 < b0) {
@@ -181,52 +221,52 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
     }
   }
   __syncthreads();
-  const bool drafts = p.history && p.tokens, in_place = p.logits == p.out;
-  // A thread has eight neighbouring tokens and walks the sequence's rows with their words in registers.
-  for (int i = tid * 8; i < n_slot; i += ADJUST_THREADS * 8) {
-    const int n = min(8, n_slot - i);
-    const bool whole = p.vector && n == 8;
-    const T* in = static_cast<const T*>(p.logits) + v0 + i;
-    T* out = static_cast<T*>(p.out) + v0 + i;
-    const uint8_t* mask = p.mask ? reinterpret_cast<const uint8_t*>(p.mask) + (v0 + i) / 8 : nullptr;
-    W w[8], any = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      w[e] = i + e < n_slot ? slot[i + e] : (W)0;
-      any |= w[e];
+  const bool drafts = p.history && p.tokens;
+  if (drafts) {
+    // drafts may touch tokens that nothing else does
+    for (int row = row0 + 1 + tid; row < row1; row += ADJUST_THREADS) {
+      const int x = *(p.tokens + row);
+      if ((uint32_t)(x - v0) < (uint32_t)n_slot && slot[x - v0] == 0) {
+        int before = row0 + 1;                            // once only: where it is drafted first
+        while (before < row && *(p.tokens + before) != x) ++before;
+        if (before == row) {
+          const int at = atomicAdd(&s_listed, 1);
+          if (at < ADJUST_LIST) s_list[at] = (uint16_t)(x - v0);
+        }
+      }
+      if ((uint32_t)x >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
     }
+  }
+  for (int i = tid; i < n_slot; i += ADJUST_THREADS)
+    if (slot[i] != 0) {
+      const int at = atomicAdd(&s_listed, 1);
+      if (at < ADJUST_LIST) s_list[at] = (uint16_t)i;
+    }
+  __syncthreads();
+  // ---- the touched tokens, over what the copy has left; a thread has a token and walks the sequence's rows
+  const T* in = static_cast<const T*>(p.logits) + v0;
+  T* out = static_cast<T*>(p.out) + v0;
+  const bool listed = s_listed <= ADJUST_LIST;
+  const int hits = listed ? s_listed : n_slot;
+  for (int h = tid; h < hits; h += ADJUST_THREADS) {
+    const int i = listed ? s_list[h] : h;
+    W w = slot[i];
+    if (!listed && w == 0 && !drafts) continue;
+    const uint32_t* mask = p.mask ? p.mask + (v0 + i) / 32 : nullptr;
     for (int r0 = row0; r0 < row1; r0 += AHEAD) {
-      Eight<T> x[AHEAD];
-      uint32_t allowed[AHEAD];
+      T x[AHEAD];
+      uint32_t word[AHEAD];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
         if (r0 + k < row1) {
-          if (whole) x[k].load(in + (r0 + k) * p.stride);
-          else x[k].load(in + (r0 + k) * p.stride, n);
-          allowed[k] = mask ? *(mask + 4 * (r0 + k) * p.mask_stride) : 0xffu;
+          x[k] = *(in + (r0 + k) * p.stride + i);
+          word[k] = mask ? *(mask + (r0 + k) * p.mask_stride) : 0xffffffffu;
         }
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
         if (r0 + k < row1) {
-          const int row = r0 + k;
-          if (drafts && row > row0) {                    // the row's own token comes before it
-            const int token = *(p.tokens + row);
-            if ((uint32_t)(token - v0 - i) < (uint32_t)n) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) w[e] += token - v0 - i == e;
-              any |= 1;
-            }
-            if ((uint32_t)token >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
-          }
-          if (any) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (w[e]) x[k].set(e, adjusted<W>(x[k].get(e), w[e], q));
-          }
-          if (allowed[k] != 0xffu) x[k].mask(allowed[k]);
-          if (in_place && !any && allowed[k] == 0xffu) continue;
-          if (whole) x[k].store(out + row * p.out_stride);
-          else x[k].store(out + row * p.out_stride, n);
+          if (drafts && r0 + k > row0) w += *(p.tokens + r0 + k) == v0 + i;   // the row's own token comes before it
+          if (w && (word[k] >> ((v0 + i) & 31) & 1)) round_to(adjusted<W>(value_of(x[k]), w, q), out + (r0 + k) * p.out_stride + i);
         }
     }
   }

@@ -137,6 +137,19 @@ def test_long_lists_and_histories(most, dtype):
     assert case.status.item() == 0
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+def test_drafts_of_one_token(in_place):
+    """A token that only the drafts bring, several times over; a history that touches more tokens than a slice's list holds."""
+    case = Case([7, 3], 40000, [30000, 3], seed=4, bias=0)
+    case.history[0, :30000] = np.random.default_rng(1).permutation(40000)[:30000]
+    case.history[1] = 5
+    case.prompt = [10000, 0]
+    case.tokens[:] = [39999] * 3 + [7] * 4 + [39999, 12345, 12345]
+    case.run(in_place)
+    case.check()
+    assert case.status.item() == 0
+
+
 def test_values_that_are_not_finite():
     case = Case([2], 300, [12], torch.float32, bias=0)
     case.history[0, :4] = [0, 1, 2, 3]
