@@ -145,32 +145,36 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
     const int groups = (n_slot + 7) / 8, whole = p.vector ? n_slot / 8 : 0;
     const uint8_t* mask = reinterpret_cast<const uint8_t*>(p.mask) + v0 / 8;
     const long long mask_stride = 4 * p.mask_stride;
-    for (int row = row0; row < row1 && !(in_place && !p.mask); ++row) {
-      const T* from = in + row * p.stride;
-      T* to = out + row * p.out_stride;
-      for (int i0 = tid; i0 < groups; i0 += AHEAD * ADJUST_THREADS) {
-        Eight<T> x[AHEAD];
-        uint32_t allowed[AHEAD];
+    // rows (65,536 at a time) and groups of eight as one range
+    for (int first = row0; first < row1 && !(in_place && !p.mask); first += 65536) {
+    const int pieces = min(row1 - first, 65536) * groups;
+    for (int i0 = tid; i0 < pieces; i0 += AHEAD * ADJUST_THREADS) {
+      Eight<T> x[AHEAD];
+      uint32_t allowed[AHEAD];
+      int row[AHEAD], at[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          const int i = i0 + k * ADJUST_THREADS;
-          if (i < groups) {
-            allowed[k] = p.mask ? *(mask + row * mask_stride + i) : 0xffu;
-            if (i < whole) x[k].load(from + 8 * i);
-            else x[k].load(from + 8 * i, n_slot - 8 * i);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-          const int i = i0 + k * ADJUST_THREADS;
-          if (i < groups) {
-            if (allowed[k] != 0xffu) x[k].mask(allowed[k]);
-            else if (in_place) continue;
-            if (i < whole) x[k].store(to + 8 * i);
-            else x[k].store(to + 8 * i, n_slot - 8 * i);
-          }
+      for (int k = 0; k < AHEAD; ++k) {
+        const int i = i0 + k * ADJUST_THREADS;
+        if (i < pieces) {
+          const int r = i / groups;
+          row[k] = first + r;
+          at[k] = i - r * groups;
+          const T* from = in + row[k] * p.stride + 8 * at[k];
+          allowed[k] = p.mask ? *(mask + row[k] * mask_stride + at[k]) : 0xffu;
+          if (at[k] < whole) x[k].load(from);
+          else x[k].load(from, n_slot - 8 * at[k]);
         }
       }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (i0 + k * ADJUST_THREADS < pieces) {
+          T* to = out + row[k] * p.out_stride + 8 * at[k];
+          if (allowed[k] != 0xffu) x[k].mask(allowed[k]);
+          else if (in_place) continue;
+          if (at[k] < whole) x[k].store(to);
+          else x[k].store(to, n_slot - 8 * at[k]);
+        }
+    }
     }
   }
   if (p.bias) {
