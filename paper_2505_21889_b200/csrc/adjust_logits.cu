@@ -23,7 +23,7 @@ struct AdjustParams {
   const float* bias;
   const uint32_t* mask;
   int32_t* status;
-  int batch, total_rows, vocab, max_len, bias_entries, entry_shift, slice, slices, vector;
+  int batch, total_rows, vocab, max_len, bias_entries, entry_shift, slice, slice_bits, slices, vector;
 };
 
 constexpr int ADJUST_THREADS = 512;
@@ -59,7 +59,9 @@ template <> struct Eight<uint16_t> {
   __device__ __forceinline__ void mask(uint32_t allowed) {                    // -inf where the bit is 0
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t keep = (allowed >> (2 * i) & 1 ? 0xffffu : 0u) | (allowed >> (2 * i) & 2 ? 0xffff0000u : 0u);
+      // bits 2i and 2i + 1 as the signs of two bytes, and those signs over two halves
+      uint32_t keep;
+      asm("prmt.b32 %0, %1, 0, 0x9988;" : "=r"(keep) : "r"((allowed >> (2 * i) & 3u) * (1u << 7 | 1u << 14)));
       x[i] = (x[i] & keep) | (0xff80ff80u & ~keep);
     }
   }
@@ -106,8 +108,8 @@ template <> struct Eight<float> {
   }
 };
 
-// places of the list of a slice's touched tokens
-constexpr int ADJUST_LIST = 4096;
+// most tokens of a slice, and places of the list of the touched ones
+constexpr int ADJUST_SLICE = 16384, ADJUST_LIST = 4096;
 
 template <typename T, typename W>
 __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const AdjustParams p) {
@@ -139,42 +141,41 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
   __syncthreads();
   // ---- every logit: copied, or -inf where the mask says so; in place only the latter
   {
-    const T* in = static_cast<const T*>(p.logits) + v0;
-    T* out = static_cast<T*>(p.out) + v0;
     const bool in_place = p.logits == p.out;
     const int groups = (n_slot + 7) / 8, whole = p.vector ? n_slot / 8 : 0;
-    const uint8_t* mask = reinterpret_cast<const uint8_t*>(p.mask) + v0 / 8;
-    const long long mask_stride = 4 * p.mask_stride;
-    // rows (65,536 at a time) and groups of eight as one range
-    for (int first = row0; first < row1 && !(in_place && !p.mask); first += 65536) {
-    const int pieces = min(row1 - first, 65536) * groups;
-    for (int i0 = tid; i0 < pieces; i0 += AHEAD * ADJUST_THREADS) {
+    // A pass of the CTA is AHEAD groups of eight a thread: a row or a part of it, or several rows of a small slice
+    const int bits = p.slice_bits - 3, rows = max(1, AHEAD * ADJUST_THREADS >> bits);
+    const T* from[AHEAD];
+    T* to[AHEAD];
+    const uint8_t* mask[AHEAD];
+    int row_of[AHEAD], at[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = tid + k * ADJUST_THREADS;
+      at[k] = i & ((1 << bits) - 1);
+      row_of[k] = at[k] < groups ? i >> bits : 1 << 30;   // (past every row)
+      from[k] = static_cast<const T*>(p.logits) + (i >> bits) * p.stride + v0 + 8 * at[k];
+      to[k] = static_cast<T*>(p.out) + (i >> bits) * p.out_stride + v0 + 8 * at[k];
+      mask[k] = reinterpret_cast<const uint8_t*>(p.mask) + (i >> bits) * 4 * p.mask_stride + v0 / 8 + at[k];
+    }
+    for (int row = row0; row < row1 && !(in_place && !p.mask); row += rows) {
       Eight<T> x[AHEAD];
       uint32_t allowed[AHEAD];
-      int row[AHEAD], at[AHEAD];
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const int i = i0 + k * ADJUST_THREADS;
-        if (i < pieces) {
-          const int r = i / groups;
-          row[k] = first + r;
-          at[k] = i - r * groups;
-          const T* from = in + row[k] * p.stride + 8 * at[k];
-          allowed[k] = p.mask ? *(mask + row[k] * mask_stride + at[k]) : 0xffu;
-          if (at[k] < whole) x[k].load(from);
-          else x[k].load(from, n_slot - 8 * at[k]);
-        }
-      }
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
-        if (i0 + k * ADJUST_THREADS < pieces) {
-          T* to = out + row[k] * p.out_stride + 8 * at[k];
+        if (row_of[k] < row1 - row) {
+          allowed[k] = p.mask ? *(mask[k] + row * 4 * p.mask_stride) : 0xffu;
+          if (at[k] < whole) x[k].load(from[k] + row * p.stride);
+          else x[k].load(from[k] + row * p.stride, n_slot - 8 * at[k]);
+        }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (row_of[k] < row1 - row) {
           if (allowed[k] != 0xffu) x[k].mask(allowed[k]);
           else if (in_place) continue;
-          if (at[k] < whole) x[k].store(to);
-          else x[k].store(to, n_slot - 8 * at[k]);
+          if (at[k] < whole) x[k].store(to[k] + row * p.out_stride);
+          else x[k].store(to[k] + row * p.out_stride, n_slot - 8 * at[k]);
         }
-    }
     }
   }
   if (p.bias) {
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
         if (i < prompt) atomicOr(&slot[x - v0], (W)1 << PROMPT_BIT<W>);
         else atomicAdd(&slot[x - v0], (W)1);
       }
-      if ((uint32_t)x >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
+      if (tells && (uint32_t)x >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
     };
     // four tokens at a time from where the row is 16-byte aligned on, four such vectors on their way
     const int head = min(len, (int)((16 - (reinterpret_cast<uintptr_t>(history) & 15)) & 15) / 4), vectors = (len - head) / 4;
@@ -241,11 +242,32 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
       if ((uint32_t)x >= (uint32_t)p.vocab) err |= EFIM_DEV_BAD_TOKEN;
     }
   }
-  for (int i = tid; i < n_slot; i += ADJUST_THREADS)
-    if (slot[i] != 0) {
-      const int at = atomicAdd(&s_listed, 1);
-      if (at < ADJUST_LIST) s_list[at] = (uint16_t)i;
+  {
+    // a thread's touched tokens as bits, 16 bytes of words at a time; a warp's take their places together
+    constexpr int PER = 16 / sizeof(W);
+    uint32_t mine = 0;
+    for (int k = 0; k * ADJUST_THREADS * PER < p.slice; ++k) {
+      const int i = (k * ADJUST_THREADS + tid) * PER;
+      if (i >= p.slice) break;
+      W w[PER];
+      *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(slot + i);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) mine |= (w[e] != 0 ? 1u : 0u) << (k * PER + e);
     }
+    int upto = __popc(mine);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, d);
+      if ((tid & 31) >= d) upto += y;
+    }
+    int at = 0;
+    if ((tid & 31) == 31 && upto) at = atomicAdd(&s_listed, upto);
+    at = __shfl_sync(0xffffffffu, at, 31) + upto - __popc(mine);
+    for (; mine; mine &= mine - 1, ++at) {
+      const int bit = __ffs(mine) - 1;
+      if (at < ADJUST_LIST) s_list[at] = (uint16_t)((bit / PER * ADJUST_THREADS + tid) * PER + bit % PER);
+    }
+  }
   __syncthreads();
   // ---- the touched tokens, over what the copy has left; a thread has a token and walks the sequence's rows
   const T* in = static_cast<const T*>(p.logits) + v0;
@@ -279,7 +301,7 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
 
 template <typename T, typename W>
 static efim_status adjust_launch(const AdjustParams& p, cudaStream_t stream) {
-  constexpr int kMaxDevices = 64, kMost = 16384 * (int)sizeof(W);
+  constexpr int kMaxDevices = 64, kMost = ADJUST_SLICE * (int)sizeof(W);
   static std::atomic<bool> done[kMaxDevices];
   int dev = 0;
   EFIM_CUDA_TRY(cudaGetDevice(&dev));
@@ -349,8 +371,9 @@ extern "C" efim_status efim_adjust_logits(const efim_adjust_desc* d, void* d_out
   p.entry_shift = bits((long long)d->max_len + d->total_rows);
   const bool narrow = p.entry_shift + bits(d->d_bias ? d->bias_entries : 0) <= 31;
   if (!narrow) p.entry_shift = 32;
-  p.slice = narrow ? 16384 : 8192;
+  p.slice = narrow ? ADJUST_SLICE : ADJUST_SLICE / 2;
   while (p.slice > 2048 && (long long)d->batch * ((d->vocab + p.slice - 1) / p.slice) < 2LL * sm_count()) p.slice /= 2;
+  while (1 << p.slice_bits < p.slice) ++p.slice_bits;
   p.slices = (d->vocab + p.slice - 1) / p.slice;
   if ((long long)p.batch * p.slices > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
