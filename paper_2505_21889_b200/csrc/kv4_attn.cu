@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <climits>
+#include <type_traits>
 
 namespace efim {
 
@@ -119,13 +120,22 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4AttnParams& p, int s) {
 // The work of a call is a line of trips (a trip: PG pages by each of a CTA's warps), unit after unit: (sequence, kv head, tile of rows).  Each CTA has
 // an equal piece of the line, so all end together whatever the lengths are; a unit that lies in one piece is finished
 // there, the pieces of the others leave partial results, which a second kernel joins.  A piece has at most two such: of a unit that began before it
-// (kept in the CTA's first place), and of one that goes on behind it (second place).  A unit's start (queries, first pages, results)
-// costs about as much as START trips and, where pieces are a good deal longer than that, stands in the line as that many before its own.
+// (kept in the CTA's first place), and of one that goes on behind it (second place).  The line is measured in
+// what trips cost: COST of a tile's 8-row parts that have rows; a unit's start (queries, first pages, results) stands in it with START
+// before the unit's trips, where pieces are a good deal longer than that.  (Microseconds of a trip with 1 / 2 / 3 / 4 parts, NT = 4: 0.81 / 0.93 /
+// 1.21 / 1.41, its start 6 to 9; with NT = 1 1.9, its start 6.)
 template <int NT>
 struct Kv4Line {
-  static constexpr int TRIP = 16 * KV4_WARPS * kv4_pages(NT), START = NT == 4 ? 5 : 3;     // (TRIP: keys of a trip)
+  static constexpr int TRIP = 16 * KV4_WARPS * kv4_pages(NT);              // keys of a trip
+  static constexpr int START = NT == 1 ? 3 : 35, MOST = NT == 1 ? 1 : NT + 3;
+  static __device__ __forceinline__ int cost(int rows) { return NT == 1 ? 1 : (rows + 7) / 8 + 3; }
   static __device__ __forceinline__ int trips(const Kv4Seq& w) { return max(1, (w.ctx + TRIP - 1) / TRIP); }
   static __device__ __forceinline__ int tiles(const Kv4Seq& w, int G) { return (w.new_len * G + 8 * NT - 1) / (8 * NT); }
+  // of a kv head: all tiles but the last are full
+  static __device__ __forceinline__ long long costs(const Kv4Seq& w, int G) {
+    const int n = tiles(w, G);
+    return n == 0 ? 0 : (n - 1LL) * MOST + cost(w.new_len * G - (n - 1) * 8 * NT);
+  }
 };
 // what a CTA leaves for the joining kernel
 struct Kv4Piece {
@@ -156,19 +166,19 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   pdl_launch();
   // ---- this CTA's piece of the line
   long long x0, x1;                       // in trips
-  int seq, off;                           // its first sequence, and what of that one lies before it
+  int seq;                                // its first sequence
+  long long off;                          // what of that one, then of the unit at hand, lies before it
   int start = 0;                          // what a unit's start counts
   if (p.whole) {                          // units that are never cut, one a CTA
     seq = blockIdx.x / p.units_per_seq;
     x0 = x1 = off = 0;
   } else {
     const int per = (p.batch + KV4_THREADS - 1) / KV4_THREADS, first = min(p.batch, tid * per), last = min(p.batch, first + per);
-    auto units_of = [&](const Kv4Seq& q) { return (long long)Line::tiles(q, G) * p.Hkv; };
-    long long mine[2] = {0, 0};           // trips, units
+    long long mine[2] = {0, 0};           // of trips, units
     for (int i = first; i < last; ++i) {
       const Kv4Seq q = kv4_seq(p, i);
-      mine[0] += units_of(q) * Line::trips(q);
-      mine[1] += units_of(q);
+      mine[0] += Line::costs(q, G) * Line::trips(q) * p.Hkv;
+      mine[1] += (long long)Line::tiles(q, G) * p.Hkv;
     }
     long long upto[2] = {mine[0], mine[1]}, total[2] = {0, 0};
 #pragma unroll
@@ -190,7 +200,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       }
     start = total[0] >= 4LL * Line::START * gridDim.x ? Line::START : 0;
     const long long all = total[0] + start * total[1], before = upto[0] - mine[0] + start * (upto[1] - mine[1]);
-    const long long share = max((long long)p.least_trips, (all + gridDim.x - 1) / gridDim.x);
+    const long long share = max((long long)p.least_trips * Line::MOST, (all + gridDim.x - 1) / gridDim.x);
     x0 = blockIdx.x * share;
     x1 = min(all, x0 + share);
     if (x0 >= all) {
@@ -202,7 +212,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       int i = first;
       for (; i < last - 1; ++i) {
         const Kv4Seq q = kv4_seq(p, i);
-        const long long y = units_of(q) * (start + Line::trips(q));
+        const long long y = ((long long)start * Line::tiles(q, G) + Line::costs(q, G) * Line::trips(q)) * p.Hkv;
         if (x0 < at + y) break;
         at += y;
       }
@@ -211,21 +221,24 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     }
     __syncthreads();
     seq = s_seq;
-    off = (int)min(x0 - s_at, 0x7fffffffLL);
+    off = x0 - s_at;
   }
   Kv4Seq w = kv4_seq(p, seq);
-  int unit;                               // of the sequence's units (kv head, tile): the one at hand, `off` of it done
+  int kvh, tile;                          // the unit at hand, `off` of it done
   if (p.whole) {
-    unit = blockIdx.x % p.units_per_seq;
-    const int tiles = Line::tiles(w, G);
+    const int unit = blockIdx.x % p.units_per_seq;
     if (w.err && unit == 0 && tid == 0 && p.status) atomicOr(p.status, w.err);
-    if (unit / p.row_tiles >= p.Hkv || unit % p.row_tiles >= tiles) return;
-    unit = unit / p.row_tiles * tiles + unit % p.row_tiles;
-    x1 = Line::trips(w);
+    kvh = unit / p.row_tiles;
+    tile = unit % p.row_tiles;
+    if (tile >= Line::tiles(w, G)) return;
+    x1 = (long long)Line::trips(w) * Line::cost(min(ROWS, w.new_len * G - tile * ROWS));
   } else {
-    const int n = start + Line::trips(w);
-    unit = off / n;
-    off %= n;
+    const int n = Line::trips(w), tiles = Line::tiles(w, G);
+    const long long per_head = (long long)start * tiles + Line::costs(w, G) * n, full = start + (long long)Line::MOST * n;
+    kvh = (int)(off / per_head);
+    off -= kvh * per_head;
+    tile = (int)min(off / full, tiles - 1LL);
+    off -= tile * full;
   }
   Kv4Piece left{-1, 0, 0, 0};
   if (!p.whole && blockIdx.x == 0)        // one CTA reports the lengths that do not fit
@@ -235,18 +248,18 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   auto token_of = [&](int row) { return p.max_new == 1 ? 0 : row / G; };
   while (x0 < x1) {
   const int tiles = Line::tiles(w, G);
-  const int kvh = unit / tiles, tile = unit % tiles;
-  const int unit_len = start + Line::trips(w), here = (int)min((long long)(unit_len - off), x1 - x0);   // of the unit in this piece
-  const int trip0 = max(off - start, 0), trip1 = off + here - start;
-  const bool first_part = trip0 > 0, ends = off + here == unit_len;        // the unit began before this piece; it ends in it
-  if (trip1 <= 0) break;                  // (the piece ends before the unit's first trip: it begins in the next one)
+  const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0), cost = Line::cost(n_rows);
+  // (a unit's length fits 32 bits: 2^31 keys in trips of 64 or more)
+  const int unit_len = start + Line::trips(w) * cost, from = (int)off, here = (int)min((long long)(unit_len - from), x1 - x0);   // of the unit in this piece
+  const int trip0 = max(from - start, 0) / cost, trip1 = max(from + here - start, 0) / cost;
+  const bool first_part = trip0 > 0, ends = from + here == unit_len;       // the unit began before this piece; it ends in it
+  if (trip1 <= trip0) break;              // (the piece ends before the unit's first trip: it begins in the next one)
   const int32_t* bt = p.block_table + (size_t)seq * p.max_pages_per_seq;
   // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece
   const int begin = trip0 * Line::TRIP, first_pg = (begin >> 4) + PG * warp;
   auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
-  const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
   // keys that the tile's last row sees, of this piece
-  const int end = min(min(w.ctx, w.cached + token_of(row0 + n_rows - 1) + 1), trip1 * Line::TRIP);
+  const int end = (int)min((long long)min(w.ctx, w.cached + token_of(row0 + n_rows - 1) + 1), (long long)trip1 * Line::TRIP);
   const int last_pg = (end - 1) >> 4;
   const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
   // Lane l holds where the l-th of this warp's pages is (then of the next 32): (page, kv head) in the pools, -1 for no page.
@@ -385,6 +398,9 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   // trips whose pages every row sees in full
   const int seen = max(first_limit, 0) >> 4, n_full = seen >= first_pg + PG ? (seen - first_pg - PG) / (KV4_WARPS * PG) + 1 : 0;
 
+  // The walk over the pages, for as many 8-row tiles as have rows (a call's sequences bring different numbers of them).
+  auto walk = [&](auto active) {
+  constexpr int NA = decltype(active)::value;
   int at = 0;                             // where in the ring the trip's pages are
   for (int i = 0; i < n_trips; ++i) {
     __syncwarp();                         // everyone is done with the stage of the last trip
@@ -396,7 +412,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 #pragma unroll
     for (int x = 0; x < PG; ++x) key0[x] = (missing >> (ST * PG - 1 - x)) & 1u ? INT_MAX - 16 : page_of(i * PG + x) << 4;
     // ---- S^T
-    float sx[PG][NT][4];
+    float sx[PG][NA][4];
 #pragma unroll
     for (int x = 0; x < PG; ++x) {
       __half2 scale[2];                    // of the two tokens: the lane's blocks of 16 dims, D / 64 of them
@@ -426,7 +442,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
         for (int k = 0; k < 2; ++k) {
           const uint32_t a[4] = {kx[0][2 * k], kx[1][2 * k], kx[0][2 * k + 1], kx[1][2 * k + 1]};
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
+          for (int n = 0; n < NA; ++n) {
             uint2 u;
             if constexpr (Q_IN_REGS) u = make_uint2(qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
             else u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
@@ -440,7 +456,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 #pragma unroll
       for (int x = 0; x < PG; ++x)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NA; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (key0[x] + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[x][n][e] = -INFINITY;
@@ -461,9 +477,9 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     }
     // ---- the reference; values that are NaN
     bool grow = false, nan = false;
-    float mx[NT][2];
+    float mx[NA][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NA; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         mx[n][e] = fmaxf(sx[0][n][e], sx[0][n][e + 2]);
@@ -477,7 +493,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     // own scores: its bits do not depend on the other rows.
     if (__any_sync(0xffffffffu, grow | nan)) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NA; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float x = mx[n][e];
@@ -512,9 +528,9 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     }
 #pragma unroll
     for (int x = 0; x < PG; ++x) {
-      uint32_t pb[NT][2];
+      uint32_t pb[NA][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NA; ++n)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float x0 = kv4_ex2(fmaf(sx[x][n][2 * h], sc[n][0], -m_off[n][0])), x1 = kv4_ex2(fmaf(sx[x][n][2 * h + 1], sc[n][1], -m_off[n][1]));
@@ -555,11 +571,24 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
         for (int e = 0; e < 4; ++e) {
           const uint32_t a[4] = {lo[0][e], hi[0][e], lo[1][e], hi[1][e]};
 #pragma unroll
-          for (int n = 0; n < NT; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
+          for (int n = 0; n < NA; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
         }
       }
     }
     at = at == (ST - 1) * STAGE ? 0 : at + STAGE;
+  }
+  };
+  using std::integral_constant;
+  if constexpr (NT == 1) {
+    walk(integral_constant<int, 1>());
+  } else if constexpr (NT == 2) {
+    if (n_rows <= 8) walk(integral_constant<int, 1>());
+    else walk(integral_constant<int, 2>());
+  } else {
+    if (n_rows <= 8) walk(integral_constant<int, 1>());
+    else if (n_rows <= 16) walk(integral_constant<int, 2>());
+    else if (n_rows <= 24) walk(integral_constant<int, 3>());
+    else walk(integral_constant<int, 4>());
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   // ---- fold the lanes' sums, then the 4 warps (the exchange buffer takes their rings' place)
@@ -622,8 +651,12 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   x0 += here;
   off = 0;
   if (x0 < x1) {
-    if (++unit == tiles * p.Hkv) {
-      unit = 0;
+    if (++tile == tiles) {
+      tile = 0;
+      ++kvh;
+    }
+    if (kvh == p.Hkv) {
+      kvh = 0;
       do w = kv4_seq(p, ++seq);
       while (w.new_len == 0);                       // (the line goes on, so there is one)
     }
