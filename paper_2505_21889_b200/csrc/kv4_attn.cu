@@ -666,12 +666,13 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   if (!p.whole && tid == 0) p.pieces[blockIdx.x] = left;
 }
 
-// Joins a unit's partial results: lse = log2 sum 2^lse_c, o = sum 2^(lse_c - lse) o_c.  The CTA of the piece that the unit begins in: its second place, then
-// the first places of those behind it until the unit ends.  A warp has a row, lanes over head_dim.
+// Joins a unit's partial results: lse = log2 sum 2^lse_c, o = sum 2^(lse_c - lse) o_c.  A CTA has four rows of the unit that goes on behind a
+// piece: its second place, then the first places of the pieces behind it until the unit ends.  A warp has a row, lanes over head_dim; the
+// weights of 32 pieces are computed by the lanes together, four pieces' rows are on their way at a time.
 template <int D, int NT>
 __global__ void __launch_bounds__(KV4_THREADS) kv4_join_kernel(const Kv4AttnParams p) {
-  constexpr int EPL = D / 32, ROWS = 8 * NT;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int EPL = D / 32, ROWS = 8 * NT, AT_ONCE = 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.y * KV4_WARPS + warp;
   pdl_wait();
   pdl_launch();
   const Kv4Piece me = p.pieces[blockIdx.x];
@@ -686,37 +687,50 @@ __global__ void __launch_bounds__(KV4_THREADS) kv4_join_kernel(const Kv4AttnPara
     }
   }
   const Kv4Seq w = kv4_seq(p, me.seq);
-  const int G = p.Hq / p.Hkv, row0 = me.tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0);
-  for (int r = warp; r < n_rows; r += KV4_WARPS) {
-    const size_t first = ((size_t)blockIdx.x * 2 + 1) * ROWS + r;              // the c-th one: ROWS places on, then every 2 ROWS
-    auto place = [&](int c) { return first + (c == 0 ? 0 : (size_t)(2 * c - 1) * ROWS); };
-    float M = -INFINITY;
-    for (int c = lane; c < n; c += 32) M = max_nan(M, p.part_lse[place(c)]);   // a NaN piece makes the row NaN
+  const int G = p.Hq / p.Hkv, row = me.tile * ROWS + r;
+  if (row >= w.new_len * G) return;
+  const size_t first = ((size_t)blockIdx.x * 2 + 1) * ROWS + r;                // the c-th one: ROWS places on, then every 2 ROWS
+  auto place = [&](int c) { return first + (c == 0 ? 0 : (size_t)(2 * c - 1) * ROWS); };
+  float M = -INFINITY;
+  for (int c = lane; c < n; c += 32) M = max_nan(M, p.part_lse[place(c)]);     // a NaN piece makes the row NaN
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, d));
-    float L = 0.f, acc[EPL];
+  for (int d = 16; d > 0; d >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, d));
+  float L = 0.f, acc[EPL];
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
-    if (!(M == -INFINITY)) {                        // else a row without keys
-      for (int c = 0; c < n; ++c) {
-        const float lse = p.part_lse[place(c)];
-        if (lse == -INFINITY) continue;             // (a piece that the row sees nothing of)
-        const float wi = exp2f(lse - M);
-        L += wi;
-        const float* po = p.part_o + place(c) * D + lane * EPL;
+  for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+  for (int c0 = 0; c0 < n && !(M == -INFINITY); c0 += 32) {                    // (else a row without keys)
+    const float lse = c0 + lane < n ? p.part_lse[place(c0 + lane)] : -INFINITY;
+    const float wi = lse == -INFINITY ? 0.f : exp2f(lse - M);
+    L += wi;
+    const int some = min(32, n - c0);
+    for (int k0 = 0; k0 < some; k0 += AT_ONCE) {
+      float x[AT_ONCE][EPL];
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) acc[e] = fmaf(wi, po[e], acc[e]);
-      }
+      for (int k = 0; k < AT_ONCE; ++k)
+        if (k0 + k < some) {
+          const float* po = p.part_o + place(c0 + k0 + k) * D + lane * EPL;
+          if constexpr (EPL == 4) *reinterpret_cast<float4*>(x[k]) = *reinterpret_cast<const float4*>(po);
+          else *reinterpret_cast<float2*>(x[k]) = *reinterpret_cast<const float2*>(po);
+        }
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k)
+        if (k0 + k < some) {
+          const float wk = __shfl_sync(0xffffffffu, wi, k0 + k);
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) acc[e] = fmaf(wk, x[k][e], acc[e]);
+        }
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    const size_t row_head = (size_t)(w.first_row + (row0 + r) / G) * p.Hq + me.head * G + (row0 + r) % G;
-    uint16_t* out = p.out + row_head * D + lane * EPL;
-    if constexpr (EPL == 4)
-      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-    else
-      *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-    if (p.lse && lane == 0) p.lse[row_head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
   }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const size_t row_head = (size_t)(w.first_row + row / G) * p.Hq + me.head * G + row % G;
+  uint16_t* out = p.out + row_head * D + lane * EPL;
+  if constexpr (EPL == 4)
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+  else
+    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  if (p.lse && lane == 0) p.lse[row_head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
 // One wave of CTAs, fewer where their pieces would fall below KV4_LEAST keys.  Units that fit KV4_WHOLE keys are not cut.
@@ -753,7 +767,7 @@ static efim_status kv4_launch_nt(const Kv4AttnParams& p, const Kv4Plan& pl, cuda
     if (dev >= 0 && dev < kMaxDevices) done[dev].store(true, std::memory_order_release);
   }
   EFIM_CUDA_TRY(launch_pdl(kv4_attn_kernel<D, NT>, dim3((unsigned)pl.ctas), dim3(KV4_THREADS), smem, s, p));
-  if (!pl.whole) EFIM_CUDA_TRY(launch_pdl(kv4_join_kernel<D, NT>, dim3((unsigned)pl.ctas), dim3(KV4_THREADS), 0, s, p));
+  if (!pl.whole) EFIM_CUDA_TRY(launch_pdl(kv4_join_kernel<D, NT>, dim3((unsigned)pl.ctas, 8 * NT / KV4_WARPS), dim3(KV4_THREADS), 0, s, p));
   return EFIM_OK;
 }
 template <int D>

@@ -94,10 +94,16 @@ Lengths longest(const efim_batch_desc* b) {
   }
   return r;
 }
-// Rows a kv head up to which the keys are taken from the codes by the decode kernel.
-constexpr long long KV4_DIRECT_ROWS = 64;
-bool goes_direct(const efim_cache4_desc* cache, const Lengths& most) {
-  return (long long)most.new_len * (cache->num_q_heads / cache->num_kv_heads) <= KV4_DIRECT_ROWS;
+// Rows a (sequence, kv head) up to which the keys are taken from the codes by the decode kernel: its time grows with the rows, the other way's first
+// with the pages that are unpacked.  Microseconds, direct / unpacked: 16 x 5k keys at 32/8 heads 32 rows 93 / 197, 64 148 / 200, 96 202 / 201, 128 255 / 203;
+// at 28/4 56 rows 89 / 101, 84 116 / 101; 8 x 4k at 32/32 64 rows 200 / 314, 128 362 / 320; 64 x 2k at 32/8 64 rows 235 / 278, 96 329 / 285; 16 x 5k at
+// 8/8 x 64 64 rows 112 / 119, 128 183 / 121.  With few pages, where both are latencies: 1 x 4k at 32/8 8 rows 21.5 / 27.6, 16 25.6 / 27.7, 32 35.8 / 27.6.
+bool goes_direct(const efim_cache4_desc* cache, const efim_batch_desc* batch, const Lengths& most) {
+  long long page_heads = 0;
+  for (int s = 0; s < batch->batch; ++s)
+    if (batch->h_new_len[s] > 0) page_heads += ((long long)batch->h_cached_len[s] + batch->h_new_len[s] + 15) / 16 * cache->num_kv_heads;
+  const long long rows = (long long)most.new_len * (cache->num_q_heads / cache->num_kv_heads);
+  return rows <= (page_heads < 64LL * sm_count() ? 16 : 80);
 }
 efim_status check(const efim_cache4_desc* cache, const efim_batch_desc* batch) {
   const efim_status st = check_cache4(cache);
@@ -112,7 +118,7 @@ extern "C" size_t efim_kv4_prefill_workspace_bytes(const efim_cache4_desc* cache
   using namespace efim;
   if (check(cache, batch) != EFIM_OK || batch->batch == 0 || batch->total_new_tokens == 0) return 0;
   const Lengths most = longest(batch);
-  if (goes_direct(cache, most)) return kv4_plan(cache, batch->batch, most.new_len, most.ctx).bytes;
+  if (goes_direct(cache, batch, most)) return kv4_plan(cache, batch->batch, most.new_len, most.ctx).bytes;
   const StagePlan pl = stage_plan(cache, batch);
   if (pl.pages * cache->num_kv_heads > 0x7fffffffLL) return 0;
   efim_cache_desc c;
@@ -130,7 +136,7 @@ extern "C" efim_status efim_kv4_append_prefill_attn(const efim_cache4_desc* cach
   if (batch->batch == 0 || batch->total_new_tokens == 0) return EFIM_OK;
   if (!d_q || !d_out || ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out)) & 15)) return EFIM_ERR_INVALID_ARG;
   const Lengths most = longest(batch);
-  if (goes_direct(cache, most)) {
+  if (goes_direct(cache, batch, most)) {
     Kv4AttnParams p{};
     p.q = static_cast<const uint16_t*>(d_q);
     p.len = batch->d_cached_len;
