@@ -31,55 +31,65 @@ struct Kv4AppendParams {
 
 constexpr int KV4_APPEND_THREADS = 256;
 
-// 8 weights from position d on
-__device__ __forceinline__ void kv4_load_weights(const void* weight, int f32, float offset, int d, float* w) {
+// 8 weights from position d on, as the products take them
+__device__ __forceinline__ void kv4_load_weights(const void* weight, int f32, float offset, int d, float2* w) {
+  if (!weight) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = 1.f;
-  if (!weight) return;
+    for (int i = 0; i < 4; ++i) w[i] = make_float2(1.f, 1.f);
+    return;
+  }
   if (f32) {
     const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(weight) + d);
-    *reinterpret_cast<float4*>(w) = src[0];
-    *reinterpret_cast<float4*>(w + 4) = src[1];
+    const float4 u = src[0], v = src[1];
+    w[0] = make_float2(u.x, u.y);
+    w[1] = make_float2(u.z, u.w);
+    w[2] = make_float2(v.x, v.y);
+    w[3] = make_float2(v.z, v.w);
   } else {
     const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(weight) + d);
     const uint32_t p[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[2 * i] = bf16lo(p[i]);
-      w[2 * i + 1] = bf16hi(p[i]);
-    }
+    for (int i = 0; i < 4; ++i) w[i] = make_float2(bf16lo(p[i]), bf16hi(p[i]));
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] += offset;
+  for (int i = 0; i < 4; ++i) w[i] = add2(w[i], make_float2(offset, offset));
 }
 
 // Eight of a block's sixteen values (bf16 numbers; the other eight are the neighbour lane's) to a word of codes and the block's scale.
-// Rounding x / s without a division: x and every border t s between two codes are numbers of at most 8 significant bits, so
-// they are equal or at least 2^-8 of them apart.  y = x (1 / s) is within 2^-22 of x / s, and rounded to a multiple of 2^-12 (by the
-// sum with 3072) it is the border itself where x is, else on the right side of it.
+// Rounding without divisions.  The largest value a is compared with 6 g times the borders between scales, and each x with the borders t s g
+// between codes: all of these are numbers of at most 8 significant bits, so two of them are equal or at least 2^-8 of them apart.  The
+// quotients a / (6 g) and x / (s g), as products with approximate inverses, are within 2^-21; rounded, to 14 significant bits and to a
+// multiple of 2^-12 (by the sum with 3072), they are a border where it is one, else on the right side of it.
 __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g, uint32_t* scale) {
-  float x[8], top = 0.f;
+  float2 x[4];
+  float top = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = bf16lo(w[i]) * inv_g;
-    x[2 * i + 1] = bf16hi(w[i]) * inv_g;
+    x[i] = make_float2(bf16lo(w[i]), bf16hi(w[i]));
+    top = max_nan(max_nan(top, fabsf(x[i].x)), fabsf(x[i].y));
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(x[i]));
   top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = __fdiv_rn(top, 6.f);
-  if (top < 0.001953125f) top = 0.001953125f;       // (a NaN stays: the block is NaN)
+  const float quotient = top * (inv_g * 0.16666667f);
+  float s = __uint_as_float((__float_as_uint(quotient) + 0x200u) & ~0x3ffu);
+  if (!(s >= 0.001953125f)) s = top == top ? 0.001953125f : top;              // (a NaN stays: the block is NaN)
   uint32_t s8, sf;
   asm("{\n.reg .b16 h;\ncvt.rn.satfinite.e4m3x2.f32 h, %2, %3;\ncvt.u32.u16 %0, h;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}"
-      : "=r"(s8), "=r"(sf) : "f"(0.f), "f"(top));
+      : "=r"(s8), "=r"(sf) : "f"(0.f), "f"(s));
   *scale = s8 & 0xff;
-  const float inv_s = __frcp_rn(__half2float(__ushort_as_half((unsigned short)sf)));
+  float inv_s;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv_s) : "f"(__half2float(__ushort_as_half((unsigned short)sf))));
+  inv_s *= inv_g;                                                              // (a power of two)
+  float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = copysignf(__fadd_rn(__fadd_rn(__fmul_rn(x[i], inv_s), 3072.f), -3072.f), x[i]);
+  for (int i = 0; i < 4; ++i) {
+    const float2 z = add2(add2(mul2(x[i], make_float2(inv_s, inv_s)), make_float2(3072.f, 3072.f)), make_float2(-3072.f, -3072.f));
+    y[2 * i] = copysignf(z.x, x[i].x);
+    y[2 * i + 1] = copysignf(z.y, x[i].y);
+  }
   uint32_t codes;
   asm("{\n.reg .b8 a, b, c, d;\ncvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\ncvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
       "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\ncvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\nmov.b32 %0, {a, b, c, d};\n}"
-      : "=r"(codes) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+      : "=r"(codes) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
   return codes;
 }
 
@@ -121,15 +131,20 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
   } else {
     page = *(p.block_table + (size_t)at.seq * p.max_pages_per_seq + page_idx);
   }
-  float c[8], s[8];
+  float2 c[4], s[4];
   if (p.cos_sin && in_table) {
     // 8 pairs: (f, f + D/2) from f = 8 j on, or the 4 + 4 neighbours of the two vectors
     const float* cs = p.cos_sin + (size_t)pos * D + j * (p.interleaved ? 4 : 8);
     const int second = p.interleaved ? D / 4 : 4;
-    *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(cs);
-    *reinterpret_cast<float4*>(c + 4) = *reinterpret_cast<const float4*>(cs + second);
-    *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(cs + D / 2);
-    *reinterpret_cast<float4*>(s + 4) = *reinterpret_cast<const float4*>(cs + D / 2 + second);
+    auto four = [](const float* src, float2* to) {
+      const float4 u = *reinterpret_cast<const float4*>(src);
+      to[0] = make_float2(u.x, u.y);
+      to[1] = make_float2(u.z, u.w);
+    };
+    four(cs, c);
+    four(cs + second, c + 2);
+    four(cs + D / 2, s);
+    four(cs + D / 2 + second, s + 2);
   }
   if (placed && (page < 0 || page >= p.num_pages)) {
     if (lane == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
@@ -141,18 +156,15 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     uint32_t y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     if (base + step < nh) fetch(h + step);
     if (base < nk) {
-      float x[16];
+      float2 x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[2 * e] = bf16lo(y[e]);
-        x[2 * e + 1] = bf16hi(y[e]);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = make_float2(bf16lo(y[e]), bf16hi(y[e]));
       if (p.normed) {
         auto squares = [&]() {
-          float s2[2] = {0.f, 0.f};
+          float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s2[e & 1] = fmaf(x[e], x[e], s2[e & 1]);
-          float ss = s2[0] + s2[1];
+          for (int e = 0; e < 8; ++e) s2 = fma2(x[e], x[e], s2);
+          float ss = s2.x + s2.y;
 #pragma unroll
           for (int d = HALF / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
           return ss;
@@ -163,40 +175,44 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
           // them).  A row with an infinity or a NaN stays what the formula makes of it.
           const float down = ss <= FLT_MAX ? 1.f : 8.470329472543003e-22f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] *= down;
+          for (int e = 0; e < 8; ++e) x[e] = mul2(x[e], make_float2(down, down));
           if (down != 1.f) eps = 0.f;
           ss = squares();
         }
         const float r = rsqrtf(fmaf(ss, 1.f / D, eps));
+        const float2 rr = make_float2(r, r);
         const void* weight = h < nq ? p.q_weight : p.k_weight;
-        float w[8];
+        float2 w[4];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           kv4_load_weights(weight, p.weight_f32, p.weight_offset, (j + half * HALF) * 8, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[8 * half + e] = x[8 * half + e] * r * w[e];
+          for (int e = 0; e < 4; ++e) x[4 * half + e] = mul2(mul2(x[4 * half + e], rr), w[e]);
         }
       }
       if (h < nk) {
         if (!p.cos_sin) {
           if (p.normed) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+            for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[e].x, x[e].y);
           }
         } else if (!in_table) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = 0;     // no rotation for this row: a query of zeros
         } else if (!p.interleaved) {
+          const float2 minus = make_float2(-1.f, -1.f);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int f = 2 * e;
-            y[e] = pack_bf16x2(fmaf(x[f], c[f], -(x[8 + f] * s[f])), fmaf(x[f + 1], c[f + 1], -(x[9 + f] * s[f + 1])));
-            y[4 + e] = pack_bf16x2(fmaf(x[8 + f], c[f], x[f] * s[f]), fmaf(x[9 + f], c[f + 1], x[f + 1] * s[f + 1]));
+            const float2 lo = fma2(x[e], c[e], mul2(mul2(x[4 + e], s[e]), minus)), hi = fma2(x[4 + e], c[e], mul2(x[e], s[e]));
+            y[e] = pack_bf16x2(lo.x, lo.y);
+            y[4 + e] = pack_bf16x2(hi.x, hi.y);
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            y[e] = pack_bf16x2(fmaf(x[2 * e], c[e], -(x[2 * e + 1] * s[e])), fmaf(x[2 * e + 1], c[e], x[2 * e] * s[e]));
+          for (int e = 0; e < 8; ++e) {
+            const float ce = e % 2 ? c[e / 2].y : c[e / 2].x, se = e % 2 ? s[e / 2].y : s[e / 2].x;
+            y[e] = pack_bf16x2(fmaf(x[e].x, ce, -(x[e].y * se)), fmaf(x[e].y, ce, x[e].x * se));
+          }
         }
         if (h < nq) {
           uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)t * p.Hq + h) * D + j * 8);
