@@ -473,7 +473,7 @@ efim_status efim_kv4_append_prefill_attn(const efim_cache4_desc* cache, const ef
  * d_positions, d_slots and d_sequences may each be NULL; new tokens past `rows` have none of them and set EFIM_DEV_BAD_POSITION.
  * Lengths that are negative count as 0 tokens; those, lengths beyond the table (its places are filled, the tokens beyond get slot -1) and a
  * number of free pages outside [0, free_capacity], which is clamped, set EFIM_DEV_BAD_POSITION.
- * Two kernels; may be captured.  Workspace: efim_step_tables_workspace_bytes(batch) bytes (enough for fewer sequences, too), 4-byte
+ * One kernel or two; may be captured.  Workspace: efim_step_tables_workspace_bytes(batch) bytes (enough for fewer sequences, too), 4-byte
  * aligned, exclusively this call's until the stream has passed it.
  */
 size_t efim_step_tables_workspace_bytes(int32_t batch);

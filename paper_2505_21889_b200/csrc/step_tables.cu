@@ -159,6 +159,99 @@ __global__ void __launch_bounds__(TABLES_THREADS) tables_write_kernel(const Tabl
   }
 }
 
+// Both in one CTA, for few sequences and small tables, where a launch is most of the time: a warp has two rows (16 sequences of up to 9 tokens, tables
+// of 1,024: 4.6 us).
+constexpr int TABLES_ONE_THREADS = 1024, TABLES_ONE_ROWS = 64, TABLES_ONE_WORDS = 32768;
+__global__ void __launch_bounds__(TABLES_ONE_THREADS) tables_one_kernel(const TablesParams p) {
+  __shared__ int s_pages[TABLES_ONE_ROWS];          // that each row takes
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_launch();
+  // a table of its own: all of the old one, over which the rows' new places go later on
+  if (p.table_in != p.table_out) {
+    const int n = p.batch * p.width;
+    if (((reinterpret_cast<uintptr_t>(p.table_in) | reinterpret_cast<uintptr_t>(p.table_out)) & 15) == 0) {
+      for (int i = tid; i < n / 4; i += TABLES_ONE_THREADS) reinterpret_cast<int4*>(p.table_out)[i] = *(reinterpret_cast<const int4*>(p.table_in) + i);
+      for (int i = n / 4 * 4 + tid; i < n; i += TABLES_ONE_THREADS) p.table_out[i] = *(p.table_in + i);
+    } else {
+      for (int i = tid; i < n; i += TABLES_ONE_THREADS) p.table_out[i] = *(p.table_in + i);
+    }
+  }
+  const int have0 = *p.num_free, have = min(max(have0, 0), p.capacity);
+  int err = have != have0 ? EFIM_DEV_BAD_POSITION : 0;
+  RowSpan r[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = warp + 32 * k;
+    if (s >= p.batch) break;
+    r[k] = row_span(p, s);
+    if (r[k].bad) err |= EFIM_DEV_BAD_POSITION;
+    const int32_t* row = p.table_in + (size_t)s * p.width;
+    int n = 0;
+    for (int e = r[k].first + lane; e < r[k].last; e += 32) n += *(row + e) < 0;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) s_pages[s] = n;
+  }
+  __syncthreads();                                  // (everything that is read of num_free and the places to fill has been)
+  // every warp adds up what stands before each row, and all
+  long long total = 0, tokens = 0, before[2] = {0, 0}, first[2] = {0, 0};
+  for (int i = 0; i < p.batch; i += 32) {
+    const bool in = i + lane < p.batch;
+    const int pages = in ? s_pages[i + lane] : 0, fresh = in ? row_span(p, i + lane).fresh : 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const bool ahead = i + lane < warp + 32 * k;
+      before[k] += __reduce_add_sync(0xffffffffu, ahead ? pages : 0);
+      // (lengths up to 2^31 - 1: their halves are added)
+      first[k] += ((long long)__reduce_add_sync(0xffffffffu, ahead ? (unsigned)fresh >> 16 : 0u) << 16) + __reduce_add_sync(0xffffffffu, ahead ? (unsigned)fresh & 0xffffu : 0u);
+    }
+    total += __reduce_add_sync(0xffffffffu, pages);
+    tokens += ((long long)__reduce_add_sync(0xffffffffu, (unsigned)fresh >> 16) << 16) + __reduce_add_sync(0xffffffffu, (unsigned)fresh & 0xffffu);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = warp + 32 * k;
+    if (s >= p.batch) break;
+    const int32_t* in = p.table_in + (size_t)s * p.width;
+    int32_t* out = p.table_out + (size_t)s * p.width;
+    long long rank = before[k];
+    for (int e0 = r[k].first; e0 < r[k].last; e0 += 32) {
+      const int e = e0 + lane;
+      int page = e < r[k].last ? *(in + e) : 0;
+      const unsigned missing = __ballot_sync(0xffffffffu, page < 0);
+      const long long mine = rank + __popc(missing & ((1u << lane) - 1));
+      if (page < 0) page = mine < have ? *(p.free_pages + (have - 1 - mine)) : -1;
+      if (e < r[k].last) out[e] = page;
+      rank += __popc(missing);
+    }
+    if (lane == 0) p.q_indptr[s] = (int32_t)min(first[k], (long long)INT_MAX);
+    __syncwarp();
+    for (int i = lane; i < r[k].fresh; i += 32) {
+      const long long at = first[k] + i;
+      if (at >= p.rows) break;
+      const int pos = r[k].cached + i, place = pos >> 4;
+      if (p.positions) p.positions[at] = pos;
+      if (p.sequences) p.sequences[at] = s;
+      if (p.slots) {
+        const int page = place < p.width ? out[place] : -1;
+        p.slots[at] = page < 0 ? -1 : (int64_t)page * 16 + (pos & 15);
+      }
+    }
+  }
+  for (long long at = tokens + tid; at < p.rows; at += TABLES_ONE_THREADS) {
+    if (p.positions) p.positions[at] = -1;
+    if (p.sequences) p.sequences[at] = -1;
+    if (p.slots) p.slots[at] = -1;
+  }
+  if (tid == 0) {
+    p.q_indptr[p.batch] = (int32_t)min(tokens, (long long)INT_MAX);
+    *p.num_free_out = (int32_t)max(have - total, 0LL);
+    if (total > have) err |= EFIM_DEV_NO_PAGE;
+    if (tokens > INT_MAX || (tokens > p.rows && (p.positions || p.slots || p.sequences))) err |= EFIM_DEV_BAD_POSITION;
+  }
+  if (err && lane == 0 && p.status) atomicOr(p.status, err);
+}
+
 __global__ void __launch_bounds__(TABLES_THREADS) tables_release_kernel(const TablesParams p) {
   pdl_wait();
   pdl_launch();
@@ -233,6 +326,11 @@ extern "C" efim_status efim_step_tables(int32_t batch, const int32_t* d_cached_l
   p.capacity = free_capacity;
   p.rows = rows;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // (the rows are the caller's bound of the new tokens; a copy of the table counts too)
+  if (batch <= TABLES_ONE_ROWS && (long long)rows + (d_block_table == d_block_table_out ? 0LL : (long long)batch * max_pages_per_seq) <= TABLES_ONE_WORDS) {
+    EFIM_CUDA_TRY(launch_pdl(tables_one_kernel, dim3(1), dim3(TABLES_ONE_THREADS), 0, s, p));
+    return EFIM_OK;
+  }
   const unsigned ctas = (unsigned)(((long long)batch + TABLES_THREADS / 32 - 1) / (TABLES_THREADS / 32));
   EFIM_CUDA_TRY(launch_pdl(tables_count_kernel<false>, dim3(ctas), dim3(TABLES_THREADS), 0, s, p));
   EFIM_CUDA_TRY(launch_pdl(tables_write_kernel, dim3(batch), dim3(TABLES_THREADS), 0, s, p));
