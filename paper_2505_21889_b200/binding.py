@@ -262,6 +262,25 @@ def _stream_ptr(stream):
     return stream.cuda_stream
 
 
+def _current_stream_of(index):
+    """torch's current stream, if its device is number `index`."""
+    global _current_stream_of
+    from torch import _C
+    raw_stream, device = _C._cuda_getCurrentRawStream, _C._cuda_getDevice
+
+    def _current_stream_of(index):
+        now = device()
+        if now != index:
+            raise ValueError(f"the tensors are on device {index}, the current one is {now}: torch.cuda.device(...) first")
+        return raw_stream(now)
+    return _current_stream_of(index)
+
+
+def _stream_beside(stream, index):
+    """The stream of a call on tensors of device `index`; without one given, torch's current stream, which has to be of that device."""
+    return _current_stream_of(index) if stream is None else _stream_ptr(stream)
+
+
 def _torch():
     import torch
     return torch
@@ -445,7 +464,7 @@ class Cache4:
                "codes are [pages, kv heads, 16, head_dim / 2], scales [pages, kv heads, 16, head_dim / 16]")
         _check(len({x.device for x in pools}) == 1, "codes and scales are on one device")
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = pools
-        self.head_dim = 2 * half
+        self.head_dim, self.device_index = 2 * half, k_codes.get_device()
         self.desc = _Cache4Desc(*(x.data_ptr() for x in pools), n, page, num_q_heads, hkv, 2 * half, k_scale, v_scale)
 
     @classmethod
@@ -459,14 +478,14 @@ class Cache4:
 def efim_kv4_append(cache: Cache4, batch: Batch, norm, rope, q, k, v, q_out, status=None, stream=None):
     """Norm (a QkNorm, or None), rotation (a Rope, or None) and append to a 4-bit cache; operands as for efim_qk_norm_append."""
     st = _calls.kv4_append(_addr(cache.desc), _addr(batch.desc), None if norm is None else _addr(norm.desc), 0 if norm is None else norm.head_dim,
-                           _rope_addr(cache, rope), q, k, v, q_out, status, _stream_ptr(stream))
+                           _rope_addr(cache, rope), q, k, v, q_out, status, _stream_beside(stream, cache.device_index))
     if st != 0:
         raise EfimError(st, "efim_kv4_append")
 
 
 def efim_kv4_unpack(cache: Cache4, pages, k_out, v_out, status=None, stream=None):
     """The int32 `pages` of a 4-bit cache as bf16 pages [n, num_kv_heads, 16, head_dim]; k_out or v_out may be None."""
-    st = _calls.kv4_unpack(_addr(cache.desc), pages, k_out, v_out, status, _stream_ptr(stream))
+    st = _calls.kv4_unpack(_addr(cache.desc), pages, k_out, v_out, status, _stream_beside(stream, cache.device_index))
     if st != 0:
         raise EfimError(st, "efim_kv4_unpack")
 
@@ -480,7 +499,7 @@ def efim_kv4_decode_attn(cache: Cache4, batch: int, d_ctx_len, max_ctx_len, d_bl
     """Attention of the new tokens (one a sequence; with q_indptr up to max_new_len) over a 4-bit cache that holds them already.  ctx_len
     counts all of a sequence's keys.  q and out: packed [rows, num_q_heads, head_dim]."""
     st = _calls.kv4_decode_attn(_addr(cache.desc), batch, d_ctx_len, int(max_ctx_len), d_block_table, q_indptr, max_new_len, q, out, lse,
-                                sm_scale, workspace, status, _stream_ptr(stream))
+                                sm_scale, workspace, status, _stream_beside(stream, cache.device_index))
     if st != 0:
         raise EfimError(st, "efim_kv4_decode_attn")
 
@@ -491,7 +510,7 @@ def efim_kv4_prefill_workspace_bytes(cache: Cache4, batch: Batch) -> int:
 
 def efim_kv4_append_prefill_attn(cache: Cache4, batch: Batch, q, out, lse=None, sm_scale=0.0, workspace=None, status=None, stream=None):
     """Attention of a turn's new tokens, appended already, over a 4-bit cache."""
-    st = _calls.kv4_append_prefill_attn(_addr(cache.desc), _addr(batch.desc), q, out, lse, sm_scale, workspace, status, _stream_ptr(stream))
+    st = _calls.kv4_append_prefill_attn(_addr(cache.desc), _addr(batch.desc), q, out, lse, sm_scale, workspace, status, _stream_beside(stream, cache.device_index))
     if st != 0:
         raise EfimError(st, "efim_kv4_append_prefill_attn")
 
@@ -512,7 +531,7 @@ def efim_step_tables(cached_len, new_len, block_table, free_pages, num_free, q_i
     lengths on the device.  Without block_table_out and num_free_out those are changed in place; slots are int64, all else int32."""
     _own_workspace(workspace, stream)
     st = _calls.step_tables(cached_len, new_len, block_table, free_pages, num_free, q_indptr, positions, slots, sequences, block_table_out,
-                            num_free_out, workspace, status, _stream_ptr(stream))
+                            num_free_out, workspace, status, _stream_beside(stream, cached_len.get_device()))
     if st != 0:
         raise EfimError(st, "efim_step_tables")
 
@@ -520,7 +539,7 @@ def efim_step_tables(cached_len, new_len, block_table, free_pages, num_free, q_i
 def efim_release_pages(keep_len, block_table, free_pages, num_free, workspace=None, status=None, stream=None):
     """Pages behind each row's first keep_len tokens back to the stack of free ones."""
     _own_workspace(workspace, stream)
-    st = _calls.release_pages(keep_len, block_table, free_pages, num_free, workspace, status, _stream_ptr(stream))
+    st = _calls.release_pages(keep_len, block_table, free_pages, num_free, workspace, status, _stream_beside(stream, keep_len.get_device()))
     if st != 0:
         raise EfimError(st, "efim_release_pages")
 
@@ -533,7 +552,7 @@ def efim_adjust_logits(row_indptr, logits, out=None, history=None, lengths=None,
     bias_indptr, bias_tokens, bias_values = bias if bias is not None else (None, None, None)
     _check(bias is None or (bias_tokens.numel() == bias_values.numel()), "the bias has as many tokens as values")
     st = _calls.adjust_logits(row_indptr, logits, out, row_indptr.shape[0] - 1, history, lengths, prompt_len, tokens, repetition, presence,
-                              frequency, bias_indptr, bias_tokens, bias_values, mask, status, _stream_ptr(stream))
+                              frequency, bias_indptr, bias_tokens, bias_values, mask, status, _stream_beside(stream, logits.get_device()))
     if st != 0:
         raise EfimError(st, "efim_adjust_logits")
 

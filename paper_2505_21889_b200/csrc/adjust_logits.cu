@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(ADJUST_THREADS) adjust_logits_kernel(const Adj
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
         if (row_of[k] < row1 - row) {
-          allowed[k] = p.mask ? *(mask[k] + row * 4 * p.mask_stride) : 0xffu;
+          allowed[k] = p.mask ? *(mask[k] + 4LL * row * p.mask_stride) : 0xffu;
           if (at[k] < whole) x[k].load(from[k] + row * p.stride);
           else x[k].load(from[k] + row * p.stride, n_slot - 8 * at[k]);
         }

@@ -1,9 +1,8 @@
-// efim_kv4_decode_attn: attention of one or a few new tokens a sequence over a 4-bit cache, with keys split over CTAs and a
-// log-sum-exp merge.
+// efim_kv4_decode_attn: attention of one or a few new tokens a sequence over a 4-bit cache.
 //
-// One CTA = (sequence, kv head, tile of 8 NT rows, key chunk); a row is a (new token, query head of the group) pair.  Its 4 warps walk
-// pages (16 tokens) round-robin, each with a ring of its own that cp.async fills.  A page is one 16-token tile of mma.sync m16n8k16
-// (fp16 in, fp32 accumulation), rows along n:
+// A unit of work is a (sequence, kv head, tile of up to 8 NT rows); a row is a (new token, query head of the group) pair.  One wave of CTAs shares all units'
+// keys out evenly (Kv4Line), a second kernel joins the units that are cut.  A CTA's 4 warps walk pages (16 tokens), each with a ring of its own that
+// cp.async fills.  A page is one 16-token tile of mma.sync m16n8k16 (fp16 in, fp32 accumulation), rows along n:
 //   S^T [16 tokens][rows]  = K [16][D] Q^T [D][rows]
 //   O^T [D][rows]         += V^T [D][16] P^T [16][rows]
 // The operands K and V are made in registers: a code times its block's scale is exact in fp16 (cvt from 4-bit floats, one product), and
@@ -13,8 +12,14 @@
 //      side, so that a conversion gives a pair of tokens
 // with the page's tokens numbered such that neither read meets a bank twice (kv4_token, kv4_v_piece).
 // Queries enter as fp16 after a shift by a power of two per row that takes the row's largest value to [2^14, 2^15): exact for
-// values down to 2^-28 of it.  P = 2^(s - m + 11) enters as fp16 (a rounding of 2^-12 of each, between 2^15 and, at full precision, 2^-25 of
+// values down to 2^-28 of it.  P = 2^(s - m + 11) enters as fp16 (a rounding of 2^-11 of each, between 2^15 and, at full precision, 2^-25 of
 // the largest); the sums that it is divided by are the unrounded fp32 values.
+//
+// Bound: with up to 8 rows the instructions, then HBM: of the 311 that a page (2,304 bytes) of one kv head costs a warp, 64 are conversions and 64
+// products, 16 matrix products; 64 users x 1-16k keys at 32/8 heads x 128 take 140 us (4.5 TB/s of codes and scales; their copies alone 115, the rest alone
+// 120).  What brought it from 174: two pages a trip 161, even pieces in one wave and starts that count 150, no branch around a page's copies 142,
+// three CTAs an SM instead of four with spills 140.  Not kept: bulk copies (four of 128 to 1,024 bytes a page: 173), four pages a trip, two or five CTAs.
+// With more rows, and few users, the latency of one warp's chain: its registers leave two CTAs an SM.
 #include "kv4_attn.cuh"
 #include "token_place.cuh"
 #include <algorithm>
@@ -247,421 +252,421 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 
   auto token_of = [&](int row) { return p.max_new == 1 ? 0 : row / G; };
   while (x0 < x1) {
-  const int tiles = Line::tiles(w, G);
-  const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0), cost = Line::cost(n_rows);
-  // (a unit's length fits 32 bits: 2^31 keys in trips of 64 or more)
-  const int unit_len = start + Line::trips(w) * cost, from = (int)off, here = (int)min((long long)(unit_len - from), x1 - x0);   // of the unit in this piece
-  const int trip0 = max(from - start, 0) / cost, trip1 = max(from + here - start, 0) / cost;
-  const bool first_part = trip0 > 0, ends = from + here == unit_len;       // the unit began before this piece; it ends in it
-  if (trip1 <= trip0) break;              // (the piece ends before the unit's first trip: it begins in the next one)
-  const int32_t* bt = p.block_table + (size_t)seq * p.max_pages_per_seq;
-  // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece
-  const int begin = trip0 * Line::TRIP, first_pg = (begin >> 4) + PG * warp;
-  auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
-  // keys that the tile's last row sees, of this piece
-  const int end = (int)min((long long)min(w.ctx, w.cached + token_of(row0 + n_rows - 1) + 1), (long long)trip1 * Line::TRIP);
-  const int last_pg = (end - 1) >> 4;
-  const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
-  // Lane l holds where the l-th of this warp's pages is (then of the next 32): (page, kv head) in the pools, -1 for no page.
-  int at_cache;
-  bool hole = false;                      // some pages are missing: every trip looks at its own
-  auto look_up = [&](int i) {
-    const int pg = page_of(i + lane);
-    at_cache = -1;
-    if (pg <= last_pg) {
-      const int pid = *(bt + pg);
-      if ((uint32_t)pid < (uint32_t)p.num_pages) at_cache = pid * p.Hkv + kvh;
-      else if (p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
-    }
-    hole |= __any_sync(0xffffffffu, pg <= last_pg && at_cache < 0);
-  };
-  look_up(0);
-  // query rows, a warp a row: on their way before the pages are
-  uint2 q_raw[ROWS / KV4_WARPS];
-#pragma unroll
-  for (int i = 0; i < ROWS / KV4_WARPS; ++i) {
-    const int r = i * KV4_WARPS + warp;
-    q_raw[i] = make_uint2(0, 0);
-    if (r < n_rows) {
-      const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
-      const uint16_t* q = p.q + ((size_t)(w.first_row + token) * p.Hq + h) * D + lane * (D / 32);
-      if constexpr (D == 128) q_raw[i] = *reinterpret_cast<const uint2*>(q);
-      else q_raw[i].x = *reinterpret_cast<const uint32_t*>(q);
-    }
-  }
-
-  const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * STAGE);
-  const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * STAGE);
-  constexpr int PIECES = CODES / 16, PS = 2 * SCALES / 16;                // 16-byte pieces of a page's codes (K or V), of its scales
-  // where this lane's pieces come from and go to: of every page's codes, of one page's scales
-  const uint8_t *k_src = p.k_codes + lane * 16, *v_src = p.v_codes + lane * 16;
-  const uint8_t* s_src = lane % PS < PS / 2 ? p.k_scales + lane % PS * 16 : p.v_scales + (lane % PS - PS / 2) * 16;
-  const uint32_t k_dst = ring + lane * 16, v_dst = ring + CODES + kv4_v_piece<D>(lane / (D / 32), lane % (D / 32));
-  const uint32_t s_dst = ring + lane / PS * PAGE + 2 * CODES + lane % PS * 16;
-  uint32_t missing = 0;                   // a bit per page, the last one sent for lowest: not there (kept where there is a hole)
-  auto issue = [&](int i, uint32_t to) {  // send for the pages of this warp's i-th trip, to `to` bytes into the ring
-    if (i < n_trips) {
-      int at[PG];
-#pragma unroll
-      for (int x = 0; x < PG; ++x) {
-        at[x] = __shfl_sync(0xffffffffu, at_cache, (i * PG + x) & 31);
-        if (hole) missing = missing << 1 | (uint32_t)at[x] >> 31;
-        at[x] = max(at[x], 0);            // (a page of the pool stands in for one that is not there)
-        const uint8_t *k = k_src + (uint64_t)at[x] * CODES, *v = v_src + (uint64_t)at[x] * CODES;
-#pragma unroll
-        for (int u = 0; u < PIECES; u += 32) {
-          kv4_cp16(k_dst + to + x * PAGE + u * 16, k + u * 16);
-          kv4_cp16(v_dst + to + x * PAGE + u * 16, v + u * 16);
-        }
+    const int tiles = Line::tiles(w, G);
+    const int row0 = tile * ROWS, n_rows = min(ROWS, w.new_len * G - row0), cost = Line::cost(n_rows);
+    // (a unit's length fits 32 bits: 2^31 keys in trips of 64 or more)
+    const int unit_len = start + Line::trips(w) * cost, from = (int)off, here = (int)min((long long)(unit_len - from), x1 - x0);   // of the unit in this piece
+    const int trip0 = max(from - start, 0) / cost, trip1 = max(from + here - start, 0) / cost;
+    const bool first_part = trip0 > 0, ends = from + here == unit_len;       // the unit began before this piece; it ends in it
+    if (trip1 <= trip0) break;              // (the piece ends before the unit's first trip: it begins in the next one)
+    const int32_t* bt = p.block_table + (size_t)seq * p.max_pages_per_seq;
+    // warp x has pages PG (x + 4 i) + {0 .. PG-1} of the piece
+    const int begin = trip0 * Line::TRIP, first_pg = (begin >> 4) + PG * warp;
+    auto page_of = [&](int i) { return first_pg + (PG == 1 ? KV4_WARPS * i : i % PG + KV4_WARPS * PG * (i / PG)); };
+    // keys that the tile's last row sees, of this piece
+    const int end = (int)min((long long)min(w.ctx, w.cached + token_of(row0 + n_rows - 1) + 1), (long long)trip1 * Line::TRIP);
+    const int last_pg = (end - 1) >> 4;
+    const int n_trips = end > begin && first_pg <= last_pg ? (last_pg - first_pg) / (KV4_WARPS * PG) + 1 : 0;
+    // Lane l holds where the l-th of this warp's pages is (then of the next 32): (page, kv head) in the pools, -1 for no page.
+    int at_cache;
+    bool hole = false;                      // some pages are missing: every trip looks at its own
+    auto look_up = [&](int i) {
+      const int pg = page_of(i + lane);
+      at_cache = -1;
+      if (pg <= last_pg) {
+        const int pid = *(bt + pg);
+        if ((uint32_t)pid < (uint32_t)p.num_pages) at_cache = pid * p.Hkv + kvh;
+        else if (p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
       }
-      const int mine = lane < PS ? at[0] : at[PG - 1];
-      if (lane < PG * PS) kv4_cp16(s_dst + to, s_src + (uint64_t)mine * SCALES);
-      if (((i * PG + PG) & 31) == 0) look_up(i * PG + PG);
-    } else {
-      missing <<= PG;
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
+      hole |= __any_sync(0xffffffffu, pg <= last_pg && at_cache < 0);
+    };
+    look_up(0);
+    // query rows, a warp a row: on their way before the pages are
+    uint2 q_raw[ROWS / KV4_WARPS];
 #pragma unroll
-  for (int i = 0; i < ST - 1; ++i) issue(i, i * STAGE);
-
-  // ---- query rows as fp16, shifted
-#pragma unroll
-  for (int i = 0; i < ROWS / KV4_WARPS; ++i) {
-    const int r = i * KV4_WARPS + warp;
-    const float x[4] = {bf16lo(q_raw[i].x), bf16hi(q_raw[i].x), bf16lo(q_raw[i].y), bf16hi(q_raw[i].y)};
-    float top = 0.f;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) top = max_nan(top, fabsf(x[e]));
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
-    // 2^-(exponent of the largest) and back; a row with an infinity or a NaN becomes NaN
-    const int ex = (int)(__float_as_uint(top) >> 23);                    // biased; subnormal rows count as 2^-126
-    const bool bad = ex >= 255;
-    const float down = __uint_as_float((uint32_t)min(254, max(1, 268 - max(ex, 1))) << 23);    // 2^(14 - exponent), 2^127 at most
-#pragma unroll
-    for (int e = 0; e < D / 32; e += 2) {
-      const float lo = bad ? NAN : x[e] * down, hi = bad ? NAN : x[e + 1] * down;
-      const int d = lane * (D / 32) + e;
-      *reinterpret_cast<uint32_t*>(&s_q[r][d % (D / 4) / 4 * 16 + d / (D / 4) * 4 + d % 4]) = kv4_pack_half2(lo, hi);
-    }
-    if (lane == 0) s_scale[r] = fmaxf(fminf(p.scale_log2 / down, FLT_MAX), FLT_MIN);   // (by a power of two: exact)
-    if (lane < 8) s_nan[r][lane] = 0;
-  }
-  __syncthreads();
-  // B fragments of row g: the dims that the K fragments have, D/4 from t D/4 on
-  uint32_t qf[Q_IN_REGS ? NT : 1][KS][2];
-  if constexpr (Q_IN_REGS) {
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const uint2 u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * k + 4 * t]);
-        qf[n][k][0] = u.x;
-        qf[n][k][1] = u.y;
+    for (int i = 0; i < ROWS / KV4_WARPS; ++i) {
+      const int r = i * KV4_WARPS + warp;
+      q_raw[i] = make_uint2(0, 0);
+      if (r < n_rows) {
+        const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
+        const uint16_t* q = p.q + ((size_t)(w.first_row + token) * p.Hq + h) * D + lane * (D / 32);
+        if constexpr (D == 128) q_raw[i] = *reinterpret_cast<const uint2*>(q);
+        else q_raw[i].x = *reinterpret_cast<const uint32_t*>(q);
       }
-  }
-  float o[NT][KS][4];                     // O^T: dims g D/8 + 2 k + (e / 2), rows 8 n + 2 t + (e % 2)
-  // Scores stay as the products leave them; times sc they are in log2.  Per row: the score that the reference stands at, the one from which
-  // on it moves, and what is taken off a score (in log2, KV4_P_SHIFT less than the reference).  Before any score: p = 2^(-inf) = 0.
-  float m_next[NT][2], m_off[NT][2], l_part[NT][2], sc[NT][2];
-  int limit[NT][2];                       // keys that rows 8 n + 2 t + {0, 1} see
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[n][k][e] = 0.f;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int r = n * 8 + 2 * t + e;
-      m_next[n][e] = -FLT_MAX;
-      m_off[n][e] = -KV4_P_SHIFT;
-      l_part[n][e] = 0.f;
-      sc[n][e] = s_scale[r];
-      limit[n][e] = min(end, w.cached + token_of(row0 + min(r, n_rows - 1)) + 1);
     }
-  }
-  const int first_limit = min(end, w.cached + token_of(row0) + 1);
-  const int tok0 = kv4_token(g >> 1, g & 1, 0);             // this lane's key in S^T; the other is 8 on
-  // this lane's places in a staged page
-  const uint8_t* k_at = ring_ptr + (D == 128 ? tok0 * 64 + t * 16 : tok0 * 32 + t * 8);
-  const uint8_t* ks_at = ring_ptr + 2 * CODES + (D == 128 ? tok0 * 8 + 2 * t : tok0 * 4 + t);
-  const uint8_t *v_at[2], *vs_at[2];                        // of tokens 2t, 2t+1 (the others are 8 rows on)
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int token = kv4_token(t, e, 0);
-    v_at[e] = ring_ptr + CODES + (D == 128 ? kv4_v_piece<D>(token, g >> 1) + (g & 1) * 8 : kv4_v_piece<D>(token, g >> 2) + (g & 3) * 4);
-    vs_at[e] = ring_ptr + 2 * CODES + SCALES + (D == 128 ? token * 8 + g : token * 4 + (g >> 1));
-  }
 
-  // trips whose pages every row sees in full
-  const int seen = max(first_limit, 0) >> 4, n_full = seen >= first_pg + PG ? (seen - first_pg - PG) / (KV4_WARPS * PG) + 1 : 0;
-
-  // The walk over the pages, for as many 8-row tiles as have rows (a call's sequences bring different numbers of them).
-  auto walk = [&](auto active) {
-  constexpr int NA = decltype(active)::value;
-  int at = 0;                             // where in the ring the trip's pages are
-  for (int i = 0; i < n_trips; ++i) {
-    __syncwarp();                         // everyone is done with the stage of the last trip
-    issue(i + ST - 1, at == 0 ? (ST - 1) * STAGE : at - STAGE);
-    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
-    __syncwarp();
-    const bool border = i >= n_full || hole;
-    int key0[PG];                         // first keys; past every limit where there is no page (looked at where border is)
+    const uint32_t ring = kv4_smem(kv4_smem_raw) + warp * (ST * STAGE);
+    const uint8_t* ring_ptr = kv4_smem_raw + warp * (ST * STAGE);
+    constexpr int PIECES = CODES / 16, PS = 2 * SCALES / 16;                // 16-byte pieces of a page's codes (K or V), of its scales
+    // where this lane's pieces come from and go to: of every page's codes, of one page's scales
+    const uint8_t *k_src = p.k_codes + lane * 16, *v_src = p.v_codes + lane * 16;
+    const uint8_t* s_src = lane % PS < PS / 2 ? p.k_scales + lane % PS * 16 : p.v_scales + (lane % PS - PS / 2) * 16;
+    const uint32_t k_dst = ring + lane * 16, v_dst = ring + CODES + kv4_v_piece<D>(lane / (D / 32), lane % (D / 32));
+    const uint32_t s_dst = ring + lane / PS * PAGE + 2 * CODES + lane % PS * 16;
+    uint32_t missing = 0;                   // a bit per page, the last one sent for lowest: not there (kept where there is a hole)
+    auto issue = [&](int i, uint32_t to) {  // send for the pages of this warp's i-th trip, to `to` bytes into the ring
+      if (i < n_trips) {
+        int at[PG];
 #pragma unroll
-    for (int x = 0; x < PG; ++x) key0[x] = (missing >> (ST * PG - 1 - x)) & 1u ? INT_MAX - 16 : page_of(i * PG + x) << 4;
-    // ---- S^T
-    float sx[PG][NA][4];
+        for (int x = 0; x < PG; ++x) {
+          at[x] = __shfl_sync(0xffffffffu, at_cache, (i * PG + x) & 31);
+          if (hole) missing = missing << 1 | (uint32_t)at[x] >> 31;
+          at[x] = max(at[x], 0);            // (a page of the pool stands in for one that is not there)
+          const uint8_t *k = k_src + (uint64_t)at[x] * CODES, *v = v_src + (uint64_t)at[x] * CODES;
 #pragma unroll
-    for (int x = 0; x < PG; ++x) {
-      __half2 scale[2];                    // of the two tokens: the lane's blocks of 16 dims, D / 64 of them
-      uint32_t kw[2][D / 32];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if constexpr (D == 128) {
-          const uint4 u = *reinterpret_cast<const uint4*>(k_at + at + x * PAGE + h * 512);
-          kw[h][0] = u.x, kw[h][1] = u.y, kw[h][2] = u.z, kw[h][3] = u.w;
-          scale[h] = as_half2(scales_to_half2(*reinterpret_cast<const uint16_t*>(ks_at + at + x * PAGE + h * 64)));
-        } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(k_at + at + x * PAGE + h * 256);
-          kw[h][0] = u.x, kw[h][1] = u.y;
-          scale[h] = as_half2(scales_to_half2(ks_at[at + x * PAGE + h * 32]));
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < D / 32; ++q) {   // 8 dims of each token: two k-steps
-        uint32_t kx[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          codes_to_half2(kw[h][q], kx[h]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) kx[h][e] = mul_half2(kx[h][e], q / 2 ? __high2half2(scale[h]) : __low2half2(scale[h]));
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t a[4] = {kx[0][2 * k], kx[1][2 * k], kx[0][2 * k + 1], kx[1][2 * k + 1]};
-#pragma unroll
-          for (int n = 0; n < NA; ++n) {
-            uint2 u;
-            if constexpr (Q_IN_REGS) u = make_uint2(qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
-            else u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
-            if (q == 0 && k == 0) kv4_mma_first(sx[x][n], a, u.x, u.y);
-            else kv4_mma(sx[x][n], a, u.x, u.y);
+          for (int u = 0; u < PIECES; u += 32) {
+            kv4_cp16(k_dst + to + x * PAGE + u * 16, k + u * 16);
+            kv4_cp16(v_dst + to + x * PAGE + u * 16, v + u * 16);
           }
         }
+        const int mine = lane < PS ? at[0] : at[PG - 1];
+        if (lane < PG * PS) kv4_cp16(s_dst + to, s_src + (uint64_t)mine * SCALES);
+        if (((i * PG + PG) & 31) == 0) look_up(i * PG + PG);
+      } else {
+        missing <<= PG;
       }
-    }
-    if (border) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-      for (int x = 0; x < PG; ++x)
+    for (int i = 0; i < ST - 1; ++i) issue(i, i * STAGE);
+
+    // ---- query rows as fp16, shifted
 #pragma unroll
-        for (int n = 0; n < NA; ++n)
+    for (int i = 0; i < ROWS / KV4_WARPS; ++i) {
+      const int r = i * KV4_WARPS + warp;
+      const float x[4] = {bf16lo(q_raw[i].x), bf16hi(q_raw[i].x), bf16lo(q_raw[i].y), bf16hi(q_raw[i].y)};
+      float top = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (key0[x] + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[x][n][e] = -INFINITY;
-    }
-    // ---- the values' scales: of tokens 2t, 2t+1, 2t+8, 2t+9
-    uint32_t vs[PG];
+      for (int e = 0; e < D / 32; ++e) top = max_nan(top, fabsf(x[e]));
 #pragma unroll
-    for (int x = 0; x < PG; ++x) {
-      constexpr int H = D == 128 ? 64 : 32;
-      const uint32_t b00 = vs_at[0][at + x * PAGE], b01 = vs_at[1][at + x * PAGE], b10 = vs_at[0][at + x * PAGE + H], b11 = vs_at[1][at + x * PAGE + H];
-      vs[x] = __byte_perm(__byte_perm(b00, b01, 0x5540), __byte_perm(b10, b11, 0x5540), 0x5410);
-      if (border) {
-        // what stands behind the last key is anything, a NaN's scale too: P is 0 there, 0 times NaN is not
+      for (int d = 16; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
+      // 2^-(exponent of the largest) and back; a row with an infinity or a NaN becomes NaN
+      const int ex = (int)(__float_as_uint(top) >> 23);                    // biased; subnormal rows count as 2^-126
+      const bool bad = ex >= 255;
+      const float down = __uint_as_float((uint32_t)min(254, max(1, 268 - max(ex, 1))) << 23);    // 2^(14 - exponent), 2^127 at most
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (key0[x] + kv4_token(t, q & 1, q >> 1) >= end) vs[x] &= ~(0xffu << (8 * q));
+      for (int e = 0; e < D / 32; e += 2) {
+        const float lo = bad ? NAN : x[e] * down, hi = bad ? NAN : x[e + 1] * down;
+        const int d = lane * (D / 32) + e;
+        *reinterpret_cast<uint32_t*>(&s_q[r][d % (D / 4) / 4 * 16 + d / (D / 4) * 4 + d % 4]) = kv4_pack_half2(lo, hi);
       }
+      if (lane == 0) s_scale[r] = fmaxf(fminf(p.scale_log2 / down, FLT_MAX), FLT_MIN);   // (by a power of two: exact)
+      if (lane < 8) s_nan[r][lane] = 0;
     }
-    // ---- the reference; values that are NaN
-    bool grow = false, nan = false;
-    float mx[NA][2];
+    __syncthreads();
+    // B fragments of row g: the dims that the K fragments have, D/4 from t D/4 on
+    uint32_t qf[Q_IN_REGS ? NT : 1][KS][2];
+    if constexpr (Q_IN_REGS) {
 #pragma unroll
-    for (int n = 0; n < NA; ++n)
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const uint2 u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * k + 4 * t]);
+          qf[n][k][0] = u.x;
+          qf[n][k][1] = u.y;
+        }
+    }
+    float o[NT][KS][4];                     // O^T: dims g D/8 + 2 k + (e / 2), rows 8 n + 2 t + (e % 2)
+    // Scores stay as the products leave them; times sc they are in log2.  Per row: the score that the reference stands at, the one from which
+    // on it moves, and what is taken off a score (in log2, KV4_P_SHIFT less than the reference).  Before any score: p = 2^(-inf) = 0.
+    float m_next[NT][2], m_off[NT][2], l_part[NT][2], sc[NT][2];
+    int limit[NT][2];                       // keys that rows 8 n + 2 t + {0, 1} see
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][k][e] = 0.f;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        mx[n][e] = fmaxf(sx[0][n][e], sx[0][n][e + 2]);
-#pragma unroll
-        for (int x = 1; x < PG; ++x) mx[n][e] = fmaxf(fmaxf(mx[n][e], sx[x][n][e]), sx[x][n][e + 2]);
-        grow |= mx[n][e] > m_next[n][e];
+        const int r = n * 8 + 2 * t + e;
+        m_next[n][e] = -FLT_MAX;
+        m_off[n][e] = -KV4_P_SHIFT;
+        l_part[n][e] = 0.f;
+        sc[n][e] = s_scale[r];
+        limit[n][e] = min(end, w.cached + token_of(row0 + min(r, n_rows - 1)) + 1);
       }
+    }
+    const int first_limit = min(end, w.cached + token_of(row0) + 1);
+    const int tok0 = kv4_token(g >> 1, g & 1, 0);             // this lane's key in S^T; the other is 8 on
+    // this lane's places in a staged page
+    const uint8_t* k_at = ring_ptr + (D == 128 ? tok0 * 64 + t * 16 : tok0 * 32 + t * 8);
+    const uint8_t* ks_at = ring_ptr + 2 * CODES + (D == 128 ? tok0 * 8 + 2 * t : tok0 * 4 + t);
+    const uint8_t *v_at[2], *vs_at[2];                        // of tokens 2t, 2t+1 (the others are 8 rows on)
 #pragma unroll
-    for (int x = 0; x < PG; ++x) nan |= (((vs[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
-    // Lazy rescale: the reference of a row only moves when a score exceeds it by more than 2^4 (always at the first), and each row's by its
-    // own scores: its bits do not depend on the other rows.
-    if (__any_sync(0xffffffffu, grow | nan)) {
+    for (int e = 0; e < 2; ++e) {
+      const int token = kv4_token(t, e, 0);
+      v_at[e] = ring_ptr + CODES + (D == 128 ? kv4_v_piece<D>(token, g >> 1) + (g & 1) * 8 : kv4_v_piece<D>(token, g >> 2) + (g & 3) * 4);
+      vs_at[e] = ring_ptr + 2 * CODES + SCALES + (D == 128 ? token * 8 + g : token * 4 + (g >> 1));
+    }
+
+    // trips whose pages every row sees in full
+    const int seen = max(first_limit, 0) >> 4, n_full = seen >= first_pg + PG ? (seen - first_pg - PG) / (KV4_WARPS * PG) + 1 : 0;
+
+    // The walk over the pages, for as many 8-row tiles as have rows (a call's sequences bring different numbers of them).
+    auto walk = [&](auto active) {
+      constexpr int NA = decltype(active)::value;
+      int at = 0;                             // where in the ring the trip's pages are
+      for (int i = 0; i < n_trips; ++i) {
+        __syncwarp();                         // everyone is done with the stage of the last trip
+        issue(i + ST - 1, at == 0 ? (ST - 1) * STAGE : at - STAGE);
+        asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+        __syncwarp();
+        const bool border = i >= n_full || hole;
+        int key0[PG];                         // first keys; past every limit where there is no page (looked at where border is)
 #pragma unroll
-      for (int n = 0; n < NA; ++n)
+        for (int x = 0; x < PG; ++x) key0[x] = (missing >> (ST * PG - 1 - x)) & 1u ? INT_MAX - 16 : page_of(i * PG + x) << 4;
+        // ---- S^T
+        float sx[PG][NA][4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float x = mx[n][e];
+        for (int x = 0; x < PG; ++x) {
+          __half2 scale[2];                    // of the two tokens: the lane's blocks of 16 dims, D / 64 of them
+          uint32_t kw[2][D / 32];
 #pragma unroll
-          for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
-          if (x > m_next[n][e]) {
-            float off = fmaf(x, sc[n][e], -KV4_P_SHIFT);
-            if (!(fabsf(off) <= FLT_MAX)) off = NAN;        // scores that leave fp32
-            const float alpha = m_next[n][e] == -FLT_MAX ? 0.f : kv4_ex2(m_off[n][e] - off);
-            m_next[n][e] = x + KV4_LAG / sc[n][e];
-            m_off[n][e] = off;
-            l_part[n][e] *= alpha;
+          for (int h = 0; h < 2; ++h) {
+            if constexpr (D == 128) {
+              const uint4 u = *reinterpret_cast<const uint4*>(k_at + at + x * PAGE + h * 512);
+              kw[h][0] = u.x, kw[h][1] = u.y, kw[h][2] = u.z, kw[h][3] = u.w;
+              scale[h] = as_half2(scales_to_half2(*reinterpret_cast<const uint16_t*>(ks_at + at + x * PAGE + h * 64)));
+            } else {
+              const uint2 u = *reinterpret_cast<const uint2*>(k_at + at + x * PAGE + h * 256);
+              kw[h][0] = u.x, kw[h][1] = u.y;
+              scale[h] = as_half2(scales_to_half2(ks_at[at + x * PAGE + h * 32]));
+            }
+          }
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              o[n][k][e] *= alpha;
-              o[n][k][e + 2] *= alpha;
+          for (int q = 0; q < D / 32; ++q) {   // 8 dims of each token: two k-steps
+            uint32_t kx[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              codes_to_half2(kw[h][q], kx[h]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) kx[h][e] = mul_half2(kx[h][e], q / 2 ? __high2half2(scale[h]) : __low2half2(scale[h]));
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t a[4] = {kx[0][2 * k], kx[1][2 * k], kx[0][2 * k + 1], kx[1][2 * k + 1]};
+#pragma unroll
+              for (int n = 0; n < NA; ++n) {
+                uint2 u;
+                if constexpr (Q_IN_REGS) u = make_uint2(qf[n][2 * q + k][0], qf[n][2 * q + k][1]);
+                else u = *reinterpret_cast<const uint2*>(&s_q[n * 8 + g][16 * (2 * q + k) + 4 * t]);
+                if (q == 0 && k == 0) kv4_mma_first(sx[x][n], a, u.x, u.y);
+                else kv4_mma(sx[x][n], a, u.x, u.y);
+              }
             }
           }
         }
-      // Rows that see a value that is NaN are marked and get their NaN at the end; in the products such values are zeros, since rows that
-      // do not see them have a P of 0 there.
+        if (border) {
 #pragma unroll
-      for (int x = 0; x < PG; ++x)
+          for (int x = 0; x < PG; ++x)
+#pragma unroll
+            for (int n = 0; n < NA; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (key0[x] + tok0 + (e >> 1) * 8 >= limit[n][e & 1]) sx[x][n][e] = -INFINITY;
+        }
+        // ---- the values' scales: of tokens 2t, 2t+1, 2t+8, 2t+9
+        uint32_t vs[PG];
+#pragma unroll
+        for (int x = 0; x < PG; ++x) {
+          constexpr int H = D == 128 ? 64 : 32;
+          const uint32_t b00 = vs_at[0][at + x * PAGE], b01 = vs_at[1][at + x * PAGE], b10 = vs_at[0][at + x * PAGE + H], b11 = vs_at[1][at + x * PAGE + H];
+          vs[x] = __byte_perm(__byte_perm(b00, b01, 0x5540), __byte_perm(b10, b11, 0x5540), 0x5410);
+          if (border) {
+            // what stands behind the last key is anything, a NaN's scale too: P is 0 there, 0 times NaN is not
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (key0[x] + kv4_token(t, q & 1, q >> 1) >= end) vs[x] &= ~(0xffu << (8 * q));
+          }
+        }
+        // ---- the reference; values that are NaN
+        bool grow = false, nan = false;
+        float mx[NA][2];
+#pragma unroll
+        for (int n = 0; n < NA; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            mx[n][e] = fmaxf(sx[0][n][e], sx[0][n][e + 2]);
+#pragma unroll
+            for (int x = 1; x < PG; ++x) mx[n][e] = fmaxf(fmaxf(mx[n][e], sx[x][n][e]), sx[x][n][e + 2]);
+            grow |= mx[n][e] > m_next[n][e];
+          }
+#pragma unroll
+        for (int x = 0; x < PG; ++x) nan |= (((vs[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+        // Lazy rescale: the reference of a row only moves when a score exceeds it by more than 2^4 (always at the first), and each row's by its
+        // own scores: its bits do not depend on the other rows.
+        if (__any_sync(0xffffffffu, grow | nan)) {
+#pragma unroll
+          for (int n = 0; n < NA; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float x = mx[n][e];
+#pragma unroll
+              for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+              if (x > m_next[n][e]) {
+                float off = fmaf(x, sc[n][e], -KV4_P_SHIFT);
+                if (!(fabsf(off) <= FLT_MAX)) off = NAN;        // scores that leave fp32
+                const float alpha = m_next[n][e] == -FLT_MAX ? 0.f : kv4_ex2(m_off[n][e] - off);
+                m_next[n][e] = x + KV4_LAG / sc[n][e];
+                m_off[n][e] = off;
+                l_part[n][e] *= alpha;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                  o[n][k][e] *= alpha;
+                  o[n][k][e + 2] *= alpha;
+                }
+              }
+            }
+          // Rows that see a value that is NaN are marked and get their NaN at the end; in the products such values are zeros, since rows that
+          // do not see them have a P of 0 there.
+#pragma unroll
+          for (int x = 0; x < PG; ++x)
 #pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          if (((vs[x] >> (8 * q)) & 0x7f) != 0x7f) continue;
-          vs[x] &= ~(0xffu << (8 * q));
-          const int key = key0[x] + kv4_token(t, q & 1, q >> 1);
-          for (int r = 0; r < n_rows; ++r)
-            if (key < min(end, w.cached + token_of(row0 + r) + 1)) s_nan[r][g] = 1;
+            for (int q = 0; q < 4; ++q) {
+              if (((vs[x] >> (8 * q)) & 0x7f) != 0x7f) continue;
+              vs[x] &= ~(0xffu << (8 * q));
+              const int key = key0[x] + kv4_token(t, q & 1, q >> 1);
+              for (int r = 0; r < n_rows; ++r)
+                if (key < min(end, w.cached + token_of(row0 + r) + 1)) s_nan[r][g] = 1;
+            }
         }
-    }
 #pragma unroll
-    for (int x = 0; x < PG; ++x) {
-      uint32_t pb[NA][2];
+        for (int x = 0; x < PG; ++x) {
+          uint32_t pb[NA][2];
 #pragma unroll
-      for (int n = 0; n < NA; ++n)
+          for (int n = 0; n < NA; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float x0 = kv4_ex2(fmaf(sx[x][n][2 * h], sc[n][0], -m_off[n][0])), x1 = kv4_ex2(fmaf(sx[x][n][2 * h + 1], sc[n][1], -m_off[n][1]));
-          l_part[n][0] += x0;
-          l_part[n][1] += x1;
-          pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
-        }
-      // ---- O^T
-      uint32_t vw[2][2][D / 64];
+            for (int h = 0; h < 2; ++h) {
+              const float x0 = kv4_ex2(fmaf(sx[x][n][2 * h], sc[n][0], -m_off[n][0])), x1 = kv4_ex2(fmaf(sx[x][n][2 * h + 1], sc[n][1], -m_off[n][1]));
+              l_part[n][0] += x0;
+              l_part[n][1] += x1;
+              pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
+            }
+          // ---- O^T
+          uint32_t vw[2][2][D / 64];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if constexpr (D == 128) {
-            const uint2 u = *reinterpret_cast<const uint2*>(v_at[e] + at + x * PAGE + h * 512);
-            vw[h][e][0] = u.x, vw[h][e][1] = u.y;
-          } else {
-            vw[h][e][0] = *reinterpret_cast<const uint32_t*>(v_at[e] + at + x * PAGE + h * 256);
+            for (int e = 0; e < 2; ++e) {
+              if constexpr (D == 128) {
+                const uint2 u = *reinterpret_cast<const uint2*>(v_at[e] + at + x * PAGE + h * 512);
+                vw[h][e][0] = u.x, vw[h][e][1] = u.y;
+              } else {
+                vw[h][e][0] = *reinterpret_cast<const uint32_t*>(v_at[e] + at + x * PAGE + h * 256);
+              }
+            }
+          const __half2 scale[2] = {as_half2(scales_to_half2(vs[x] & 0xffff)), as_half2(scales_to_half2(vs[x] >> 16))};
+#pragma unroll
+          for (int q = 0; q < D / 64; ++q) {
+            // lo: even dims of the two tokens side by side, hi: odd dims
+            uint32_t lo[2][4], hi[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t a0 = vw[h][0][q], a1 = vw[h][1][q];
+              codes_to_half2((a0 & 0x0f0f0f0fu) | ((a1 << 4) & 0xf0f0f0f0u), lo[h]);
+              codes_to_half2(((a0 >> 4) & 0x0f0f0f0fu) | (a1 & 0xf0f0f0f0u), hi[h]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                lo[h][e] = mul_half2(lo[h][e], scale[h]);
+                hi[h][e] = mul_half2(hi[h][e], scale[h]);
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t a[4] = {lo[0][e], hi[0][e], lo[1][e], hi[1][e]};
+#pragma unroll
+              for (int n = 0; n < NA; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
+            }
           }
         }
-      const __half2 scale[2] = {as_half2(scales_to_half2(vs[x] & 0xffff)), as_half2(scales_to_half2(vs[x] >> 16))};
-#pragma unroll
-      for (int q = 0; q < D / 64; ++q) {
-        // lo: even dims of the two tokens side by side, hi: odd dims
-        uint32_t lo[2][4], hi[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t a0 = vw[h][0][q], a1 = vw[h][1][q];
-          codes_to_half2((a0 & 0x0f0f0f0fu) | ((a1 << 4) & 0xf0f0f0f0u), lo[h]);
-          codes_to_half2(((a0 >> 4) & 0x0f0f0f0fu) | (a1 & 0xf0f0f0f0u), hi[h]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            lo[h][e] = mul_half2(lo[h][e], scale[h]);
-            hi[h][e] = mul_half2(hi[h][e], scale[h]);
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t a[4] = {lo[0][e], hi[0][e], lo[1][e], hi[1][e]};
-#pragma unroll
-          for (int n = 0; n < NA; ++n) kv4_mma(o[n][4 * q + e], a, pb[n][0], pb[n][1]);
-        }
+        at = at == (ST - 1) * STAGE ? 0 : at + STAGE;
       }
-    }
-    at = at == (ST - 1) * STAGE ? 0 : at + STAGE;
-  }
-  };
-  using std::integral_constant;
-  if constexpr (NT == 1) {
-    walk(integral_constant<int, 1>());
-  } else if constexpr (NT == 2) {
-    if (n_rows <= 8) walk(integral_constant<int, 1>());
-    else walk(integral_constant<int, 2>());
-  } else {
-    if (n_rows <= 8) walk(integral_constant<int, 1>());
-    else if (n_rows <= 16) walk(integral_constant<int, 2>());
-    else if (n_rows <= 24) walk(integral_constant<int, 3>());
-    else walk(integral_constant<int, 4>());
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  // ---- fold the lanes' sums, then the 4 warps (the exchange buffer takes their rings' place)
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-#pragma unroll
-      for (int off = 4; off < 32; off <<= 1) l_part[n][e] += __shfl_xor_sync(0xffffffffu, l_part[n][e], off);
-      if (lane < 4) {
-        s_l[warp][n * 8 + 2 * lane + e] = l_part[n][e];
-        s_m[warp][n * 8 + 2 * lane + e] = m_next[n][e] == -FLT_MAX ? -FLT_MAX : m_off[n][e];   // (of a warp that saw nothing: no weight)
-      }
-    }
-  __syncthreads();
-  float* xo = reinterpret_cast<float*>(kv4_smem_raw);       // [warp][row][XD]
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        *reinterpret_cast<float2*>(&xo[(warp * ROWS + n * 8 + 2 * t + e) * XD + g * (D / 8) + 2 * k]) = make_float2(o[n][k][e], o[n][k][e + 2]);
-  __syncthreads();
-  for (int idx = tid; idx < n_rows * (D / 4); idx += KV4_THREADS) {
-    const int r = idx / (D / 4), d = (idx % (D / 4)) * 4;
-    float M = s_m[0][r];
-#pragma unroll
-    for (int x = 1; x < KV4_WARPS; ++x) M = fmaxf(M, s_m[x][r]);
-    float L = 0.f;
-    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int x = 0; x < KV4_WARPS; ++x) {
-      const float f = exp2f(s_m[x][r] - M);
-      const float4 y = *reinterpret_cast<const float4*>(xo + (x * ROWS + r) * XD + d);
-      L = fmaf(s_l[x][r], f, L);
-      O.x = fmaf(y.x, f, O.x);
-      O.y = fmaf(y.y, f, O.y);
-      O.z = fmaf(y.z, f, O.z);
-      O.w = fmaf(y.w, f, O.w);
-    }
-    float inv = L == 0.f ? 0.f : p.v_scale / L;
-    if (s_nan[r][d / (D / 8)]) inv = NAN;
-    const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);                    // (a sum of NaN stays NaN)
-    if (!first_part && ends) {
-      const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
-      const size_t row_head = (size_t)(w.first_row + token) * p.Hq + h;
-      *reinterpret_cast<uint2*>(p.out + row_head * D + d) =
-          make_uint2(pack_bf16x2(O.x * inv, O.y * inv), pack_bf16x2(O.z * inv, O.w * inv));
-      if (p.lse && d == 0) p.lse[row_head] = lse2 * 0.6931471805599453f;
+    };
+    using std::integral_constant;
+    if constexpr (NT == 1) {
+      walk(integral_constant<int, 1>());
+    } else if constexpr (NT == 2) {
+      if (n_rows <= 8) walk(integral_constant<int, 1>());
+      else walk(integral_constant<int, 2>());
     } else {
-      const size_t part = ((size_t)blockIdx.x * 2 + (first_part ? 0 : 1)) * ROWS + r;
-      *reinterpret_cast<float4*>(p.part_o + part * D + d) = make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
-      if (d == 0) p.part_lse[part] = lse2;
+      if (n_rows <= 8) walk(integral_constant<int, 1>());
+      else if (n_rows <= 16) walk(integral_constant<int, 2>());
+      else if (n_rows <= 24) walk(integral_constant<int, 3>());
+      else walk(integral_constant<int, 4>());
     }
-  }
-  // ---- on along the line
-  if (first_part) left.first_ends = ends;
-  else if (!ends) left = Kv4Piece{seq, kvh, tile, left.first_ends};
-  x0 += here;
-  off = 0;
-  if (x0 < x1) {
-    if (++tile == tiles) {
-      tile = 0;
-      ++kvh;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    // ---- fold the lanes' sums, then the 4 warps (the exchange buffer takes their rings' place)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) l_part[n][e] += __shfl_xor_sync(0xffffffffu, l_part[n][e], off);
+        if (lane < 4) {
+          s_l[warp][n * 8 + 2 * lane + e] = l_part[n][e];
+          s_m[warp][n * 8 + 2 * lane + e] = m_next[n][e] == -FLT_MAX ? -FLT_MAX : m_off[n][e];   // (of a warp that saw nothing: no weight)
+        }
+      }
+    __syncthreads();
+    float* xo = reinterpret_cast<float*>(kv4_smem_raw);       // [warp][row][XD]
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          *reinterpret_cast<float2*>(&xo[(warp * ROWS + n * 8 + 2 * t + e) * XD + g * (D / 8) + 2 * k]) = make_float2(o[n][k][e], o[n][k][e + 2]);
+    __syncthreads();
+    for (int idx = tid; idx < n_rows * (D / 4); idx += KV4_THREADS) {
+      const int r = idx / (D / 4), d = (idx % (D / 4)) * 4;
+      float M = s_m[0][r];
+#pragma unroll
+      for (int x = 1; x < KV4_WARPS; ++x) M = fmaxf(M, s_m[x][r]);
+      float L = 0.f;
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int x = 0; x < KV4_WARPS; ++x) {
+        const float f = exp2f(s_m[x][r] - M);
+        const float4 y = *reinterpret_cast<const float4*>(xo + (x * ROWS + r) * XD + d);
+        L = fmaf(s_l[x][r], f, L);
+        O.x = fmaf(y.x, f, O.x);
+        O.y = fmaf(y.y, f, O.y);
+        O.z = fmaf(y.z, f, O.z);
+        O.w = fmaf(y.w, f, O.w);
+      }
+      float inv = L == 0.f ? 0.f : p.v_scale / L;
+      if (s_nan[r][d / (D / 8)]) inv = NAN;
+      const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);                    // (a sum of NaN stays NaN)
+      if (!first_part && ends) {
+        const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
+        const size_t row_head = (size_t)(w.first_row + token) * p.Hq + h;
+        *reinterpret_cast<uint2*>(p.out + row_head * D + d) =
+            make_uint2(pack_bf16x2(O.x * inv, O.y * inv), pack_bf16x2(O.z * inv, O.w * inv));
+        if (p.lse && d == 0) p.lse[row_head] = lse2 * 0.6931471805599453f;
+      } else {
+        const size_t part = ((size_t)blockIdx.x * 2 + (first_part ? 0 : 1)) * ROWS + r;
+        *reinterpret_cast<float4*>(p.part_o + part * D + d) = make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
+        if (d == 0) p.part_lse[part] = lse2;
+      }
     }
-    if (kvh == p.Hkv) {
-      kvh = 0;
-      do w = kv4_seq(p, ++seq);
-      while (w.new_len == 0);                       // (the line goes on, so there is one)
+    // ---- on along the line
+    if (first_part) left.first_ends = ends;
+    else if (!ends) left = Kv4Piece{seq, kvh, tile, left.first_ends};
+    x0 += here;
+    off = 0;
+    if (x0 < x1) {
+      if (++tile == tiles) {
+        tile = 0;
+        ++kvh;
+      }
+      if (kvh == p.Hkv) {
+        kvh = 0;
+        do w = kv4_seq(p, ++seq);
+        while (w.new_len == 0);                       // (the line goes on, so there is one)
+      }
+      __syncthreads();                                // the exchange buffer becomes the rings again
     }
-    __syncthreads();                                // the exchange buffer becomes the rings again
-  }
   }
   if (!p.whole && tid == 0) p.pieces[blockIdx.x] = left;
 }
@@ -743,7 +748,7 @@ Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_
   pl.row_tiles = (rows + 8 * pl.nt - 1) / (8 * pl.nt);
   if (max_ctx < 1) max_ctx = 1;
   const int trip = 16 * KV4_WARPS * kv4_pages(pl.nt);
-  const long long trips = (max_ctx + (long long)trip - 1) / trip, units = batch * cache->num_kv_heads * pl.row_tiles;
+  const long long trips = (max_ctx + (long long)trip - 1) / trip, units = (long long)batch * cache->num_kv_heads * pl.row_tiles;
   pl.whole = max_ctx <= KV4_WHOLE;
   pl.least_trips = KV4_LEAST / trip;
   pl.ctas = pl.whole ? units : std::min<long long>((long long)sm_count() * kv4_ctas_per_sm(pl.nt), (units * trips + pl.least_trips - 1) / pl.least_trips);
