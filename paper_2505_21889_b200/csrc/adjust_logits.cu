@@ -4,6 +4,11 @@
 // holds it, and which entry of the bias list it has.  Few tokens are touched by any of that, so the rows are copied first (with the
 // mask, in place only where it takes something away); then the touched tokens, listed, are computed over it, a thread a token, walking
 // the sequence's rows and counting each row's own draft before it (a row's distribution comes after that token).
+//
+// Bound: 256 users x 1-5 rows x 131,072 places in bf16 125 us with cold caches (the copy 82, all but the copy 80: two CTAs an SM overlap them in part; the histories,
+// which each slice reads, 33); 16 users x 5 rows 22.5: the phases' latencies, one wave.  Every logit through fp32: 189.  Not kept: clusters that read a history once and
+// count in each other's shared memory (165: remote atomics, CTAs that wait for each other), half of the warps copying while the others count (198),
+// 1,024 threads (188), three CTAs by 40 registers (141).
 #include "common.cuh"
 #include <algorithm>
 #include <atomic>
