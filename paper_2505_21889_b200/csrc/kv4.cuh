@@ -53,21 +53,46 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, __half2 b) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// 16 bytes of codes (32 values, two scales) as bf16
-__device__ __forceinline__ void kv4_to_bf16(const uint4& codes, uint32_t two_scales, float g, uint4* dst) {
-  const uint32_t s2 = scales_to_half2(two_scales);
-  const float s[2] = {__half2float(__ushort_as_half((unsigned short)s2)) * g, __half2float(__ushort_as_half((unsigned short)(s2 >> 16))) * g};
-  const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};
+// a word of codes (8 values of one block) as bf16
+__device__ __forceinline__ uint4 kv4_to_bf16(uint32_t codes, uint32_t scale_byte, float g) {
+  const float s = __half2float(__ushort_as_half((unsigned short)scales_to_half2(scale_byte))) * g;
+  uint32_t h[4], r[4];
+  codes_to_half2(codes, h);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t h[4], r[4];
-    codes_to_half2(word[q], h);
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = __half22float2(as_half2(h[e]));
+    r[e] = pack_bf16x2(f.x * s, f.y * s);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// Page `page` of all heads, keys and values, to page `to` of two bf16 pools (either may be null), by the threads of a CTA: a word of codes, 16 bytes of the
+// result, a thread, so that neighbours read and write side by side; four of them on their way.
+template <int D, int THREADS>
+__device__ __forceinline__ void kv4_page_to_bf16(const uint8_t* k_codes, const uint8_t* v_codes, const uint8_t* k_scales, const uint8_t* v_scales,
+                                                 float k_scale, float v_scale, size_t page, size_t to, int Hkv, uint16_t* k_out, uint16_t* v_out) {
+  constexpr int AT_ONCE = 4;
+  const int words = Hkv * (16 * D / 8);               // of a pool's page
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
-      r[e] = pack_bf16x2(f.x * s[q / 2], f.y * s[q / 2]);
+  for (int pool = 0; pool < 2; ++pool) {
+    uint4* out = reinterpret_cast<uint4*>(pool ? v_out : k_out);
+    if (!out) continue;
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>(pool ? v_codes : k_codes) + page * words;
+    const uint8_t* scales = (pool ? v_scales : k_scales) + page * (words / 2);
+    const float g = pool ? v_scale : k_scale;
+    out += to * words;
+    for (int u0 = threadIdx.x; u0 < words; u0 += AT_ONCE * THREADS) {
+      uint32_t w[AT_ONCE], s[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+        if (u0 + i * THREADS < words) {
+          w[i] = *(codes + u0 + i * THREADS);
+          s[i] = *(scales + (u0 + i * THREADS) / 2);
+        }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+        if (u0 + i * THREADS < words) out[u0 + i * THREADS] = kv4_to_bf16(w[i], s[i], g);
     }
-    dst[q] = make_uint4(r[0], r[1], r[2], r[3]);
   }
 }
 

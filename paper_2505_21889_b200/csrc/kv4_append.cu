@@ -96,8 +96,8 @@ __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g,
 // A token's q, k and v heads go to its warps in groups of 512 / D heads.  A lane holds vector j of a head row and its partner
 // j + D/16, as in efim_qk_norm_append, so either pairing of the rotation stays inside the lane; two neighbours hold a block of sixteen.
 //
-// Bound: with many tokens the instructions (299 a warp and group, 70 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 125 us, 4.4 TB/s; with
-// three divisions a block and value by value 134.  64 registers (four CTAs an SM, 100 bytes spilled) 155.  Keys in 64 bits up to their rounding 179.
+// Bound: with many tokens the instructions (299 a warp and group, 70 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 118 us (4.7 TB/s; 125 with
+// cold caches; with divisions and value by value 134).  64 registers (four CTAs an SM, 100 bytes spilled) 155.  Keys in 64 bits up to their rounding 179.
 // With few tokens a chain of dependent loads: 64 tokens at 28/4 2.7 us.
 template <int D>
 __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
@@ -256,11 +256,9 @@ struct Kv4UnpackParams {
 
 constexpr int KV4_UNPACK_THREADS = 256;
 
-// A thread has 16 bytes of codes (32 values, 64 bytes of the result); the threads of a CTA walk one page's heads, K then V.  Bound: HBM's writes (1,600
-// pages of 8 heads x 128 36 us with launch, 134 MB).
+// One page a CTA.  Bound: HBM's writes (1,600 pages of 8 heads x 128, 134 MB: 23 us; 16 bytes of codes a thread, 64 of the result, 34).
 template <int D>
 __global__ void __launch_bounds__(KV4_UNPACK_THREADS) kv4_unpack_kernel(const Kv4UnpackParams p) {
-  constexpr int PER_HEAD = 16 * D / 32;             // 16-byte pieces of codes of one (page, head)
   pdl_wait();
   pdl_launch();
   const int i = blockIdx.x;
@@ -269,17 +267,7 @@ __global__ void __launch_bounds__(KV4_UNPACK_THREADS) kv4_unpack_kernel(const Kv
     if (threadIdx.x == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
     return;
   }
-  const int per_pool = p.Hkv * PER_HEAD;
-  for (int u = threadIdx.x; u < 2 * per_pool; u += KV4_UNPACK_THREADS) {
-    const bool key = u < per_pool;
-    const int w = key ? u : u - per_pool;
-    uint16_t* out = key ? p.k_out : p.v_out;
-    if (!out) continue;
-    const size_t at = (size_t)page * per_pool + w;
-    const uint4 codes = *reinterpret_cast<const uint4*>((key ? p.k_codes : p.v_codes) + at * 16);
-    const uint32_t two = *reinterpret_cast<const uint16_t*>((key ? p.k_scales : p.v_scales) + at * 2);
-    kv4_to_bf16(codes, two, key ? p.k_scale : p.v_scale, reinterpret_cast<uint4*>(out) + ((size_t)i * per_pool + w) * 4);
-  }
+  kv4_page_to_bf16<D, KV4_UNPACK_THREADS>(p.k_codes, p.v_codes, p.k_scales, p.v_scales, p.k_scale, p.v_scale, page, i, p.Hkv, p.k_out, p.v_out);
 }
 
 }  // namespace efim

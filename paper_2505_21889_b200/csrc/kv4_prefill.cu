@@ -17,11 +17,9 @@ struct Kv4StageParams {
 
 constexpr int KV4_STAGE_THREADS = 256;
 
-// One page of one sequence a CTA: K and V of all heads, 16 bytes of codes (32 values) a thread and trip.  Bound: HBM (4.5 bits in, 16 out a value); 16 x 5k tokens at
-// 8 heads x 128 about 90 us before the attention's first tile.
+// One page of one sequence a CTA.  Bound: HBM (4.5 bits in, 16 out a value): 16 x 2-8k tokens at 8 heads x 128 70 us; 16 bytes of codes a thread 111.
 template <int D>
 __global__ void __launch_bounds__(KV4_STAGE_THREADS) kv4_stage_kernel(const Kv4StageParams p) {
-  constexpr int PER_HEAD = 16 * D / 32;
   __shared__ int s_before[KV4_STAGE_THREADS / 32];
   const int s = blockIdx.y, i = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
@@ -44,15 +42,7 @@ __global__ void __launch_bounds__(KV4_STAGE_THREADS) kv4_stage_kernel(const Kv4S
   const bool ok = page >= 0 && page < p.num_pages && to < p.n;
   if (tid == 0) p.table[(size_t)s * p.width + i] = ok ? to : -1;      // (the attention reports what is bad)
   if (!ok) return;
-  const int per_pool = p.Hkv * PER_HEAD;
-  for (int u = tid; u < 2 * per_pool; u += KV4_STAGE_THREADS) {
-    const bool key = u < per_pool;
-    const int w = key ? u : u - per_pool;
-    const size_t at = (size_t)page * per_pool + w;
-    const uint4 codes = ldg_stream((key ? p.k_codes : p.v_codes) + at * 16);
-    const uint32_t two = *reinterpret_cast<const uint16_t*>((key ? p.k_scales : p.v_scales) + at * 2);
-    kv4_to_bf16(codes, two, key ? p.k_scale : p.v_scale, reinterpret_cast<uint4*>(key ? p.k_out : p.v_out) + ((size_t)to * per_pool + w) * 4);
-  }
+  kv4_page_to_bf16<D, KV4_STAGE_THREADS>(p.k_codes, p.v_codes, p.k_scales, p.v_scales, p.k_scale, p.v_scale, page, to, p.Hkv, p.k_out, p.v_out);
 }
 
 namespace {
