@@ -209,3 +209,23 @@ def test_graph_and_another_stream():
     case.out.fill_(7)
     graph.replay()
     assert torch.equal(first.view(torch.int16), case.out.view(torch.int16))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_far_apart(in_place):
+    """Rows 2^30 + 8 elements apart: offsets past 32 bits in bytes and in elements; nothing between the rows is touched."""
+    case = Case([2, 3], 1000, [30, 4])
+    step = (1 << 30) + 8
+    wide = torch.full((4 * step + 1000,), 3.0, dtype=torch.bfloat16, device="cuda")
+    far = wide.as_strided((5, 1000), (step, 1))
+    far.copy_(case.logits)
+    want = torch.empty_like(case.logits)
+    case.run(out=want)
+    case.check()
+    efim.efim_adjust_logits(logits=far, out=None if in_place else (near := torch.empty_like(want)), status=case.status, **case.args)
+    assert torch.equal((far if in_place else near).contiguous().view(torch.int16), want.view(torch.int16))
+    if not in_place:
+        efim.efim_adjust_logits(logits=case.logits, out=far, status=case.status, **case.args)
+        assert torch.equal(far.contiguous().view(torch.int16), want.view(torch.int16))
+    far.fill_(3.0)
+    assert bool((wide[::1021] == 3).all()) and bool((wide[1000:2000] == 3).all()) and case.status.item() == 0

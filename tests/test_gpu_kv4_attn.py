@@ -128,6 +128,56 @@ def test_plans(batch, ctx):
     assert case.status.item() == 0
 
 
+@pytest.mark.parametrize("hq,hkv,d,most", [(28, 4, 128, 9), (8, 2, 64, 5), (16, 2, 128, 2), (48, 2, 128, 3)])
+@pytest.mark.parametrize("batch,ctx", [(60, 5000), (7, 20000), (500, 1500)])
+def test_pieces(hq, hkv, d, most, batch, ctx):
+    """Rows and lengths of all kinds in one call: pieces that hold many units, a part of one, starts alone."""
+    rng = np.random.default_rng(batch + hq)
+    new = rng.integers(0, most + 1, batch)
+    lens = np.maximum((ctx * rng.random(batch) ** 3).astype(int), new)
+    lens[batch // 2], new[batch // 2] = ctx, most
+    case = Case(hq, hkv, d, lens.tolist(), new.tolist(), seed=batch, extra_rows=2)
+    case.run(max_new=most)
+    assert case.status.item() == 0
+    longest = int(np.argmax(lens))
+    case.check(only={0, longest, batch // 2, batch - 1, *rng.integers(0, batch, 4 if batch < 100 else 12).tolist()} - ({longest} if ctx > 6000 else set()))
+
+
+def test_pages_past_32_bit_offsets():
+    """A pool of more than 2^32 bytes of codes: its last pages give what a small pool gives, appended, read back and attended."""
+    hq, hkv, d, many = 8, 8, 128, 540000
+    g = torch.Generator().manual_seed(2)
+    assert many * hkv * 16 * d // 2 > 1 << 32
+    results = []
+    for pages in (many, 12):
+        codes = [torch.empty(pages, hkv, 16, d // 2, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scales = [torch.empty(pages, hkv, 16, d // 16, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        cache = efim.Cache4(*codes, *scales, hq)
+        g.manual_seed(2)
+        qkv = torch.randn(170, 3 * hq * d, generator=g).bfloat16().cuda()
+        table = torch.tensor([[pages - 1 - i for i in range(11)]], dtype=torch.int32)
+        batch = efim.Batch([3], [170], table.numpy())
+        head = efim.Batch([0], [3], table.numpy())
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        q = torch.empty(170, hq, d, dtype=torch.bfloat16, device="cuda")
+        efim.efim_kv4_append(cache, head, None, None, None, qkv[:3, hq * d:2 * hq * d], qkv[:3, 2 * hq * d:], None, status)
+        efim.efim_kv4_append(cache, batch, None, None, *qkv.split([hq * d] * 3, 1), q, status)
+        read = [torch.empty(11, hkv, 16, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        efim.efim_kv4_unpack(cache, table[0].cuda(), *read, status)
+        read[0].view(11, hkv, 16, d)[10, :, 13:] = read[1].view(11, hkv, 16, d)[10, :, 13:] = 0      # (slots that hold nothing)
+        out = torch.empty(1, hq, d, dtype=torch.bfloat16, device="cuda")
+        ctx = torch.tensor([173], dtype=torch.int32, device="cuda")
+        efim.efim_kv4_decode_attn(cache, 1, ctx, 173, table.cuda(), q[-1:], out, status=status)
+        turn = torch.empty_like(q)
+        ws = torch.empty(efim.efim_kv4_prefill_workspace_bytes(cache, batch), dtype=torch.uint8, device="cuda")
+        efim.efim_kv4_append_prefill_attn(cache, batch, q, turn, workspace=ws, status=status)
+        assert status.item() == 0
+        results.append([q, *read, out, turn])
+        del codes, scales, cache
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
 def test_new_tokens_before_the_sequence():
     """More rows than keys: the first ones see nothing."""
     case = Case(4, 2, 64, [3, 2], [5, 2])
