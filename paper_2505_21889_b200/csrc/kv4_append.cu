@@ -26,10 +26,14 @@ struct Kv4AppendParams {
   int batch, max_pages_per_seq, total_new_tokens;
   int num_pages, Hq, Hkv, max_position, interleaved, weight_f32, normed;
   int warps;                // of a token
+  int ahead;                // a token's rows are sent for into L2 by its first and last warp
   int early_next;           // let the next kernel start its set-up while this one runs
 };
 
 constexpr int KV4_APPEND_THREADS = 256;
+
+// A value that is the same in a warp's lanes, in a form that tells the compiler so: what depends on it is computed once a warp.
+__device__ __forceinline__ int kv4_uniform(int x) { return __reduce_max_sync(0xffffffffu, x); }
 
 // 8 weights from position d on, as the products take them
 __device__ __forceinline__ void kv4_load_weights(const void* weight, int f32, float offset, int d, float2* w) {
@@ -96,15 +100,16 @@ __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g,
 // A token's q, k and v heads go to its warps in groups of 512 / D heads.  A lane holds vector j of a head row and its partner
 // j + D/16, as in efim_qk_norm_append, so either pairing of the rotation stays inside the lane; two neighbours hold a block of sixteen.
 //
-// Bound: with many tokens the instructions (299 a warp and group, 70 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 118 us (4.7 TB/s; 125 with
-// cold caches; with divisions and value by value 134).  64 registers (four CTAs an SM, 100 bytes spilled) 155.  Keys in 64 bits up to their rounding 179.
+// Bound: with many tokens the instructions (70 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 102 us (5.5 TB/s).
+// What brought it there: no divisions and two values at a time 126 -> 118, warp-wide values marked as such 113, rows sent for ahead 111, a warp a token instead of
+// three 102.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115, keys in 64 bits up to their rounding (179 with cold caches, from 125).
 // With few tokens a chain of dependent loads: 64 tokens at 28/4 2.7 us.
 template <int D>
 __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
   constexpr int HALF = D / 16;                  // lanes that have a head
   constexpr int HW = 32 / HALF;
   const int lane = threadIdx.x & 31;
-  const int flat = blockIdx.x * (KV4_APPEND_THREADS / 32) + (threadIdx.x >> 5);
+  const int flat = blockIdx.x * (KV4_APPEND_THREADS / 32) + kv4_uniform(threadIdx.x >> 5);
   const int t = flat / p.warps, part = flat % p.warps;
   pdl_wait();
   if (p.early_next) pdl_launch();
@@ -124,9 +129,16 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     }
   };
   const int base0 = part * HW;
+  if (p.ahead && lane == 0) {
+    if (part == 0 && p.q) prefetch_l2(p.q + t * p.q_stride, nq * D * 2LL);
+    if (part == p.warps - 1) {
+      prefetch_l2(p.k + t * p.k_stride, p.Hkv * D * 2LL);
+      prefetch_l2(p.v + t * p.v_stride, p.Hkv * D * 2LL);
+    }
+  }
   fetch(base0 + sub);
   const TokenPlace at = find_token(p.q_indptr, p.cached_len, p.batch, t, lane);
-  const int pos = at.pos, page_idx = pos >> 4;
+  const int pos = kv4_uniform(at.pos), page_idx = pos >> 4;
   const bool in_table = !p.cos_sin || (pos >= 0 && pos < p.max_position);
   bool placed = pos >= 0 && page_idx < p.max_pages_per_seq && in_table;   // k and v have a place in the cache
   int page = 0;
@@ -155,6 +167,7 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     placed = false;
   }
   const size_t row0 = (size_t)page * p.Hkv * 16 + (pos & 15);              // + h * 16: rows of the pools
+#pragma unroll 1
   for (int base = base0; base < nh; base += step) {    // (the same for a warp's lanes: the sums below are the whole warp's)
     const int h = base + sub;
     uint32_t y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -340,9 +353,13 @@ extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim
   p.Hkv = cache->num_kv_heads;
   const int hw = 512 / D, heads = (d_q ? cache->num_q_heads : 0) + 2 * cache->num_kv_heads, groups = (heads + hw - 1) / hw;
   const long long resident = 4LL * (KV4_APPEND_THREADS / 32) * sm_count();
-  p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 10 ? (groups + 4) / 5 : 1, resident / T));
+  // Warps of a token: as many as are resident at once, up to one for every group of heads; with more tokens one, or from 16 groups on one for every ten.
+  // Microseconds with 1 / 2 / 3 / 4: 25,600 tokens at 32/8 heads x 128 (12 groups) 102 / 104 / 111 / 121, 12,800 at 64/8 (20) 93 / 87 / - / 91, at 32/32 (24) 104 / 103 /
+  // 103 / 104.  Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 78.
+  p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 16 ? (groups + 9) / 10 : 1, resident / T));
   const long long ctas = (T * p.warps + KV4_APPEND_THREADS / 32 - 1) / (KV4_APPEND_THREADS / 32);
   if (ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  p.ahead = T * p.warps > 4 * resident;
   p.early_next = ctas <= sm_count();
   auto launch = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)ctas), dim3(KV4_APPEND_THREADS), 0, static_cast<cudaStream_t>(stream), p);
