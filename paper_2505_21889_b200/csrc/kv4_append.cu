@@ -63,7 +63,7 @@ __device__ __forceinline__ void kv4_load_weights(const void* weight, int f32, fl
 // Rounding without divisions.  The largest value a is compared with 6 g times the borders between scales, and each x with the borders t s g
 // between codes: all of these are numbers of at most 8 significant bits, so two of them are equal or at least 2^-8 of them apart.  The
 // quotients a / (6 g) and x / (s g), as products with approximate inverses, are within 2^-21; rounded, to 14 significant bits and to a
-// multiple of 2^-12 (by the sum with 3072), they are a border where it is one, else on the right side of it.
+// multiple of 2^-12 (by the sum with 3/2 2^11), they are a border where it is one, else on the right side of it.
 __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g, uint32_t* scale) {
   float2 x[4];
   float top = 0.f;
@@ -83,10 +83,11 @@ __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g,
   float inv_s;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv_s) : "f"(__half2float(__ushort_as_half((unsigned short)sf))));
   inv_s *= inv_g;                                                              // (a power of two)
+  constexpr float TO_GRID = 1.5f * 2048.f;
   float y[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 z = add2(add2(mul2(x[i], make_float2(inv_s, inv_s)), make_float2(3072.f, 3072.f)), make_float2(-3072.f, -3072.f));
+    const float2 z = add2(add2(mul2(x[i], make_float2(inv_s, inv_s)), make_float2(TO_GRID, TO_GRID)), make_float2(-TO_GRID, -TO_GRID));
     y[2 * i] = copysignf(z.x, x[i].x);
     y[2 * i + 1] = copysignf(z.y, x[i].y);
   }
@@ -101,8 +102,9 @@ __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g,
 // j + D/16, as in efim_qk_norm_append, so either pairing of the rotation stays inside the lane; two neighbours hold a block of sixteen.
 //
 // Bound: with many tokens the instructions (70 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 102 us (5.5 TB/s).
-// What brought it there: no divisions and two values at a time 126 -> 118, warp-wide values marked as such 113, rows sent for ahead 111, a warp a token instead of
-// three 102.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115, keys in 64 bits up to their rounding (179 with cold caches, from 125).
+// What brought it there, as replayed from a graph: warp-wide values marked as such 118 -> 113, rows sent for ahead 111, a warp a
+// token instead of three 102.  Timed by events around single calls: divisions and value by value 134, neither 125; keys in 64 bits
+// up to their rounding 179.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115 where 78 registers took 113.
 // With few tokens a chain of dependent loads: 64 tokens at 28/4 2.7 us.
 template <int D>
 __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
