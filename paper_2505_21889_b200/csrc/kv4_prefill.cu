@@ -86,9 +86,11 @@ Lengths longest(const efim_batch_desc* b) {
   return r;
 }
 // Rows a (sequence, kv head) up to which the keys are taken from the codes by the decode kernel: its time grows with the rows, the other way's first
-// with the pages that are unpacked.  Microseconds, direct / unpacked: 16 x 5k keys at 32/8 heads 32 rows 93 / 197, 64 148 / 200, 96 202 / 201, 128 255 / 203;
-// at 28/4 56 rows 89 / 101, 84 116 / 101; 8 x 4k at 32/32 64 rows 200 / 314, 128 362 / 320; 64 x 2k at 32/8 64 rows 235 / 278, 96 329 / 285; 16 x 5k at
-// 8/8 x 64 64 rows 112 / 119, 128 183 / 121.  With few pages, where both are latencies: 1 x 4k at 32/8 8 rows 21.5 / 27.6, 16 25.6 / 27.7, 32 35.8 / 27.6.
+// with the pages that are unpacked.  Microseconds, direct / unpacked: 16 x 5k keys at 32/8 heads 32 rows 83 / 155, 64 134 / 158, 80 175 / 160; at 28/4
+// 63 rows 81 / 86, 77 99 / 86; 8 x 4k at 32/32 64 rows 191 / 222, 80 247 / 220; 64 x 2k at 32/8 64 rows 224 / 220, 80 292 / 222; 16 x 5k at 8/8 x 64
+// 64 rows 101 / 102, 80 128 / 103.  With few pages, where both are latencies: 1 x 4k at 32/8 8 rows 21.6 / 26.7, 16 25.6 / 27.1, 24 35.8 / 26.7; 4 x 4k
+// 16 rows 29.7 / 42, 48 50 / 45.  At 65 to 80 rows the direct way is 10 to 31 % longer; it is taken up to 80 for its weights of 11
+// bits, where the bf16 kernel's have 8.
 bool goes_direct(const efim_cache4_desc* cache, const efim_batch_desc* batch, const Lengths& most) {
   long long page_heads = 0;
   for (int s = 0; s < batch->batch; ++s)
