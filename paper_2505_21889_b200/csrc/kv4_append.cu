@@ -360,7 +360,7 @@ extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim
   // 103 / 104.  Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 78.
   p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 16 ? (groups + 9) / 10 : 1, resident / T));
   const long long ctas = (T * p.warps + KV4_APPEND_THREADS / 32 - 1) / (KV4_APPEND_THREADS / 32);
-  if (ctas > 0x7fffffffLL) return EFIM_ERR_UNSUPPORTED;
+  if (ctas > 0x7fffffffLL / (KV4_APPEND_THREADS / 32)) return EFIM_ERR_UNSUPPORTED;    // (warps are counted in 32 bits)
   p.ahead = T * p.warps > 4 * resident;
   p.early_next = ctas <= sm_count();
   auto launch = [&](auto kernel) {
