@@ -409,9 +409,10 @@ typedef struct {
 } efim_cache4_desc;
 
 /*
- * Step 1 over a 4-bit cache: q and k normalised if `norm` is not NULL (as efim_qk_norm_append does it), rotated by their positions if
- * `rope` holds a table, rounded to bf16; q goes to d_q_out, k and v to their blocks.  Operands, strides, d_q_out (packed, d_q itself
- * where that is packed, too) and errors as for efim_qk_norm_append.  total_new_tokens may be more than the device's q_indptr[batch]: the
+ * Step 1 over a 4-bit cache: q and k normalised if `norm` is not NULL, rotated by their positions if `rope` holds a table, rounded to bf16;
+ * q goes to d_q_out as efim_qk_norm_append (efim_kv_append) rounds it, k and v to their blocks.  What is held of k is whole numbers, so its norm and
+ * rotation are those of 64-bit arithmetic on the given bf16 and fp32 numbers, rounded to fp32 and that to bf16, both to nearest even.  Operands,
+ * strides, d_q_out (packed, d_q itself where that is packed, too) and errors as for efim_qk_norm_append.  total_new_tokens may be more than the device's q_indptr[batch]: the
  * rows behind the last sequence's are left as they were.  One kernel; no workspace; may be captured.
  */
 efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim_batch_desc* batch, const efim_qk_norm_desc* norm,

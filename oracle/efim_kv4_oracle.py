@@ -19,6 +19,22 @@ def nearest(x, values):
     return np.where((down < up) | ((down == up) & (hi % 2 == 1)), hi - 1, hi)
 
 
+def key(x, table, interleaved=False, weight=None, eps=0.0):
+    """Heads x [..., D], normalised where there are weights and rotated by table rows [..., D] (cos, then sin; None: not), rounded to fp32, and that to bf16.
+    -> numbers of 8 bits, as float64"""
+    x, half = np.asarray(x, np.float64), x.shape[-1] // 2
+    with np.errstate(all="ignore"):
+        if weight is not None:
+            x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * weight
+        if table is not None:
+            cos, sin = np.float64(table[..., :half]), np.float64(table[..., half:])
+            a, b = (x[..., 0::2], x[..., 1::2]) if interleaved else (x[..., :half], x[..., half:])
+            x = np.stack([a * cos - b * sin, b * cos + a * sin], -1 if interleaved else -2).reshape(x.shape)
+        bits = x.astype(np.float32).view(np.uint32).astype(np.uint64)
+    bits = np.where(np.isnan(x), 0x7fc00000, bits + 0x7fff + (bits >> 16 & 1) & 0xffff0000)
+    return bits.astype(np.uint32).view(np.float32).astype(np.float64)
+
+
 def quantize(x, g):
     """x: float64 [..., D], numbers with few bits (bf16).  -> codes uint8 [..., D / 2], scales uint8 [..., D / 16]."""
     x = np.asarray(x, np.float64).reshape(*x.shape[:-1], -1, 16)

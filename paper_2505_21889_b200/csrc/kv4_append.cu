@@ -4,6 +4,7 @@
 #include "token_place.cuh"
 #include <float.h>
 #include <algorithm>
+#include <type_traits>
 
 namespace efim {
 
@@ -23,6 +24,7 @@ struct Kv4AppendParams {
   const float* cos_sin;     // [max_position][D] or null
   int32_t* status;
   float eps, weight_offset, k_inv, v_inv;   // the pools' scales, inverted
+  float key_error;          // how far fp32 may be off in a key, of the terms it is the sum of
   int batch, max_pages_per_seq, total_new_tokens;
   int num_pages, Hq, Hkv, max_position, interleaved, weight_f32, normed;
   int warps;                // of a token
@@ -98,14 +100,87 @@ __device__ __forceinline__ uint32_t kv4_quantize(const uint32_t* w, float inv_g,
   return codes;
 }
 
+// A lane's 16 values of a head as codes and scales.
+struct Kv4Codes { uint32_t c0, c1, s0, s1; };
+__device__ __forceinline__ Kv4Codes kv4_quantize_both(const uint32_t* w, float inv_g) {
+  Kv4Codes z;
+  z.c0 = kv4_quantize(w, inv_g, &z.s0);
+  z.c1 = kv4_quantize(w + 4, inv_g, &z.s1);
+  return z;
+}
+
+// A key by its definition: normed and rotated in 64 bits, rounded to fp32 and that to bf16.  `row` and `cs` (or null) are the lane's first vector of
+// the head and its first rotary value.  Called by whole warps.
+template <int D>
+__device__ __forceinline__ Kv4Codes kv4_key_in_64_bits(const uint4* row, const void* weight, const float* cs, int j, int normed, int weight_f32,
+                                                    int interleaved, float eps, float offset, float inv_g) {
+  constexpr int HALF = D / 16;
+  const uint4 a = row[0], b = row[HALF];
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  double r = 1.;
+  if (normed) {
+    double ss = 0.;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double lo = bf16lo(w[e]), hi = bf16hi(w[e]);
+      ss = fma(lo, lo, fma(hi, hi, ss));
+    }
+#pragma unroll
+    for (int d = HALF / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+    r = rsqrt(ss / D + eps);
+  }
+  auto value = [&](int e, int odd) {                     // of w[e]: dim 2e + odd of the lane's first eight, then of its second
+    double x = odd ? bf16hi(w[e]) : bf16lo(w[e]);
+    if (normed) {
+      x *= r;
+      if (weight) {
+        const int d = (j + e / 4 * HALF) * 8 + e % 4 * 2 + odd;
+        x *= (weight_f32 ? (double)static_cast<const float*>(weight)[d] : (double)bf16lo(static_cast<const uint16_t*>(weight)[d])) + offset;
+      }
+    }
+    return x;
+  };
+  uint32_t y[8];
+  if (!cs) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2((float)value(e, 0), (float)value(e, 1));
+  } else if (interleaved) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double x0 = value(e, 0), x1 = value(e, 1), c = cs[e / 4 * (D / 4) + e % 4], s = cs[D / 2 + e / 4 * (D / 4) + e % 4];
+      y[e] = pack_bf16x2((float)(x0 * c - x1 * s), (float)(x1 * c + x0 * s));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float lo[2], hi[2];
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        const double x0 = value(e, odd), x1 = value(4 + e, odd), c = cs[2 * e + odd], s = cs[D / 2 + 2 * e + odd];
+        lo[odd] = (float)(x0 * c - x1 * s);
+        hi[odd] = (float)(x1 * c + x0 * s);
+      }
+      y[e] = pack_bf16x2(lo[0], lo[1]);
+      y[4 + e] = pack_bf16x2(hi[0], hi[1]);
+    }
+  }
+  return kv4_quantize_both(y, inv_g);
+}
+
 // A token's q, k and v heads go to its warps in groups of 512 / D heads.  A lane holds vector j of a head row and its partner
 // j + D/16, as in efim_qk_norm_append, so either pairing of the rotation stays inside the lane; two neighbours hold a block of sixteen.
 //
-// Bound: with many tokens the instructions (70 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 102 us (5.5 TB/s).
-// What brought it there, as replayed from a graph: warp-wide values marked as such 118 -> 113, rows sent for ahead 111, a warp a
-// token instead of three 102.  Timed by events around single calls: divisions and value by value 134, neither 125; keys in 64 bits
-// up to their rounding 179.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115 where 78 registers took 113.
-// With few tokens a chain of dependent loads: 64 tokens at 28/4 2.7 us.
+// Keys are what norm and rotation give in 64 bits, in codes: whole numbers, so an error of fp32 next to a border is a code off, or a block.  fp32 knows how far
+// it may be off (key_error); where both ends of that have the same codes and scales they are the key's, else the group of heads is done again in
+// 64 bits behind the loop.  At 32/8 heads x 128 with norms three groups of keys in four have a value whose ends round to different bf16 numbers (without, one in three), one in 160
+// has ends of different codes (one in 700).
+//
+// Bound: with many tokens the instructions (75 % of the issue slots): 25,600 tokens at 32/8 heads x 128 with norms 113 us (5.0 TB/s), 102 by keys in fp32.
+// What brought it there, as replayed from a graph, keys in fp32: warp-wide values marked as such 118 -> 113, rows sent for ahead 111, a warp a
+// token instead of three 102.  Of the 64 bits: every group whose ends round differently again 143, those of different codes 124 (a call inside the loop)
+// -> 117 (behind the loop) -> 113 (in line).  Timed by events around single calls: divisions and value by value 134, neither 125; all keys in
+// 64 bits 179.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115 where 78 registers took 113.
+// With few tokens a chain of dependent loads: 64 tokens at 28/4 2.9 us.
 template <int D>
 __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
   constexpr int HALF = D / 16;                  // lanes that have a head
@@ -150,6 +225,7 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     page = *(p.block_table + (size_t)at.seq * p.max_pages_per_seq + page_idx);
   }
   float2 c[4], s[4];
+  float key_error = p.key_error;                // times |x| + |y| of a pair: how far its rotated values may be off
   if (p.cos_sin && in_table) {
     // 8 pairs: (f, f + D/2) from f = 8 j on, or the 4 + 4 neighbours of the two vectors
     const float* cs = p.cos_sin + (size_t)pos * D + j * (p.interleaved ? 4 : 8);
@@ -163,16 +239,39 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     four(cs + second, c + 2);
     four(cs + D / 2, s);
     four(cs + D / 2 + second, s + 2);
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fmaxf(fabsf(c[e].x), fabsf(c[e].y)), fmaxf(fabsf(s[e].x), fabsf(s[e].y))));
+    key_error *= most;
   }
   if (placed && (page < 0 || page >= p.num_pages)) {
     if (lane == 0 && p.status) atomicOr(p.status, EFIM_DEV_BAD_PAGE);
     placed = false;
   }
   const size_t row0 = (size_t)page * p.Hkv * 16 + (pos & 15);              // + h * 16: rows of the pools
+  auto store = [&](int h, const Kv4Codes& z) {
+    if (h >= nq && h < nh && placed) {
+      const bool key = h < nk;
+      const size_t row = row0 + (size_t)(h - (key ? nq : nk)) * 16;
+      uint8_t* codes = (key ? p.k_codes : p.v_codes) + row * (D / 2) + j * 4;
+      *reinterpret_cast<uint32_t*>(codes) = z.c0;
+      *reinterpret_cast<uint32_t*>(codes + D / 4) = z.c1;
+      if ((j & 1) == 0) {
+        uint8_t* scales = (key ? p.k_scales : p.v_scales) + row * (D / 16) + j / 2;
+        scales[0] = (uint8_t)z.s0;
+        scales[D / 32] = (uint8_t)z.s1;
+      }
+    }
+  };
+  int key_group = 0;                                   // of the groups that have keys
+  uint32_t again = 0;                                  // those that fp32 does not decide, a bit each (the last one for all from the 32nd on)
 #pragma unroll 1
   for (int base = base0; base < nh; base += step) {    // (the same for a warp's lanes: the sums below are the whole warp's)
     const int h = base + sub;
     uint32_t y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t inner[8] = {};
+    const bool key = h >= nq && h < nk && placed;
+    bool unsure = false, lost = false;             // fp32 does not say which bf16 number one of a key's values is; its bounds do not hold
     if (base + step < nh) fetch(h + step);
     if (base < nk) {
       float2 x[8];
@@ -192,10 +291,11 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
         if (__any_sync(0xffffffffu, !(ss <= FLT_MAX))) {
           // Squares of values beyond 1e18 leave fp32: such heads are taken 2^-70 as large (exact, and eps no longer counts beside
           // them).  A row with an infinity or a NaN stays what the formula makes of it.
-          const float down = ss <= FLT_MAX ? 1.f : 8.470329472543003e-22f;
+          lost = !(ss <= FLT_MAX);
+          const float down = lost ? 8.470329472543003e-22f : 1.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = mul2(x[e], make_float2(down, down));
-          if (down != 1.f) eps = 0.f;
+          if (lost) eps = 0.f;
           ss = squares();
         }
         const float r = rsqrtf(fmaf(ss, 1.f / D, eps));
@@ -209,11 +309,29 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
           for (int e = 0; e < 4; ++e) x[4 * half + e] = mul2(mul2(x[4 * half + e], rr), w[e]);
         }
       }
-      if (h < nk) {
+      // Rotation and rounding.  Of a key y is what a value becomes that is as much larger as fp32 may be off, `inner` one that is as much smaller.
+      auto turn = [&](auto is_key) {
+        constexpr bool KEY = decltype(is_key)::value;
+        float2 terms = make_float2(0.f, 0.f);
+        auto round = [&](int e, float2 v, float2 t) {
+          if (!KEY) {
+            y[e] = pack_bf16x2(v.x, v.y);
+          } else {
+            const float2 off = mul2(t, make_float2(copysignf(key_error, v.x), copysignf(key_error, v.y)));
+            const float2 far = add2(v, off), near = sub2(v, off);
+            y[e] = pack_bf16x2(far.x, far.y);
+            inner[e] = pack_bf16x2(near.x, near.y);
+            unsure |= y[e] != inner[e];
+          }
+        };
         if (!p.cos_sin) {
           if (p.normed) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(x[e].x, x[e].y);
+            for (int e = 0; e < 8; ++e) {
+              const float2 t = make_float2(fabsf(x[e].x), fabsf(x[e].y));
+              terms = add2(terms, t);
+              round(e, x[e], t);
+            }
           }
         } else if (!in_table) {
 #pragma unroll
@@ -223,37 +341,57 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 lo = fma2(x[e], c[e], mul2(mul2(x[4 + e], s[e]), minus)), hi = fma2(x[4 + e], c[e], mul2(x[e], s[e]));
-            y[e] = pack_bf16x2(lo.x, lo.y);
-            y[4 + e] = pack_bf16x2(hi.x, hi.y);
+            const float2 t = make_float2(fabsf(x[e].x) + fabsf(x[4 + e].x), fabsf(x[e].y) + fabsf(x[4 + e].y));
+            terms = add2(terms, t);
+            round(e, lo, t);
+            round(4 + e, hi, t);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float ce = e % 2 ? c[e / 2].y : c[e / 2].x, se = e % 2 ? s[e / 2].y : s[e / 2].x;
-            y[e] = pack_bf16x2(fmaf(x[e].x, ce, -(x[e].y * se)), fmaf(x[e].y, ce, x[e].x * se));
+            const float ce = e % 2 ? c[e / 2].y : c[e / 2].x, se = e % 2 ? s[e / 2].y : s[e / 2].x, t = fabsf(x[e].x) + fabsf(x[e].y);
+            round(e, make_float2(fmaf(x[e].x, ce, -(x[e].y * se)), fmaf(x[e].y, ce, x[e].x * se)), make_float2(t, t));
+            terms = add2(terms, make_float2(t, t));
           }
         }
-        if (h < nq) {
-          uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)t * p.Hq + h) * D + j * 8);
-          dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
-          dst[HALF] = make_uint4(y[4], y[5], y[6], y[7]);
+        if (KEY) {
+          const float sum = terms.x + terms.y;
+          lost |= !(sum <= FLT_MAX);
+          if (sum == 0.f) unsure = false;           // (zeros, whatever their signs)
         }
+      };
+      if (h < nq) turn(std::false_type());
+      else if (h < nk) turn(std::true_type());     // (a value stays as it is)
+      if (h < nq) {
+        uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)t * p.Hq + h) * D + j * 8);
+        dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+        dst[HALF] = make_uint4(y[4], y[5], y[6], y[7]);
       }
     }
     if (base + HW <= nq) continue;                 // query heads alone
-    const bool key = h < nk;
-    const float inv = key ? p.k_inv : p.v_inv;
-    uint32_t s0, s1;
-    const uint32_t c0 = kv4_quantize(y, inv, &s0), c1 = kv4_quantize(y + 4, inv, &s1);
-    if (h >= nq && h < nh && placed) {
-      const size_t row = row0 + (size_t)(h - (key ? nq : nk)) * 16;
-      uint8_t* codes = (key ? p.k_codes : p.v_codes) + row * (D / 2) + j * 4;
-      *reinterpret_cast<uint32_t*>(codes) = c0;
-      *reinterpret_cast<uint32_t*>(codes + D / 4) = c1;
-      if ((j & 1) == 0) {
-        uint8_t* scales = (key ? p.k_scales : p.v_scales) + row * (D / 16) + j / 2;
-        scales[0] = (uint8_t)s0;
-        scales[D / 32] = (uint8_t)s1;
+    const float inv = h < nk ? p.k_inv : p.v_inv;
+    const Kv4Codes z = kv4_quantize_both(y, inv);
+    store(h, z);
+    if (base >= nk) continue;
+    if (__any_sync(0xffffffffu, key && (unsure || lost))) {
+      // Codes and scales rise with their values' sizes: where those of both ends are the same, so are those between them.
+      const Kv4Codes u = kv4_quantize_both(inner, inv);
+      if (__any_sync(0xffffffffu, key && (lost || z.c0 != u.c0 || z.c1 != u.c1 || z.s0 != u.s0 || z.s1 != u.s1))) again |= 1u << min(key_group, 31);
+    }
+    ++key_group;
+  }
+  if (again) {
+    key_group = 0;
+#pragma unroll 1
+    for (int base = base0; base < nk; base += step) {
+      if (base + HW <= nq) continue;
+      if (again >> min(key_group++, 31) & 1) {
+        const int h = base + sub;
+        const bool key = h >= nq && h < nk && placed;
+        const Kv4Codes z = kv4_key_in_64_bits<D>(kin + (key ? h - nq : 0) * (D / 8), p.k_weight,
+                                                 p.cos_sin && in_table ? p.cos_sin + (size_t)pos * D + j * (p.interleaved ? 4 : 8) : nullptr, j, p.normed,
+                                                 p.weight_f32, p.interleaved, p.eps, p.weight_offset, p.k_inv);
+        if (key) store(h, z);
       }
     }
   }
@@ -338,6 +476,9 @@ extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim
     p.weight_offset = norm->weight_offset;
     p.eps = norm->eps;
   }
+  // Bounds of the error of fp32, u = 2^-24: the rotation's product and sum 2 u of |a c| + |b s|; a norm before them 13.5 u (twelve sums of squares and the mean 13 u, of
+  // which the inverse root has half and 4 u of its own, a weight's sum, two products).
+  p.key_error = norm ? 9.5367431640625e-07f : 2.384185791015625e-07f;          // 16 u, 4 u
   p.cached_len = batch->d_cached_len;
   p.q_indptr = batch->d_q_indptr;
   p.block_table = batch->d_block_table;
@@ -356,8 +497,8 @@ extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim
   const int hw = 512 / D, heads = (d_q ? cache->num_q_heads : 0) + 2 * cache->num_kv_heads, groups = (heads + hw - 1) / hw;
   const long long resident = 4LL * (KV4_APPEND_THREADS / 32) * sm_count();
   // Warps of a token: as many as are resident at once, up to one for every group of heads; with more tokens one, or from 16 groups on one for every ten.
-  // Microseconds with 1 / 2 / 3 / 4: 25,600 tokens at 32/8 heads x 128 (12 groups) 102 / 104 / 111 / 121, 12,800 at 64/8 (20) 93 / 87 / - / 91, at 32/32 (24) 104 / 103 /
-  // 103 / 104.  Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 78.
+  // Microseconds with 1 / 2 / 3 / 4: 25,600 tokens at 32/8 heads x 128 (12 groups) 113 / 117 / 125 / 137, 12,800 at 64/8 (20) 98 / 92 / 93 / 99, at 32/32 (24) 126 / 126 /
+  // 128 / 129.  Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 72, with norms 88 -> 84.
   p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 16 ? (groups + 9) / 10 : 1, resident / T));
   const long long ctas = (T * p.warps + KV4_APPEND_THREADS / 32 - 1) / (KV4_APPEND_THREADS / 32);
   if (ctas > 0x7fffffffLL / (KV4_APPEND_THREADS / 32)) return EFIM_ERR_UNSUPPORTED;    // (warps are counted in 32 bits)
