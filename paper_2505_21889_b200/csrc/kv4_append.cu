@@ -32,7 +32,7 @@ struct Kv4AppendParams {
   int early_next;           // let the next kernel start its set-up while this one runs
 };
 
-constexpr int KV4_APPEND_THREADS = 256;
+constexpr int KV4_APPEND_THREADS = 256, KV4_APPEND_CTAS = 3;     // threads; CTAs that an SM holds, by 80 registers
 
 // A value that is the same in a warp's lanes, in a form that tells the compiler so: what depends on it is computed once a warp.
 __device__ __forceinline__ int kv4_uniform(int x) { return __reduce_max_sync(0xffffffffu, x); }
@@ -179,7 +179,8 @@ __device__ __forceinline__ Kv4Codes kv4_key_in_64_bits(const uint4* row, const v
 // What brought it there, as replayed from a graph, keys in fp32: warp-wide values marked as such 118 -> 113, rows sent for ahead 111, a warp a
 // token instead of three 102.  Of the 64 bits: every group whose ends round differently again 143, those of different codes 124 (a call inside the loop)
 // -> 117 (behind the loop) -> 113 (in line).  Timed by events around single calls: divisions and value by value 134, neither 125; all keys in
-// 64 bits 179.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115 where 78 registers took 113.
+// 64 bits 179.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115 where 78 registers took 113; a promise of three CTAs to the compiler, which then
+// takes 76 registers instead of 80 and more instructions, 125.
 // With few tokens a chain of dependent loads: 64 tokens at 28/4 2.9 us.
 template <int D>
 __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
@@ -495,10 +496,11 @@ extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim
   p.Hq = cache->num_q_heads;
   p.Hkv = cache->num_kv_heads;
   const int hw = 512 / D, heads = (d_q ? cache->num_q_heads : 0) + 2 * cache->num_kv_heads, groups = (heads + hw - 1) / hw;
-  const long long resident = 4LL * (KV4_APPEND_THREADS / 32) * sm_count();
+  const long long resident = (long long)KV4_APPEND_CTAS * (KV4_APPEND_THREADS / 32) * sm_count();
   // Warps of a token: as many as are resident at once, up to one for every group of heads; with more tokens one, or from 16 groups on one for every ten.
   // Microseconds with 1 / 2 / 3 / 4: 25,600 tokens at 32/8 heads x 128 (12 groups) 113 / 117 / 125 / 137, 12,800 at 64/8 (20) 98 / 92 / 93 / 99, at 32/32 (24) 126 / 126 /
-  // 128 / 129.  Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 72, with norms 88 -> 84.
+  // 128 / 129; 592 tokens at 32/8 with 6 warps 6.4, with 8, a few of which are a second wave, 8.3, 1,184 with 3 8.5, with 4 10.8.
+  // Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 72, with norms 88 -> 84.
   p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 16 ? (groups + 9) / 10 : 1, resident / T));
   const long long ctas = (T * p.warps + KV4_APPEND_THREADS / 32 - 1) / (KV4_APPEND_THREADS / 32);
   if (ctas > 0x7fffffffLL / (KV4_APPEND_THREADS / 32)) return EFIM_ERR_UNSUPPORTED;    // (warps are counted in 32 bits)
