@@ -115,7 +115,8 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4AttnParams& p, int s) {
     w.new_len = p.max_new;
   }
   if (w.ctx > p.key_cap) {
-    w.err = EFIM_DEV_BAD_POSITION;
+    // (a turn's bound is of the sequences with new tokens: one without any may be longer)
+    if (!p.len_is_cached || w.new_len > 0) w.err = EFIM_DEV_BAD_POSITION;
     w.ctx = p.key_cap;
   }
   w.ctx = max(w.ctx, 0);
