@@ -183,6 +183,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     long long mine[2] = {0, 0};           // of trips, units
     for (int i = first; i < last; ++i) {
       const Kv4Seq q = kv4_seq(p, i);
+      if (q.err && blockIdx.x == 0 && p.status) atomicOr(p.status, q.err);   // (one CTA reports the lengths that do not fit)
       mine[0] += Line::costs(q, G) * Line::trips(q) * p.Hkv;
       mine[1] += (long long)Line::tiles(q, G) * p.Hkv;
     }
@@ -247,9 +248,6 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
     off -= tile * full;
   }
   Kv4Piece left{-1, 0, 0, 0};
-  if (!p.whole && blockIdx.x == 0)        // one CTA reports the lengths that do not fit
-    for (int i = tid; i < p.batch; i += KV4_THREADS)
-      if (const int err = kv4_seq(p, i).err; err && p.status) atomicOr(p.status, err);
 
   auto token_of = [&](int row) { return p.max_new == 1 ? 0 : row / G; };
   while (x0 < x1) {
