@@ -438,9 +438,9 @@ efim_status efim_kv4_unpack(const efim_cache4_desc* cache, const int32_t* d_page
  * are not computed.  Rows without keys get 0 and lse -inf; rows behind the last sequence's are left as they were.  Keys of a page outside the
  * pool count as absent and set EFIM_DEV_BAD_PAGE.  A query row with an infinity or a NaN gives NaN; so does a value that is NaN, in its
  * sixteen places, to the rows that see it, and to no others.
- * d_out may be d_q, and overlaps nothing else that is read.  Workspace: 256-byte aligned, efim_kv4_decode_workspace_bytes() for exactly these arguments (0: none needed),
- * exclusively this call's until the stream has passed it.  One kernel, two where the keys are split; may be captured; the same inputs
- * give the same bits.
+ * d_out may be d_q, and overlaps nothing else that is read.  Workspace: 256-byte aligned, efim_kv4_decode_workspace_bytes() for exactly these
+ * arguments (0: none needed; with max_ctx_len <= 0 it is enough for a table of any width), exclusively this call's until the stream has passed
+ * it.  One kernel, two where the keys are split; may be captured; the same inputs give the same bits.
  */
 size_t efim_kv4_decode_workspace_bytes(const efim_cache4_desc* cache, int32_t batch, int32_t max_new_len, int32_t max_ctx_len);
 efim_status efim_kv4_decode_attn(const efim_cache4_desc* cache, int32_t batch, const int32_t* d_ctx_len, int32_t max_ctx_len,

@@ -745,7 +745,6 @@ Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_
   const long long rows = (long long)max_new * G;
   pl.nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   pl.row_tiles = (rows + 8 * pl.nt - 1) / (8 * pl.nt);
-  if (max_ctx < 1) max_ctx = 1;
   const int trip = 16 * KV4_WARPS * kv4_pages(pl.nt);
   const long long trips = (max_ctx + (long long)trip - 1) / trip, units = (long long)batch * cache->num_kv_heads * pl.row_tiles;
   pl.whole = max_ctx <= KV4_WHOLE;
@@ -815,7 +814,8 @@ efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max
 
 extern "C" size_t efim_kv4_decode_workspace_bytes(const efim_cache4_desc* cache, int32_t batch, int32_t max_new_len, int32_t max_ctx_len) {
   if (efim::check_cache4(cache) != EFIM_OK || batch <= 0 || max_new_len <= 0) return 0;
-  return efim::kv4_plan(cache, batch, max_new_len, max_ctx_len).bytes;
+  // (a plan's size does not fall with the keys: the longest context's is enough for every table's capacity)
+  return efim::kv4_plan(cache, batch, max_new_len, max_ctx_len <= 0 ? INT_MAX : max_ctx_len).bytes;
 }
 
 extern "C" efim_status efim_kv4_decode_attn(const efim_cache4_desc* cache, int32_t batch, const int32_t* d_ctx_len, int32_t max_ctx_len,
