@@ -12,7 +12,7 @@
 //      side, so that a conversion gives a pair of tokens
 // with the page's tokens numbered such that neither read meets a bank twice (kv4_token, kv4_v_piece).
 // Queries enter as fp16 after a shift by a power of two per row that takes the row's largest value to [2^14, 2^15): exact for
-// values down to 2^-28 of it.  P = 2^(s - m + 11) enters as fp16 (a rounding of 2^-11 of each, between 2^15 and, at full precision, 2^-25 of
+// values down to 2^-28 of it, smaller ones to within 2^-39.  P = 2^(s - m + 11) enters as fp16 (a rounding of 2^-11 of each, between 2^15 and, at full precision, 2^-25 of
 // the largest); the sums that it is divided by are the unrounded fp32 values.
 //
 // Bound: with up to 8 rows the instructions, then HBM: of the 311 that a page (2,304 bytes) of one kv head costs a warp, 64 are conversions and 64
@@ -33,6 +33,9 @@ constexpr int KV4_WARPS = 4;
 constexpr int KV4_THREADS = 32 * KV4_WARPS;
 constexpr float KV4_P_SHIFT = 11.f;     // P's largest value, log2, with the reference right; the reference may be 4 behind
 constexpr float KV4_LAG = 4.f;
+// References (log2) from here on are rounded by 2^-4 and more, by which P = 2^(score - reference) would be off, and from 2^25 on beyond fp16: the weights of
+// such a row are taken from the scores' differences to the one at which the reference moves.
+constexpr float KV4_FAR = 1048576.f;
 
 __host__ __device__ constexpr int kv4_page_bytes(int D) { return 2 * (kv4_code_bytes(D) + kv4_scale_bytes(D)); }
 // pages that a warp takes at a time, and sets of them in its ring
@@ -399,6 +402,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       vs_at[e] = ring_ptr + 2 * CODES + SCALES + (D == 128 ? token * 8 + g : token * 4 + (g >> 1));
     }
 
+    bool far_off = false;                   // a row of the warp has a reference of KV4_FAR or more
     // trips whose pages every row sees in full
     const int seen = max(first_limit, 0) >> 4, n_full = seen >= first_pg + PG ? (seen - first_pg - PG) / (KV4_WARPS * PG) + 1 : 0;
 
@@ -504,10 +508,14 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
 #pragma unroll
               for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
               if (x > m_next[n][e]) {
-                float off = fmaf(x, sc[n][e], -KV4_P_SHIFT);
+                float off = fmaf(x, sc[n][e], -KV4_P_SHIFT), next = x + KV4_LAG / sc[n][e];
+                if (fabsf(off) >= KV4_FAR) {
+                  next = __fadd_rd(x, KV4_LAG / sc[n][e]);      // (P is 2^15 there: no score between it and the reference's may come out larger)
+                  off = fmaf(next, sc[n][e], -(KV4_P_SHIFT + KV4_LAG));
+                }
                 if (!(fabsf(off) <= FLT_MAX)) off = NAN;        // scores that leave fp32
                 const float alpha = m_next[n][e] == -FLT_MAX ? 0.f : kv4_ex2(m_off[n][e] - off);
-                m_next[n][e] = x + KV4_LAG / sc[n][e];
+                m_next[n][e] = next;
                 m_off[n][e] = off;
                 l_part[n][e] *= alpha;
 #pragma unroll
@@ -517,6 +525,10 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
                 }
               }
             }
+          bool off = false;
+#pragma unroll
+          for (int n = 0; n < NA; ++n) off |= fabsf(m_off[n][0]) >= KV4_FAR || fabsf(m_off[n][1]) >= KV4_FAR;
+          far_off = __any_sync(0xffffffffu, off);
           // Rows that see a value that is NaN are marked and get their NaN at the end; in the products such values are zeros, since rows that
           // do not see them have a P of 0 there.
 #pragma unroll
@@ -530,6 +542,24 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
                 if (key < min(end, w.cached + token_of(row0 + r) + 1)) s_nan[r][g] = 1;
             }
         }
+        // ---- the weights' exponents in the scores' place
+        if (!far_off) {
+#pragma unroll
+          for (int x = 0; x < PG; ++x)
+#pragma unroll
+            for (int n = 0; n < NA; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sx[x][n][e] = fmaf(sx[x][n][e], sc[n][e & 1], -m_off[n][e & 1]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < PG; ++x)
+#pragma unroll
+            for (int n = 0; n < NA; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                sx[x][n][e] = fabsf(m_off[n][e & 1]) >= KV4_FAR ? fmaf(sx[x][n][e] - m_next[n][e & 1], sc[n][e & 1], KV4_P_SHIFT + KV4_LAG)
+                                                                : fmaf(sx[x][n][e], sc[n][e & 1], -m_off[n][e & 1]);
+        }
 #pragma unroll
         for (int x = 0; x < PG; ++x) {
           uint32_t pb[NA][2];
@@ -537,7 +567,7 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
           for (int n = 0; n < NA; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float x0 = kv4_ex2(fmaf(sx[x][n][2 * h], sc[n][0], -m_off[n][0])), x1 = kv4_ex2(fmaf(sx[x][n][2 * h + 1], sc[n][1], -m_off[n][1]));
+              const float x0 = kv4_ex2(sx[x][n][2 * h]), x1 = kv4_ex2(sx[x][n][2 * h + 1]);
               l_part[n][0] += x0;
               l_part[n][1] += x1;
               pb[n][h] = kv4_movm_t(kv4_pack_half2(x0, x1));
