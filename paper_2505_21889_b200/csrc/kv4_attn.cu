@@ -666,17 +666,16 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
       }
       float inv = L == 0.f ? 0.f : p.v_scale / L;
       if (s_nan[r][d / (D / 8)]) inv = NAN;
-      const float lse2 = L == 0.f ? -INFINITY : M + log2f(L);                    // (a sum of NaN stays NaN)
       if (!first_part && ends) {
         const int token = token_of(row0 + r), h = kvh * G + row0 + r - token * G;
         const size_t row_head = (size_t)(w.first_row + token) * p.Hq + h;
         *reinterpret_cast<uint2*>(p.out + row_head * D + d) =
             make_uint2(pack_bf16x2(O.x * inv, O.y * inv), pack_bf16x2(O.z * inv, O.w * inv));
-        if (p.lse && d == 0) p.lse[row_head] = lse2 * 0.6931471805599453f;
+        if (p.lse && d == 0) p.lse[row_head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;   // (a sum of NaN stays NaN)
       } else {
         const size_t part = ((size_t)blockIdx.x * 2 + (first_part ? 0 : 1)) * ROWS + r;
         *reinterpret_cast<float4*>(p.part_o + part * D + d) = make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
-        if (d == 0) p.part_lse[part] = lse2;
+        if (d == 0) p.part_sum[part] = make_float2(L == 0.f ? -INFINITY : M, L);
       }
     }
     // ---- on along the line
@@ -700,7 +699,8 @@ __global__ void __launch_bounds__(KV4_THREADS, kv4_ctas_per_sm(NT)) kv4_attn_ker
   if (!p.whole && tid == 0) p.pieces[blockIdx.x] = left;
 }
 
-// Joins a unit's partial results: lse = log2 sum 2^lse_c, o = sum 2^(lse_c - lse) o_c.  A CTA has four rows of the unit that goes on behind a
+// Joins a unit's partial results (reference M_c, sum L_c, o_c): w_c = L_c 2^(M_c - max M), o = sum w_c o_c / sum w_c.  (The two apart: M_c + log2 L_c in one
+// number would lose the sum beside a large reference.)  A CTA has four rows of the unit that goes on behind a
 // piece: its second place, then the first places of the pieces behind it until the unit ends.  A warp has a row, lanes over head_dim; the
 // weights of 32 pieces are computed by the lanes together, four pieces' rows are on their way at a time.
 template <int D, int NT>
@@ -726,15 +726,15 @@ __global__ void __launch_bounds__(KV4_THREADS) kv4_join_kernel(const Kv4AttnPara
   const size_t first = ((size_t)blockIdx.x * 2 + 1) * ROWS + r;                // the c-th one: ROWS places on, then every 2 ROWS
   auto place = [&](int c) { return first + (c == 0 ? 0 : (size_t)(2 * c - 1) * ROWS); };
   float M = -INFINITY;
-  for (int c = lane; c < n; c += 32) M = max_nan(M, p.part_lse[place(c)]);     // a NaN piece makes the row NaN
+  for (int c = lane; c < n; c += 32) M = max_nan(M, p.part_sum[place(c)].x);   // a NaN piece makes the row NaN
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) M = max_nan(M, __shfl_xor_sync(0xffffffffu, M, d));
   float L = 0.f, acc[EPL];
 #pragma unroll
   for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
   for (int c0 = 0; c0 < n && !(M == -INFINITY); c0 += 32) {                    // (else a row without keys)
-    const float lse = c0 + lane < n ? p.part_lse[place(c0 + lane)] : -INFINITY;
-    const float wi = lse == -INFINITY ? 0.f : exp2f(lse - M);
+    const float2 sum = c0 + lane < n ? p.part_sum[place(c0 + lane)] : make_float2(-INFINITY, 0.f);
+    const float wi = sum.x == -INFINITY ? 0.f : sum.y * exp2f(sum.x - M);
     L += wi;
     const int some = min(32, n - c0);
     for (int k0 = 0; k0 < some; k0 += AT_ONCE) {
@@ -782,9 +782,9 @@ Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_
   pl.ctas = pl.whole ? units : std::min<long long>((long long)sm_count() * kv4_ctas_per_sm(pl.nt), (units * trips + pl.least_trips - 1) / pl.least_trips);
   const size_t parts = pl.whole ? 0 : (size_t)pl.ctas * 2 * 8 * pl.nt;
   auto round = [](size_t n) { return (n + 255) / 256 * 256; };
-  pl.lse_bytes = round(parts * 4);
+  pl.sum_bytes = round(parts * 8);
   pl.piece_bytes = pl.whole ? 0 : round((size_t)pl.ctas * sizeof(Kv4Piece));
-  pl.bytes = pl.lse_bytes + pl.piece_bytes + parts * cache->head_dim * 4;
+  pl.bytes = pl.sum_bytes + pl.piece_bytes + parts * cache->head_dim * 4;
   return pl;
 }
 
@@ -819,9 +819,9 @@ efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max
   if (pl.bytes > 0) {
     if (!ws || ws_bytes < pl.bytes) return EFIM_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(ws) & 255) return EFIM_ERR_INVALID_ARG;
-    p.part_lse = static_cast<float*>(ws);
-    p.pieces = reinterpret_cast<Kv4Piece*>(static_cast<char*>(ws) + pl.lse_bytes);
-    p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.lse_bytes + pl.piece_bytes);
+    p.part_sum = static_cast<float2*>(ws);
+    p.pieces = reinterpret_cast<Kv4Piece*>(static_cast<char*>(ws) + pl.sum_bytes);
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + pl.sum_bytes + pl.piece_bytes);
   }
   p.k_codes = static_cast<const uint8_t*>(cache->d_k_codes);
   p.v_codes = static_cast<const uint8_t*>(cache->d_v_codes);

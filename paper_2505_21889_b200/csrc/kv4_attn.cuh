@@ -14,7 +14,7 @@ struct Kv4AttnParams {
   uint16_t* out;
   float* lse;                 // natural log, or null
   float* part_o;              // [CTAs][2][rows of a tile][D]
-  float* part_lse;            // [CTAs][2][rows of a tile], base-2 log
+  float2* part_sum;           // [CTAs][2][rows of a tile]: reference (base-2 log), sum of weights relative to it
   struct Kv4Piece* pieces;    // [CTAs]
   int32_t* status;
   int batch, total_rows, max_new, Hq, Hkv, max_pages_per_seq, num_pages, row_tiles, units_per_seq, whole, least_trips, len_is_cached;
@@ -28,7 +28,7 @@ struct Kv4Plan {
   long long row_tiles;        // tiles of a sequence's (new token, head of the group) rows
   long long ctas;
   int whole, least_trips;
-  size_t lse_bytes, piece_bytes, bytes;
+  size_t sum_bytes, piece_bytes, bytes;
 };
 Kv4Plan kv4_plan(const efim_cache4_desc* cache, int batch, int max_new, int max_ctx);
 
