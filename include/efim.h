@@ -434,8 +434,8 @@ efim_status efim_kv4_unpack(const efim_cache4_desc* cache, const int32_t* d_page
  *   out[t,h,:] = sum_j softmax_j(sm_scale * q[t,h,:].k[j,h/G,:]) v[j,h/G,:],   lse as for efim_append_prefill_attn
  * on what the cache holds; queries are taken exactly down to 2^-28 of the row's largest value (below, to within 2^-39 of it), probabilities with 11
  * bits, everything else is fp32, the output bf16.  Scores are finite numbers of fp32 in units of log 2: a row with a larger one is NaN.
- * sm_scale <= 0 selects 1/sqrt(head_dim).  max_ctx_len (<= 0: the table's capacity) and max_new_len bound the lengths and fix the plan; total_rows is
- * how many rows d_q and d_out have.  What is beyond these bounds sets EFIM_DEV_BAD_POSITION: keys beyond are not seen, rows beyond
+ * sm_scale <= 0 selects 1/sqrt(head_dim).  max_ctx_len (<= 0: the table's capacity; at most 2^31 - 2^10, EFIM_ERR_UNSUPPORTED above) and max_new_len bound
+ * the lengths and fix the plan; total_rows is how many rows d_q and d_out have.  What is beyond these bounds sets EFIM_DEV_BAD_POSITION: keys beyond are not seen, rows beyond
  * are not computed.  Rows without keys get 0 and lse -inf; rows behind the last sequence's are left as they were.  Keys of a page outside the
  * pool count as absent and set EFIM_DEV_BAD_PAGE.  A query row with an infinity or a NaN gives NaN; so does a value that is NaN, in its
  * sixteen places, to the rows that see it, and to no others.

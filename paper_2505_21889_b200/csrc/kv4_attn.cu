@@ -810,8 +810,10 @@ static efim_status kv4_launch(const Kv4AttnParams& p, const Kv4Plan& pl, cudaStr
 
 efim_status kv4_attn_run(const efim_cache4_desc* cache, Kv4AttnParams p, int max_ctx, float sm_scale, void* ws, size_t ws_bytes, void* stream) {
   const long long cap = (long long)p.max_pages_per_seq * cache->page_size;
-  if (max_ctx <= 0) max_ctx = (int)std::min<long long>(cap, 0x7fffffff);
+  constexpr int MOST = INT_MAX - 1023;      // keys, and those of a trip that ends behind them, count in 32 bits
+  if (max_ctx <= 0) max_ctx = (int)std::min<long long>(cap, MOST);
   if (max_ctx > cap) return EFIM_ERR_OUT_OF_RANGE;
+  if (max_ctx > MOST) return EFIM_ERR_UNSUPPORTED;
   const long long G = cache->num_q_heads / cache->num_kv_heads;
   if ((long long)p.max_new * G > 0x3fffffff || (long long)p.batch * p.max_new * p.Hq > 0x7fffffff) return EFIM_ERR_UNSUPPORTED;
   const Kv4Plan pl = kv4_plan(cache, p.batch, p.max_new, max_ctx);
