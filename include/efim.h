@@ -452,7 +452,8 @@ efim_status efim_kv4_decode_attn(const efim_cache4_desc* cache, int32_t batch, c
 /*
  * Step 2 over a 4-bit cache for a turn's increments, whatever their length: efim_append_prefill_attn on what the cache holds, the new tokens
  * appended already.  Few rows (new tokens times heads of a group) a sequence go through the kernel of efim_kv4_decode_attn; for more the
- * batch's pages are unpacked to bf16 in the workspace, exactly, and the tensor-core kernel of efim_append_prefill_attn runs on them.
+ * batch's pages are unpacked to bf16 in the workspace, exactly, and the tensor-core kernel of efim_append_prefill_attn runs on them.  Which
+ * way a batch takes depends on the most new tokens of a sequence and on the batch's pages: the weights have 11 bits on the one, 8 on the other.
  * Arguments, results and errors as for efim_append_prefill_attn (the host mirrors are read during the call, stream capture as
  * there); rows that see a value that is NaN are NaN there, and may be NaN where a row of the same sequence sees one.
  * Workspace: efim_kv4_prefill_workspace_bytes() for exactly these lengths, 256-byte aligned.  d_out may be d_q.
@@ -473,8 +474,9 @@ efim_status efim_kv4_append_prefill_attn(const efim_cache4_desc* cache, const ef
  *     slots[r] = 16 page + position % 16 (-1 where there is no page);  all three -1 for rows from q_indptr[batch] to rows - 1
  * d_block_table_out (all other places are copied) and d_num_free_out may be d_block_table and d_num_free; they overlap nothing otherwise.
  * d_positions, d_slots and d_sequences may each be NULL; new tokens past `rows` have none of them and set EFIM_DEV_BAD_POSITION.
- * Lengths that are negative count as 0 tokens; those, lengths beyond the table (its places are filled, the tokens beyond get slot -1) and a
- * number of free pages outside [0, free_capacity], which is clamped, set EFIM_DEV_BAD_POSITION.
+ * A sequence with a negative length, or with more than 2^31 - 1 tokens, has 0 cached and 0 new ones; such sequences, lengths beyond the table
+ * (its places are filled, the tokens beyond get slot -1) and a number of free pages outside [0, free_capacity], which is clamped, set
+ * EFIM_DEV_BAD_POSITION.  With batch 0 nothing is written.
  * One kernel or two; may be captured.  Workspace: efim_step_tables_workspace_bytes(batch) bytes (enough for fewer sequences, too), 4-byte
  * aligned, exclusively this call's until the stream has passed it.
  */

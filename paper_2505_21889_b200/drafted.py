@@ -7,8 +7,9 @@ library when infilled code repeats its prefix and suffix.  Per step, for all use
   logits     one matrix product of this toy model
   decision   efim_verify_drafts       accepted drafts and the next token, greedily or by given random numbers
 
-With a cache held in 4 bits the step needs nothing from the host: pages and rows come from the lengths on the device
-(efim_step_tables), and efim_kv4_append and efim_kv4_decode_attn stand in place of the middle two.  Penalties go between logits and decision
+With a cache held in 4 bits pages and rows come from the lengths on the device (efim_step_tables), and efim_kv4_append and
+efim_kv4_decode_attn stand in place of the middle two: calls that read no lengths on the host, and so can be captured.  This loop, with either
+cache, reads back what each step accepted and keeps the histories' lengths on the host.  Penalties go between logits and decision
 (efim_adjust_logits).
 
 The accepted drafts' keys and values stay, the next step writes over the others'.  Without drafts the same loop decodes one token a
