@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
         }
         if (KEY) {
           const float sum = terms.x + terms.y;
-          lost |= !(sum <= FLT_MAX);
+          lost |= !(sum <= 1.2676506e30f);          // 2^100: beyond it products with a scaled table's values may leave fp32
           if (sum == 0.f) unsure = false;           // (zeros, whatever their signs)
         }
       };

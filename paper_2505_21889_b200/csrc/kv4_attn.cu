@@ -15,7 +15,7 @@
 // values down to 2^-28 of it, smaller ones to within 2^-39.  P = 2^(s - m + 11) enters as fp16 (a rounding of 2^-11 of each, between 2^15 and, at full precision, 2^-25 of
 // the largest); the sums that it is divided by are the unrounded fp32 values.
 //
-// Bound: with up to 8 rows the instructions, then HBM: of the 311 that a page (2,304 bytes) of one kv head costs a warp, 64 are conversions and 64
+// Bound: with up to 8 rows the instructions, then HBM: of the 296 that a page (2,304 bytes) of one kv head costs (the kernel's, starts included), 64 are conversions and 64
 // products, 16 matrix products; 64 users x 1-16k keys at 32/8 heads x 128 take 140 us (4.5 TB/s of codes and scales; their copies alone 115, the rest alone
 // 120).  What brought it from 174: two pages a trip 161, even pieces in one wave and starts that count 150, no branch around a page's copies 142,
 // three CTAs an SM instead of four with spills 140.  Not kept: bulk copies (four of 128 to 1,024 bytes a page: 173), four pages a trip, two or five CTAs.

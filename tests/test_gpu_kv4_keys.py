@@ -89,3 +89,12 @@ def test_ends_of_the_range():
         special[0], special[1, 0, ::3], special[2, 1, 7], special[3, 0, 70], special[4, 1, 40] = 0.0, -0.0, float("inf"), float("nan"), -float("inf")
         for weight in (None, torch.full((128,), 1.5, device="cuda")):
             _check(special, 2, 0, _table(128, 64), interleaved, weight)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_products_beyond_fp32_that_cancel(interleaved):
+    """In one pair of a head: the result's sign is that of the sum, not of the product that left fp32."""
+    k = _keys(64, 2, 128, 6)
+    k[:, :, 3], k[:, :, 2 if interleaved else 67] = 1e38, 1.1e38
+    for g in (2.0 ** 60, 0.5):
+        _check(k, 2, 0, _table(128, 64, 8.0), interleaved, g=g)
