@@ -181,7 +181,7 @@ __device__ __forceinline__ Kv4Codes kv4_key_in_64_bits(const uint4* row, const v
 // -> 117 (behind the loop) -> 113 (in line).  Timed by events around single calls: divisions and value by value 134, neither 125; all keys in
 // 64 bits 179.  Not kept: 64 registers (four CTAs an SM, 48 bytes spilled) 115 where 78 registers took 113; a promise of three CTAs to the compiler, which then
 // takes 76 registers instead of 80 and more instructions, 125.
-// With few tokens a chain of dependent loads: 64 tokens at 28/4 2.9 us.
+// With few tokens a chain of dependent loads: 64 tokens at 28/4 3.0 us.
 template <int D>
 __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv4AppendParams p) {
   constexpr int HALF = D / 16;                  // lanes that have a head
