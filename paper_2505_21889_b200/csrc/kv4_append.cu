@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     }
   };
   int key_group = 0;                                   // of the groups that have keys
-  uint32_t again = 0;                                  // those that fp32 does not decide, a bit each (the last one for all from the 32nd on)
+  uint32_t again = 0;                                  // those that fp32 does not decide, a bit each (a warp has fewer than 16 groups)
 #pragma unroll 1
   for (int base = base0; base < nh; base += step) {    // (the same for a warp's lanes: the sums below are the whole warp's)
     const int h = base + sub;
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
     if (__any_sync(0xffffffffu, key && (unsure || lost))) {
       // Codes and scales rise with their values' sizes: where those of both ends are the same, so are those between them.
       const Kv4Codes u = kv4_quantize_both(inner, inv);
-      if (__any_sync(0xffffffffu, key && (lost || z.c0 != u.c0 || z.c1 != u.c1 || z.s0 != u.s0 || z.s1 != u.s1))) again |= 1u << min(key_group, 31);
+      if (__any_sync(0xffffffffu, key && (lost || z.c0 != u.c0 || z.c1 != u.c1 || z.s0 != u.s0 || z.s1 != u.s1))) again |= 1u << key_group;
     }
     ++key_group;
   }
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(KV4_APPEND_THREADS) kv4_append_kernel(const Kv
 #pragma unroll 1
     for (int base = base0; base < nk; base += step) {
       if (base + HW <= nq) continue;
-      if (again >> min(key_group++, 31) & 1) {
+      if (again >> key_group++ & 1) {
         const int h = base + sub;
         const bool key = h >= nq && h < nk && placed;
         const Kv4Codes z = kv4_key_in_64_bits<D>(kin + (key ? h - nq : 0) * (D / 8), p.k_weight,
@@ -501,6 +501,7 @@ extern "C" efim_status efim_kv4_append(const efim_cache4_desc* cache, const efim
   // Microseconds with 1 / 2 / 3 / 4: 25,600 tokens at 32/8 heads x 128 (12 groups) 113 / 117 / 125 / 137, 12,800 at 64/8 (20) 98 / 92 / 93 / 99, at 32/32 (24) 126 / 126 /
   // 128 / 129; 592 tokens at 32/8 with 6 warps 6.4, with 8, a few of which are a second wave, 8.3, 1,184 with 3 8.5, with 4 10.8.
   // Rows sent for ahead where there are several waves: 25,600 at 28/4 84 -> 72, with norms 88 -> 84.
+  // (No warp has more than 15 groups: the kernel marks them in a word.)
   p.warps = (int)std::min<long long>(groups, std::max<long long>(groups >= 16 ? (groups + 9) / 10 : 1, resident / T));
   const long long ctas = (T * p.warps + KV4_APPEND_THREADS / 32 - 1) / (KV4_APPEND_THREADS / 32);
   if (ctas > 0x7fffffffLL / (KV4_APPEND_THREADS / 32)) return EFIM_ERR_UNSUPPORTED;    // (warps are counted in 32 bits)

@@ -98,3 +98,10 @@ def test_products_beyond_fp32_that_cancel(interleaved):
     k[:, :, 3], k[:, :, 2 if interleaved else 67] = 1e38, 1.1e38
     for g in (2.0 ** 60, 0.5):
         _check(k, 2, 0, _table(128, 64, 8.0), interleaved, g=g)
+
+
+@pytest.mark.parametrize("tokens,hq,hkv,d", [(3000, 40, 40, 128), (4000, 20, 20, 128), (700, 200, 100, 64)])
+def test_many_heads(tokens, hq, hkv, d):
+    """Several groups of keys a warp, beside warps that have none."""
+    weight = (1 + 0.2 * torch.randn(d, generator=torch.Generator().manual_seed(3))).cuda()
+    _check(_keys(tokens, hkv, d, hkv), hq, 0, _table(d, tokens), False, weight)
